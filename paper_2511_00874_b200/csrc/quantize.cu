@@ -20,6 +20,7 @@
 #include <cuda_bf16.h>
 
 #include "common.cuh"
+#include "grid_e4m3.cuh"
 
 namespace srq {
 
@@ -347,7 +348,6 @@ __global__ void scales_kernel(const uint32_t* amax_rm, int64_t n_rm, float* inv_
 // MODE: bit 0 = stochastic rounding (else round to nearest), bit 1 = E4M3 grid (else integer grid),
 // bit 2 = stochastic rounding with 8 random bits per element (integer grid only; the thresholds are
 // then handed to the same arithmetic as words (b << 24) | 2^23, whose top 24 bits are (2 b + 1) 2^15).
-constexpr int MODE_SR = 1, MODE_E4M3 = 2, MODE_SR8 = 4;
 
 // Integer grid: returns the 32-bit sum whose top byte is the code (two's complement).
 template <int MODE, bool NOTTED = false>
@@ -361,30 +361,6 @@ __device__ __forceinline__ uint32_t quantize_sum(float x, float inv, uint32_t wo
     } else {
         return (uint32_t)__float2int_rd(s) + 0x00800000u;
     }
-}
-
-// E4M3 grid: Def. 1 with the step of the binade of t = x * (1/D): for 2^e <= |t| < 2^(e+1) (e >= -6;
-// smaller |t| use e = -6, the subnormal spacing) the step is 2^(e-3) and u = t 2^(3-e) is rounded to
-// an integer q in [-16, 16] by the same exact fixed-point rule as above.  With E = e + 127 the biased
-// exponent of t, the code is sign | ((E - 120) << 3) + |q| - 8: |q| = 16 carries into the exponent
-// field (next binade), |q| < 8 only occurs for E = 121 and gives the subnormal codes, q = 0 gives +0.
-// Returns the code in the low byte.
-template <int MODE, bool NOTTED = false>
-__device__ __forceinline__ uint32_t quantize_e4m3(float x, float inv, uint32_t word, uint32_t sh) {
-    // sh = 3 - k for the E4Mk grid (k mantissa bits; 0 for E4M3 itself): the step of binade e is
-    // 2^(e-k), q counts those steps, and q << sh is the same value in the E4M3 code's units of 2^(e-3)
-    const float t = __fmul_rn(x, inv);
-    const uint32_t E = max((__float_as_uint(t) >> 23) & 0xFFu, 121u);          // |t| <= 448: E <= 135
-    const float s = __fmul_rn(t, __uint_as_float((281u - sh - E) << 23));       // t 2^(k-e) 2^24, exact
-    uint32_t sum;
-    if constexpr ((MODE & MODE_SR) != 0) {
-        const int c = __float2int_ru(s);
-        asm("mad.hi.u32 %0, %1, 16777216, %2;" : "=r"(sum) : "r"(NOTTED ? word : ~word), "r"((uint32_t)c));
-    } else {
-        sum = (uint32_t)__float2int_rd(s) + 0x00800000u;
-    }
-    const int q = (int)sum >> 24;
-    return ((uint32_t)q & 0x80u) | ((E << 3) + ((uint32_t)abs(q) << sh) - 968u);
 }
 
 // 8-random-bit mode: the threshold words of four consecutive elements from the stream word that holds
