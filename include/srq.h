@@ -80,12 +80,14 @@ typedef enum {
 } srq_status_t;
 
 typedef enum { SRQ_F32 = 0, SRQ_BF16 = 1 } srq_dtype_t;
-typedef enum { SRQ_PER_TENSOR = 0, SRQ_PER_ROW = 1 } srq_scale_t;
+/* SRQ_PER_BLOCK: one step size per block of 128 values; the srq_*_blocks and srq_rmsnorm / srq_glu entry points
+ * only (the block's shape is srq_blocks_t.tile_rows), which take no other mode. */
+typedef enum { SRQ_PER_TENSOR = 0, SRQ_PER_ROW = 1, SRQ_PER_BLOCK = 2 } srq_scale_t;
 /* SRQ_SR8: stochastic rounding with 8 random bits per element instead of 24 (the paper's hardware
  * section argues that a few pseudo-random bits per rounding suffice): eps = (b + 1/2) / 256 with b
  * byte (i & 3) of word ((i >> 2) & 3) of Philox block i >> 4, so that one block serves 16 elements.
  * P(round up) is the fraction rounded to the nearest 1/256.  Integer grid only. */
-typedef enum { SRQ_SR = 0, SRQ_RTN = 1, SRQ_SR8 = 2 } srq_round_t;
+typedef enum { SRQ_SR = 0, SRQ_RTN = 1, SRQ_SR8 = 2, SRQ_RNE = 3 /* nearest, ties to even; block entry points only */ } srq_round_t;
 /* Grid of a quantization point: integers times the step size (bits 2..8), or 8-bit floating-point
  * values times the step size.  SRQ_GRID_E4M3 with bits = 8 is E4M3 (1 sign, 4 exponent, 3 mantissa
  * bits, bias 7, no infinities, largest value 448); bits = 7, 6, 5 select E4M2, E4M1, E4M0, the
@@ -352,6 +354,108 @@ srq_status_t srq_dequant_i32(const int32_t *acc, int64_t ld_acc, int64_t M, int6
                              const float *s_row, int32_t row_stride,
                              const float *s_col, int32_t col_stride,
                              void *out, int64_t ldo, int32_t out_bf16, void *cuda_stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * Block-scaled E4M3 operators: the quantizer, the product, the norm and the gated feed-forward block around
+ * a linear layer, with one step size for every 128 values along the contracted axis (1 x 128) or for every
+ * 128 x 128 tile.  Finer step sizes keep a few large activations from costing all the others their precision;
+ * the products take the step sizes apart again: every 128-long piece of the contraction is summed on the
+ * tensor cores in binary32 and scaled before it is added to the total.
+ *
+ * Conventions, where they differ from the calls above
+ *   - No workspace and no header: `device_status` is an optional caller-owned device word (4-byte aligned).
+ *     A call does not clear it; it receives SRQ_ERR_NONFINITE or SRQ_ERR_TIMEOUT if the device meets such a
+ *     condition and it holds zero.  Zero it once, read it after as many calls as you like.
+ *   - Step size of a block: D = absmax / 448, the quotient is x * inv with inv = 448 / absmax rounded toward
+ *     zero; a block whose absmax is 0 or at most 7 * 2^-122 (the reciprocal would overflow) has D = 0 and
+ *     codes 0.
+ *   - Rounding: SRQ_RNE (nearest, ties to even, the conversion instruction's rule) or SRQ_SR (Def. 3, with the
+ *     thresholds of the flat index in the matrix that is being quantized, the source's own for both
+ *     layouts).  q->bits must be 8, q->format SRQ_GRID_E4M3, q->scale SRQ_PER_BLOCK; q->absmax is ignored.
+ *   - The last block of a row may be shorter than 128.
+ */
+
+/* A matrix of E4M3 codes [rows, cols] with its step sizes, on the device: element (r, c) stands for
+ * code * scale[(r / tile_rows) * ld_scale + c / 128]. */
+typedef struct {
+    uint8_t *codes;      /* [rows, ld], 16-byte aligned; padding bytes are neither read nor written */
+    int64_t ld;          /* pitch in bytes, >= cols, a multiple of 16 */
+    float *scale;        /* [ceil(rows / tile_rows), ld_scale], 4-byte aligned */
+    int64_t ld_scale;    /* pitch in floats, >= ceil(cols / 128); a multiple of 4 with a 16-byte aligned base is faster */
+    int32_t tile_rows;   /* 1: blocks of 1 x 128; 128: tiles of 128 x 128 */
+} srq_blocks_t;
+
+/* x[rows, cols] (pitch ld elements; 16-byte aligned base) as block codes: row-major into rm (blocks along the
+ * columns of x) and / or transposed into tr (a [cols, rows] matrix, blocks along the rows of x); NULL skips a
+ * layout.  With tile_rows = 128 both layouts hold the same codes and step sizes (transposed). */
+srq_status_t srq_quantize_blocks(const void *x, srq_dtype_t dt, int64_t rows, int64_t cols, int64_t ld,
+                                 const srq_qspec_t *q, const srq_blocks_t *rm, const srq_blocks_t *tr,
+                                 uint32_t *device_status, void *cuda_stream);
+
+/* The same for a source that is itself block-coded (an 8-bit activation checkpoint): its numbers are
+ * formed in binary32 and quantized anew, e.g. turned over for a contraction over the tokens. */
+srq_status_t srq_requantize_blocks(const srq_blocks_t *x, int64_t rows, int64_t cols,
+                                   const srq_qspec_t *q, const srq_blocks_t *rm, const srq_blocks_t *tr,
+                                   uint32_t *device_status, void *cuda_stream);
+
+/* out[M, N] (+)= A B^T, A[M, Kc] and B[N, Kc] block-coded with the contracted axis contiguous:
+ *   out[i, j] = sum over blocks k of  sA[i, k] * sB[j, k] * sum_{c in block k} a[i, c] * b[j, c]
+ * in binary32, the inner sums on the tensor cores.  out is binary32 or bfloat16 (out_dt, rounded once, to
+ * nearest even), pitch ldo elements.  accumulate = 1 adds to a binary32 out instead of overwriting it.  Any M
+ * from one token up; the sum's order depends on the sizes only, so results repeat bit for bit (with
+ * accumulate = 1 too: one addition per element). */
+srq_status_t srq_gemm_blocks(const srq_blocks_t *a, const srq_blocks_t *b, int64_t M, int64_t N, int64_t Kc,
+                             void *out, srq_dtype_t out_dt, int64_t ldo, int32_t accumulate,
+                             uint32_t *device_status, void *cuda_stream);
+
+/* Root-mean-square norm with the residual's addition, output as block codes (tile_rows = 1):
+ *   r = x + residual (residual may be NULL: r = x),  rstd = 1 / sqrt(mean(r^2) + eps),  y = r * rstd * w.
+ * x, residual and r_out have type dt and pitches in elements, w[cols] type w_dt; everything is computed in
+ * binary32 from the unrounded sum r.  y (block codes of y), y_out (y itself, type dt), r_out (r, rounded to
+ * dt) and rstd ([rows], for the backward pass) may each be NULL, but not y and y_out both.
+ * Base pointers are 16-byte aligned; pitches that are multiples of 8 elements and extents that are multiples
+ * of 8 take the vector path. */
+srq_status_t srq_rmsnorm_fwd(const void *x, int64_t ldx, const void *residual, int64_t ld_residual, srq_dtype_t dt,
+                             const void *w, srq_dtype_t w_dt, int64_t rows, int64_t cols, float eps,
+                             const srq_qspec_t *q, const srq_blocks_t *y, void *y_out, int64_t ld_y,
+                             void *r_out, int64_t ld_r, float *rstd, uint32_t *device_status, void *cuda_stream);
+
+/* Bytes of workspace srq_rmsnorm_bwd needs when dw is wanted (at most 512 partial rows of the weight's gradient). */
+size_t srq_rmsnorm_workspace_bytes(int64_t rows, int64_t cols);
+
+/* Its backward pass.  With n = r * rstd:
+ *   dx = rstd * (w * dy - n * mean(w * dy * n)) + d_residual      (the gradient of x and of the residual)
+ *   dw = sum over rows of dy * n                                    (binary32 [cols])
+ * dy is the gradient at y, d_residual (optional) the one that arrives at r, r is srq_rmsnorm_fwd's r_out (x
+ * where it had no residual).  dx or dw may be NULL.  The sum over rows has a fixed order. */
+srq_status_t srq_rmsnorm_bwd(const void *dy, int64_t ld_dy, const void *r, int64_t ld_r, const void *d_residual, int64_t ld_dres,
+                             srq_dtype_t dt, const void *w, srq_dtype_t w_dt, const float *rstd, int64_t rows, int64_t cols,
+                             void *dx, int64_t ld_dx, float *dw, void *ws, size_t ws_bytes, void *cuda_stream);
+
+typedef enum { SRQ_SILU = 0, SRQ_GELU = 1 /* tanh form */ } srq_act_t;
+
+/* Gated feed-forward block: both projections, the activation and the product in one kernel.
+ *   g = X Wg^T,  u = X Wu^T,  h = act(g) * u          X[T, K], Wg and Wu [F, K] block-coded
+ * h (block codes, tile_rows = 1: what the down projection reads) and h_out (h itself, type h_dt) may each be
+ * NULL, but not both.  gate and up, if not NULL, receive g and u as block codes (tile_rows = 1): the
+ * checkpoints srq_glu_bwd reads, 2 bytes per element instead of 4 or 8.  Wg and Wu share tile_rows.
+ * Codes are rounded to nearest (SRQ_RNE). */
+srq_status_t srq_glu_fwd(const srq_blocks_t *x, const srq_blocks_t *wg, const srq_blocks_t *wu, int64_t T, int64_t F, int64_t K,
+                         srq_act_t act, const srq_blocks_t *h, void *h_out, srq_dtype_t h_dt, int64_t ld_h,
+                         const srq_blocks_t *gate, const srq_blocks_t *up, uint32_t *device_status, void *cuda_stream);
+
+/* Its backward pass up to the products, from the checkpoints (g, u as their codes stand for):
+ *   dg = dh * u * act'(g),   du = dh * act(g),   h = act(g) * u
+ * dh[T, F] has type dt.  Any output may be NULL, all have tile_rows = 1:
+ *   dg, du [T, F]        for dX = dg Wg + du Wu (write both into one [T, 2F] matrix, next to each other, where F is
+ *                        a multiple of 128, and the sum of the two products is one product)
+ *   dg_t, du_t [F, T]    for dWg = dg^T X, dWu = du^T X
+ *   h_t [F, T]           for the down projection's dW = dY^T h
+ * q->tensor_id, + 1 and + 2 are the threshold streams of dg, du and h under SRQ_SR. */
+srq_status_t srq_glu_bwd(const void *dh, srq_dtype_t dt, int64_t ld_dh, const srq_blocks_t *gate, const srq_blocks_t *up,
+                         int64_t T, int64_t F, srq_act_t act, const srq_qspec_t *q,
+                         const srq_blocks_t *dg, const srq_blocks_t *du, const srq_blocks_t *dg_t, const srq_blocks_t *du_t,
+                         const srq_blocks_t *h_t, uint32_t *device_status, void *cuda_stream);
 
 /* Waits for the stream, then returns the device status word of the workspace: SRQ_OK, or the
  * first device-side condition recorded by the calls that used this workspace since its header

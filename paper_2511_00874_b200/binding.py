@@ -21,14 +21,17 @@ LIB_PATH = os.path.join(_PKG, "libsrq.so")
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_ACC_OVERFLOW, ERR_CUDA, ERR_NONFINITE, \
     ERR_TIMEOUT = range(8)
 F32, BF16 = 0, 1
-PER_TENSOR, PER_ROW = 0, 1
-SR, RTN, SR8 = 0, 1, 2
+PER_TENSOR, PER_ROW, PER_BLOCK = 0, 1, 2
+SR, RTN, SR8, RNE = 0, 1, 2, 3
 GRID_INT, GRID_E4M3, GRID_NONE = 0, 1, 2
+SILU, GELU = 0, 1
 
 EXPORTS = ["srq_quantize_workspace_bytes", "srq_gemm_workspace_bytes", "srq_workspace_bytes",
            "sr_quantize", "sr_quantize_static", "srq_absmax", "srq_absmax_cols", "srq_gemm_i8", "srq_gemm_e4m3", "qlinear_fwd", "qlinear_bwd_input", "qlinear_bwd_weight", "qlinear_bwd",
            "srq_gemm_i8_ex", "qlinear_fwd_ex", "qlinear_bwd_ex", "srq_dequant_i32",
-           "srq_poll_status", "srq_status_string", "srq_launch_count", "srq_selftest_bounded_wait", "srq_selftest_mma_rate", "srq_set_product_timer", "srq_plan_splits"]
+           "srq_poll_status", "srq_status_string", "srq_launch_count", "srq_selftest_bounded_wait", "srq_selftest_mma_rate", "srq_set_product_timer", "srq_plan_splits",
+           "srq_quantize_blocks", "srq_requantize_blocks", "srq_gemm_blocks", "srq_rmsnorm_fwd", "srq_rmsnorm_workspace_bytes",
+           "srq_rmsnorm_bwd", "srq_glu_fwd", "srq_glu_bwd"]
 
 
 class SrqError(RuntimeError):
@@ -71,6 +74,11 @@ class QSpec:
     def c(self) -> _QSpec:
         return _QSpec(self.bits, self.scale, self.round, self.format, self.seed, self.tensor_id,
                       self.index_offset, None if self.absmax is None else self.absmax.data_ptr())
+
+
+class _Blocks(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("ld", ctypes.c_int64), ("scale", ctypes.c_void_p), ("ld_scale", ctypes.c_int64),
+                ("tile_rows", ctypes.c_int32)]
 
 
 _lib: Optional[ctypes.CDLL] = None
@@ -129,6 +137,18 @@ def lib() -> ctypes.CDLL:
     L.srq_set_product_timer.restype = ctypes.c_int
     L.srq_plan_splits.argtypes = [i64, i32, i32, ctypes.POINTER(i32), ctypes.POINTER(i32)]
     L.srq_plan_splits.restype = None
+    bp, i, f = ctypes.POINTER(_Blocks), ctypes.c_int, ctypes.c_float
+    L.srq_quantize_blocks.argtypes = [vp, i, i64, i64, i64, qp, bp, bp, vp, vp]
+    L.srq_requantize_blocks.argtypes = [bp, i64, i64, qp, bp, bp, vp, vp]
+    L.srq_gemm_blocks.argtypes = [bp, bp, i64, i64, i64, vp, i, i64, i32, vp, vp]
+    L.srq_rmsnorm_fwd.argtypes = [vp, i64, vp, i64, i, vp, i, i64, i64, f, qp, bp, vp, i64, vp, i64, vp, vp, vp]
+    L.srq_rmsnorm_workspace_bytes.argtypes = [i64, i64]
+    L.srq_rmsnorm_workspace_bytes.restype = sz
+    L.srq_rmsnorm_bwd.argtypes = [vp, i64, vp, i64, vp, i64, i, vp, i, vp, i64, i64, vp, i64, vp, vp, sz, vp]
+    L.srq_glu_fwd.argtypes = [bp, bp, bp, i64, i64, i64, i, bp, vp, i, i64, bp, bp, vp, vp]
+    L.srq_glu_bwd.argtypes = [vp, i, i64, bp, bp, i64, i64, i, qp, bp, bp, bp, bp, bp, vp, vp]
+    for name in ("srq_quantize_blocks", "srq_requantize_blocks", "srq_gemm_blocks", "srq_rmsnorm_fwd", "srq_rmsnorm_bwd", "srq_glu_fwd", "srq_glu_bwd"):
+        getattr(L, name).restype = ctypes.c_int
     L.srq_poll_status.argtypes = [vp, vp]
     L.srq_poll_status.restype = ctypes.c_int
     L.srq_status_string.argtypes = [ctypes.c_int]
@@ -519,3 +539,187 @@ def new_product_timer(n: int, device="cuda") -> torch.Tensor:
 def srq_poll_status(ws: torch.Tensor) -> int:
     """Synchronises the current stream and returns the device status word of ``ws``."""
     return int(lib().srq_poll_status(ws.data_ptr(), _stream()))
+
+
+# ---------------------------------------------------------------------------------------------
+# block-scaled E4M3 operators
+# ---------------------------------------------------------------------------------------------
+BLOCK = 128
+BLOCK_RNE = QSpec(8, PER_BLOCK, RNE, format=GRID_E4M3)     # round to nearest even; SR: block_sr(seed, tensor_id)
+
+
+def block_sr(seed: int, tensor_id: int, index_offset: int = 0) -> QSpec:
+    """Stochastic rounding to block codes with the thresholds of (seed, tensor_id, index_offset)."""
+    return QSpec(8, PER_BLOCK, SR, seed, tensor_id, index_offset, GRID_E4M3)
+
+
+@dataclass
+class Blocks:
+    """A block-coded matrix (srq_blocks_t): ``codes`` uint8 [rows, cols] with a row pitch that is a multiple
+    of 16, ``scale`` float32 [ceil(rows / tile_rows), ceil(cols / 128)]; ``tile_rows`` is 1 (blocks of
+    1 x 128) or 128 (tiles of 128 x 128)."""
+    codes: torch.Tensor
+    scale: torch.Tensor
+    tile_rows: int = 1
+
+    @property
+    def shape(self):
+        return self.codes.shape
+
+    def c(self) -> _Blocks:
+        codes, scale = self.codes, self.scale
+        if codes.element_size() != 1 or codes.dim() != 2 or codes.stride(1) != 1 or not codes.is_cuda:
+            raise ValueError("codes must be a 2-D CUDA tensor of bytes with unit inner stride")
+        if scale.dtype != torch.float32 or scale.dim() != 2 or scale.stride(1) != 1 or not scale.is_cuda:
+            raise ValueError("step sizes must be a 2-D float32 CUDA tensor with unit inner stride")
+        rows, cols = codes.shape
+        if scale.shape[0] < -(-rows // self.tile_rows) or scale.shape[1] < -(-cols // BLOCK):
+            raise ValueError(f"step sizes of shape {tuple(scale.shape)} do not cover a {rows} x {cols} matrix")
+        # the pitch of a single row says nothing: torch is free to report any
+        ld = codes.stride(0) if rows > 1 else -(-max(codes.stride(0), cols) // 16) * 16
+        return _Blocks(codes.data_ptr(), ld, scale.data_ptr(), scale.stride(0) if scale.shape[0] > 1 else max(scale.stride(0), scale.shape[1]),
+                       self.tile_rows)
+
+    def dequantize(self) -> torch.Tensor:
+        """The numbers the matrix stands for, in float32."""
+        rows, cols = self.codes.shape
+        s = self.scale.repeat_interleave(self.tile_rows, 0)[:rows].repeat_interleave(BLOCK, 1)[:, :cols]
+        return self.codes.view(torch.float8_e4m3fn).float() * s
+
+
+def new_blocks(rows: int, cols: int, tile_rows: int = 1, device="cuda") -> Blocks:
+    """Uninitialised block-coded matrix whose pitches meet the alignment rules (codes 16 bytes, step sizes 16 bytes)."""
+    codes = torch.empty((rows, -(-cols // 16) * 16), dtype=torch.uint8, device=device)[:, :cols]
+    nb = -(-cols // BLOCK)
+    scale = torch.empty((-(-rows // tile_rows), -(-nb // 4) * 4), dtype=torch.float32, device=device)[:, :nb]
+    return Blocks(codes, scale, tile_rows)
+
+
+def _bref(b: Optional[Blocks], shape=None, name=""):
+    if b is None:
+        return None
+    if shape is not None and tuple(b.codes.shape) != shape:
+        raise ValueError(f"{name} must be {shape[0]} x {shape[1]}, got {tuple(b.codes.shape)}")
+    return ctypes.byref(b.c())
+
+
+def _status_word(device_status: Optional[torch.Tensor]):
+    if device_status is None:
+        return None
+    if device_status.dtype != torch.int32 or not device_status.is_cuda:
+        raise TypeError("device_status must be an int32 CUDA tensor of one element")
+    return device_status.data_ptr()
+
+
+def _pitch(t: Optional[torch.Tensor]) -> int:
+    return 0 if t is None else t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def srq_quantize_blocks(x, q: QSpec, rm: Optional[Blocks] = None, tr: Optional[Blocks] = None,
+                        device_status: Optional[torch.Tensor] = None) -> None:
+    """x[rows, cols] (float32, bfloat16, or a Blocks matrix: srq_requantize_blocks) as block codes, row-major
+    into ``rm`` and / or transposed into ``tr`` ([cols, rows])."""
+    rows, cols = x.shape
+    cq = q.c()
+    r, t = _bref(rm, (rows, cols), "rm"), _bref(tr, (cols, rows), "tr")
+    if isinstance(x, Blocks):
+        st = lib().srq_requantize_blocks(ctypes.byref(x.c()), rows, cols, ctypes.byref(cq), r, t, _status_word(device_status), _stream())
+        _check(st, "srq_requantize_blocks")
+        return
+    _dev2d(x, "x")
+    st = lib().srq_quantize_blocks(x.data_ptr(), _dtype_of(x), rows, cols, _pitch(x), ctypes.byref(cq), r, t,
+                                   _status_word(device_status), _stream())
+    _check(st, "srq_quantize_blocks")
+
+
+def srq_gemm_blocks(a: Blocks, b: Blocks, out: torch.Tensor, accumulate: bool = False,
+                    device_status: Optional[torch.Tensor] = None) -> None:
+    """out[M, N] (+)= a[M, Kc] b[N, Kc]^T over block codes; out is float32 or bfloat16."""
+    (M, Kc), (N, Kb) = a.shape, b.shape
+    _dev2d(out, "out")
+    if Kc != Kb or tuple(out.shape) != (M, N):
+        raise ValueError("srq_gemm_blocks: shapes must be a[M,Kc], b[N,Kc], out[M,N]")
+    st = lib().srq_gemm_blocks(ctypes.byref(a.c()), ctypes.byref(b.c()), M, N, Kc, out.data_ptr(), _dtype_of(out), _pitch(out),
+                               int(accumulate), _status_word(device_status), _stream())
+    _check(st, "srq_gemm_blocks")
+
+
+def srq_rmsnorm_fwd(x: torch.Tensor, residual: Optional[torch.Tensor], w: torch.Tensor, eps: float, y: Optional[Blocks],
+                    r_out: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None, y_out: Optional[torch.Tensor] = None,
+                    q: QSpec = BLOCK_RNE, device_status: Optional[torch.Tensor] = None) -> None:
+    """r = x + residual, y = r / rms(r) * w: y as block codes and / or in ``y_out``, r in ``r_out``, 1 / rms in ``rstd``."""
+    _dev2d(x, "x")
+    rows, cols = x.shape
+    dt = _dtype_of(x)
+    for t, name in ((residual, "residual"), (r_out, "r_out"), (y_out, "y_out")):
+        if t is not None:
+            _dev2d(t, name)
+            if t.dtype != x.dtype or t.shape != x.shape:
+                raise ValueError(f"{name} must have the shape and type of x")
+    if not w.is_cuda or w.shape != (cols,) or (cols > 1 and w.stride(0) != 1):
+        raise ValueError("w must be a CUDA tensor of cols values")
+    if rstd is not None and (rstd.dtype != torch.float32 or rstd.numel() < rows or not rstd.is_contiguous()):
+        raise ValueError("rstd must hold rows float32 values")
+    cq = q.c()
+    st = lib().srq_rmsnorm_fwd(x.data_ptr(), _pitch(x), _ptr(residual), _pitch(residual), dt, w.data_ptr(), _dtype_of(w), rows, cols,
+                               eps, ctypes.byref(cq), _bref(y, (rows, cols), "y"), _ptr(y_out), _pitch(y_out), _ptr(r_out), _pitch(r_out),
+                               _ptr(rstd), _status_word(device_status), _stream())
+    _check(st, "srq_rmsnorm_fwd")
+
+
+def srq_rmsnorm_workspace_bytes(rows: int, cols: int) -> int:
+    return int(lib().srq_rmsnorm_workspace_bytes(rows, cols))
+
+
+def srq_rmsnorm_bwd(dy: torch.Tensor, r: torch.Tensor, w: torch.Tensor, rstd: torch.Tensor, d_residual: Optional[torch.Tensor] = None,
+                    dx: Optional[torch.Tensor] = None, dw: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None) -> None:
+    """dx = rstd (w dy - n mean(w dy n)) + d_residual and dw = sum over rows of dy n, with n = r rstd."""
+    _dev2d(dy, "dy")
+    rows, cols = dy.shape
+    for t, name in ((r, "r"), (d_residual, "d_residual"), (dx, "dx")):
+        if t is not None:
+            _dev2d(t, name)
+            if t.dtype != dy.dtype or t.shape != dy.shape:
+                raise ValueError(f"{name} must have the shape and type of dy")
+    if not w.is_cuda or w.shape != (cols,) or (cols > 1 and w.stride(0) != 1):
+        raise ValueError("w must be a CUDA tensor of cols values")
+    for t, n, name in ((rstd, rows, "rstd"), (dw, cols, "dw")):
+        if t is not None and (t.dtype != torch.float32 or t.numel() < n or not t.is_contiguous() or not t.is_cuda):
+            raise ValueError(f"{name} must hold {n} float32 values")
+    if ws is None and dw is not None:
+        ws = new_workspace(srq_rmsnorm_workspace_bytes(rows, cols), dy.device)
+    st = lib().srq_rmsnorm_bwd(dy.data_ptr(), _pitch(dy), r.data_ptr(), _pitch(r), _ptr(d_residual), _pitch(d_residual), _dtype_of(dy),
+                               w.data_ptr(), _dtype_of(w), rstd.data_ptr(), rows, cols, _ptr(dx), _pitch(dx), _ptr(dw),
+                               _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size(), _stream())
+    _check(st, "srq_rmsnorm_bwd")
+
+
+def srq_glu_fwd(x: Blocks, wg: Blocks, wu: Blocks, act: int, h: Optional[Blocks], gate: Optional[Blocks] = None, up: Optional[Blocks] = None,
+                h_out: Optional[torch.Tensor] = None, device_status: Optional[torch.Tensor] = None) -> None:
+    """h = act(x wg^T) * (x wu^T) as block codes and / or in ``h_out``; ``gate`` and ``up`` receive the two
+    projections as 8-bit checkpoints for srq_glu_bwd."""
+    (T, K), (F, Kg) = x.shape, wg.shape
+    if Kg != K or tuple(wu.shape) != (F, K):
+        raise ValueError("srq_glu_fwd: shapes must be x[T,K], wg[F,K], wu[F,K]")
+    if h_out is not None:
+        _dev2d(h_out, "h_out")
+        if tuple(h_out.shape) != (T, F):
+            raise ValueError("h_out must be [T, F]")
+    st = lib().srq_glu_fwd(ctypes.byref(x.c()), ctypes.byref(wg.c()), ctypes.byref(wu.c()), T, F, K, act, _bref(h, (T, F), "h"),
+                           _ptr(h_out), F32 if h_out is None else _dtype_of(h_out), _pitch(h_out),
+                           _bref(gate, (T, F), "gate"), _bref(up, (T, F), "up"), _status_word(device_status), _stream())
+    _check(st, "srq_glu_fwd")
+
+
+def srq_glu_bwd(dh: torch.Tensor, gate: Blocks, up: Blocks, act: int, q: QSpec, dg: Optional[Blocks] = None, du: Optional[Blocks] = None,
+                dg_t: Optional[Blocks] = None, du_t: Optional[Blocks] = None, h_t: Optional[Blocks] = None,
+                device_status: Optional[torch.Tensor] = None) -> None:
+    """Gradients of both projections from the 8-bit checkpoints, as block codes along the features (dg, du)
+    and along the tokens (dg_t, du_t), and h itself along the tokens (h_t)."""
+    _dev2d(dh, "dh")
+    T, F = dh.shape
+    cq = q.c()
+    st = lib().srq_glu_bwd(dh.data_ptr(), _dtype_of(dh), _pitch(dh), _bref(gate, (T, F), "gate"), _bref(up, (T, F), "up"), T, F, act,
+                           ctypes.byref(cq), _bref(dg, (T, F), "dg"), _bref(du, (T, F), "du"), _bref(dg_t, (F, T), "dg_t"),
+                           _bref(du_t, (F, T), "du_t"), _bref(h_t, (F, T), "h_t"), _status_word(device_status), _stream())
+    _check(st, "srq_glu_bwd")

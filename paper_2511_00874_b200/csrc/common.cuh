@@ -212,4 +212,57 @@ void set_product_timer(unsigned long long* slots, int64_t n);
 // on operands resident in shared memory; *ops receives the integer operations of the launch.
 srq_status_t launch_mma_rate(int32_t k_blocks, uint32_t* status, int64_t* ops, cudaStream_t stream);
 
+// ------------------------------------------------------------------------------------------
+// Block-scaled operators (quantize_blocks.cu, rmsnorm.cu, gemm_blocks.cu)
+// ------------------------------------------------------------------------------------------
+// A block-coded matrix as the kernels take it; codes == nullptr: not wanted.
+struct Blocks {
+    uint8_t* codes = nullptr; int64_t ld = 0;
+    float* scale = nullptr; int64_t ld_scale = 0;
+    int32_t tile_rows = 1;
+};
+inline Blocks to_blocks(const srq_blocks_t* b) {
+    Blocks r;
+    if (b) { r.codes = b->codes; r.ld = b->ld; r.scale = b->scale; r.ld_scale = b->ld_scale; r.tile_rows = b->tile_rows; }
+    return r;
+}
+
+// What is being quantized to blocks: a matrix, or the three gradients of a gated block.
+struct BlockSource {
+    const void* x = nullptr; int32_t dt = 0; int64_t ld = 0;   // SRQ_F32 / SRQ_BF16 matrix
+    Blocks coded;                                              // or a block-coded one
+    int64_t rows = 0, cols = 0;
+};
+struct BlockRounding { int32_t sr = 0; uint64_t index_offset = 0; uint64_t seed = 0, tensor_id = 0; };
+
+cudaError_t launch_quantize_blocks(const BlockSource& src, const BlockRounding& rnd, const Blocks& rm, const Blocks& tr,
+                                   uint32_t* status, cudaStream_t stream);
+cudaError_t launch_glu_bwd(const void* dh, int32_t dt, int64_t ld_dh, const Blocks& gate, const Blocks& up, int64_t T, int64_t F,
+                           int32_t act, const BlockRounding& rnd, const Blocks& dg, const Blocks& du, const Blocks& dg_t,
+                           const Blocks& du_t, const Blocks& h_t, uint32_t* status, cudaStream_t stream);
+
+struct NormFwdArgs {
+    const void* x; int64_t ldx; const void* residual; int64_t ld_residual; int32_t dt;
+    const void* w; int32_t w_dt; int64_t rows, cols; float eps;
+    BlockRounding rnd; Blocks y; void* y_out; int64_t ld_y; void* r_out; int64_t ld_r; float* rstd; uint32_t* status;
+};
+cudaError_t launch_rmsnorm_fwd(const NormFwdArgs& a, cudaStream_t stream);
+struct NormBwdArgs {
+    const void* dy; int64_t ld_dy; const void* r; int64_t ld_r; const void* d_residual; int64_t ld_dres; int32_t dt;
+    const void* w; int32_t w_dt; const float* rstd; int64_t rows, cols; void* dx; int64_t ld_dx; float* dw; float* partial;
+};
+size_t rmsnorm_partial_bytes(int64_t rows, int64_t cols);
+cudaError_t launch_rmsnorm_bwd(const NormBwdArgs& a, cudaStream_t stream);
+
+struct GemmBlocksArgs {
+    Blocks a, b; int64_t M, N, Kc;
+    void* out; int32_t out_dt; int64_t ldo; int32_t accumulate;
+};
+srq_status_t launch_gemm_blocks(const GemmBlocksArgs& g, uint32_t* status, cudaStream_t stream);
+struct GluArgs {
+    Blocks x, wg, wu; int64_t T, F, K; int32_t act;
+    Blocks h, gate, up; void* h_out; int32_t h_dt; int64_t ld_h;
+};
+srq_status_t launch_glu_fwd(const GluArgs& g, uint32_t* status, cudaStream_t stream);
+
 }  // namespace srq
