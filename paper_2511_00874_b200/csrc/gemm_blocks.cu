@@ -12,6 +12,8 @@
 // gemm_blocks_kernel: 256 x 256 tiles on CTA pairs (tcgen05.mma.cta_group::2, M256 N256 K32), persistent.
 //   warp 0      TMA producer (128-byte swizzled tiles, ring of 5 stages of 32 KB)
 //   warp 1      TMEM and MMA issue (leader CTA): one k-block into one TMEM buffer at a time, in turn
+//   warps 2-3   step sizes: four k-blocks at a time from global memory into a shared ring, so that the warps that
+//               add up hold no addresses and no prefetched values in their registers
 //   warps 4-11  two groups of four; a thread owns one row of the CTA's 128 and 128 of the 256 columns: group
 //               g columns 128 g .. in a plain product; in the gated block, whose 256 columns are 128 of the
 //               gate and 128 of the up projection (one CTA of the pair stages Wg, the other Wu), columns
@@ -35,12 +37,16 @@ namespace srq {
 constexpr int GB_M = 128, GB_N = 256, GB_K = 128;      // rows per CTA, tile columns, bytes (= codes) per k-block
 constexpr int GB_STAGES = 5;
 constexpr int GB_STAGE_BYTES = GB_M * GB_K + (GB_N / 2) * GB_K;
-constexpr int GB_THREADS = 384;
-// Registers: 384 threads start with 168 each; the first warpgroup keeps 40 and the two that hold 128 sums per
-// thread take 232 (40 + 2 x 232 = 3 x 168: exactly what the block was launched with).
-constexpr int GB_REGS_FEW = 40, GB_REGS_MANY = 232;
-constexpr int GB_OUT_BYTES = 32 * 128;                 // staging block of an epilogue warp
+constexpr int GB_ADD_WARPS = 16;                       // warps that read TMEM, scale, add up and store
+constexpr int GB_CGROUPS = GB_ADD_WARPS / 4;           // column groups of the tile; a thread holds one row of one group
+constexpr int GB_COLS = GB_N / GB_CGROUPS;             // sums per thread
+constexpr int GB_THREADS = 128 + 32 * GB_ADD_WARPS;
+// Registers: 640 threads start with 96 each; the first warpgroup keeps 32 and the four that hold 64 sums per thread
+// take 112 (32 + 4 x 112 = 5 x 96: exactly what the block was launched with).
+constexpr int GB_REGS_FEW = 32, GB_REGS_MANY = 112;
+constexpr int GB_OUT_BYTES = 32 * 64;                  // staging block of an epilogue warp: 32 rows of 64 bytes
 constexpr int GB_UMMA_K = 32;
+constexpr int GB_SCALE_SLOTS = 3;                      // chunks of four k-blocks whose step sizes are in shared memory
 
 struct GemmBlocksParams {
     int64_t M, N;                       // N: columns of out, or of h (the gated block's F)
@@ -54,28 +60,49 @@ struct GemmBlocksParams {
 };
 
 struct GbTail {
-    uint64_t full[GB_STAGES], empty[GB_STAGES], tmem_full[2], tmem_empty[2], drain;
+    uint64_t full[GB_STAGES], empty[GB_STAGES], tmem_full[2][2], tmem_empty[2][2], drain;     // [half][buffer]
     uint32_t tmem_base;
     volatile uint32_t abort_flag;
-    alignas(16) float col_scale[2][2][4][128];     // [group][chunk parity][k-block of the chunk][column]
-    uint32_t amax[2][3][2][GB_M];                  // gated block: [tile parity][which][group][row]
+    uint64_t scale_full[GB_SCALE_SLOTS], scale_empty[GB_SCALE_SLOTS];
+    alignas(16) float row_scale[GB_SCALE_SLOTS][4][GB_M];   // [slot][k-block of the chunk][row]
+    alignas(16) float col_scale[GB_SCALE_SLOTS][4][GB_N];   // [..][column of the tile], or [0], [1]: one per 128 columns
+    uint32_t amax[2][3][GB_CGROUPS][GB_M];         // gated block: [tile parity][which][column group][row]
 };
-constexpr size_t gb_smem() { return 1024 + (size_t)GB_STAGES * GB_STAGE_BYTES + 8 * GB_OUT_BYTES + sizeof(GbTail); }
+constexpr size_t gb_smem() { return 1024 + (size_t)GB_STAGES * GB_STAGE_BYTES + GB_ADD_WARPS * GB_OUT_BYTES + sizeof(GbTail); }
 
 __device__ __forceinline__ void gb_give_up(volatile uint32_t* abort_flag, uint32_t* status) {
     *abort_flag = 1u;
     note(status, SRQ_ERR_TIMEOUT);
 }
 
-// 32 lanes x 32 columns of TMEM, in registers once tmem_ready has passed (which ties the registers to the wait).
-__device__ __forceinline__ void tmem_ready(uint32_t (&v)[32]) {
-    asm volatile("tcgen05.wait::ld.sync.aligned;"
-        : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]),
-          "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15]),
-          "+r"(v[16]), "+r"(v[17]), "+r"(v[18]), "+r"(v[19]), "+r"(v[20]), "+r"(v[21]), "+r"(v[22]), "+r"(v[23]),
-          "+r"(v[24]), "+r"(v[25]), "+r"(v[26]), "+r"(v[27]), "+r"(v[28]), "+r"(v[29]), "+r"(v[30]), "+r"(v[31])
-        :: "memory");
+__device__ __forceinline__ uint32_t elect_one() {
+    uint32_t e;
+    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(e));
+    return e;
 }
+
+// Bounded wait of the warps that add up, on a barrier's shared address.  The usual case is one try; when the limit has
+// passed or another role has given up it returns all the same, so that the caller needs no second path: its
+// results are then garbage, the status says so, and every wait after it returns as soon.
+__device__ __forceinline__ bool try_wait_addr(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n.reg .pred p;\n"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+        "selp.u32 %0, 1, 0, p;\n}"
+        : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+__device__ __forceinline__ void wait_or_abort(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag, uint32_t* status) {
+    if (try_wait_addr(bar, parity)) return;
+    const uint64_t t0 = global_ns();
+    while (!try_wait_addr(bar, parity)) {
+        if (*abort_flag) break;
+        if (global_ns() - t0 > WAIT_LIMIT_NS) { gb_give_up(abort_flag, status); break; }
+    }
+}
+
+// 32 lanes x 16 columns of TMEM (in registers after tmem_ld_wait).
 __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&v)[16]) {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
@@ -83,13 +110,6 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&v)[16]) {
           "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
         : "r"(taddr) : "memory");
 }
-__device__ __forceinline__ void tmem_ready(uint32_t (&v)[16]) {
-    asm volatile("tcgen05.wait::ld.sync.aligned;"
-        : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]),
-          "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15])
-        :: "memory");
-}
-
 // Step sizes of k-blocks 4 c .. 4 c + 3 of one scale row (zeros past num_kb).
 __device__ __forceinline__ float4 scales4(const float* row, int32_t c, int32_t num_kb, bool vec) {
     const int32_t k = 4 * c;
@@ -103,10 +123,13 @@ __device__ __forceinline__ float4 scales4(const float* row, int32_t c, int32_t n
 }
 __device__ __forceinline__ float pick4(const float4& f, int32_t i) { return i == 0 ? f.x : i == 1 ? f.y : i == 2 ? f.z : f.w; }
 
-// Sixty-four consecutive codes of a row from column c (rows start on 16-byte boundaries).
-__device__ __forceinline__ void store_codes64(uint8_t* row, int64_t c, int64_t cols, const uint32_t (&w)[16]) {
+__device__ __forceinline__ float2 pair(uint32_t a, uint32_t b) { return make_float2(__uint_as_float(a), __uint_as_float(b)); }
+
+// 4 W consecutive codes of a row from column c (rows start on 16-byte boundaries, c is a multiple of 16).
+template <int W>
+__device__ __forceinline__ void store_codes(uint8_t* row, int64_t c, int64_t cols, const uint32_t (&w)[W]) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
+    for (int q = 0; q < W / 4; ++q) {
         if (c + 16 * q + 16 <= cols) {
             *reinterpret_cast<uint4*>(row + c + 16 * q) = make_uint4(w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]);
         } else {
@@ -115,6 +138,16 @@ __device__ __forceinline__ void store_codes64(uint8_t* row, int64_t c, int64_t c
                 if (c + 16 * q + e < cols) row[c + 16 * q + e] = (uint8_t)(w[4 * q + (e >> 2)] >> (8 * (e & 3)));
         }
     }
+}
+
+// Thread `lane` holds 64 bytes of row `lane` of a block of 32 rows: writes them in the 64-byte swizzle of the output's
+// tensor map (16-byte chunk index xor row / 2 mod 4), which also spreads the 16-byte stores of a warp over all banks.
+__device__ __forceinline__ void stage_rows64(uint32_t stage, int lane, const uint32_t (&w)[16]) {
+    const uint32_t row = stage + (uint32_t)lane * 64u;
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(row + (uint32_t)((q ^ ((lane >> 1) & 3)) << 4)),
+                     "r"(w[4 * q]), "r"(w[4 * q + 1]), "r"(w[4 * q + 2]), "r"(w[4 * q + 3]) : "memory");
 }
 
 // GLU: the gated block's epilogue instead of the plain one.  COLV: b has a step size per row (per column of
@@ -128,14 +161,15 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     uint8_t* out_stage = smem + (size_t)GB_STAGES * GB_STAGE_BYTES;
-    GbTail* T = (GbTail*)(out_stage + 8 * GB_OUT_BYTES);
+    GbTail* T = (GbTail*)(out_stage + GB_ADD_WARPS * GB_OUT_BYTES);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_ctarank();
     const bool leader = rank == 0;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < GB_STAGES; ++s) { mbar_init(&T->full[s], 1); mbar_init(&T->empty[s], 1); }
-        for (int b = 0; b < 2; ++b) { mbar_init(&T->tmem_full[b], 1); mbar_init(&T->tmem_empty[b], 16); }   // 8 warps x 2 CTAs
+        for (int b = 0; b < 4; ++b) { mbar_init(&T->tmem_full[0][b], 1); mbar_init(&T->tmem_empty[0][b], GB_ADD_WARPS); }   // half of the warps of both CTAs
+        for (int b = 0; b < GB_SCALE_SLOTS; ++b) { mbar_init(&T->scale_full[b], 64); mbar_init(&T->scale_empty[b], GB_ADD_WARPS); }
         mbar_init(&T->drain, 1);
         T->abort_flag = 0u;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -165,7 +199,8 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
             for (int64_t u = group; u < tiles && ok; u += groups) {
                 const int32_t tn = (int32_t)(u % P.tiles_n), tm = (int32_t)(u / P.tiles_n);
                 const int32_t row_a = (tm * 2 + (int32_t)rank) * GB_M;
-                const int32_t row_b = GLU ? tn * 128 : tn * GB_N + (int32_t)rank * 128;
+                // b's rows so that the first 64 of both CTAs are one half of the tile's columns and the last 64 the other
+                const int32_t row_b = GLU ? tn * 128 : tn * GB_N + (int32_t)rank * 64;
                 for (int32_t kb = 0; kb < P.num_kb; ++kb, ++it) {
                     const uint32_t s = it % GB_STAGES, ph = (it / GB_STAGES) & 1u;
                     if (!mbar_wait(&T->empty[s], ph ^ 1u, &T->abort_flag)) { gb_give_up(&T->abort_flag, P.status); ok = false; break; }
@@ -174,6 +209,7 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                     uint8_t* sa = smem + (size_t)s * GB_STAGE_BYTES;
                     tma_load_2d<2>(sa, &map_a, kb * GB_K, row_a, bar);
                     tma_load_2d<2>(sa + GB_M * GB_K, mb, kb * GB_K, row_b, bar);
+                    tma_load_2d<2>(sa + GB_M * GB_K + 64 * GB_K, mb, kb * GB_K, row_b + (GLU ? 64 : 128), bar);
                 }
             }
             if (!ok) {
@@ -193,217 +229,249 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
         }
     } else if (warp == 1) {
         // ------------------------------------------------------------------ MMA issuer (leader CTA only)
-        if (lane == 0 && leader) {
-            const uint32_t idesc = make_idesc(1, GB_M * 2, GB_N);
-            bool ok = true, ready = false;
-            uint32_t s = 0, ph = 0, it = 0;
+        // The whole warp walks the loop and one elected lane issues: what the instructions take (descriptors, barrier
+        // addresses) is then uniform to the compiler and stays in uniform registers.  With a single thread in the loop
+        // every MMA cost some 95 cycles and every commit 61 to issue, more than the MMAs themselves take.
+        if (leader) {
+            constexpr uint32_t idesc = make_idesc(1, GB_M * 2, GB_N / 2);
+            const uint32_t elected = elect_one();
+            bool ok = true;
+            uint32_t s = 0, ph = 0, buf = 0, buf_ph = 1;
             const uint64_t desc0 = make_smem_desc(smem_u32(smem));
-            uint64_t da = desc0;
             for (int64_t u = group; u < tiles && ok; u += groups) {
-                for (int32_t kb = 0; kb < P.num_kb; ++kb, ++it) {
-                    const uint32_t buf = it & 1u, use = it >> 1;
-                    if (!mbar_wait(&T->tmem_empty[buf], (use & 1u) ^ 1u, &T->abort_flag)) { gb_give_up(&T->abort_flag, P.status); ok = false; break; }
-                    if (!ready && !mbar_wait(&T->full[s], ph, &T->abort_flag)) { gb_give_up(&T->abort_flag, P.status); ok = false; break; }
-                    tc_fence_after();
-                    const uint32_t d_tmem = tmem_base + buf * GB_N;
-                    const uint64_t db = da + (uint64_t)((GB_M * GB_K) >> 4);
-                    const uint32_t ns = s + 1 == (uint32_t)GB_STAGES ? 0u : s + 1, nph = ns == 0u ? ph ^ 1u : ph;
-                    umma<2, 1>(d_tmem, da, db, idesc, 0u);
-                    ready = mbar_test_wait(&T->full[ns], nph);
+                for (int32_t kb = 0; kb < P.num_kb; ++kb) {
+                    ok = mbar_wait(&T->full[s], ph, &T->abort_flag);
+                    const uint64_t da = desc0 + (uint64_t)(s * (GB_STAGE_BYTES >> 4)), db = da + (uint64_t)((GB_M * GB_K) >> 4);
 #pragma unroll
-                    for (int k = 1; k < GB_K / GB_UMMA_K; ++k)
-                        umma<2, 1>(d_tmem, da + (uint64_t)((k * GB_UMMA_K) >> 4), db + (uint64_t)((k * GB_UMMA_K) >> 4), idesc, 1u);
-                    umma_commit<2>(&T->empty[s], true);
-                    umma_commit<2>(&T->tmem_full[buf], true);
-                    s = ns; ph = nph;
-                    da = ns == 0u ? desc0 : da + (uint64_t)(GB_STAGE_BYTES >> 4);
+                    for (int h = 0; h < 2; ++h) {
+                        ok = ok && mbar_wait(&T->tmem_empty[h][buf], buf_ph, &T->abort_flag);
+                        ok = !__any_sync(0xFFFFFFFFu, !ok);
+                        if (!ok) break;
+                        tc_fence_after();
+                        if (elected) {
+#pragma unroll
+                            for (int k = 0; k < GB_K / GB_UMMA_K; ++k)
+                                umma<2, 1>(tmem_base + buf * GB_N + h * (GB_N / 2), da + (uint64_t)((k * GB_UMMA_K) >> 4),
+                                           db + (uint64_t)((h * 64 * GB_K + k * GB_UMMA_K) >> 4), idesc, k ? 1u : 0u);
+                            umma_commit<2>(&T->tmem_full[h][buf], true);
+                            if (h == 1) umma_commit<2>(&T->empty[s], true);
+                        }
+                        __syncwarp();
+                    }
+                    if (!ok) { gb_give_up(&T->abort_flag, P.status); break; }
+                    s = s + 1 == (uint32_t)GB_STAGES ? 0u : s + 1;
+                    ph ^= s == 0u ? 1u : 0u;
+                    buf_ph ^= buf;
+                    buf ^= 1u;
                 }
             }
-            if (!ok) {
+            if (!ok && elected) {
                 umma_commit<2>(&T->drain, false);
                 const uint64_t t0 = global_ns();
                 while (!mbar_try_wait(&T->drain, 0u) && global_ns() - t0 < WAIT_LIMIT_NS) {}
+            }
+        }
+    } else {
+        // ------------------------------------------------------------------ step sizes (warps 2 and 3)
+        // They run up to GB_SCALE_SLOTS chunks ahead, so that the latency of one load after the other does not
+        // matter (and their registers are few).
+        const int t = threadIdx.x - 64;                  // 0..63: rows t and t + 64, columns t + 64 j
+        uint32_t slot = 0, ph = 0;
+        bool ok = true;
+        auto put = [&](float* dst, int ld, const Blocks& m, int64_t r, int64_t end, int32_t chunk, bool vec) {
+            const float* row = r < end ? m.scale + (m.tile_rows > 1 ? r / QBLK : r) * m.ld_scale : nullptr;
+            const float4 f = scales4(row, chunk, P.num_kb, vec);
+            dst[0] = f.x; dst[ld] = f.y; dst[2 * ld] = f.z; dst[3 * ld] = f.w;
+        };
+        for (int64_t u = group; u < tiles && ok; u += groups) {
+            const int32_t tn = (int32_t)(u % P.tiles_n), tm = (int32_t)(u / P.tiles_n);
+            const int64_t row = ((int64_t)tm * 2 + rank) * GB_M + t, col = (int64_t)tn * TILE_COLS;
+            for (int32_t chunk = 0; 4 * chunk < P.num_kb; ++chunk) {
+                if (!mbar_wait(&T->scale_empty[slot], ph ^ 1u, &T->abort_flag)) { gb_give_up(&T->abort_flag, P.status); ok = false; break; }
+#pragma unroll 1
+                for (int j = 0; j < 2; ++j) put(&T->row_scale[slot][0][t + 64 * j], GB_M, P.a, row + 64 * j, P.M, chunk, P.a_vec);
+                if constexpr (COLV) {
+#pragma unroll 1
+                    for (int j = 0; j < 4; ++j)
+                        put(&T->col_scale[slot][0][t + 64 * j], GB_N, GLU && j >= 2 ? P.b2 : P.b, col + t + 64 * (GLU ? j & 1 : j), P.N, chunk, P.b_vec);
+                } else if (t < 2) {
+                    put(&T->col_scale[slot][0][t], GB_N, GLU && t == 1 ? P.b2 : P.b, GLU ? col : col + 128 * t, P.N, chunk, P.b_vec);
+                }
+                mbar_arrive(&T->scale_full[slot]);
+                slot = slot + 1 == (uint32_t)GB_SCALE_SLOTS ? 0u : slot + 1;
+                ph ^= slot == 0u ? 1u : 0u;
             }
         }
     }
     } else {
         // ------------------------------------------------------------------ scaling and epilogue (warps 4..11)
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(GB_REGS_MANY));
-        const int quarter = warp & 3, egrp = (warp - 4) >> 2, etid = (threadIdx.x - 128) & 127;
+        const int quarter = warp & 3, cg = (warp - 4) >> 2;
         const int trow = quarter * 32 + lane;            // row within this CTA's 128
-        const uint32_t empty0 = map_to_cta(smem_u32(&T->tmem_empty[0]), 0), empty1 = map_to_cta(smem_u32(&T->tmem_empty[1]), 0);
+        const uint32_t half = (uint32_t)(GB_COLS * cg / 128);      // of the tile's columns in TMEM: an MMA of its own
+        const uint32_t empty0 = map_to_cta(smem_u32(&T->tmem_empty[half][0]), 0);
         const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16);
-        // first TMEM column of each 32-column piece this thread adds up
-        auto piece = [&](int c) -> uint32_t { return GLU ? (uint32_t)((c >> 1) * 128 + 64 * egrp + 32 * (c & 1)) : (uint32_t)(128 * egrp + 32 * c); };
+        // first tile column of each of this thread's 32-column pieces: neighbours, or, in the gated block, the same columns
+        // of the gate and of the up projection
+        constexpr int PIECES = GB_COLS / 32;
+        auto piece = [&](int c) -> uint32_t {
+            return GLU ? (uint32_t)((c / (PIECES / 2)) * 128 + (GB_COLS / 2) * cg + 32 * (c % (PIECES / 2))) : (uint32_t)(GB_COLS * cg + 32 * c);
+        };
+        // and where they are in a TMEM buffer: a half holds 128 columns of out, or 64 gate and 64 up columns
+        auto column = [&](int c) -> uint32_t { return GLU ? (piece(c) & 64u) * 2u + (piece(c) & 63u) + (piece(c) >> 7) * 64u : piece(c); };
         const uint32_t stage = smem_u32(out_stage + (warp - 4) * GB_OUT_BYTES);
-        bool ok = true;
-        uint32_t it = 0, chunks = 0, par = 0;
+        const uint32_t full0 = smem_u32(&T->tmem_full[half][0]);
+        uint32_t buf = 0, buf_ph = 0, par = 0, slot = 0, slot_ph = 0;
         for (int64_t u = group; u < tiles; u += groups) {
+            float2 sum[GB_COLS / 2];                       // two by two
+#pragma unroll
+            for (int i = 0; i < GB_COLS / 2; ++i) sum[i] = make_float2(0.0f, 0.0f);
+#pragma unroll 1
+            for (int32_t left = P.num_kb; left > 0; left -= 4) {
+                wait_or_abort(smem_u32(&T->scale_full[0]) + 8 * slot, slot_ph, &T->abort_flag, P.status);
+                const float* rs = &T->row_scale[slot][0][trow];
+                const float* cs = T->col_scale[slot][0];
+#pragma unroll 1
+                for (int32_t j = min(left, 4); j > 0; --j, rs += GB_M, cs += GB_N) {
+                    const float sa = *rs;
+                    float2 s0 = make_float2(sa, sa), s1 = s0;
+                    if constexpr (!COLV) {
+                        const float f0 = __fmul_rn(sa, cs[GLU ? 0 : GB_COLS * cg / 128]);
+                        s0 = s1 = make_float2(f0, f0);
+                        if constexpr (GLU) { const float f1 = __fmul_rn(sa, cs[1]); s1 = make_float2(f1, f1); }
+                    }
+                    wait_or_abort(full0 + 8 * buf, buf_ph, &T->abort_flag, P.status);
+                    tc_fence_after();
+                    const uint32_t tb = taddr + buf * GB_N;
+// the buffer is handed back as soon as its last piece is in registers
+                    auto release = [&]() {
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive_cluster(empty0 + 8 * buf);
+                    };
+                    if constexpr (!COLV) {
+#pragma unroll
+                        for (int c = 0; c < PIECES; ++c) {
+                            uint32_t v[32];
+                            tmem_ld32(tb + column(c), v);
+                            tmem_ld_wait();
+                            if (c + 1 == PIECES) release();
+#pragma unroll
+                            for (int i = 0; i < 16; ++i)
+                                sum[16 * c + i] = __ffma2_rn(pair(v[2 * i], v[2 * i + 1]), c < PIECES / 2 ? s0 : s1, sum[16 * c + i]);
+                        }
+                    } else {
+                        // half as many columns at a time: the columns' step sizes take registers too
+#pragma unroll
+                        for (int c = 0; c < 2 * PIECES; ++c) {
+                            uint32_t v[16];
+                            tmem_ld16(tb + column(c >> 1) + 16 * (c & 1), v);
+                            tmem_ld_wait();
+                            if (c + 1 == 2 * PIECES) release();
+                            const float* f0 = cs + piece(c >> 1) + 16 * (c & 1);
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) {
+                                const float4 f = *reinterpret_cast<const float4*>(f0 + 4 * q);
+                                float2& x = sum[8 * c + 2 * q];
+                                float2& y = sum[8 * c + 2 * q + 1];
+                                x = __ffma2_rn(pair(v[4 * q], v[4 * q + 1]), __fmul2_rn(make_float2(f.x, f.y), s0), x);
+                                y = __ffma2_rn(pair(v[4 * q + 2], v[4 * q + 3]), __fmul2_rn(make_float2(f.z, f.w), s0), y);
+                            }
+                        }
+                    }
+                    buf_ph ^= buf;
+                    buf ^= 1u;
+                }
+                __syncwarp();                              // this chunk's step sizes have been read
+                if (lane == 0) mbar_arrive(&T->scale_empty[slot]);
+                slot = slot + 1 == (uint32_t)GB_SCALE_SLOTS ? 0u : slot + 1;
+                slot_ph ^= slot == 0u ? 1u : 0u;
+            }
+
             const int32_t tn = (int32_t)(u % P.tiles_n), tm = (int32_t)(u / P.tiles_n);
             const int64_t row0 = ((int64_t)tm * 2 + rank) * GB_M, row = row0 + trow;
             const int64_t col0 = (int64_t)tn * TILE_COLS;
-            // this thread's scale rows
-            const float* ra = row < P.M ? P.a.scale + (P.a.tile_rows > 1 ? row / QBLK : row) * P.a.ld_scale : nullptr;
-            const float* rb = nullptr;                     // one step size per 128 columns ...
-            const float* rb2 = nullptr;
-            const float* rc = nullptr;                     // ... or this thread's share of the columns' own
-            if constexpr (!COLV) {
-                const int64_t tb = GLU ? tn : (int64_t)tn * 2 + egrp;
-                if (tb * QBLK < P.N) {
-                    rb = P.b.scale + tb * P.b.ld_scale;
-                    if constexpr (GLU) rb2 = P.b2.scale + tb * P.b2.ld_scale;
-                }
-            } else {
-                const int64_t c = GLU ? col0 + 64 * egrp + (etid & 63) : col0 + 128 * egrp + etid;
-                const Blocks& w = GLU && etid >= 64 ? P.b2 : P.b;
-                if (c < P.N) rc = w.scale + c * w.ld_scale;
-            }
-            float acc[128];
+            float acc[GB_COLS];
 #pragma unroll
-            for (int i = 0; i < 128; ++i) acc[i] = 0.0f;
-            float4 na = scales4(ra, 0, P.num_kb, P.a_vec), nb, nb2 = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            if constexpr (!COLV) {
-                nb = scales4(rb, 0, P.num_kb, P.b_vec);
-                if constexpr (GLU) nb2 = scales4(rb2, 0, P.num_kb, P.b_vec);
-            } else {
-                nb = scales4(rc, 0, P.num_kb, P.b_vec);
-            }
-            float4 ca = na, cb = nb, cb2 = nb2;
-#pragma unroll 1
-            for (int32_t kb = 0; kb < P.num_kb; ++kb, ++it) {
-                const int32_t in4 = kb & 3, chunk = kb >> 2;
-                if (in4 == 0) ++chunks;
-                float (*cs)[128] = T->col_scale[egrp][chunks & 1];
-                if (in4 == 0) {
-                    ca = na; cb = nb; cb2 = nb2;
-                    if constexpr (COLV) {
-                        // the chunk before last is what this buffer held: every warp of the group has left it
-                        cs[0][etid] = cb.x; cs[1][etid] = cb.y; cs[2][etid] = cb.z; cs[3][etid] = cb.w;
-                        asm volatile("bar.sync %0, 128;" ::"r"(1 + egrp) : "memory");
-                    }
-                    na = scales4(ra, chunk + 1, P.num_kb, P.a_vec);
-                    if constexpr (!COLV) {
-                        nb = scales4(rb, chunk + 1, P.num_kb, P.b_vec);
-                        if constexpr (GLU) nb2 = scales4(rb2, chunk + 1, P.num_kb, P.b_vec);
-                    } else {
-                        nb = scales4(rc, chunk + 1, P.num_kb, P.b_vec);
-                    }
-                }
-                const float sa = pick4(ca, in4);
-                float s0 = sa, s1 = sa;
-                if constexpr (!COLV) {
-                    s0 = __fmul_rn(sa, pick4(cb, in4));
-                    if constexpr (GLU) s1 = __fmul_rn(sa, pick4(cb2, in4)); else s1 = s0;
-                }
-                const uint32_t buf = it & 1u, use = it >> 1;
-                if (ok && !mbar_wait(&T->tmem_full[buf], use & 1u, &T->abort_flag)) { gb_give_up(&T->abort_flag, P.status); ok = false; }
-                if (__any_sync(0xFFFFFFFFu, !ok)) ok = false;
-                tc_fence_after();
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    uint32_t v[32];
-                    tmem_ld32(taddr + buf * GB_N + piece(c), v);
-                    tmem_ready(v);
-                    if (c == 3) {
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive_cluster(buf ? empty1 : empty0);
-                    }
-                    if constexpr (!COLV) {
-                        const float s = c < 2 ? s0 : s1;
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) acc[32 * c + i] = fmaf(__uint_as_float(v[i]), s, acc[32 * c + i]);
-                    } else {
-#pragma unroll
-                        for (int q = 0; q < 8; ++q) {
-                            const float4 f = *reinterpret_cast<const float4*>(&cs[in4][32 * c + 4 * q]);
-                            acc[32 * c + 4 * q + 0] = fmaf(__uint_as_float(v[4 * q + 0]), sa * f.x, acc[32 * c + 4 * q + 0]);
-                            acc[32 * c + 4 * q + 1] = fmaf(__uint_as_float(v[4 * q + 1]), sa * f.y, acc[32 * c + 4 * q + 1]);
-                            acc[32 * c + 4 * q + 2] = fmaf(__uint_as_float(v[4 * q + 2]), sa * f.z, acc[32 * c + 4 * q + 2]);
-                            acc[32 * c + 4 * q + 3] = fmaf(__uint_as_float(v[4 * q + 3]), sa * f.w, acc[32 * c + 4 * q + 3]);
-                        }
-                    }
-                }
-            }
-
+            for (int i = 0; i < GB_COLS / 2; ++i) { acc[2 * i] = sum[i].x; acc[2 * i + 1] = sum[i].y; }
             if constexpr (GLU) {
-                // acc: 64 gate columns, then the same 64 up columns
-                const int64_t f0 = col0 + 64 * egrp;
+                // acc: GH gate columns, then the same GH up columns
+                constexpr int GH = GB_COLS / 2;
+                const int64_t f0 = col0 + GH * cg;
                 const bool live = row < P.M;
+                // the absmax of the row's 128 columns from those of the column groups
+                auto row_max = [&](int which) -> uint32_t {
+                    uint32_t m = 0u;
+#pragma unroll
+                    for (int i = 0; i < GB_CGROUPS; ++i) m = max(m, T->amax[par][which][i][trow]);
+                    return m;
+                };
                 auto emit = [&](const Blocks& o, uint32_t m, const float* val) {
                     float step, inv;
                     block_step(m, &step, &inv);
-                    uint32_t w[16];
+                    uint32_t w[GH / 4];
 #pragma unroll
-                    for (int q = 0; q < 16; ++q)
+                    for (int q = 0; q < GH / 4; ++q)
                         w[q] = e4m3x4(__fmul_rn(val[4 * q], inv), __fmul_rn(val[4 * q + 1], inv), __fmul_rn(val[4 * q + 2], inv), __fmul_rn(val[4 * q + 3], inv));
-                    if (!live || !ok) return;
+                    if (!live) return;
                     if (block_nonfinite(m)) note(P.status, SRQ_ERR_NONFINITE);
-                    if (egrp == 0) o.scale[row * o.ld_scale + tn] = step;
-                    store_codes64(o.codes + row * o.ld, f0, P.N, w);
+                    if (cg == 0) o.scale[row * o.ld_scale + tn] = step;
+                    store_codes(o.codes + row * o.ld, f0, P.N, w);
                 };
                 if (P.gate.codes || P.up.codes) {
                     uint32_t mg = 0u, mu = 0u;
 #pragma unroll
-                    for (int i = 0; i < 64; ++i) { mg = max(mg, abs_word(acc[i])); mu = max(mu, abs_word(acc[64 + i])); }
-                    T->amax[par][0][egrp][trow] = mg; T->amax[par][1][egrp][trow] = mu;
-                    asm volatile("bar.sync 3, 256;" ::: "memory");
-                    mg = max(mg, T->amax[par][0][egrp ^ 1][trow]); mu = max(mu, T->amax[par][1][egrp ^ 1][trow]);
-                    if (P.gate.codes) emit(P.gate, mg, acc);
-                    if (P.up.codes) emit(P.up, mu, acc + 64);
+                    for (int i = 0; i < GH; ++i) { mg = max(mg, abs_word(acc[i])); mu = max(mu, abs_word(acc[GH + i])); }
+                    T->amax[par][0][cg][trow] = mg; T->amax[par][1][cg][trow] = mu;
+                    asm volatile("bar.sync 3, %0;" ::"n"(32 * GB_ADD_WARPS) : "memory");
+                    if (P.gate.codes) emit(P.gate, row_max(0), acc);
+                    if (P.up.codes) emit(P.up, row_max(1), acc + GH);
                 }
                 uint32_t mh = 0u;
                 if (P.gelu) {
 #pragma unroll
-                    for (int i = 0; i < 64; ++i) { acc[i] = act_of<true>(acc[i]) * acc[64 + i]; mh = max(mh, abs_word(acc[i])); }
+                    for (int i = 0; i < GH; ++i) { acc[i] = act_of<true>(acc[i]) * acc[GH + i]; mh = max(mh, abs_word(acc[i])); }
                 } else {
 #pragma unroll
-                    for (int i = 0; i < 64; ++i) { acc[i] = act_of<false>(acc[i]) * acc[64 + i]; mh = max(mh, abs_word(acc[i])); }
+                    for (int i = 0; i < GH; ++i) { acc[i] = act_of<false>(acc[i]) * acc[GH + i]; mh = max(mh, abs_word(acc[i])); }
                 }
-                if (P.out && live && ok) {
-                    const bool vec = P.h_vec && f0 + 64 <= P.N;
+                if (P.out && live) {
+                    const bool vec = P.h_vec && f0 + GH <= P.N;
 #pragma unroll
-                    for (int q = 0; q < 8; ++q) {
+                    for (int q = 0; q < GH / 8; ++q) {
                         if (P.out_bf16) store8((__nv_bfloat16*)P.out + row * P.ldo, f0 + 8 * q, P.N, vec, acc + 8 * q);
                         else store8((float*)P.out + row * P.ldo, f0 + 8 * q, P.N, vec, acc + 8 * q);
                     }
                 }
                 if (P.h.codes) {
-                    T->amax[par][2][egrp][trow] = mh;
-                    asm volatile("bar.sync 3, 256;" ::: "memory");
-                    mh = max(mh, T->amax[par][2][egrp ^ 1][trow]);
-                    emit(P.h, mh, acc);
+                    T->amax[par][2][cg][trow] = mh;
+                    asm volatile("bar.sync 3, %0;" ::"n"(32 * GB_ADD_WARPS) : "memory");
+                    emit(P.h, row_max(2), acc);
                 }
                 par ^= 1;            // these words are written again two tiles on, a barrier after everyone has read them
             } else {
                 const int32_t wrow = (int32_t)(row0 + quarter * 32);
-                const int64_t c_first = col0 + 128 * egrp;
-                if (P.tma_out && P.out_bf16) {
+                const int64_t c_first = col0 + GB_COLS * cg;
+                if (P.tma_out) {
+                    // 64 bytes of every row at a time through the warp's staging block
+                    constexpr int F32_BLOCKS = GB_COLS / 16;
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        uint32_t w[32];
+                    for (int j = 0; j < F32_BLOCKS; ++j) {
+                        uint32_t w[16];
+                        if (P.out_bf16) {
+                            if (j >= F32_BLOCKS / 2) break;
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) w[i] = pack_bf16(acc[64 * j + 2 * i], acc[64 * j + 2 * i + 1]);
+                            for (int i = 0; i < 16; ++i) w[i] = j < F32_BLOCKS / 2 ? pack_bf16(acc[(32 * j + 2 * i) % GB_COLS], acc[(32 * j + 2 * i + 1) % GB_COLS]) : 0u;
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(acc[16 * j + i]);
+                        }
                         if (lane == 0) bulk_wait_read();
                         __syncwarp();
-                        stage_block(stage, lane, w);
+                        stage_rows64(stage, lane, w);
                         fence_async_smem();
                         __syncwarp();
-                        const int64_t c = c_first + 64 * j;
-                        if (lane == 0 && wrow < P.M && c < P.N) { tma_store_2d(&map_out, stage, (int32_t)c, wrow); bulk_commit(); }
-                    }
-                } else if (P.tma_out) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        uint32_t w[32];
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) w[i] = __float_as_uint(acc[32 * j + i]);
-                        if (lane == 0) bulk_wait_read();
-                        __syncwarp();
-                        stage_block(stage, lane, w);
-                        fence_async_smem();
-                        __syncwarp();
-                        const int64_t c = c_first + 32 * j;
+                        const int64_t c = c_first + (P.out_bf16 ? 32 : 16) * j;
                         if (lane == 0 && wrow < P.M && c < P.N) {
                             if (P.accumulate) tma_reduce_add_2d(&map_out, stage, (int32_t)c, wrow);
                             else tma_store_2d(&map_out, stage, (int32_t)c, wrow);
@@ -414,12 +482,12 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                     if (P.out_bf16) {
                         __nv_bfloat16* dst = (__nv_bfloat16*)P.out + row * P.ldo;
 #pragma unroll
-                        for (int i = 0; i < 128; ++i)
+                        for (int i = 0; i < GB_COLS; ++i)
                             if (c_first + i < P.N) dst[c_first + i] = __float2bfloat16_rn(acc[i]);
                     } else {
                         float* dst = (float*)P.out + row * P.ldo;
 #pragma unroll
-                        for (int i = 0; i < 128; ++i)
+                        for (int i = 0; i < GB_COLS; ++i)
                             if (c_first + i < P.N) dst[c_first + i] = P.accumulate ? __fadd_rn(dst[c_first + i], acc[i]) : acc[i];
                     }
                 }
@@ -612,7 +680,7 @@ gemm_blocks_small_kernel(const __grid_constant__ CUtensorMap map_a, const __grid
             for (int c = 0; c < C::COLS / 16; ++c) {
                 uint32_t v[16];
                 tmem_ld16(taddr + buf * C::COLS + 16 * c, v);
-                tmem_ready(v);
+                tmem_ld_wait();
                 const float s = GLU && c >= BN / 16 ? sw2 : sw;
                 const float* tk = &ts[in4][(16 * c) % BN];
 #pragma unroll
@@ -718,10 +786,10 @@ static bool encode_result(CUtensorMap* map, void* base, bool bf16, int64_t rows,
     const unsigned esize = bf16 ? 2 : 4;
     cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
     cuuint64_t strides[1] = {(cuuint64_t)ld * esize};
-    cuuint32_t box[2] = {128 / esize, 32};
+    cuuint32_t box[2] = {64 / esize, 32};
     cuuint32_t estr[2] = {1, 1};
     return enc(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, base, dims, strides, box, estr,
-               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -848,9 +916,9 @@ static srq_status_t run_pairs(const BlocksDevice& d, GemmBlocksParams& P, bool g
     P.tiles_m = (int32_t)((P.M + 2 * GB_M - 1) / (2 * GB_M));
     P.tiles_n = (int32_t)((P.N + (glu ? 128 : GB_N) - 1) / (glu ? 128 : GB_N));
     CUtensorMap ma, mb, mb2, mo;
-    if (!encode_codes(&ma, P.a, P.M, Kc, GB_M) || !encode_codes(&mb, P.b, P.N, Kc, 128)) return SRQ_ERR_CUDA;
+    if (!encode_codes(&ma, P.a, P.M, Kc, GB_M) || !encode_codes(&mb, P.b, P.N, Kc, 64)) return SRQ_ERR_CUDA;
     mb2 = mb; mo = mb;
-    if (glu && !encode_codes(&mb2, P.b2, P.N, Kc, 128)) return SRQ_ERR_CUDA;
+    if (glu && !encode_codes(&mb2, P.b2, P.N, Kc, 64)) return SRQ_ERR_CUDA;
     const int per16 = P.out_bf16 ? 8 : 4;
     const bool out16 = P.out && (uintptr_t)P.out % 16 == 0 && P.ldo % per16 == 0;
     P.h_vec = out16;
