@@ -14,6 +14,13 @@ constexpr int QBLK = 128;                    // values per step size
 constexpr float E4M3_MAX = 448.0f;
 
 __device__ __forceinline__ uint32_t abs_word(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
+// max(|m|, |a|, |b|) in one instruction; a NaN among them gives a NaN with a positive pattern, so that the pattern
+// of a block's maximum still orders as an unsigned number and shows values that are not finite.
+__device__ __forceinline__ float absmax3(float m, float a, float b) {
+    float r;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(m), "f"(a), "f"(b));
+    return r;
+}
 __device__ __forceinline__ void note(uint32_t* status, uint32_t code) { if (status) record_status(status, code); }
 
 // Step size and reciprocal of a block from the bit pattern of its absmax: the rule of the other quantizers
@@ -60,7 +67,10 @@ __device__ __forceinline__ float logistic_of(float g, float* dz) {
         z = c2 * g * fmaf(k, gg, 1.0f);
         *dz = c2 * fmaf(3.0f * k, gg, 1.0f);
     }
-    return __fdividef(1.0f, 1.0f + __expf(-z));
+    float e, p;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(z * -1.4426950408889634f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(p) : "f"(1.0f + e));
+    return p;
 }
 template <bool GELU>
 __device__ __forceinline__ float act_of(float g) {

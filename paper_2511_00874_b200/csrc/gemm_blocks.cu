@@ -66,7 +66,8 @@ struct GbTail {
     uint64_t scale_full[GB_SCALE_SLOTS], scale_empty[GB_SCALE_SLOTS];
     alignas(16) float row_scale[GB_SCALE_SLOTS][4][GB_M];   // [slot][k-block of the chunk][row]
     alignas(16) float col_scale[GB_SCALE_SLOTS][4][GB_N];   // [..][column of the tile], or [0], [1]: one per 128 columns
-    uint32_t amax[2][3][GB_CGROUPS][GB_M];         // gated block: [tile parity][which][column group][row]
+    uint32_t amax[2][3][GB_CGROUPS][GB_M];         // gated block: [tile parity][h, gate, up][column group][row]
+    float inv[2][3][GB_M];
 };
 constexpr size_t gb_smem() { return 1024 + (size_t)GB_STAGES * GB_STAGE_BYTES + GB_ADD_WARPS * GB_OUT_BYTES + sizeof(GbTail); }
 
@@ -399,55 +400,59 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                 constexpr int GH = GB_COLS / 2;
                 const int64_t f0 = col0 + GH * cg;
                 const bool live = row < P.M;
-                // the absmax of the row's 128 columns from those of the column groups
-                auto row_max = [&](int which) -> uint32_t {
-                    uint32_t m = 0u;
-#pragma unroll
-                    for (int i = 0; i < GB_CGROUPS; ++i) m = max(m, T->amax[par][which][i][trow]);
-                    return m;
-                };
-                auto emit = [&](const Blocks& o, uint32_t m, const float* val) {
-                    float step, inv;
-                    block_step(m, &step, &inv);
-                    uint32_t w[GH / 4];
-#pragma unroll
-                    for (int q = 0; q < GH / 4; ++q)
-                        w[q] = e4m3x4(__fmul_rn(val[4 * q], inv), __fmul_rn(val[4 * q + 1], inv), __fmul_rn(val[4 * q + 2], inv), __fmul_rn(val[4 * q + 3], inv));
-                    if (!live) return;
-                    if (block_nonfinite(m)) note(P.status, SRQ_ERR_NONFINITE);
-                    if (cg == 0) o.scale[row * o.ld_scale + tn] = step;
-                    store_codes(o.codes + row * o.ld, f0, P.N, w);
-                };
-                if (P.gate.codes || P.up.codes) {
-                    uint32_t mg = 0u, mu = 0u;
-#pragma unroll
-                    for (int i = 0; i < GH; ++i) { mg = max(mg, abs_word(acc[i])); mu = max(mu, abs_word(acc[GH + i])); }
-                    T->amax[par][0][cg][trow] = mg; T->amax[par][1][cg][trow] = mu;
-                    asm volatile("bar.sync 3, %0;" ::"n"(32 * GB_ADD_WARPS) : "memory");
-                    if (P.gate.codes) emit(P.gate, row_max(0), acc);
-                    if (P.up.codes) emit(P.up, row_max(1), acc + GH);
-                }
-                uint32_t mh = 0u;
+                const bool ckpt = P.gate.codes || P.up.codes;
+                float h[GH], mg = 0.0f, mu = 0.0f, mh = 0.0f;
                 if (P.gelu) {
 #pragma unroll
-                    for (int i = 0; i < GH; ++i) { acc[i] = act_of<true>(acc[i]) * acc[GH + i]; mh = max(mh, abs_word(acc[i])); }
+                    for (int i = 0; i < GH; ++i) h[i] = act_of<true>(acc[i]) * acc[GH + i];
                 } else {
 #pragma unroll
-                    for (int i = 0; i < GH; ++i) { acc[i] = act_of<false>(acc[i]) * acc[GH + i]; mh = max(mh, abs_word(acc[i])); }
+                    for (int i = 0; i < GH; ++i) h[i] = act_of<false>(acc[i]) * acc[GH + i];
+                }
+#pragma unroll
+                for (int i = 0; i < GH; i += 2) mh = absmax3(mh, h[i], h[i + 1]);
+                if (ckpt) {
+#pragma unroll
+                    for (int i = 0; i < GH; i += 2) { mg = absmax3(mg, acc[i], acc[i + 1]); mu = absmax3(mu, acc[GH + i], acc[GH + i + 1]); }
                 }
                 if (P.out && live) {
                     const bool vec = P.h_vec && f0 + GH <= P.N;
 #pragma unroll
                     for (int q = 0; q < GH / 8; ++q) {
-                        if (P.out_bf16) store8((__nv_bfloat16*)P.out + row * P.ldo, f0 + 8 * q, P.N, vec, acc + 8 * q);
-                        else store8((float*)P.out + row * P.ldo, f0 + 8 * q, P.N, vec, acc + 8 * q);
+                        if (P.out_bf16) store8((__nv_bfloat16*)P.out + row * P.ldo, f0 + 8 * q, P.N, vec, h + 8 * q);
+                        else store8((float*)P.out + row * P.ldo, f0 + 8 * q, P.N, vec, h + 8 * q);
                     }
                 }
-                if (P.h.codes) {
-                    T->amax[par][2][cg][trow] = mh;
-                    asm volatile("bar.sync 3, %0;" ::"n"(32 * GB_ADD_WARPS) : "memory");
-                    emit(P.h, row_max(2), acc);
+                // a row's 128 columns are in GB_CGROUPS threads: they meet once with their maxima, and thread cg of the row
+                // does the divisions of matrix cg (h, gate, up) for all of them
+                T->amax[par][0][cg][trow] = abs_word(mh);
+                if (ckpt) { T->amax[par][1][cg][trow] = abs_word(mg); T->amax[par][2][cg][trow] = abs_word(mu); }
+                asm volatile("bar.sync 3, %0;" ::"n"(32 * GB_ADD_WARPS) : "memory");
+                for (int which = cg; which < (ckpt ? 3 : 1); which += GB_CGROUPS) {
+                    const Blocks& o = which == 0 ? P.h : which == 1 ? P.gate : P.up;
+                    uint32_t m = 0u;
+#pragma unroll
+                    for (int i = 0; i < GB_CGROUPS; ++i) m = max(m, T->amax[par][which][i][trow]);
+                    float step, inv;
+                    block_step(m, &step, &inv);
+                    T->inv[par][which][trow] = inv;
+                    if (live && o.codes) {
+                        if (block_nonfinite(m)) note(P.status, SRQ_ERR_NONFINITE);
+                        o.scale[row * o.ld_scale + tn] = step;
+                    }
                 }
+                asm volatile("bar.sync 3, %0;" ::"n"(32 * GB_ADD_WARPS) : "memory");
+                auto emit = [&](const Blocks& o, int which, const float* val) {
+                    if (!live || !o.codes) return;
+                    const float inv = T->inv[par][which][trow];
+                    uint32_t w[GH / 4];
+#pragma unroll
+                    for (int q = 0; q < GH / 4; ++q)
+                        w[q] = e4m3x4(__fmul_rn(val[4 * q], inv), __fmul_rn(val[4 * q + 1], inv), __fmul_rn(val[4 * q + 2], inv), __fmul_rn(val[4 * q + 3], inv));
+                    store_codes(o.codes + row * o.ld, f0, P.N, w);
+                };
+                emit(P.h, 0, h);
+                if (ckpt) { emit(P.gate, 1, acc); emit(P.up, 2, acc + GH); }
                 par ^= 1;            // these words are written again two tiles on, a barrier after everyone has read them
             } else {
                 const int32_t wrow = (int32_t)(row0 + quarter * 32);
@@ -722,7 +727,7 @@ gemm_blocks_small_kernel(const __grid_constant__ CUtensorMap map_a, const __grid
             const int64_t row = t0 + t;
             if constexpr (GLU) {
                 auto emit = [&](const Blocks& o, const float (&val)[4]) {
-                    uint32_t m = max(max(abs_word(val[0]), abs_word(val[1])), max(abs_word(val[2]), abs_word(val[3])));
+                    uint32_t m = abs_word(absmax3(absmax3(val[0], val[1], val[2]), val[3], 0.0f));
                     m = __reduce_max_sync(0xFFFFFFFFu, m);
                     float step, inv;
                     block_step(m, &step, &inv);

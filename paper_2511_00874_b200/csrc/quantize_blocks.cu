@@ -38,8 +38,7 @@ __device__ __forceinline__ void emit_tile(const float (&v)[4][8], const uint32_t
     if (want_rm || tile_tr) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) row_max[i] = max(row_max[i], abs_word(v[i][j]));
+            row_max[i] = abs_word(absmax3(absmax3(v[i][0], v[i][1], v[i][2]), absmax3(v[i][3], v[i][4], v[i][5]), absmax3(v[i][6], v[i][7], 0.0f)));
 #pragma unroll
             for (int s = 1; s < 16; s <<= 1) row_max[i] = max(row_max[i], __shfl_xor_sync(0xFFFFFFFFu, row_max[i], s));
         }
@@ -56,7 +55,7 @@ __device__ __forceinline__ void emit_tile(const float (&v)[4][8], const uint32_t
         if (want_tr && !tile_tr) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                uint32_t m = max(max(abs_word(v[0][j]), abs_word(v[1][j])), max(abs_word(v[2][j]), abs_word(v[3][j])));
+                uint32_t m = abs_word(absmax3(absmax3(v[0][j], v[1][j], v[2][j]), v[3][j], 0.0f));
                 m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 16));
                 if (lane < 16) atomicMax(&S->col_max[j * 16 + p.l], m);
             }

@@ -48,9 +48,7 @@ __device__ __forceinline__ void norm_emit(const NormFwdParams& P, int64_t row, i
     const NormFwdArgs& a = P.a;
     const bool in = row < a.rows && c < a.cols;
     if (a.y.codes) {
-        uint32_t m = 0u;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) m = max(m, abs_word(y[e]));
+        uint32_t m = abs_word(absmax3(absmax3(y[0], y[1], y[2]), absmax3(y[3], y[4], y[5]), absmax3(y[6], y[7], 0.0f)));
 #pragma unroll
         for (int s = 1; s < 16; s <<= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, s));
         float step, inv;
