@@ -25,11 +25,17 @@ __device__ __forceinline__ void note(uint32_t* status, uint32_t code) { if (stat
 
 // Step size and reciprocal of a block from the bit pattern of its absmax: the rule of the other quantizers
 // with qmax = 448.  448 / m overflows binary32 exactly for m <= 7 * 2^-122, which stands for all zeros.
-__device__ __forceinline__ void block_step(uint32_t amax_bits, float* step, float* inv) {
+__device__ __forceinline__ float block_inv(uint32_t amax_bits) {
     const float m = __uint_as_float(amax_bits);
-    const bool live = m > 0x1.Cp-120f;
-    *inv = live ? __fdiv_rz(E4M3_MAX, m) : 0.0f;
-    *step = live ? __fdiv_rn(m, E4M3_MAX) : 0.0f;
+    return m > 0x1.Cp-120f ? __fdiv_rz(E4M3_MAX, m) : 0.0f;
+}
+__device__ __forceinline__ float block_size(uint32_t amax_bits) {
+    const float m = __uint_as_float(amax_bits);
+    return m > 0x1.Cp-120f ? __fdiv_rn(m, E4M3_MAX) : 0.0f;
+}
+__device__ __forceinline__ void block_step(uint32_t amax_bits, float* step, float* inv) {
+    *inv = block_inv(amax_bits);
+    *step = block_size(amax_bits);
 }
 // One NaN or infinite value makes the block's absmax (compared as an unsigned pattern) reach this.
 __device__ __forceinline__ bool block_nonfinite(uint32_t amax_bits) { return amax_bits >= 0x7F800000u; }

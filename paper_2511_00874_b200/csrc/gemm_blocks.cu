@@ -141,6 +141,14 @@ __device__ __forceinline__ void store_codes(uint8_t* row, int64_t c, int64_t col
     }
 }
 
+// The same for 32 bytes per row in the 32-byte swizzle (16-byte chunk index xor row / 4 mod 2).
+__device__ __forceinline__ void stage_rows32(uint32_t stage, int lane, const uint32_t (&w)[8]) {
+    const uint32_t row = stage + (uint32_t)lane * 32u;
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(row + (uint32_t)((q ^ ((lane >> 2) & 1)) << 4)),
+                     "r"(w[4 * q]), "r"(w[4 * q + 1]), "r"(w[4 * q + 2]), "r"(w[4 * q + 3]) : "memory");
+}
 // Thread `lane` holds 64 bytes of row `lane` of a block of 32 rows: writes them in the 64-byte swizzle of the output's
 // tensor map (16-byte chunk index xor row / 2 mod 4), which also spreads the 16-byte stores of a warp over all banks.
 __device__ __forceinline__ void stage_rows64(uint32_t stage, int lane, const uint32_t (&w)[16]) {
@@ -157,7 +165,8 @@ template <bool GLU, bool COLV>
 __global__ void __launch_bounds__(GB_THREADS, 1)
 gemm_blocks_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                    const __grid_constant__ CUtensorMap map_b2, const __grid_constant__ CUtensorMap map_out,
-                   const __grid_constant__ GemmBlocksParams P) {
+                   const __grid_constant__ CUtensorMap map_gate, const __grid_constant__ CUtensorMap map_up,
+                   const __grid_constant__ GemmBlocksParams P) {      // map_out: of out, or of h's codes
     pdl_trigger();                       // the wait follows the set-up below, which touches only shared memory and TMEM
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -398,6 +407,7 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
             if constexpr (GLU) {
                 // acc: GH gate columns, then the same GH up columns
                 constexpr int GH = GB_COLS / 2;
+                static_assert(GH == 32, "a warp's block of codes is 32 x 32");
                 const int64_t f0 = col0 + GH * cg;
                 const bool live = row < P.M;
                 const bool ckpt = P.gate.codes || P.up.codes;
@@ -423,36 +433,55 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                         else store8((float*)P.out + row * P.ldo, f0 + 8 * q, P.N, vec, h + 8 * q);
                     }
                 }
-                // a row's 128 columns are in GB_CGROUPS threads: they meet once with their maxima, and thread cg of the row
-                // does the divisions of matrix cg (h, gate, up) for all of them
+                // a row's 128 columns are in GB_CGROUPS threads: they meet with their maxima, and thread cg of the row does the
+                // divisions of matrix cg (h, gate, up) for all of them
                 T->amax[par][0][cg][trow] = abs_word(mh);
                 if (ckpt) { T->amax[par][1][cg][trow] = abs_word(mg); T->amax[par][2][cg][trow] = abs_word(mu); }
                 asm volatile("bar.sync 3, %0;" ::"n"(32 * GB_ADD_WARPS) : "memory");
-                for (int which = cg; which < (ckpt ? 3 : 1); which += GB_CGROUPS) {
-                    const Blocks& o = which == 0 ? P.h : which == 1 ? P.gate : P.up;
+                float m_mine = 0.0f, inv_mine;
+                if (cg < (ckpt ? 3 : 1)) {
                     uint32_t m = 0u;
 #pragma unroll
-                    for (int i = 0; i < GB_CGROUPS; ++i) m = max(m, T->amax[par][which][i][trow]);
-                    float step, inv;
-                    block_step(m, &step, &inv);
-                    T->inv[par][which][trow] = inv;
-                    if (live && o.codes) {
-                        if (block_nonfinite(m)) note(P.status, SRQ_ERR_NONFINITE);
-                        o.scale[row * o.ld_scale + tn] = step;
-                    }
+                    for (int i = 0; i < GB_CGROUPS; ++i) m = max(m, T->amax[par][cg][i][trow]);
+                    m_mine = __uint_as_float(m);
+                    T->inv[par][cg][trow] = inv_mine = block_inv(m);
                 }
                 asm volatile("bar.sync 3, %0;" ::"n"(32 * GB_ADD_WARPS) : "memory");
-                auto emit = [&](const Blocks& o, int which, const float* val) {
-                    if (!live || !o.codes) return;
+                const int32_t wrow = (int32_t)(row0 + quarter * 32);
+                auto emit = [&](const Blocks& o, const CUtensorMap* map, int which, uint32_t buffer, const float* val) {
+                    if (!o.codes) return;
                     const float inv = T->inv[par][which][trow];
                     uint32_t w[GH / 4];
 #pragma unroll
                     for (int q = 0; q < GH / 4; ++q)
                         w[q] = e4m3x4(__fmul_rn(val[4 * q], inv), __fmul_rn(val[4 * q + 1], inv), __fmul_rn(val[4 * q + 2], inv), __fmul_rn(val[4 * q + 3], inv));
-                    store_codes(o.codes + row * o.ld, f0, P.N, w);
+                    if (!P.tma_out) {
+                        if (live) store_codes(o.codes + row * o.ld, f0, P.N, w);
+                        return;
+                    }
+                    // 32 rows of 32 codes through shared memory: straight from the registers each store instruction touched 32
+                    // lines for 16 bytes each, and a tile's codes took longer than half of its main loop
+                    stage_rows32(buffer, lane, w);
+                    fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0 && wrow < P.M && f0 < P.N) { tma_store_2d(map, buffer, (int32_t)f0, wrow); bulk_commit(); }
                 };
-                emit(P.h, 0, h);
-                if (ckpt) { emit(P.gate, 1, acc); emit(P.up, 2, acc + GH); }
+                if (lane == 0) bulk_wait_read();         // the last tile's codes have left the two buffers
+                __syncwarp();
+                if (ckpt) {
+                    emit(P.gate, &map_gate, 1, stage, acc);
+                    emit(P.up, &map_up, 2, stage + 1024, acc + GH);
+                    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");      // the gate's
+                    __syncwarp();
+                }
+                emit(P.h, &map_out, 0, stage, h);
+                if (cg < (ckpt ? 3 : 1) && live) {
+                    const Blocks& o = cg == 0 ? P.h : cg == 1 ? P.gate : P.up;
+                    if (o.codes) {
+                        if (block_nonfinite(__float_as_uint(m_mine))) note(P.status, SRQ_ERR_NONFINITE);
+                        o.scale[row * o.ld_scale + tn] = block_size(__float_as_uint(m_mine));
+                    }
+                }
                 par ^= 1;            // these words are written again two tiles on, a barrier after everyone has read them
             } else {
                 const int32_t wrow = (int32_t)(row0 + quarter * 32);
@@ -785,17 +814,17 @@ static bool encode_codes(CUtensorMap* map, const Blocks& b, int64_t rows, int64_
     return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, (void*)b.codes, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-static bool encode_result(CUtensorMap* map, void* base, bool bf16, int64_t rows, int64_t cols, int64_t ld) {
+// What leaves through block stores: boxes of 32 rows, 64 bytes of binary32 or bfloat16 (esize 4 or 2) or 32 codes (esize 1) wide.
+static bool encode_result(CUtensorMap* map, void* base, unsigned esize, int64_t rows, int64_t cols, int64_t ld) {
     EncodeTiledFn enc = get_encode();
     if (!enc) return false;
-    const unsigned esize = bf16 ? 2 : 4;
     cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
     cuuint64_t strides[1] = {(cuuint64_t)ld * esize};
-    cuuint32_t box[2] = {64 / esize, 32};
+    cuuint32_t box[2] = {esize == 1 ? 32u : 64u / esize, 32};
     cuuint32_t estr[2] = {1, 1};
-    return enc(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, base, dims, strides, box, estr,
-               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
-               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    return enc(map, esize == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : esize == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2,
+               base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, esize == 1 ? CU_TENSOR_MAP_SWIZZLE_32B : CU_TENSOR_MAP_SWIZZLE_64B,
+               CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // Per device: SM count, resident CTA pairs, resident clusters of the few-token kernel by cluster size.
@@ -879,14 +908,14 @@ static cudaError_t launch_small_bn(const CUtensorMap& ma, const CUtensorMap& mb,
 
 template <bool GLU, bool COLV>
 static cudaError_t launch_pair(const CUtensorMap& ma, const CUtensorMap& mb, const CUtensorMap& mb2, const CUtensorMap& mo,
-                               const GemmBlocksParams& P, unsigned pairs, cudaStream_t stream) {
+                               const CUtensorMap& mg, const CUtensorMap& mu, const GemmBlocksParams& P, unsigned pairs, cudaStream_t stream) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(pairs * 2); cfg.blockDim = dim3(GB_THREADS); cfg.dynamicSmemBytes = gb_smem(); cfg.stream = stream;
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeClusterDimension; at[0].val.clusterDim.x = 2; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
     at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization; at[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at; cfg.numAttrs = pdl_allowed(stream) ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, gemm_blocks_kernel<GLU, COLV>, ma, mb, mb2, mo, P);
+    return cudaLaunchKernelEx(&cfg, gemm_blocks_kernel<GLU, COLV>, ma, mb, mb2, mo, mg, mu, P);
 }
 
 // Few-token form: as many tokens per CTA as cover M, 128 at most (64 in the gated block, whose sums are two).
@@ -920,22 +949,26 @@ static srq_status_t run_pairs(const BlocksDevice& d, GemmBlocksParams& P, bool g
     if (d.pairs <= 0) return SRQ_ERR_UNSUPPORTED;
     P.tiles_m = (int32_t)((P.M + 2 * GB_M - 1) / (2 * GB_M));
     P.tiles_n = (int32_t)((P.N + (glu ? 128 : GB_N) - 1) / (glu ? 128 : GB_N));
-    CUtensorMap ma, mb, mb2, mo;
+    CUtensorMap ma, mb, mb2, mo, mg, mu;
     if (!encode_codes(&ma, P.a, P.M, Kc, GB_M) || !encode_codes(&mb, P.b, P.N, Kc, 64)) return SRQ_ERR_CUDA;
-    mb2 = mb; mo = mb;
+    mb2 = mb; mo = mb; mg = mb; mu = mb;
     if (glu && !encode_codes(&mb2, P.b2, P.N, Kc, 64)) return SRQ_ERR_CUDA;
     const int per16 = P.out_bf16 ? 8 : 4;
     const bool out16 = P.out && (uintptr_t)P.out % 16 == 0 && P.ldo % per16 == 0;
     P.h_vec = out16;
     // a row must also end on a 16-byte boundary: a block store that reaches over the map's edge may write the whole
     // last 16-byte piece
-    P.tma_out = !glu && out16 && P.N % per16 == 0 && encode_result(&mo, P.out, P.out_bf16, P.M, P.N, P.ldo);
+    if (!glu) P.tma_out = out16 && P.N % per16 == 0 && encode_result(&mo, P.out, P.out_bf16 ? 2 : 4, P.M, P.N, P.ldo);
+    else
+        P.tma_out = P.N % 16 == 0 && (!P.h.codes || encode_result(&mo, P.h.codes, 1, P.M, P.N, P.h.ld)) &&
+                    (!P.gate.codes || encode_result(&mg, P.gate.codes, 1, P.M, P.N, P.gate.ld)) &&
+                    (!P.up.codes || encode_result(&mu, P.up.codes, 1, P.M, P.N, P.up.ld));
     const int64_t tiles = (int64_t)P.tiles_m * P.tiles_n;
     const unsigned pairs = (unsigned)(tiles < d.pairs ? tiles : d.pairs);
     const bool colv = P.b.tile_rows == 1;
     cudaError_t e;
-    if (glu) e = colv ? launch_pair<true, true>(ma, mb, mb2, mo, P, pairs, stream) : launch_pair<true, false>(ma, mb, mb2, mo, P, pairs, stream);
-    else e = colv ? launch_pair<false, true>(ma, mb, mb2, mo, P, pairs, stream) : launch_pair<false, false>(ma, mb, mb2, mo, P, pairs, stream);
+    if (glu) e = colv ? launch_pair<true, true>(ma, mb, mb2, mo, mg, mu, P, pairs, stream) : launch_pair<true, false>(ma, mb, mb2, mo, mg, mu, P, pairs, stream);
+    else e = colv ? launch_pair<false, true>(ma, mb, mb2, mo, mg, mu, P, pairs, stream) : launch_pair<false, false>(ma, mb, mb2, mo, mg, mu, P, pairs, stream);
     count_launch();
     return e == cudaSuccess ? SRQ_OK : SRQ_ERR_CUDA;
 }
