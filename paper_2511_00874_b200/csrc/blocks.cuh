@@ -23,14 +23,35 @@ __device__ __forceinline__ float absmax3(float m, float a, float b) {
 }
 __device__ __forceinline__ void note(uint32_t* status, uint32_t code) { if (status) record_status(status, code); }
 
-// Step size and reciprocal of a block from the bit pattern of its absmax: the rule of the other quantizers
-// with qmax = 448.  448 / m overflows binary32 exactly for m <= 7 * 2^-122, which stands for all zeros.
+// Step size and reciprocal of a block from the bit pattern of its absmax m: the rule of the other quantizers with
+// qmax = 448.  448 / m overflows binary32 exactly for m <= 7 * 2^-122, which stands for all zeros.
+// The library's correctly rounded divisions took a good part of the kernels' time where a few threads divide and
+// the rest wait.  In the range where nothing over- or underflows both quotients are formed from an approximation
+// and the sign or size of the exact residual (a - q b in one fused multiply-add; Markstein, IBM J. Res. Dev.
+// 34(1), 1990):
+//   inv  = largest q with q m <= 448: after one correction q is at most one unit off, and the residuals of q and of
+//          its upper neighbour say which of the three numbers it is;
+//   step = m / 448 to nearest: q = m c, c = 1 / 448 to nearest, corrected once.
+constexpr float DIV_LO = 0x1p-100f, DIV_HI = 0x1p100f;
 __device__ __forceinline__ float block_inv(uint32_t amax_bits) {
     const float m = __uint_as_float(amax_bits);
+    if (m > DIV_LO && m < DIV_HI) {
+        float r;
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(m));
+        float q = __fmul_rn(E4M3_MAX, r);
+        q = __fmaf_rn(__fmaf_rn(-q, m, E4M3_MAX), r, q);
+        const float up = __uint_as_float(__float_as_uint(q) + 1u), down = __uint_as_float(__float_as_uint(q) - 1u);
+        return __fmaf_rn(-up, m, E4M3_MAX) >= 0.0f ? up : __fmaf_rn(-q, m, E4M3_MAX) >= 0.0f ? q : down;
+    }
     return m > 0x1.Cp-120f ? __fdiv_rz(E4M3_MAX, m) : 0.0f;
 }
 __device__ __forceinline__ float block_size(uint32_t amax_bits) {
     const float m = __uint_as_float(amax_bits);
+    if (m > DIV_LO && m < DIV_HI) {
+        constexpr float c = 1.0f / 448.0f;
+        const float q = __fmul_rn(m, c);
+        return __fmaf_rn(__fmaf_rn(-E4M3_MAX, q, m), c, q);
+    }
     return m > 0x1.Cp-120f ? __fdiv_rn(m, E4M3_MAX) : 0.0f;
 }
 __device__ __forceinline__ void block_step(uint32_t amax_bits, float* step, float* inv) {

@@ -123,6 +123,27 @@ def test_quantizer_zero_tiny_and_wide_blocks():
         check_quantizer(x, x, q, 128, 128)
 
 
+def test_step_sizes_of_a_million_maxima():
+    # one value per block: step size and (through the codes of the block's other values) reciprocal of every mantissa class
+    g = np.random.default_rng(5)
+    n = 1 << 20
+    bits = g.integers(0, 1 << 23, n, dtype=np.uint32) | (g.integers(1, 254, n, dtype=np.uint32) << 23)
+    bits[:4096] = (127 << 23) + np.arange(4096, dtype=np.uint32)                  # mantissas next to a power of two
+    bits[4096:8192] = (128 << 23) - 1 - np.arange(4096, dtype=np.uint32)
+    bits[8192:12288] = np.arange(4096, dtype=np.uint32) + np.float32(7.0).view(np.uint32) - 2048       # and next to 448 / 2^k
+    m = bits.view(np.float32)
+    x = np.zeros((n // 64, 64, 128), np.float32)
+    x[..., 0] = m.reshape(-1, 64)
+    f = g.uniform(0.4, 1.0, (n // 64, 64, 3)).astype(np.float32)
+    x[..., 1:4] = x[..., :1] * f
+    x = x.reshape(n // 64, 64 * 128)
+    codes, step = ref.quantize(x)
+    b = srq.new_blocks(n // 64, 64 * 128)
+    srq.srq_quantize_blocks(torch.from_numpy(x).cuda(), srq.BLOCK_RNE, b)
+    assert np.array_equal(b.scale.cpu().numpy(), step)
+    assert np.array_equal(b.codes.cpu().numpy(), codes)
+
+
 @pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
 def test_quantizer_reports_values_that_are_not_finite(value):
     x = skewed(130, 130, 5)
