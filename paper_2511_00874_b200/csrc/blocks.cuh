@@ -84,25 +84,36 @@ __device__ __forceinline__ void e4m3x4_to_f32(uint32_t w, float v[4]) {
 //   GELU (tanh)  z = 2 u(g)       act = g p     act' = p + g p (1 - p) 2 u'(g),   u = c (g + 0.044715 g^3)
 // ((1 + tanh u) / 2 = 1 / (1 + e^-2u): no cancellation for negative g).  e^-z overflows to infinity for
 // very negative z, and p is then 0.
-template <bool GELU>
-__device__ __forceinline__ float logistic_of(float g, float* dz) {
-    float z = g;
-    *dz = 1.0f;
-    if constexpr (GELU) {
-        const float c2 = 1.5957691216057308f, k = 0.044715f;     // 2 sqrt(2 / pi)
-        const float gg = g * g;
-        z = c2 * g * fmaf(k, gg, 1.0f);
-        *dz = c2 * fmaf(3.0f * k, gg, 1.0f);
-    }
-    float e, p;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(z * -1.4426950408889634f));
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(p) : "f"(1.0f + e));
-    return p;
+__device__ __forceinline__ float exp2_fast(float x) {
+    float e;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x));
+    return e;
 }
+__device__ __forceinline__ float rcp_fast(float x) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+// p of two values; dz: z'(g), GELU only (it is 1 for SiLU).
 template <bool GELU>
-__device__ __forceinline__ float act_of(float g) {
-    float dz;
-    return g * logistic_of<GELU>(g, &dz);
+__device__ __forceinline__ float2 logistic2(float2 g, float2* dz) {
+    const float2 minus_log2e = make_float2(-1.4426950408889634f, -1.4426950408889634f), one = make_float2(1.0f, 1.0f);
+    float2 z = g;
+    if constexpr (GELU) {
+        const float c = 1.5957691216057308f, k = 0.044715f;      // 2 sqrt(2 / pi)
+        const float2 c2 = make_float2(c, c), gg = __fmul2_rn(g, g);
+        z = __fmul2_rn(__fmul2_rn(c2, g), __ffma2_rn(make_float2(k, k), gg, one));
+        *dz = __fmul2_rn(c2, __ffma2_rn(make_float2(3.0f * k, 3.0f * k), gg, one));
+    }
+    const float2 e = __fmul2_rn(z, minus_log2e);
+    const float2 d = __fadd2_rn(make_float2(exp2_fast(e.x), exp2_fast(e.y)), one);
+    return make_float2(rcp_fast(d.x), rcp_fast(d.y));
+}
+// act(g) * u of two values.
+template <bool GELU>
+__device__ __forceinline__ float2 gated2(float2 g, float2 u) {
+    float2 unused;
+    return __fmul2_rn(__fmul2_rn(g, logistic2<GELU>(g, &unused)), u);
 }
 
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
@@ -187,7 +198,8 @@ __device__ __forceinline__ uint32_t encode4(const float v0, const float v1, cons
         const uint32_t c2 = quantize_e4m3<MODE_SR | MODE_E4M3>(v2, i2, r2, 0), c3 = quantize_e4m3<MODE_SR | MODE_E4M3>(v3, i3, r3, 0);
         return __byte_perm(__byte_perm(c0, c1, 0x0040), __byte_perm(c2, c3, 0x0040), 0x5410);
     } else {
-        return e4m3x4(__fmul_rn(v0, i0), __fmul_rn(v1, i1), __fmul_rn(v2, i2), __fmul_rn(v3, i3));
+        const float2 a = __fmul2_rn(make_float2(v0, v1), make_float2(i0, i1)), b = __fmul2_rn(make_float2(v2, v3), make_float2(i2, i3));
+        return e4m3x4(a.x, a.y, b.x, b.y);
     }
 }
 

@@ -28,6 +28,7 @@
 #include <cuda.h>
 
 #include <mutex>
+#include <type_traits>
 
 #include "blocks.cuh"
 #include "tensor_core.cuh"
@@ -412,13 +413,14 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                 const bool live = row < P.M;
                 const bool ckpt = P.gate.codes || P.up.codes;
                 float h[GH], mg = 0.0f, mu = 0.0f, mh = 0.0f;
-                if (P.gelu) {
+                auto gate_all = [&](auto gelu) {
 #pragma unroll
-                    for (int i = 0; i < GH; ++i) h[i] = act_of<true>(acc[i]) * acc[GH + i];
-                } else {
-#pragma unroll
-                    for (int i = 0; i < GH; ++i) h[i] = act_of<false>(acc[i]) * acc[GH + i];
-                }
+                    for (int i = 0; i < GH; i += 2) {
+                        const float2 y = gated2<decltype(gelu)::value>(make_float2(acc[i], acc[i + 1]), make_float2(acc[GH + i], acc[GH + i + 1]));
+                        h[i] = y.x; h[i + 1] = y.y;
+                    }
+                };
+                if (P.gelu) gate_all(std::true_type()); else gate_all(std::false_type());
 #pragma unroll
                 for (int i = 0; i < GH; i += 2) mh = absmax3(mh, h[i], h[i + 1]);
                 if (ckpt) {
@@ -454,7 +456,7 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                     uint32_t w[GH / 4];
 #pragma unroll
                     for (int q = 0; q < GH / 4; ++q)
-                        w[q] = e4m3x4(__fmul_rn(val[4 * q], inv), __fmul_rn(val[4 * q + 1], inv), __fmul_rn(val[4 * q + 2], inv), __fmul_rn(val[4 * q + 3], inv));
+                        w[q] = encode4<false>(val[4 * q], val[4 * q + 1], val[4 * q + 2], val[4 * q + 3], inv, inv, inv, inv, 0, 0, 0, 0);
                     if (!P.tma_out) {
                         if (live) store_codes(o.codes + row * o.ld, f0, P.N, w);
                         return;
@@ -773,7 +775,10 @@ gemm_blocks_small_kernel(const __grid_constant__ CUtensorMap map_a, const __grid
                 if (P.gate.codes) emit(P.gate, x);
                 if (P.up.codes) emit(P.up, y);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] = (P.gelu ? act_of<true>(x[e]) : act_of<false>(x[e])) * y[e];
+                for (int e = 0; e < 4; e += 2) {
+                    const float2 g2 = make_float2(x[e], x[e + 1]), u2 = make_float2(y[e], y[e + 1]), h2 = P.gelu ? gated2<true>(g2, u2) : gated2<false>(g2, u2);
+                    x[e] = h2.x; x[e + 1] = h2.y;
+                }
                 if (P.h.codes) emit(P.h, x);
             }
             if (P.out) {

@@ -1,254 +1,508 @@
 // Block-scaled E4M3 quantizer (1 x 128 blocks or 128 x 128 tiles, row-major and / or transposed) and the
 // backward pass of the gated feed-forward block, which is the same kernel over values it computes itself.
 //
-// One CTA of 512 threads per 128 x 128 tile.  Thread (g, l), g = 0..31, l = 0..15, holds rows 4 g .. 4 g + 3 of
-// columns 8 l .. 8 l + 7 in registers, so that
+// 128 x 128 tiles, 512 threads per CTA, persistent CTAs.  Thread (g, l), g = 0..31, l = 0..15, holds rows
+// 4 g .. 4 g + 3 of columns 8 l .. 8 l + 7 in registers, so that
 //   - a row's 128 values sit in 16 neighbouring lanes: its absmax is four shuffles;
 //   - a column's 128 values sit in 32 threads of 16 warps: its absmax is one shuffle and one shared atomic;
 //   - the transposed codes of a thread are 8 words of 4 bytes, which meet in a swizzled shared tile.
-// The tile is read once whatever is written: both layouts and both kinds of step size come from the registers.
-// Bound by HBM.
+// A tile is read once whatever is written: both layouts and both kinds of step size come from the registers.
+// While a tile is worked on, the next one is on its way into shared memory (cp.async, 16 bytes at a time: smaller
+// pieces were measured to cost a shared-memory wavefront per lane); tiles that reach over the matrix's edge, and sources
+// whose alignment does not allow it, are read directly with bounds checks.
+// The kernels are bound by instruction issue as much as by HBM, hence the two-at-a-time binary32 instructions.
+#include <mutex>
+#include <type_traits>
+
 #include "blocks.cuh"
 
 namespace srq {
 
 constexpr int TQ_THREADS = 512;
 
+// NOUT matrices are quantized from one tile (1, or the three of the gated block's backward pass).
+template <int NOUT>
 struct TileShared {
-    uint32_t col_max[QBLK];          // [column % 8][column / 8]: a warp's atomics hit 16 different banks
-    float col_inv[QBLK];             // same order
-    uint32_t tile_max;
-    uint32_t words[QBLK * 32];       // transposed codes: column c's rows 4 g .. 4 g + 3 at [c][g ^ 2 (c / 8)]
+    uint32_t col_max[2][NOUT][QBLK];     // [tile parity][matrix][column % 8][column / 8]: a warp's atomics hit 16 banks
+    alignas(8) float col_inv[NOUT][QBLK];          // [column % 8 / 2][column / 8][column % 2]: read two by two
+    uint32_t tile_max[2];
+    alignas(16) uint32_t words[NOUT][QBLK * 32];   // transposed codes: column c's rows 4 g .. 4 g + 3 at [c][g ^ 2 (c / 8)]
 };
 
 struct TilePos {
-    int64_t r0, c0, rows, cols;      // tile origin, extents of the matrix
-    int g, l;                        // row quad and column octet of the thread
+    int64_t r0, c0;                      // tile origin
+    bool full;                           // inside the matrix and read ahead through shared memory
 };
 
-// Quantizes the tile held as v (zeros outside the matrix) into rm and / or tr.  rnd: thresholds (SR only).
-// All threads of the CTA call it together.
-template <bool SR>
-__device__ __forceinline__ void emit_tile(const float (&v)[4][8], const uint32_t (&rnd)[SR ? 4 : 1][8], const Blocks& rm,
-                                          const Blocks& tr, const TilePos& p, TileShared* S, uint32_t* status) {
-    const int tid = threadIdx.x, lane = tid & 31;
-    const bool want_rm = rm.codes != nullptr, want_tr = tr.codes != nullptr;
-    const bool tile_rm = want_rm && rm.tile_rows > 1, tile_tr = want_tr && tr.tile_rows > 1;
-    uint32_t row_max[4] = {0u, 0u, 0u, 0u};
-    if (want_rm || tile_tr) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            row_max[i] = abs_word(absmax3(absmax3(v[i][0], v[i][1], v[i][2]), absmax3(v[i][3], v[i][4], v[i][5]), absmax3(v[i][6], v[i][7], 0.0f)));
-#pragma unroll
-            for (int s = 1; s < 16; s <<= 1) row_max[i] = max(row_max[i], __shfl_xor_sync(0xFFFFFFFFu, row_max[i], s));
-        }
-    }
-    if (want_tr || tile_rm) {        // the CTA has to meet
-        if (tid < QBLK) S->col_max[tid] = 0u;
-        if (tid == 0) S->tile_max = 0u;
-        __syncthreads();
-        if (tile_rm || tile_tr) {
-            uint32_t m = max(max(row_max[0], row_max[1]), max(row_max[2], row_max[3]));
-            m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 16));
-            if (lane == 0) atomicMax(&S->tile_max, m);
-        }
-        if (want_tr && !tile_tr) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                uint32_t m = abs_word(absmax3(absmax3(v[0][j], v[1][j], v[2][j]), v[3][j], 0.0f));
-                m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 16));
-                if (lane < 16) atomicMax(&S->col_max[j * 16 + p.l], m);
-            }
-        }
-        __syncthreads();
-        if (want_tr && tid < QBLK) {
-            const int64_t c = p.c0 + (tid & 15) * 8 + (tid >> 4);
-            const uint32_t m = tile_tr ? S->tile_max : S->col_max[tid];
-            float step, inv;
-            block_step(m, &step, &inv);
-            S->col_inv[tid] = inv;
-            if (block_nonfinite(m)) note(status, SRQ_ERR_NONFINITE);
-            if (!tile_tr && c < p.cols) tr.scale[c * tr.ld_scale + p.r0 / QBLK] = step;
-            if (tile_tr && tid == 0) tr.scale[(p.c0 / QBLK) * tr.ld_scale + p.r0 / QBLK] = step;
-        }
-    }
-    if (want_rm) {
-        // the divisions of four rows once per thread: lane l of a row's sixteen does row l % 4's
-        const int pick = p.l & 3;
-        uint32_t m = pick == 0 ? row_max[0] : pick == 1 ? row_max[1] : pick == 2 ? row_max[2] : row_max[3];
-        if (tile_rm) m = S->tile_max;
-        float step, inv;
-        block_step(m, &step, &inv);
-        if (block_nonfinite(m)) note(status, SRQ_ERR_NONFINITE);
-        const int64_t r_mine = p.r0 + 4 * p.g + pick;
-        if (!tile_rm && p.l < 4 && r_mine < p.rows) rm.scale[r_mine * rm.ld_scale + p.c0 / QBLK] = step;
-        if (tile_rm && tid == 0) rm.scale[(p.r0 / QBLK) * rm.ld_scale + p.c0 / QBLK] = step;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float f = __shfl_sync(0xFFFFFFFFu, inv, (lane & 16) + i);
-            const int64_t r = p.r0 + 4 * p.g + i, c = p.c0 + 8 * p.l;
-            uint32_t w[2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-                w[h] = encode4<SR>(v[i][4 * h], v[i][4 * h + 1], v[i][4 * h + 2], v[i][4 * h + 3], f, f, f, f,
-                                   rnd[SR ? i : 0][4 * h], rnd[SR ? i : 0][4 * h + 1], rnd[SR ? i : 0][4 * h + 2], rnd[SR ? i : 0][4 * h + 3]);
-            if (r < p.rows && c < p.cols) store_codes8(rm.codes + r * rm.ld, c, p.cols, w[0], w[1]);
-        }
-    }
-    if (want_tr) {
-        __syncthreads();             // reciprocals are there
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float f = S->col_inv[j * 16 + p.l];
-            S->words[(8 * p.l + j) * 32 + (p.g ^ (2 * p.l))] =
-                encode4<SR>(v[0][j], v[1][j], v[2][j], v[3][j], f, f, f, f, rnd[0][j], rnd[SR ? 1 : 0][j], rnd[SR ? 2 : 0][j], rnd[SR ? 3 : 0][j]);
-        }
-        __syncthreads();
-        const int warp = tid >> 5;
-        const int64_t r = p.r0 + 4 * lane;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const int cc = 8 * warp + k;
-            const int64_t c = p.c0 + cc;
-            if (c >= p.cols || r >= p.rows) continue;
-            const uint32_t w = S->words[cc * 32 + (lane ^ (2 * warp))];
-            uint8_t* dst = tr.codes + c * tr.ld + r;
-            if (r + 4 <= p.rows) *reinterpret_cast<uint32_t*>(dst) = w;
-            else
-                for (int e = 0; e < 4 && r + e < p.rows; ++e) dst[e] = (uint8_t)(w >> (8 * e));
-        }
-    }
-}
-
-__device__ __forceinline__ TilePos tile_pos(int64_t rows, int64_t cols) {
-    const int64_t n_tc = (cols + QBLK - 1) / QBLK;
+__device__ __forceinline__ TilePos tile_at(uint32_t tile, uint32_t tiles_c, int64_t rows, int64_t cols, int vec) {
     TilePos p;
-    p.r0 = (int64_t)blockIdx.x / n_tc * QBLK;
-    p.c0 = (int64_t)blockIdx.x % n_tc * QBLK;
-    p.rows = rows; p.cols = cols;
-    p.l = threadIdx.x & 15; p.g = threadIdx.x >> 4;
+    const uint32_t tr = tile / tiles_c;
+    p.r0 = (int64_t)tr * QBLK;
+    p.c0 = (int64_t)(tile - tr * tiles_c) * QBLK;
+    p.full = vec && p.r0 + QBLK <= rows && p.c0 + QBLK <= cols;
     return p;
 }
 
-// Eight consecutive numbers of a block-coded row (c a multiple of 8; columns >= cols read as 0).
-__device__ __forceinline__ void load_coded8(const Blocks& b, int64_t r, int64_t c, int64_t cols, float v[8]) {
-    const uint8_t* row = b.codes + r * b.ld;
-    uint2 w = make_uint2(0u, 0u);
-    if (c + 8 <= cols) {
-        w = *reinterpret_cast<const uint2*>(row + c);
-    } else {
-        for (int e = 0; e < 8; ++e)
-            if (c + e < cols) (e < 4 ? w.x : w.y) |= (uint32_t)row[c + e] << (8 * (e & 3));
-    }
-    const float s = c < cols ? b.scale[(b.tile_rows > 1 ? r / QBLK : r) * b.ld_scale + c / QBLK] : 0.0f;
-    e4m3x4_to_f32(w.x, v);
-    e4m3x4_to_f32(w.y, v + 4);
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group 0;" ::: "memory"); }
+__device__ __forceinline__ uint32_t shared_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+// Read-ahead shared memory: a matrix's tile in one buffer (bfloat16: each thread its own values; binary32: a row's 16-byte
+// chunks lane by lane, since a thread's own eight values are two chunks and every sector would be asked for twice,
+// so the next tile is asked for only when every thread has read its share); a block-coded matrix's tile row by
+// row, and its rows' step sizes (two buffers each, in turn).
+template <typename T> __host__ __device__ constexpr int matrix_slot() { return TQ_THREADS * 32 * (int)sizeof(T); }
+constexpr int CODED_TILE = QBLK * QBLK;
+__host__ __device__ constexpr int coded_slot() { return 2 * (CODED_TILE + QBLK * 4); }
+
+// Thread's share of a matrix / a block-coded matrix: into shared memory ahead of time, and from there (ahead) or
+// from global memory (with bounds checks) into registers.
+template <typename T>
+__device__ __forceinline__ void fetch_matrix(uint8_t* slot, const T* x, int64_t ld, const TilePos& p) {
+    if constexpr (sizeof(T) == 4) {
+        const int k = threadIdx.x & 31, row = threadIdx.x >> 5;            // chunk k of rows row, row + 16, ...
+        const T* src = x + (p.r0 + row) * ld + p.c0 + 4 * k;
+        // neighbouring chunks change places in every other group of eight: a thread's two reads hit all banks
+        const uint32_t dst = shared_addr(slot) + row * 512 + ((k ^ ((k >> 3) & 1)) << 4);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = __fmul_rn(v[e], s);
+        for (int i = 0; i < 8; ++i, src += 16 * ld) cp_async16(dst + i * 16 * 512, src);
+    } else {
+        const int l = threadIdx.x & 15, g = threadIdx.x >> 4;
+        const T* src = x + (p.r0 + 4 * g) * ld + p.c0 + 8 * l;
+        const uint32_t dst = shared_addr(slot) + threadIdx.x * 16;
+#pragma unroll
+        for (int i = 0; i < 4; ++i, src += ld) cp_async16(dst + i * TQ_THREADS * 16, src);
+    }
+}
+template <typename T>
+__device__ __forceinline__ void read_matrix(const uint8_t* slot, const T* x, int64_t ld, int64_t rows, int64_t cols, int vec, const TilePos& p, float (&v)[4][8]) {
+    const int l = threadIdx.x & 15, g = threadIdx.x >> 4;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (p.full) {
+            const uint4* s = reinterpret_cast<const uint4*>(slot) + threadIdx.x;
+            if constexpr (sizeof(T) == 4) {
+                const uint4* row = reinterpret_cast<const uint4*>(slot) + (4 * g + i) * 32;
+                const uint4 a = row[(2 * l) ^ ((l >> 2) & 1)], b = row[(2 * l + 1) ^ ((l >> 2) & 1)];
+                v[i][0] = __uint_as_float(a.x); v[i][1] = __uint_as_float(a.y); v[i][2] = __uint_as_float(a.z); v[i][3] = __uint_as_float(a.w);
+                v[i][4] = __uint_as_float(b.x); v[i][5] = __uint_as_float(b.y); v[i][6] = __uint_as_float(b.z); v[i][7] = __uint_as_float(b.w);
+            } else {
+                const uint4 a = s[i * TQ_THREADS];
+                v[i][0] = bf16_lo(a.x); v[i][1] = bf16_hi(a.x); v[i][2] = bf16_lo(a.y); v[i][3] = bf16_hi(a.y);
+                v[i][4] = bf16_lo(a.z); v[i][5] = bf16_hi(a.z); v[i][6] = bf16_lo(a.w); v[i][7] = bf16_hi(a.w);
+            }
+        } else {
+            const int64_t r = p.r0 + 4 * g + i;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[i][j] = 0.0f;
+            if (r < rows) load8(x + r * ld, p.c0 + 8 * l, cols, vec, v[i]);
+        }
+    }
+}
+__device__ __forceinline__ void fetch_coded(uint8_t* slot, const Blocks& b, const TilePos& p) {
+    const int row = threadIdx.x >> 3, q = threadIdx.x & 7;             // eight threads to a row's 128 codes
+    const uint8_t* src = b.codes + (p.r0 + row) * b.ld + p.c0 + 16 * q;
+    const uint32_t dst = shared_addr(slot) + row * QBLK + 16 * q;
+    cp_async16(dst, src);
+    cp_async16(dst + 64 * QBLK, src + 64 * b.ld);
+}
+// The step size of row `row` of a tile, on its way to coded_scales() of its buffer.
+__device__ __forceinline__ float fetch_scale(const Blocks& b, const TilePos& p, int row) {
+    return __ldg(b.scale + (b.tile_rows > 1 ? p.r0 / QBLK : p.r0 + row) * b.ld_scale + p.c0 / QBLK);
+}
+__device__ __forceinline__ uint8_t* coded_codes(uint8_t* slot, int par) { return slot + par * CODED_TILE; }
+__device__ __forceinline__ float* coded_scales(uint8_t* slot, int par) { return reinterpret_cast<float*>(slot + 2 * CODED_TILE) + par * QBLK; }
+
+__device__ __forceinline__ void read_coded(uint8_t* slot, int par, const Blocks& b, int64_t rows, int64_t cols, const TilePos& p, float (&v)[4][8]) {
+    const int l = threadIdx.x & 15, g = threadIdx.x >> 4;
+    const float4 sc = *reinterpret_cast<const float4*>(coded_scales(slot, par) + 4 * g);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint2 w = make_uint2(0u, 0u);
+        float s = i == 0 ? sc.x : i == 1 ? sc.y : i == 2 ? sc.z : sc.w;
+        if (p.full) {
+            w = *reinterpret_cast<const uint2*>(coded_codes(slot, par) + (4 * g + i) * QBLK + 8 * l);
+        } else {
+            const int64_t r = p.r0 + 4 * g + i, c = p.c0 + 8 * l;
+            s = 0.0f;
+            if (r < rows && c < cols) {
+                const uint8_t* row = b.codes + r * b.ld;
+                if (c + 8 <= cols) w = *reinterpret_cast<const uint2*>(row + c);
+                else
+                    for (int e = 0; e < 8; ++e)
+                        if (c + e < cols) (e < 4 ? w.x : w.y) |= (uint32_t)row[c + e] << (8 * (e & 3));
+                s = b.scale[(b.tile_rows > 1 ? r / QBLK : r) * b.ld_scale + c / QBLK];
+            }
+        }
+        e4m3x4_to_f32(w.x, v[i]);
+        e4m3x4_to_f32(w.y, v[i] + 4);
+        const float2 s2 = make_float2(s, s);
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+            const float2 y = __fmul2_rn(make_float2(v[i][e], v[i][e + 1]), s2);
+            v[i][e] = y.x; v[i][e + 1] = y.y;
+        }
+    }
+}
+
+template <int NOUT>
+struct TileOut {
+    Blocks rm[NOUT], tr[NOUT];           // codes == nullptr: not wanted
+    int64_t rows, cols;
+    uint64_t index_offset;
+    PhiloxKeys keys[NOUT];
+    uint32_t* status;
+};
+
+// Quantizes the NOUT matrices whose tile is held as v (zeros outside the matrix).  All threads of the CTA call it
+// together, after a barrier that follows the previous call; `next` asks for the next tile.
+template <int NOUT, bool SR, bool FULL, typename Next>
+__device__ __forceinline__ void emit_tile(const float (&v)[NOUT][4][8], const TileOut<NOUT>& O, const TilePos& p, int par,
+                                          TileShared<NOUT>* S, Next&& next) {
+    const int tid = threadIdx.x, lane = tid & 31, l = tid & 15, g = tid >> 4;
+    const int64_t r_first = p.r0 + 4 * g, c_first = p.c0 + 8 * l;
+    bool any_tr = false, tiles = false;
+#pragma unroll
+    for (int n = 0; n < NOUT; ++n) {
+        any_tr |= O.tr[n].codes != nullptr;
+        tiles |= (O.rm[n].codes && O.rm[n].tile_rows > 1) || (O.tr[n].codes && O.tr[n].tile_rows > 1);
+    }
+    const bool meet = any_tr || tiles;
+    next();
+    // ---- maxima
+    uint32_t row_max[NOUT][4];
+#pragma unroll
+    for (int n = 0; n < NOUT; ++n) {
+        const bool tile_n = NOUT == 1 && tiles;            // 128 x 128 tiles: the quantizer only
+        if (O.rm[n].codes || tile_n) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float (&x)[8] = v[n][i];
+                row_max[n][i] = abs_word(absmax3(absmax3(x[0], x[1], x[2]), absmax3(x[3], x[4], x[5]), absmax3(x[6], x[7], 0.0f)));
+#pragma unroll
+                for (int s = 1; s < 16; s <<= 1) row_max[n][i] = max(row_max[n][i], __shfl_xor_sync(0xFFFFFFFFu, row_max[n][i], s));
+            }
+        }
+        if (tile_n) {
+            uint32_t m = max(max(row_max[n][0], row_max[n][1]), max(row_max[n][2], row_max[n][3]));
+            m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 16));
+            if (lane == 0) atomicMax(&S->tile_max[par], m);
+        }
+        if (O.tr[n].codes && O.tr[n].tile_rows == 1) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                uint32_t m = abs_word(absmax3(absmax3(v[n][0][j], v[n][1][j], v[n][2][j]), v[n][3][j], 0.0f));
+                m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 16));
+                if (lane < 16) atomicMax(&S->col_max[par][n][j * 16 + l], m);
+            }
+        }
+    }
+    if (meet) {
+        __syncthreads();
+        // ---- columns' step sizes, and the other parity's maxima back to zero for the next tile
+        for (int t = tid; t < NOUT * QBLK; t += TQ_THREADS) {
+            const int n = t / QBLK, k = t & (QBLK - 1);
+            const Blocks& o = O.tr[n];
+            S->col_max[par ^ 1][n][k] = 0u;
+            if (t == 0) S->tile_max[par ^ 1] = 0u;
+            if (!o.codes) continue;
+            const int64_t c = p.c0 + (k & 15) * 8 + (k >> 4);
+            const bool tile = o.tile_rows > 1;
+            const uint32_t m = tile ? S->tile_max[par] : S->col_max[par][n][k];
+            S->col_inv[n][(k >> 5) * 32 + (k & 15) * 2 + ((k >> 4) & 1)] = block_inv(m);
+            if (block_nonfinite(m)) note(O.status, SRQ_ERR_NONFINITE);
+            if (!tile && (FULL || c < O.cols)) o.scale[c * o.ld_scale + p.r0 / QBLK] = block_size(m);
+            if (tile && k == 0) o.scale[(p.c0 / QBLK) * o.ld_scale + p.r0 / QBLK] = block_size(m);
+        }
+    }
+    // ---- row-major codes
+#pragma unroll
+    for (int n = 0; n < NOUT; ++n) {
+        const Blocks& o = O.rm[n];
+        if (!o.codes) continue;
+        const bool tile = NOUT == 1 && o.tile_rows > 1;
+        // the divisions of four rows once per thread: lane l of a row's sixteen does row l % 4's
+        const int pick = l & 3;
+        uint32_t m = pick == 0 ? row_max[n][0] : pick == 1 ? row_max[n][1] : pick == 2 ? row_max[n][2] : row_max[n][3];
+        if (tile) m = S->tile_max[par];
+        const float inv = block_inv(m);
+        if (block_nonfinite(m)) note(O.status, SRQ_ERR_NONFINITE);
+        const int64_t r_mine = r_first + pick;
+        if (!tile && l < 4 && (FULL || r_mine < O.rows)) o.scale[r_mine * o.ld_scale + p.c0 / QBLK] = block_size(m);
+        if (tile && tid == 0) o.scale[(p.r0 / QBLK) * o.ld_scale + p.c0 / QBLK] = block_size(m);
+        uint8_t* dst = o.codes + r_first * o.ld + c_first;
+#pragma unroll
+        for (int i = 0; i < 4; ++i, dst += o.ld) {
+            const float f = __shfl_sync(0xFFFFFFFFu, inv, (lane & 16) + i);
+            const float (&x)[8] = v[n][i];
+            uint32_t rnd[8] = {};
+            if constexpr (SR) thresholds8(O.index_offset + (uint64_t)(r_first + i) * (uint64_t)O.cols + (uint64_t)c_first, O.keys[n], rnd);
+            const uint32_t w0 = encode4<SR>(x[0], x[1], x[2], x[3], f, f, f, f, rnd[0], rnd[1], rnd[2], rnd[3]);
+            const uint32_t w1 = encode4<SR>(x[4], x[5], x[6], x[7], f, f, f, f, rnd[4], rnd[5], rnd[6], rnd[7]);
+            if (FULL) *reinterpret_cast<uint2*>(dst) = make_uint2(w0, w1);
+            else if (r_first + i < O.rows && c_first < O.cols) store_codes8(dst - c_first, c_first, O.cols, w0, w1);
+        }
+    }
+    if (!any_tr) return;
+    // ---- transposed codes, through shared memory
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < NOUT; ++n) {
+        if (!O.tr[n].codes) continue;
+        uint32_t* words = S->words[n] + (8 * l) * 32 + (g ^ (2 * l));
+        if constexpr (SR) {
+            uint32_t w[8] = {};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {                  // a row's thresholds at a time
+                uint32_t rnd[8];
+                thresholds8(O.index_offset + (uint64_t)(r_first + i) * (uint64_t)O.cols + (uint64_t)c_first, O.keys[n], rnd);
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    w[j] |= (quantize_e4m3<MODE_SR | MODE_E4M3>(v[n][i][j], S->col_inv[n][(j >> 1) * 32 + 2 * l + (j & 1)], rnd[j], 0) & 0xFFu) << (8 * i);
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) words[j * 32] = w[j];
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; j += 2) {
+                const float2 f = *reinterpret_cast<const float2*>(&S->col_inv[n][(j >> 1) * 32 + 2 * l]);
+                float2 t[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) t[i] = __fmul2_rn(make_float2(v[n][i][j], v[n][i][j + 1]), f);
+                words[j * 32] = e4m3x4(t[0].x, t[1].x, t[2].x, t[3].x);
+                words[(j + 1) * 32] = e4m3x4(t[0].y, t[1].y, t[2].y, t[3].y);
+            }
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < NOUT; ++n) {
+        const Blocks& o = O.tr[n];
+        if (!o.codes) continue;
+        if (FULL) {
+            // sixteen codes per store: chunk q of column c; its four words sit in chunk q ^ (l / 2), halves swapped for odd l
+            // (l = c / 8)
+            const int q = tid & 7;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int cc = (tid >> 3) + 64 * h, lc = cc >> 3;
+                const uint4 w = *reinterpret_cast<const uint4*>(&S->words[n][cc * 32 + ((q ^ (lc >> 1)) << 2)]);
+                *reinterpret_cast<uint4*>(o.codes + (p.c0 + cc) * o.ld + p.r0 + 16 * q) = (lc & 1) ? make_uint4(w.z, w.w, w.x, w.y) : w;
+            }
+        } else {
+            const int warp = tid >> 5;
+            const int64_t r = p.r0 + 4 * lane;
+#pragma unroll 1
+            for (int k = 0; k < 8; ++k) {
+                const int cc = 8 * warp + k;
+                const int64_t c = p.c0 + cc;
+                if (c >= O.cols || r >= O.rows) continue;
+                const uint32_t w = S->words[n][cc * 32 + (lane ^ (2 * warp))];
+                uint8_t* dst = o.codes + c * o.ld + r;
+                if (r + 4 <= O.rows) *reinterpret_cast<uint32_t*>(dst) = w;
+                else
+                    for (int e = 0; e < 4 && r + e < O.rows; ++e) dst[e] = (uint8_t)(w >> (8 * e));
+            }
+        }
+    }
+}
+
+template <int NOUT>
+__device__ __forceinline__ void clear_maxima(TileShared<NOUT>* S) {
+    for (int t = threadIdx.x; t < 2 * NOUT * QBLK; t += TQ_THREADS) S->col_max[0][0][t] = 0u;
+    if (threadIdx.x < 2) S->tile_max[threadIdx.x] = 0u;
 }
 
 struct QuantBlocksParams {
     BlockSource src;
-    Blocks rm, tr;
-    uint64_t index_offset;
-    PhiloxKeys keys;
-    int32_t vec;                     // 16-byte loads of the source allowed
-    uint32_t* status;
+    TileOut<1> out;
+    uint32_t tiles, tiles_c;
+    int32_t vec;                         // the source's alignment allows 16-byte (codes: 8-byte) accesses
 };
 
 // SRC: 0 binary32, 1 bfloat16, 2 block codes.
 template <int SRC, bool SR>
 __global__ void __launch_bounds__(TQ_THREADS, SR ? 1 : 2) quantize_blocks_kernel(const __grid_constant__ QuantBlocksParams P) {
     pdl_enter();
-    __shared__ TileShared S;
-    const TilePos p = tile_pos(P.src.rows, P.src.cols);
-    float v[4][8];
-    uint32_t rnd[SR ? 4 : 1][8] = {};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int64_t r = p.r0 + 4 * p.g + i, c = p.c0 + 8 * p.l;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[i][j] = 0.0f;
-        if (r < p.rows) {
-            if constexpr (SRC == 0) load8((const float*)P.src.x + r * P.src.ld, c, p.cols, P.vec, v[i]);
-            else if constexpr (SRC == 1) load8((const __nv_bfloat16*)P.src.x + r * P.src.ld, c, p.cols, P.vec, v[i]);
-            else load_coded8(P.src.coded, r, c, p.cols, v[i]);
+    extern __shared__ __align__(16) uint8_t ahead[];
+    __shared__ TileShared<1> S;
+    using T = std::conditional_t<SRC == 0, float, __nv_bfloat16>;
+    const int64_t rows = P.out.rows, cols = P.out.cols;
+    int par = 0;
+    auto fetch = [&](const TilePos& p, int to) {
+        if (p.full) {
+            if constexpr (SRC == 2) fetch_coded(coded_codes(ahead, to), P.src.coded, p);
+            else fetch_matrix<T>(ahead, (const T*)P.src.x, P.src.ld, p);
         }
-        if constexpr (SR) thresholds8(P.index_offset + (uint64_t)r * (uint64_t)p.cols + (uint64_t)c, P.keys, rnd[i]);
+        cp_async_commit();
+    };
+    clear_maxima(&S);
+    TilePos p = tile_at(blockIdx.x, P.tiles_c, rows, cols, P.vec);
+    fetch(p, 0);
+    if (SRC == 2 && threadIdx.x < QBLK && p.full) coded_scales(ahead, 0)[threadIdx.x] = fetch_scale(P.src.coded, p, threadIdx.x);
+#pragma unroll 1
+    for (uint32_t tile = blockIdx.x; tile < P.tiles; par ^= 1) {
+        float v[1][4][8];
+        cp_async_wait();
+        __syncthreads();                 // everybody's pieces have landed, the last tile's shared words have been read
+        if constexpr (SRC == 2) read_coded(ahead, par, P.src.coded, rows, cols, p, v[0]);
+        else read_matrix<T>(ahead, (const T*)P.src.x, P.src.ld, rows, cols, P.vec, p, v[0]);
+        const uint32_t next_tile = tile + gridDim.x;
+        const TilePos np = tile_at(next_tile < P.tiles ? next_tile : tile, P.tiles_c, rows, cols, P.vec);
+        float next_scale = 0.0f;
+        auto next = [&] {
+            if (SRC == 0) __syncthreads();
+            if (next_tile >= P.tiles) return;
+            fetch(np, par ^ 1);
+            if (SRC == 2 && threadIdx.x < QBLK && np.full) next_scale = fetch_scale(P.src.coded, np, threadIdx.x);
+        };
+        if (p.full) emit_tile<1, SR, true>(v, P.out, p, par, &S, next);
+        else emit_tile<1, SR, false>(v, P.out, p, par, &S, next);
+        if (SRC == 2 && threadIdx.x < QBLK) coded_scales(ahead, par ^ 1)[threadIdx.x] = next_scale;
+        tile = next_tile;
+        p = np;
     }
-    emit_tile<SR>(v, rnd, P.rm, P.tr, p, &S, P.status);
 }
 
 struct GluBwdParams {
     const void* dh; int64_t ld_dh;
-    Blocks gate, up, dg, du, dg_t, du_t, h_t;
-    int64_t T, F;
-    uint64_t index_offset;
-    PhiloxKeys keys[3];              // of dg, du, h
+    Blocks gate, up;
+    TileOut<3> out;                      // dg, du, h
+    uint32_t tiles, tiles_c;
     int32_t vec;
-    uint32_t* status;
 };
 
-// dg = dh u act'(g), du = dh act(g), h = act(g) u over one tile, each quantized as it is formed.  dh and
-// the codes of g and u stay in registers; the activation is evaluated anew for each of the three.
+// dg = dh u act'(g), du = dh act(g), h = act(g) u over a tile, all three formed with one evaluation of the activation.
 template <typename T, bool GELU, bool SR>
 __global__ void __launch_bounds__(TQ_THREADS, 1) glu_bwd_kernel(const __grid_constant__ GluBwdParams P) {
     pdl_enter();
-    __shared__ TileShared S;
-    const TilePos p = tile_pos(P.T, P.F);
-    float dh[4][8], g[4][8], u[4][8];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int64_t r = p.r0 + 4 * p.g + i, c = p.c0 + 8 * p.l;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) dh[i][j] = g[i][j] = u[i][j] = 0.0f;
-        if (r < p.rows) {
-            if (P.dh) load8((const T*)P.dh + r * P.ld_dh, c, p.cols, P.vec, dh[i]);
-            load_coded8(P.gate, r, c, p.cols, g[i]);
-            load_coded8(P.up, r, c, p.cols, u[i]);
+    extern __shared__ __align__(16) uint8_t dyn[];
+    TileShared<3>* S = reinterpret_cast<TileShared<3>*>(dyn);
+    uint8_t* ahead_dh = dyn + (sizeof(TileShared<3>) + 15) / 16 * 16;
+    uint8_t* ahead_g = ahead_dh + matrix_slot<T>();
+    uint8_t* ahead_u = ahead_g + coded_slot();
+    const int64_t rows = P.out.rows, cols = P.out.cols;
+    int par = 0;
+    auto fetch = [&](const TilePos& p, int to) {
+        if (p.full) {
+            fetch_matrix<T>(ahead_dh, (const T*)P.dh, P.ld_dh, p);
+            fetch_coded(coded_codes(ahead_g, to), P.gate, p);
+            fetch_coded(coded_codes(ahead_u, to), P.up, p);
         }
-    }
-    const Blocks none;
+        cp_async_commit();
+    };
+    // threads 0 .. 127 bring the rows' step sizes of the gate, the next 128 those of the up projection
+    uint8_t* scale_slot = threadIdx.x < QBLK ? ahead_g : ahead_u;
+    const Blocks& scale_of = threadIdx.x < QBLK ? P.gate : P.up;
+    const int scale_row = threadIdx.x & (QBLK - 1);
+    const bool brings = threadIdx.x < 2 * QBLK;
+    clear_maxima(S);
+    TilePos p = tile_at(blockIdx.x, P.tiles_c, rows, cols, P.vec);
+    fetch(p, 0);
+    if (brings && p.full) coded_scales(scale_slot, 0)[scale_row] = fetch_scale(scale_of, p, scale_row);
 #pragma unroll 1
-    for (int which = 0; which < 3; ++which) {
-        const Blocks& rm = which == 0 ? P.dg : which == 1 ? P.du : none;
-        const Blocks& tr = which == 0 ? P.dg_t : which == 1 ? P.du_t : P.h_t;
-        if (!rm.codes && !tr.codes) continue;
-        float v[4][8];
-        uint32_t rnd[SR ? 4 : 1][8] = {};
+    for (uint32_t tile = blockIdx.x; tile < P.tiles; par ^= 1) {
+        float v[3][4][8];                // read as dh, g, u
+        cp_async_wait();
+        __syncthreads();                 // everybody's pieces have landed, the last tile's shared words have been read
+        read_matrix<T>(ahead_dh, (const T*)P.dh, P.ld_dh, rows, cols, P.vec, p, v[0]);
+        read_coded(ahead_g, par, P.gate, rows, cols, p, v[1]);
+        read_coded(ahead_u, par, P.up, rows, cols, p, v[2]);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                float dz;
-                const float pr = logistic_of<GELU>(g[i][j], &dz), a = g[i][j] * pr;
-                v[i][j] = which == 0 ? dh[i][j] * u[i][j] * fmaf(a * (1.0f - pr), dz, pr) : which == 1 ? dh[i][j] * a : a * u[i][j];
+            for (int j = 0; j < 8; j += 2) {
+                auto two = [&](int m) { return make_float2(v[m][i][j], v[m][i][j + 1]); };
+                auto put = [&](int m, float2 x) { v[m][i][j] = x.x; v[m][i][j + 1] = x.y; };
+                const float2 dh = two(0), g = two(1), u = two(2), one = make_float2(1.0f, 1.0f), minus = make_float2(-1.0f, -1.0f);
+                float2 dz;
+                const float2 pr = logistic2<GELU>(g, &dz), a = __fmul2_rn(g, pr);
+                float2 tail = __fmul2_rn(a, __ffma2_rn(pr, minus, one));
+                if constexpr (GELU) tail = __fmul2_rn(tail, dz);
+                put(0, __fmul2_rn(__fmul2_rn(dh, u), __fadd2_rn(tail, pr)));
+                put(1, __fmul2_rn(dh, a));
+                put(2, __fmul2_rn(a, u));
             }
-            if constexpr (SR)
-                thresholds8(P.index_offset + (uint64_t)(p.r0 + 4 * p.g + i) * (uint64_t)p.cols + (uint64_t)(p.c0 + 8 * p.l), P.keys[which], rnd[i]);
         }
-        emit_tile<SR>(v, rnd, rm, tr, p, &S, P.status);
+        const uint32_t next_tile = tile + gridDim.x;
+        const TilePos np = tile_at(next_tile < P.tiles ? next_tile : tile, P.tiles_c, rows, cols, P.vec);
+        float next_scale = 0.0f;
+        auto next = [&] {
+            if (sizeof(T) == 4) __syncthreads();
+            if (next_tile >= P.tiles) return;
+            fetch(np, par ^ 1);
+            if (brings && np.full) next_scale = fetch_scale(scale_of, np, scale_row);
+        };
+        if (p.full) emit_tile<3, SR, true>(v, P.out, p, par, S, next);
+        else emit_tile<3, SR, false>(v, P.out, p, par, S, next);
+        if (brings) coded_scales(scale_slot, par ^ 1)[scale_row] = next_scale;
+        tile = next_tile;
+        p = np;
     }
 }
 
 // ------------------------------------------------------------------------------------------
 // host side
 // ------------------------------------------------------------------------------------------
-static int64_t tiles_of(int64_t rows, int64_t cols) { return ((rows + QBLK - 1) / QBLK) * ((cols + QBLK - 1) / QBLK); }
+static uint32_t tiles_of(int64_t rows, int64_t cols) { return (uint32_t)(((rows + QBLK - 1) / QBLK) * ((cols + QBLK - 1) / QBLK)); }
+
+// SM count of the current device, and the one-time opt-in to more than 48 KB of shared memory.
+template <typename K>
+static bool prepare_kernel(K kernel, int smem) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) == cudaSuccess; }
+template <typename T>
+constexpr int glu_bwd_smem() { return (int)(sizeof(TileShared<3>) + 15) / 16 * 16 + matrix_slot<T>() + 2 * coded_slot(); }
+
+template <typename T>
+static bool prepare_glu() {
+    const int n = glu_bwd_smem<T>();
+    return prepare_kernel(glu_bwd_kernel<T, false, false>, n) && prepare_kernel(glu_bwd_kernel<T, false, true>, n) &&
+           prepare_kernel(glu_bwd_kernel<T, true, false>, n) && prepare_kernel(glu_bwd_kernel<T, true, true>, n);
+}
+static int tile_device() {
+    static int sms[64] = {};
+    static std::mutex mu;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
+    std::lock_guard<std::mutex> lock(mu);
+    if (sms[dev] == 0) {
+        int n = 0;
+        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0) return 0;
+        if (!prepare_kernel(quantize_blocks_kernel<0, false>, matrix_slot<float>()) || !prepare_kernel(quantize_blocks_kernel<0, true>, matrix_slot<float>()) ||
+            !prepare_kernel(quantize_blocks_kernel<1, false>, matrix_slot<__nv_bfloat16>()) || !prepare_kernel(quantize_blocks_kernel<1, true>, matrix_slot<__nv_bfloat16>()) ||
+            !prepare_kernel(quantize_blocks_kernel<2, false>, coded_slot()) || !prepare_kernel(quantize_blocks_kernel<2, true>, coded_slot()) ||
+            !prepare_glu<float>() || !prepare_glu<__nv_bfloat16>())
+            return 0;
+        sms[dev] = n;
+    }
+    return sms[dev];
+}
+// Persistent CTAs, at most as many as are resident at a time.  CTA i takes tiles i, i + grid, ...: the CTAs with one tile
+// more than the others come first and land on different SMs.
+static unsigned persistent_grid(uint32_t tiles, uint32_t resident) { return tiles < resident ? tiles : resident; }
 
 cudaError_t launch_quantize_blocks(const BlockSource& src, const BlockRounding& rnd, const Blocks& rm, const Blocks& tr,
                                    uint32_t* status, cudaStream_t stream) {
+    const int sms = tile_device();
+    if (sms == 0) return cudaErrorUnknown;
     QuantBlocksParams P;
-    P.src = src; P.rm = rm; P.tr = tr; P.index_offset = rnd.index_offset;
-    P.keys = make_philox_keys(rnd.seed, rnd.tensor_id);
-    const int per16 = src.dt == SRQ_F32 ? 4 : 8;
-    P.vec = src.x && (uintptr_t)src.x % 16 == 0 && src.ld % per16 == 0;
-    P.status = status;
-    const dim3 grid((unsigned)tiles_of(src.rows, src.cols)), block(TQ_THREADS);
+    P.src = src;
+    P.out.rm[0] = rm; P.out.tr[0] = tr; P.out.rows = src.rows; P.out.cols = src.cols;
+    P.out.index_offset = rnd.index_offset; P.out.keys[0] = make_philox_keys(rnd.seed, rnd.tensor_id); P.out.status = status;
+    P.tiles = tiles_of(src.rows, src.cols); P.tiles_c = (uint32_t)((src.cols + QBLK - 1) / QBLK);
+    P.vec = src.coded.codes ? 1 : (uintptr_t)src.x % 16 == 0 && src.ld % (src.dt == SRQ_F32 ? 4 : 8) == 0;
+    const dim3 grid(persistent_grid(P.tiles, (uint32_t)sms * (rnd.sr ? 1 : 2))), block(TQ_THREADS);
     cudaError_t e;
-    if (src.coded.codes) e = rnd.sr ? launch_pdl(quantize_blocks_kernel<2, true>, grid, block, 0, stream, P) : launch_pdl(quantize_blocks_kernel<2, false>, grid, block, 0, stream, P);
-    else if (src.dt == SRQ_BF16) e = rnd.sr ? launch_pdl(quantize_blocks_kernel<1, true>, grid, block, 0, stream, P) : launch_pdl(quantize_blocks_kernel<1, false>, grid, block, 0, stream, P);
-    else e = rnd.sr ? launch_pdl(quantize_blocks_kernel<0, true>, grid, block, 0, stream, P) : launch_pdl(quantize_blocks_kernel<0, false>, grid, block, 0, stream, P);
+    if (src.coded.codes)
+        e = rnd.sr ? launch_pdl(quantize_blocks_kernel<2, true>, grid, block, coded_slot(), stream, P) : launch_pdl(quantize_blocks_kernel<2, false>, grid, block, coded_slot(), stream, P);
+    else if (src.dt == SRQ_BF16)
+        e = rnd.sr ? launch_pdl(quantize_blocks_kernel<1, true>, grid, block, matrix_slot<__nv_bfloat16>(), stream, P)
+                   : launch_pdl(quantize_blocks_kernel<1, false>, grid, block, matrix_slot<__nv_bfloat16>(), stream, P);
+    else
+        e = rnd.sr ? launch_pdl(quantize_blocks_kernel<0, true>, grid, block, matrix_slot<float>(), stream, P)
+                   : launch_pdl(quantize_blocks_kernel<0, false>, grid, block, matrix_slot<float>(), stream, P);
     count_launch();
     return e;
 }
@@ -256,21 +510,24 @@ cudaError_t launch_quantize_blocks(const BlockSource& src, const BlockRounding& 
 template <typename T>
 static cudaError_t launch_glu_bwd_t(const GluBwdParams& P, int32_t act, int sr, dim3 grid, cudaStream_t stream) {
     const dim3 block(TQ_THREADS);
-    if (act == SRQ_GELU) return sr ? launch_pdl(glu_bwd_kernel<T, true, true>, grid, block, 0, stream, P) : launch_pdl(glu_bwd_kernel<T, true, false>, grid, block, 0, stream, P);
-    return sr ? launch_pdl(glu_bwd_kernel<T, false, true>, grid, block, 0, stream, P) : launch_pdl(glu_bwd_kernel<T, false, false>, grid, block, 0, stream, P);
+    const size_t smem = glu_bwd_smem<T>();
+    if (act == SRQ_GELU) return sr ? launch_pdl(glu_bwd_kernel<T, true, true>, grid, block, smem, stream, P) : launch_pdl(glu_bwd_kernel<T, true, false>, grid, block, smem, stream, P);
+    return sr ? launch_pdl(glu_bwd_kernel<T, false, true>, grid, block, smem, stream, P) : launch_pdl(glu_bwd_kernel<T, false, false>, grid, block, smem, stream, P);
 }
 
 cudaError_t launch_glu_bwd(const void* dh, int32_t dt, int64_t ld_dh, const Blocks& gate, const Blocks& up, int64_t T, int64_t F,
                            int32_t act, const BlockRounding& rnd, const Blocks& dg, const Blocks& du, const Blocks& dg_t,
                            const Blocks& du_t, const Blocks& h_t, uint32_t* status, cudaStream_t stream) {
+    const int sms = tile_device();
+    if (sms == 0) return cudaErrorUnknown;
     GluBwdParams P;
     P.dh = dh; P.ld_dh = ld_dh; P.gate = gate; P.up = up;
-    P.dg = dg; P.du = du; P.dg_t = dg_t; P.du_t = du_t; P.h_t = h_t;
-    P.T = T; P.F = F; P.index_offset = rnd.index_offset;
-    for (int i = 0; i < 3; ++i) P.keys[i] = make_philox_keys(rnd.seed, rnd.tensor_id + (uint64_t)i);
+    P.out.rm[0] = dg; P.out.rm[1] = du; P.out.tr[0] = dg_t; P.out.tr[1] = du_t; P.out.tr[2] = h_t;
+    P.out.rows = T; P.out.cols = F; P.out.index_offset = rnd.index_offset; P.out.status = status;
+    for (int i = 0; i < 3; ++i) P.out.keys[i] = make_philox_keys(rnd.seed, rnd.tensor_id + (uint64_t)i);
+    P.tiles = tiles_of(T, F); P.tiles_c = (uint32_t)((F + QBLK - 1) / QBLK);
     P.vec = (uintptr_t)dh % 16 == 0 && ld_dh % (dt == SRQ_F32 ? 4 : 8) == 0;
-    P.status = status;
-    const dim3 grid((unsigned)tiles_of(T, F));
+    const dim3 grid(persistent_grid(P.tiles, (uint32_t)sms));
     const cudaError_t e = dt == SRQ_F32 ? launch_glu_bwd_t<float>(P, act, rnd.sr, grid, stream) : launch_glu_bwd_t<__nv_bfloat16>(P, act, rnd.sr, grid, stream);
     count_launch();
     return e;
