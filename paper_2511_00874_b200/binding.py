@@ -173,7 +173,8 @@ def _check(status: int, where: str) -> None:
 
 
 def _stream() -> int:
-    return torch.cuda.current_stream().cuda_stream
+    """The current stream's handle (without building the Stream object, which costs more than the call itself)."""
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 def _ptr(t: Optional[torch.Tensor]):
@@ -567,18 +568,23 @@ class Blocks:
         return self.codes.shape
 
     def c(self) -> _Blocks:
-        codes, scale = self.codes, self.scale
-        if codes.element_size() != 1 or codes.dim() != 2 or codes.stride(1) != 1 or not codes.is_cuda:
+        codes, scale, tile = self.codes, self.scale, self.tile_rows
+        rows, cols = codes.shape if codes.dim() == 2 else (-1, -1)
+        ld, unit = codes.stride() if rows >= 0 else (0, 0)
+        if unit != 1 and cols > 1 or rows < 0 or codes.element_size() != 1 or not codes.is_cuda:
             raise ValueError("codes must be a 2-D CUDA tensor of bytes with unit inner stride")
-        if scale.dtype != torch.float32 or scale.dim() != 2 or scale.stride(1) != 1 or not scale.is_cuda:
+        nr, nb = scale.shape if scale.dim() == 2 else (-1, -1)
+        ld_scale, unit = scale.stride() if nr >= 0 else (0, 0)
+        if unit != 1 and nb > 1 or nr < 0 or scale.dtype != torch.float32 or not scale.is_cuda:
             raise ValueError("step sizes must be a 2-D float32 CUDA tensor with unit inner stride")
-        rows, cols = codes.shape
-        if scale.shape[0] < -(-rows // self.tile_rows) or scale.shape[1] < -(-cols // BLOCK):
+        if nr * tile < rows or nb * BLOCK < cols:
             raise ValueError(f"step sizes of shape {tuple(scale.shape)} do not cover a {rows} x {cols} matrix")
         # the pitch of a single row says nothing: torch is free to report any
-        ld = codes.stride(0) if rows > 1 else -(-max(codes.stride(0), cols) // 16) * 16
-        return _Blocks(codes.data_ptr(), ld, scale.data_ptr(), scale.stride(0) if scale.shape[0] > 1 else max(scale.stride(0), scale.shape[1]),
-                       self.tile_rows)
+        if rows <= 1:
+            ld = -(-max(ld, cols) // 16) * 16
+        if nr <= 1 and ld_scale < nb:
+            ld_scale = nb
+        return _Blocks(codes.data_ptr(), ld, scale.data_ptr(), ld_scale, tile)
 
     def dequantize(self) -> torch.Tensor:
         """The numbers the matrix stands for, in float32."""
@@ -595,12 +601,12 @@ def new_blocks(rows: int, cols: int, tile_rows: int = 1, device="cuda") -> Block
     return Blocks(codes, scale, tile_rows)
 
 
-def _bref(b: Optional[Blocks], shape=None, name=""):
+def _bref(b: Optional[Blocks], shape, name):
     if b is None:
         return None
-    if shape is not None and tuple(b.codes.shape) != shape:
+    if b.codes.shape != shape:
         raise ValueError(f"{name} must be {shape[0]} x {shape[1]}, got {tuple(b.codes.shape)}")
-    return ctypes.byref(b.c())
+    return b.c()
 
 
 def _status_word(device_status: Optional[torch.Tensor]):
@@ -612,7 +618,11 @@ def _status_word(device_status: Optional[torch.Tensor]):
 
 
 def _pitch(t: Optional[torch.Tensor]) -> int:
-    return 0 if t is None else t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    if t is None:
+        return 0
+    rows, cols = t.shape
+    ld = t.stride(0)
+    return ld if rows > 1 or ld >= cols else cols
 
 
 def srq_quantize_blocks(x, q: QSpec, rm: Optional[Blocks] = None, tr: Optional[Blocks] = None,
@@ -620,14 +630,13 @@ def srq_quantize_blocks(x, q: QSpec, rm: Optional[Blocks] = None, tr: Optional[B
     """x[rows, cols] (float32, bfloat16, or a Blocks matrix: srq_requantize_blocks) as block codes, row-major
     into ``rm`` and / or transposed into ``tr`` ([cols, rows])."""
     rows, cols = x.shape
-    cq = q.c()
     r, t = _bref(rm, (rows, cols), "rm"), _bref(tr, (cols, rows), "tr")
     if isinstance(x, Blocks):
-        st = lib().srq_requantize_blocks(ctypes.byref(x.c()), rows, cols, ctypes.byref(cq), r, t, _status_word(device_status), _stream())
+        st = lib().srq_requantize_blocks(x.c(), rows, cols, q.c(), r, t, _status_word(device_status), _stream())
         _check(st, "srq_requantize_blocks")
         return
     _dev2d(x, "x")
-    st = lib().srq_quantize_blocks(x.data_ptr(), _dtype_of(x), rows, cols, _pitch(x), ctypes.byref(cq), r, t,
+    st = lib().srq_quantize_blocks(x.data_ptr(), _dtype_of(x), rows, cols, _pitch(x), q.c(), r, t,
                                    _status_word(device_status), _stream())
     _check(st, "srq_quantize_blocks")
 
@@ -639,7 +648,7 @@ def srq_gemm_blocks(a: Blocks, b: Blocks, out: torch.Tensor, accumulate: bool = 
     _dev2d(out, "out")
     if Kc != Kb or tuple(out.shape) != (M, N):
         raise ValueError("srq_gemm_blocks: shapes must be a[M,Kc], b[N,Kc], out[M,N]")
-    st = lib().srq_gemm_blocks(ctypes.byref(a.c()), ctypes.byref(b.c()), M, N, Kc, out.data_ptr(), _dtype_of(out), _pitch(out),
+    st = lib().srq_gemm_blocks(a.c(), b.c(), M, N, Kc, out.data_ptr(), _dtype_of(out), _pitch(out),
                                int(accumulate), _status_word(device_status), _stream())
     _check(st, "srq_gemm_blocks")
 
@@ -660,9 +669,8 @@ def srq_rmsnorm_fwd(x: torch.Tensor, residual: Optional[torch.Tensor], w: torch.
         raise ValueError("w must be a CUDA tensor of cols values")
     if rstd is not None and (rstd.dtype != torch.float32 or rstd.numel() < rows or not rstd.is_contiguous()):
         raise ValueError("rstd must hold rows float32 values")
-    cq = q.c()
     st = lib().srq_rmsnorm_fwd(x.data_ptr(), _pitch(x), _ptr(residual), _pitch(residual), dt, w.data_ptr(), _dtype_of(w), rows, cols,
-                               eps, ctypes.byref(cq), _bref(y, (rows, cols), "y"), _ptr(y_out), _pitch(y_out), _ptr(r_out), _pitch(r_out),
+                               eps, q.c(), _bref(y, (rows, cols), "y"), _ptr(y_out), _pitch(y_out), _ptr(r_out), _pitch(r_out),
                                _ptr(rstd), _status_word(device_status), _stream())
     _check(st, "srq_rmsnorm_fwd")
 
@@ -705,7 +713,7 @@ def srq_glu_fwd(x: Blocks, wg: Blocks, wu: Blocks, act: int, h: Optional[Blocks]
         _dev2d(h_out, "h_out")
         if tuple(h_out.shape) != (T, F):
             raise ValueError("h_out must be [T, F]")
-    st = lib().srq_glu_fwd(ctypes.byref(x.c()), ctypes.byref(wg.c()), ctypes.byref(wu.c()), T, F, K, act, _bref(h, (T, F), "h"),
+    st = lib().srq_glu_fwd(x.c(), wg.c(), wu.c(), T, F, K, act, _bref(h, (T, F), "h"),
                            _ptr(h_out), F32 if h_out is None else _dtype_of(h_out), _pitch(h_out),
                            _bref(gate, (T, F), "gate"), _bref(up, (T, F), "up"), _status_word(device_status), _stream())
     _check(st, "srq_glu_fwd")
@@ -718,8 +726,7 @@ def srq_glu_bwd(dh: torch.Tensor, gate: Blocks, up: Blocks, act: int, q: QSpec, 
     and along the tokens (dg_t, du_t), and h itself along the tokens (h_t)."""
     _dev2d(dh, "dh")
     T, F = dh.shape
-    cq = q.c()
     st = lib().srq_glu_bwd(dh.data_ptr(), _dtype_of(dh), _pitch(dh), _bref(gate, (T, F), "gate"), _bref(up, (T, F), "up"), T, F, act,
-                           ctypes.byref(cq), _bref(dg, (T, F), "dg"), _bref(du, (T, F), "du"), _bref(dg_t, (F, T), "dg_t"),
+                           q.c(), _bref(dg, (T, F), "dg"), _bref(du, (T, F), "du"), _bref(dg_t, (F, T), "dg_t"),
                            _bref(du_t, (F, T), "du_t"), _bref(h_t, (F, T), "h_t"), _status_word(device_status), _stream())
     _check(st, "srq_glu_bwd")

@@ -160,14 +160,14 @@ __device__ __forceinline__ void stage_rows64(uint32_t stage, int lane, const uin
                      "r"(w[4 * q]), "r"(w[4 * q + 1]), "r"(w[4 * q + 2]), "r"(w[4 * q + 3]) : "memory");
 }
 
-// GLU: the gated block's epilogue instead of the plain one.  COLV: b has a step size per row (per column of
+// map_out: of out, or of h's codes.  GLU: the gated block's epilogue instead of the plain one.  COLV: b has a step size per row (per column of
 // out), not per 128 of them.
 template <bool GLU, bool COLV>
 __global__ void __launch_bounds__(GB_THREADS, 1)
 gemm_blocks_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                    const __grid_constant__ CUtensorMap map_b2, const __grid_constant__ CUtensorMap map_out,
                    const __grid_constant__ CUtensorMap map_gate, const __grid_constant__ CUtensorMap map_up,
-                   const __grid_constant__ GemmBlocksParams P) {      // map_out: of out, or of h's codes
+                   const __grid_constant__ GemmBlocksParams P) {
     pdl_trigger();                       // the wait follows the set-up below, which touches only shared memory and TMEM
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);

@@ -3,9 +3,12 @@
 //
 // 128 x 128 tiles, 512 threads per CTA, persistent CTAs.  Thread (g, l), g = 0..31, l = 0..15, holds rows
 // 4 g .. 4 g + 3 of columns 8 l .. 8 l + 7 in registers, so that
-//   - a row's 128 values sit in 16 neighbouring lanes: its absmax is four shuffles;
-//   - a column's 128 values sit in 32 threads of 16 warps: its absmax is one shuffle and one shared atomic;
+//   - a row's 128 values sit in 16 neighbouring lanes: the absmax of four rows is a butterfly of five shuffles that leaves
+//     row l % 4's in lane l;
+//   - a column's 128 values sit in the warps' lanes l and l + 16: its absmax is half a shuffle and half a shared atomic;
 //   - the transposed codes of a thread are 8 words of 4 bytes, which meet in a swizzled shared tile.
+// (Two rows per thread and 1024 threads were measured too: twice the warps, but 69 instead of 57 instructions per value,
+// and no faster.)
 // A tile is read once whatever is written: both layouts and both kinds of step size come from the registers.
 // While a tile is worked on, the next one is on its way into shared memory (cp.async, 16 bytes at a time: smaller
 // pieces were measured to cost a shared-memory wavefront per lane); tiles that reach over the matrix's edge, and sources
@@ -19,11 +22,12 @@
 namespace srq {
 
 constexpr int TQ_THREADS = 512;
+constexpr int R = 4;                     // rows per thread
 
 // NOUT matrices are quantized from one tile (1, or the three of the gated block's backward pass).
 template <int NOUT>
 struct TileShared {
-    uint32_t col_max[2][NOUT][QBLK];     // [tile parity][matrix][column % 8][column / 8]: a warp's atomics hit 16 banks
+    uint32_t col_max[2][NOUT][QBLK];     // [tile parity][matrix][column % 4][column / 4 % 2][column / 8]: an atomic per lane and bank
     alignas(8) float col_inv[NOUT][QBLK];          // [column % 8 / 2][column / 8][column % 2]: read two by two
     uint32_t tile_max[2];
     alignas(16) uint32_t words[NOUT][QBLK * 32];   // transposed codes: column c's rows 4 g .. 4 g + 3 at [c][g ^ 2 (c / 8)]
@@ -54,7 +58,7 @@ __device__ __forceinline__ uint32_t shared_addr(const void* p) { return (uint32_
 // chunks lane by lane, since a thread's own eight values are two chunks and every sector would be asked for twice,
 // so the next tile is asked for only when every thread has read its share); a block-coded matrix's tile row by
 // row, and its rows' step sizes (two buffers each, in turn).
-template <typename T> __host__ __device__ constexpr int matrix_slot() { return TQ_THREADS * 32 * (int)sizeof(T); }
+template <typename T> __host__ __device__ constexpr int matrix_slot() { return QBLK * QBLK * (int)sizeof(T); }
 constexpr int CODED_TILE = QBLK * QBLK;
 __host__ __device__ constexpr int coded_slot() { return 2 * (CODED_TILE + QBLK * 4); }
 
@@ -63,29 +67,29 @@ __host__ __device__ constexpr int coded_slot() { return 2 * (CODED_TILE + QBLK *
 template <typename T>
 __device__ __forceinline__ void fetch_matrix(uint8_t* slot, const T* x, int64_t ld, const TilePos& p) {
     if constexpr (sizeof(T) == 4) {
-        const int k = threadIdx.x & 31, row = threadIdx.x >> 5;            // chunk k of rows row, row + 16, ...
+        const int k = threadIdx.x & 31, row = threadIdx.x >> 5;            // chunk k of rows row, row + 64 / R, ...
         const T* src = x + (p.r0 + row) * ld + p.c0 + 4 * k;
         // neighbouring chunks change places in every other group of eight: a thread's two reads hit all banks
         const uint32_t dst = shared_addr(slot) + row * 512 + ((k ^ ((k >> 3) & 1)) << 4);
 #pragma unroll
-        for (int i = 0; i < 8; ++i, src += 16 * ld) cp_async16(dst + i * 16 * 512, src);
+        for (int i = 0; i < 2 * R; ++i, src += (64 / R) * ld) cp_async16(dst + i * (64 / R) * 512, src);
     } else {
         const int l = threadIdx.x & 15, g = threadIdx.x >> 4;
-        const T* src = x + (p.r0 + 4 * g) * ld + p.c0 + 8 * l;
+        const T* src = x + (p.r0 + R * g) * ld + p.c0 + 8 * l;
         const uint32_t dst = shared_addr(slot) + threadIdx.x * 16;
 #pragma unroll
-        for (int i = 0; i < 4; ++i, src += ld) cp_async16(dst + i * TQ_THREADS * 16, src);
+        for (int i = 0; i < R; ++i, src += ld) cp_async16(dst + i * TQ_THREADS * 16, src);
     }
 }
 template <typename T>
-__device__ __forceinline__ void read_matrix(const uint8_t* slot, const T* x, int64_t ld, int64_t rows, int64_t cols, int vec, const TilePos& p, float (&v)[4][8]) {
+__device__ __forceinline__ void read_matrix(const uint8_t* slot, const T* x, int64_t ld, int64_t rows, int64_t cols, int vec, const TilePos& p, float (&v)[R][8]) {
     const int l = threadIdx.x & 15, g = threadIdx.x >> 4;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < R; ++i) {
         if (p.full) {
             const uint4* s = reinterpret_cast<const uint4*>(slot) + threadIdx.x;
             if constexpr (sizeof(T) == 4) {
-                const uint4* row = reinterpret_cast<const uint4*>(slot) + (4 * g + i) * 32;
+                const uint4* row = reinterpret_cast<const uint4*>(slot) + (R * g + i) * 32;
                 const uint4 a = row[(2 * l) ^ ((l >> 2) & 1)], b = row[(2 * l + 1) ^ ((l >> 2) & 1)];
                 v[i][0] = __uint_as_float(a.x); v[i][1] = __uint_as_float(a.y); v[i][2] = __uint_as_float(a.z); v[i][3] = __uint_as_float(a.w);
                 v[i][4] = __uint_as_float(b.x); v[i][5] = __uint_as_float(b.y); v[i][6] = __uint_as_float(b.z); v[i][7] = __uint_as_float(b.w);
@@ -95,7 +99,7 @@ __device__ __forceinline__ void read_matrix(const uint8_t* slot, const T* x, int
                 v[i][4] = bf16_lo(a.z); v[i][5] = bf16_hi(a.z); v[i][6] = bf16_lo(a.w); v[i][7] = bf16_hi(a.w);
             }
         } else {
-            const int64_t r = p.r0 + 4 * g + i;
+            const int64_t r = p.r0 + R * g + i;
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[i][j] = 0.0f;
             if (r < rows) load8(x + r * ld, p.c0 + 8 * l, cols, vec, v[i]);
@@ -106,8 +110,8 @@ __device__ __forceinline__ void fetch_coded(uint8_t* slot, const Blocks& b, cons
     const int row = threadIdx.x >> 3, q = threadIdx.x & 7;             // eight threads to a row's 128 codes
     const uint8_t* src = b.codes + (p.r0 + row) * b.ld + p.c0 + 16 * q;
     const uint32_t dst = shared_addr(slot) + row * QBLK + 16 * q;
-    cp_async16(dst, src);
-    cp_async16(dst + 64 * QBLK, src + 64 * b.ld);
+#pragma unroll
+    for (int i = 0; i < R / 2; ++i) cp_async16(dst + i * 64 * QBLK, src + i * 64 * b.ld);
 }
 // The step size of row `row` of a tile, on its way to coded_scales() of its buffer.
 __device__ __forceinline__ float fetch_scale(const Blocks& b, const TilePos& p, int row) {
@@ -116,18 +120,17 @@ __device__ __forceinline__ float fetch_scale(const Blocks& b, const TilePos& p, 
 __device__ __forceinline__ uint8_t* coded_codes(uint8_t* slot, int par) { return slot + par * CODED_TILE; }
 __device__ __forceinline__ float* coded_scales(uint8_t* slot, int par) { return reinterpret_cast<float*>(slot + 2 * CODED_TILE) + par * QBLK; }
 
-__device__ __forceinline__ void read_coded(uint8_t* slot, int par, const Blocks& b, int64_t rows, int64_t cols, const TilePos& p, float (&v)[4][8]) {
+__device__ __forceinline__ void read_coded(uint8_t* slot, int par, const Blocks& b, int64_t rows, int64_t cols, const TilePos& p, float (&v)[R][8]) {
     const int l = threadIdx.x & 15, g = threadIdx.x >> 4;
-    const float4 sc = *reinterpret_cast<const float4*>(coded_scales(slot, par) + 4 * g);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < R; ++i) {
         uint2 w = make_uint2(0u, 0u);
-        float s = i == 0 ? sc.x : i == 1 ? sc.y : i == 2 ? sc.z : sc.w;
+        float s = 0.0f;
         if (p.full) {
-            w = *reinterpret_cast<const uint2*>(coded_codes(slot, par) + (4 * g + i) * QBLK + 8 * l);
+            w = *reinterpret_cast<const uint2*>(coded_codes(slot, par) + (R * g + i) * QBLK + 8 * l);
+            s = coded_scales(slot, par)[R * g + i];
         } else {
-            const int64_t r = p.r0 + 4 * g + i, c = p.c0 + 8 * l;
-            s = 0.0f;
+            const int64_t r = p.r0 + R * g + i, c = p.c0 + 8 * l;
             if (r < rows && c < cols) {
                 const uint8_t* row = b.codes + r * b.ld;
                 if (c + 8 <= cols) w = *reinterpret_cast<const uint2*>(row + c);
@@ -160,10 +163,10 @@ struct TileOut {
 // Quantizes the NOUT matrices whose tile is held as v (zeros outside the matrix).  All threads of the CTA call it
 // together, after a barrier that follows the previous call; `next` asks for the next tile.
 template <int NOUT, bool SR, bool FULL, typename Next>
-__device__ __forceinline__ void emit_tile(const float (&v)[NOUT][4][8], const TileOut<NOUT>& O, const TilePos& p, int par,
+__device__ __forceinline__ void emit_tile(const float (&v)[NOUT][R][8], const TileOut<NOUT>& O, const TilePos& p, int par,
                                           TileShared<NOUT>* S, Next&& next) {
     const int tid = threadIdx.x, lane = tid & 31, l = tid & 15, g = tid >> 4;
-    const int64_t r_first = p.r0 + 4 * g, c_first = p.c0 + 8 * l;
+    const int64_t r_first = p.r0 + R * g, c_first = p.c0 + 8 * l;
     bool any_tr = false, tiles = false;
 #pragma unroll
     for (int n = 0; n < NOUT; ++n) {
@@ -173,30 +176,45 @@ __device__ __forceinline__ void emit_tile(const float (&v)[NOUT][4][8], const Ti
     const bool meet = any_tr || tiles;
     next();
     // ---- maxima
-    uint32_t row_max[NOUT][4];
+    uint32_t row_max[NOUT] = {};         // of row l % R
 #pragma unroll
     for (int n = 0; n < NOUT; ++n) {
         const bool tile_n = NOUT == 1 && tiles;            // 128 x 128 tiles: the quantizer only
         if (O.rm[n].codes || tile_n) {
+            uint32_t m[R];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < R; ++i) {
                 const float (&x)[8] = v[n][i];
-                row_max[n][i] = abs_word(absmax3(absmax3(x[0], x[1], x[2]), absmax3(x[3], x[4], x[5]), absmax3(x[6], x[7], 0.0f)));
-#pragma unroll
-                for (int s = 1; s < 16; s <<= 1) row_max[n][i] = max(row_max[n][i], __shfl_xor_sync(0xFFFFFFFFu, row_max[n][i], s));
+                m[i] = abs_word(absmax3(absmax3(x[0], x[1], x[2]), absmax3(x[3], x[4], x[5]), absmax3(x[6], x[7], 0.0f)));
             }
+            // halve the rows, then the lanes: lane l keeps the rows whose low bits agree with its own
+#pragma unroll
+            for (int w = 1; w < R; w <<= 1) {
+                const bool odd = (l & w) != 0;
+#pragma unroll
+                for (int i = 0; i < R / (2 * w); ++i) {
+                    const uint32_t keep = odd ? m[2 * i + 1] : m[2 * i], give = odd ? m[2 * i] : m[2 * i + 1];
+                    m[i] = max(keep, __shfl_xor_sync(0xFFFFFFFFu, give, w));
+                }
+            }
+#pragma unroll
+            for (int w = R; w < 16; w <<= 1) m[0] = max(m[0], __shfl_xor_sync(0xFFFFFFFFu, m[0], w));
+            row_max[n] = m[0];
         }
         if (tile_n) {
-            uint32_t m = max(max(row_max[n][0], row_max[n][1]), max(row_max[n][2], row_max[n][3]));
-            m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 16));
+            const uint32_t m = __reduce_max_sync(0xFFFFFFFFu, row_max[n]);
             if (lane == 0) atomicMax(&S->tile_max[par], m);
         }
         if (O.tr[n].codes && O.tr[n].tile_rows == 1) {
+            uint32_t m[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                uint32_t m = abs_word(absmax3(absmax3(v[n][0][j], v[n][1][j], v[n][2][j]), v[n][3][j], 0.0f));
-                m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 16));
-                if (lane < 16) atomicMax(&S->col_max[par][n][j * 16 + l], m);
+            for (int j = 0; j < 8; ++j)
+                m[j] = abs_word(absmax3(absmax3(v[n][0][j], v[n][1][j], v[n][2][j]), v[n][3][j], 0.0f));
+            const int b = lane >> 4;                       // lanes 0 - 15 finish columns 0 - 3 of the eight, the others 4 - 7
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t keep = b ? m[j + 4] : m[j], give = b ? m[j] : m[j + 4];
+                atomicMax(&S->col_max[par][n][j * 32 + lane], max(keep, __shfl_xor_sync(0xFFFFFFFFu, give, 16)));
             }
         }
     }
@@ -209,10 +227,11 @@ __device__ __forceinline__ void emit_tile(const float (&v)[NOUT][4][8], const Ti
             S->col_max[par ^ 1][n][k] = 0u;
             if (t == 0) S->tile_max[par ^ 1] = 0u;
             if (!o.codes) continue;
-            const int64_t c = p.c0 + (k & 15) * 8 + (k >> 4);
+            const int kl = k & 15, kj = (k >> 5) + ((k >> 4) & 1) * 4;      // column 8 kl + kj of the tile
+            const int64_t c = p.c0 + 8 * kl + kj;
             const bool tile = o.tile_rows > 1;
             const uint32_t m = tile ? S->tile_max[par] : S->col_max[par][n][k];
-            S->col_inv[n][(k >> 5) * 32 + (k & 15) * 2 + ((k >> 4) & 1)] = block_inv(m);
+            S->col_inv[n][(kj >> 1) * 32 + kl * 2 + (kj & 1)] = block_inv(m);
             if (block_nonfinite(m)) note(O.status, SRQ_ERR_NONFINITE);
             if (!tile && (FULL || c < O.cols)) o.scale[c * o.ld_scale + p.r0 / QBLK] = block_size(m);
             if (tile && k == 0) o.scale[(p.c0 / QBLK) * o.ld_scale + p.r0 / QBLK] = block_size(m);
@@ -224,18 +243,16 @@ __device__ __forceinline__ void emit_tile(const float (&v)[NOUT][4][8], const Ti
         const Blocks& o = O.rm[n];
         if (!o.codes) continue;
         const bool tile = NOUT == 1 && o.tile_rows > 1;
-        // the divisions of four rows once per thread: lane l of a row's sixteen does row l % 4's
-        const int pick = l & 3;
-        uint32_t m = pick == 0 ? row_max[n][0] : pick == 1 ? row_max[n][1] : pick == 2 ? row_max[n][2] : row_max[n][3];
-        if (tile) m = S->tile_max[par];
+        // a division per thread: lane l has its row l % R's absmax
+        const uint32_t m = tile ? S->tile_max[par] : row_max[n];
         const float inv = block_inv(m);
         if (block_nonfinite(m)) note(O.status, SRQ_ERR_NONFINITE);
-        const int64_t r_mine = r_first + pick;
-        if (!tile && l < 4 && (FULL || r_mine < O.rows)) o.scale[r_mine * o.ld_scale + p.c0 / QBLK] = block_size(m);
+        const int64_t r_mine = r_first + (l & (R - 1));
+        if (!tile && l < R && (FULL || r_mine < O.rows)) o.scale[r_mine * o.ld_scale + p.c0 / QBLK] = block_size(m);
         if (tile && tid == 0) o.scale[(p.r0 / QBLK) * o.ld_scale + p.c0 / QBLK] = block_size(m);
         uint8_t* dst = o.codes + r_first * o.ld + c_first;
 #pragma unroll
-        for (int i = 0; i < 4; ++i, dst += o.ld) {
+        for (int i = 0; i < R; ++i, dst += o.ld) {
             const float f = __shfl_sync(0xFFFFFFFFu, inv, (lane & 16) + i);
             const float (&x)[8] = v[n][i];
             uint32_t rnd[8] = {};
@@ -256,7 +273,7 @@ __device__ __forceinline__ void emit_tile(const float (&v)[NOUT][4][8], const Ti
         if constexpr (SR) {
             uint32_t w[8] = {};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {                  // a row's thresholds at a time
+            for (int i = 0; i < R; ++i) {                  // a row's thresholds at a time
                 uint32_t rnd[8];
                 thresholds8(O.index_offset + (uint64_t)(r_first + i) * (uint64_t)O.cols + (uint64_t)c_first, O.keys[n], rnd);
 #pragma unroll
@@ -269,9 +286,9 @@ __device__ __forceinline__ void emit_tile(const float (&v)[NOUT][4][8], const Ti
 #pragma unroll
             for (int j = 0; j < 8; j += 2) {
                 const float2 f = *reinterpret_cast<const float2*>(&S->col_inv[n][(j >> 1) * 32 + 2 * l]);
-                float2 t[4];
+                float2 t[R];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) t[i] = __fmul2_rn(make_float2(v[n][i][j], v[n][i][j + 1]), f);
+                for (int i = 0; i < R; ++i) t[i] = __fmul2_rn(make_float2(v[n][i][j], v[n][i][j + 1]), f);
                 words[j * 32] = e4m3x4(t[0].x, t[1].x, t[2].x, t[3].x);
                 words[(j + 1) * 32] = e4m3x4(t[0].y, t[1].y, t[2].y, t[3].y);
             }
@@ -287,20 +304,19 @@ __device__ __forceinline__ void emit_tile(const float (&v)[NOUT][4][8], const Ti
             // (l = c / 8)
             const int q = tid & 7;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
+            for (int h = 0; h < R / 2; ++h) {
                 const int cc = (tid >> 3) + 64 * h, lc = cc >> 3;
                 const uint4 w = *reinterpret_cast<const uint4*>(&S->words[n][cc * 32 + ((q ^ (lc >> 1)) << 2)]);
                 *reinterpret_cast<uint4*>(o.codes + (p.c0 + cc) * o.ld + p.r0 + 16 * q) = (lc & 1) ? make_uint4(w.z, w.w, w.x, w.y) : w;
             }
         } else {
-            const int warp = tid >> 5;
             const int64_t r = p.r0 + 4 * lane;
 #pragma unroll 1
-            for (int k = 0; k < 8; ++k) {
-                const int cc = 8 * warp + k;
+            for (int k = 0; k < 2 * R; ++k) {
+                const int cc = 2 * R * (tid >> 5) + k;
                 const int64_t c = p.c0 + cc;
                 if (c >= O.cols || r >= O.rows) continue;
-                const uint32_t w = S->words[n][cc * 32 + (lane ^ (2 * warp))];
+                const uint32_t w = S->words[n][cc * 32 + (lane ^ (2 * (cc >> 3)))];
                 uint8_t* dst = o.codes + c * o.ld + r;
                 if (r + 4 <= O.rows) *reinterpret_cast<uint32_t*>(dst) = w;
                 else
@@ -312,7 +328,7 @@ __device__ __forceinline__ void emit_tile(const float (&v)[NOUT][4][8], const Ti
 
 template <int NOUT>
 __device__ __forceinline__ void clear_maxima(TileShared<NOUT>* S) {
-    for (int t = threadIdx.x; t < 2 * NOUT * QBLK; t += TQ_THREADS) S->col_max[0][0][t] = 0u;
+    for (int t = threadIdx.x; t < 2 * NOUT * QBLK; t += blockDim.x) S->col_max[0][0][t] = 0u;
     if (threadIdx.x < 2) S->tile_max[threadIdx.x] = 0u;
 }
 
@@ -325,7 +341,7 @@ struct QuantBlocksParams {
 
 // SRC: 0 binary32, 1 bfloat16, 2 block codes.
 template <int SRC, bool SR>
-__global__ void __launch_bounds__(TQ_THREADS, SR ? 1 : 2) quantize_blocks_kernel(const __grid_constant__ QuantBlocksParams P) {
+__global__ void __launch_bounds__(TQ_THREADS, 2 - SR) quantize_blocks_kernel(const __grid_constant__ QuantBlocksParams P) {
     pdl_enter();
     extern __shared__ __align__(16) uint8_t ahead[];
     __shared__ TileShared<1> S;
@@ -405,14 +421,14 @@ __global__ void __launch_bounds__(TQ_THREADS, 1) glu_bwd_kernel(const __grid_con
     if (brings && p.full) coded_scales(scale_slot, 0)[scale_row] = fetch_scale(scale_of, p, scale_row);
 #pragma unroll 1
     for (uint32_t tile = blockIdx.x; tile < P.tiles; par ^= 1) {
-        float v[3][4][8];                // read as dh, g, u
+        float v[3][R][8];                // read as dh, g, u
         cp_async_wait();
         __syncthreads();                 // everybody's pieces have landed, the last tile's shared words have been read
         read_matrix<T>(ahead_dh, (const T*)P.dh, P.ld_dh, rows, cols, P.vec, p, v[0]);
         read_coded(ahead_g, par, P.gate, rows, cols, p, v[1]);
         read_coded(ahead_u, par, P.up, rows, cols, p, v[2]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < R; ++i) {
 #pragma unroll
             for (int j = 0; j < 8; j += 2) {
                 auto two = [&](int m) { return make_float2(v[m][i][j], v[m][i][j + 1]); };
