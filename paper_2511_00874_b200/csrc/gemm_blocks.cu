@@ -637,32 +637,39 @@ gemm_blocks_small_kernel(const __grid_constant__ CUtensorMap map_a, const __grid
             }
         }
     } else if (warp == 1) {
-        if (lane == 0) {
-            const uint32_t idesc = make_idesc(1, 128, BN);
-            uint32_t it = 0;
-            bool ok = true;
-            for (int32_t kb = kb0; kb < kb1; ++kb, ++it) {
-                const uint32_t s = it % STAGES, ph = (it / STAGES) & 1u, buf = it % BUFS, use = it / BUFS;
-                if (!mbar_wait(&T->tmem_empty[buf], (use & 1u) ^ 1u, &T->abort_flag) ||
-                    !mbar_wait(&T->full[s], ph, &T->abort_flag)) { gb_give_up(&T->abort_flag, P.status); ok = false; break; }
-                tc_fence_after();
-                const uint64_t dw = make_smem_desc(smem_u32(smem + (size_t)s * C::STAGE_BYTES));
-                const uint64_t dx = dw + (uint64_t)((C::W_BYTES * (GLU ? 2 : 1)) >> 4);
-                const uint32_t d = tmem_base + buf * C::COLS;
+        // the whole warp walks the loop, one elected lane issues (see the pair kernel)
+        constexpr uint32_t idesc = make_idesc(1, 128, BN);
+        const uint32_t elected = elect_one();
+        uint32_t s = 0, ph = 0, buf = 0, buf_ph = 1;
+        const uint64_t desc0 = make_smem_desc(smem_u32(smem));
+        bool ok = true;
+        for (int32_t kb = kb0; kb < kb1; ++kb) {
+            ok = mbar_wait(&T->full[s], ph, &T->abort_flag) && mbar_wait(&T->tmem_empty[buf], buf_ph, &T->abort_flag);
+            ok = !__any_sync(0xFFFFFFFFu, !ok);
+            if (!ok) { gb_give_up(&T->abort_flag, P.status); break; }
+            tc_fence_after();
+            const uint64_t dw = desc0 + (uint64_t)(s * (C::STAGE_BYTES >> 4)), dx = dw + (uint64_t)((C::W_BYTES * (GLU ? 2 : 1)) >> 4);
+            const uint32_t d = tmem_base + buf * C::COLS;
+            if (elected) {
 #pragma unroll
                 for (int k = 0; k < GB_K / GB_UMMA_K; ++k) {
                     const uint64_t o = (uint64_t)((k * GB_UMMA_K) >> 4);
                     umma<1, 1>(d, dw + o, dx + o, idesc, k ? 1u : 0u);
                     if constexpr (GLU) umma<1, 1>(d + BN, dw + (uint64_t)(C::W_BYTES >> 4) + o, dx + o, idesc, k ? 1u : 0u);
                 }
-                umma_commit<1>(&T->empty[s], false);
                 umma_commit<1>(&T->tmem_full[buf], false);
+                umma_commit<1>(&T->empty[s], false);
             }
-            if (!ok) {
-                umma_commit<1>(&T->drain, false);
-                const uint64_t w0 = global_ns();
-                while (!mbar_try_wait(&T->drain, 0u) && global_ns() - w0 < WAIT_LIMIT_NS) {}
-            }
+            __syncwarp();
+            s = s + 1 == (uint32_t)STAGES ? 0u : s + 1;
+            ph ^= s == 0u ? 1u : 0u;
+            buf = buf + 1 == (uint32_t)BUFS ? 0u : buf + 1;
+            buf_ph ^= buf == 0u ? 1u : 0u;
+        }
+        if (!ok && elected) {
+            umma_commit<1>(&T->drain, false);
+            const uint64_t w0 = global_ns();
+            while (!mbar_try_wait(&T->drain, 0u) && global_ns() - w0 < WAIT_LIMIT_NS) {}
         }
     } else {
         const int quarter = warp & 3, ew = warp - 2;
@@ -682,7 +689,6 @@ gemm_blocks_small_kernel(const __grid_constant__ CUtensorMap map_a, const __grid
         float acc[C::COLS];
 #pragma unroll
         for (int i = 0; i < C::COLS; ++i) acc[i] = 0.0f;
-        bool ok = true;
         float4 nw = scales4(rw, kb0 >> 2, P.num_kb, P.b_vec), nw2 = scales4(rw2, kb0 >> 2, P.num_kb, P.b_vec);
         float4 nt[TPL];
 #pragma unroll
@@ -709,8 +715,7 @@ gemm_blocks_small_kernel(const __grid_constant__ CUtensorMap map_a, const __grid
             }
             const float sw = pick4(cw, in4), sw2 = pick4(cw2, in4);
             const uint32_t buf = it % BUFS, use = it / BUFS;
-            if (ok && !mbar_wait(&T->tmem_full[buf], use & 1u, &T->abort_flag)) { gb_give_up(&T->abort_flag, P.status); ok = false; }
-            if (__any_sync(0xFFFFFFFFu, !ok)) ok = false;
+            wait_or_abort(smem_u32(&T->tmem_full[0]) + 8 * buf, use & 1u, &T->abort_flag, P.status);
             tc_fence_after();
 #pragma unroll
             for (int c = 0; c < C::COLS / 16; ++c) {
@@ -880,18 +885,33 @@ static bool blocks_device(BlocksDevice** out) {
     return true;
 }
 
-// In how many parts the contraction of `tiles` few-token tiles is cut: the split with the fewest k-blocks
-// per SM, counting whole rounds of resident clusters; ties go to fewer parts.
-static int small_parts(const BlocksDevice& d, int64_t tiles, int32_t num_kb) {
-    int best = 1;
-    int64_t best_cost = -1;
-    for (int s = 1; s <= 8 && s <= num_kb; ++s) {
-        if (d.clusters[s] <= 0) continue;
-        const int32_t per = (num_kb + s - 1) / s;
-        if ((num_kb + per - 1) / per != s) continue;                 // a part would be empty
-        const int64_t rounds = (tiles + d.clusters[s] - 1) / d.clusters[s];
-        const int64_t cost = rounds * (per + 4);                     // a round costs about four k-blocks on top
-        if (best_cost < 0 || cost < best_cost) { best = s; best_cost = cost; }
+// Which kernel, and how its tiles are cut.  Both kernels' time is modelled in units of 10 ns from measurements (N and K of 512
+// to 4096; the products of a whole family of sizes are within a fifth of it):
+//   few tokens   rounds (k-blocks of a part x cost(bn) + 300 + cost(part) (parts - 1)), where a k-block costs a CTA 28 / 38 /
+//                55 / 90 with tiles of 16 / 32 / 64 / 128 tokens (gated: 50 / 73 / 115, it adds up two projections), a further
+//                part of the contraction 20 (gated: 100) for the exchange, and a round is what is resident at a time
+//   CTA pairs    rounds x k-blocks x 55 + 400 (gated: + 250 per round for its longer epilogue)
+// 333 tokens, 2048 -> 2560: pairs 13.7 us on 20 of 74 pairs, tiles of 64 tokens 12.6; 512 tokens, 512 outputs: 12.8 and 9;
+// 1024 tokens, 2048 -> 2560: 14.3 and 35.
+struct Plan { bool pairs; int bn, parts; };
+static Plan plan_product(const BlocksDevice& d, int64_t M, int64_t N, int32_t num_kb, bool glu) {
+    Plan best = {true, 0, 0};
+    const int64_t cols = glu ? 128 : GB_N, tiles = ((M + 2 * GB_M - 1) / (2 * GB_M)) * ((N + cols - 1) / cols);
+    const int64_t per_round = (int64_t)num_kb * 55 + (glu ? 250 : 0);
+    int64_t cost = d.pairs > 0 ? (tiles + d.pairs - 1) / d.pairs * per_round + 400 : INT64_MAX;
+    static const int kCost[2][4] = {{28, 38, 55, 90}, {50, 73, 115, 0}};
+    for (int i = 0; i < (glu ? 3 : 4); ++i) {
+        const int bn = 16 << i;
+        if (i > 0 && bn / 2 >= M) break;                             // half as many would do
+        const int64_t n = ((N + 127) / 128) * ((M + bn - 1) / bn);
+        if ((M + bn - 1) / bn > 65535) continue;                     // grid limit
+        for (int s = 1; s <= 8 && s <= num_kb; ++s) {
+            if (d.clusters[s] <= 0) continue;
+            const int32_t per = (num_kb + s - 1) / s;
+            if ((num_kb + per - 1) / per != s) continue;             // a part would be empty
+            const int64_t c = (n + d.clusters[s] - 1) / d.clusters[s] * ((int64_t)per * kCost[glu][i] + 300 + (glu ? 100 : 20) * (s - 1));
+            if (c < cost) { cost = c; best = {false, bn, s}; }
+        }
     }
     return best;
 }
@@ -923,12 +943,9 @@ static cudaError_t launch_pair(const CUtensorMap& ma, const CUtensorMap& mb, con
     return cudaLaunchKernelEx(&cfg, gemm_blocks_kernel<GLU, COLV>, ma, mb, mb2, mo, mg, mu, P);
 }
 
-// Few-token form: as many tokens per CTA as cover M, 128 at most (64 in the gated block, whose sums are two).
-static srq_status_t run_small(const BlocksDevice& d, GemmBlocksParams& P, bool glu, int64_t Kc, cudaStream_t stream) {
-    int bn = 16;
-    while (bn < P.M && bn < (glu ? 64 : 128)) bn *= 2;
+static srq_status_t run_small(const Plan& plan, GemmBlocksParams& P, bool glu, int64_t Kc, cudaStream_t stream) {
+    const int bn = plan.bn, parts = plan.parts;
     const int64_t tiles_n = (P.N + 127) / 128, tiles_t = (P.M + bn - 1) / bn;
-    const int parts = small_parts(d, tiles_n * tiles_t, P.num_kb);
     CUtensorMap ma, mb, mb2;
     if (!encode_codes(&ma, P.a, P.M, Kc, bn) || !encode_codes(&mb, P.b, P.N, Kc, 128)) return SRQ_ERR_CUDA;
     mb2 = mb;
@@ -978,10 +995,9 @@ static srq_status_t run_pairs(const BlocksDevice& d, GemmBlocksParams& P, bool g
     return e == cudaSuccess ? SRQ_OK : SRQ_ERR_CUDA;
 }
 
-// Few-token kernel or CTA pairs.
-static bool use_small(const BlocksDevice& d, const GemmBlocksParams& P, bool glu) {
-    (void)d; (void)glu;
-    return P.M <= 128;
+static srq_status_t run_product(const BlocksDevice& d, GemmBlocksParams& P, bool glu, int64_t Kc, cudaStream_t stream) {
+    const Plan plan = plan_product(d, P.M, P.N, P.num_kb, glu);
+    return plan.pairs ? run_pairs(d, P, glu, Kc, stream) : run_small(plan, P, glu, Kc, stream);
 }
 
 srq_status_t launch_gemm_blocks(const GemmBlocksArgs& g, uint32_t* status, cudaStream_t stream) {
@@ -992,7 +1008,7 @@ srq_status_t launch_gemm_blocks(const GemmBlocksArgs& g, uint32_t* status, cudaS
     P.a = g.a; P.b = g.b; P.a_vec = scale_vec(g.a); P.b_vec = scale_vec(g.b);
     P.out = g.out; P.ldo = g.ldo; P.out_bf16 = g.out_dt == SRQ_BF16; P.accumulate = g.accumulate;
     P.status = status;
-    return use_small(*d, P, false) ? run_small(*d, P, false, g.Kc, stream) : run_pairs(*d, P, false, g.Kc, stream);
+    return run_product(*d, P, false, g.Kc, stream);
 }
 
 srq_status_t launch_glu_fwd(const GluArgs& g, uint32_t* status, cudaStream_t stream) {
@@ -1004,7 +1020,7 @@ srq_status_t launch_glu_fwd(const GluArgs& g, uint32_t* status, cudaStream_t str
     P.out = g.h_out; P.ldo = g.ld_h; P.out_bf16 = g.h_dt == SRQ_BF16;
     P.h = g.h; P.gate = g.gate; P.up = g.up; P.gelu = g.act == SRQ_GELU;
     P.status = status;
-    return use_small(*d, P, true) ? run_small(*d, P, true, g.K, stream) : run_pairs(*d, P, true, g.K, stream);
+    return run_product(*d, P, true, g.K, stream);
 }
 
 }  // namespace srq
