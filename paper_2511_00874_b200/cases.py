@@ -4,6 +4,7 @@
     python -m paper_2511_00874_b200.cases gemm --M 8192 --N 4096 --K 4096
     python -m paper_2511_00874_b200.cases layer --T 16384 --N 2304 --K 768
     python -m paper_2511_00874_b200.cases mma-peak --k-blocks 2048 --seconds 2
+    python -m paper_2511_00874_b200.cases mlp --T 16384 --K 2048 --N 5632
 
     python -m paper_2511_00874_b200.cases sweep --config 3
 
@@ -159,6 +160,36 @@ def case_layer(a):
             "ms": med, "ms_best": best, "TOPS": ops / med / 1e9}
 
 
+def case_mlp(a):
+    """Norm, gated feed-forward block and down projection on block-scaled codes (mlp.GatedMLP): K features, N hidden
+    features, T tokens; forward and, unless --forward-only, backward."""
+    from . import mlp
+    T, K, F = a.T, a.K, a.N
+    dt = torch.bfloat16
+    m = mlp.GatedMLP(T, K, F, B.GELU if a.act == "gelu" else B.SILU, dt)
+    mk = lambda r, c, std, seed: synth.normal((r, c), std, a.seed + seed, dt, "cuda")  # noqa: E731
+    m.load(torch.ones(K, dtype=dt, device="cuda"), mk(F, K, K ** -0.5, 1), mk(F, K, K ** -0.5, 2), mk(K, F, F ** -0.5, 3))
+    x, res, dout = mk(T, K, 1.0, 4), mk(T, K, 1.0, 5), mk(T, K, 1e-2, 6)
+    q = B.block_sr(a.seed, 1) if a.round == "sr" else B.BLOCK_RNE
+
+    def fn():
+        m.forward(x, res)
+        if not a.forward_only:
+            m.backward(dout, dout, q)
+    if a.graph:
+        fn()
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            fn()
+        fn = g.replay
+    med, best = _time(fn, a.iters, a.warmup, flush=T * F < L2_BYTES)
+    assert m.status.item() == 0
+    ops = (6.0 if a.forward_only else 18.0) * T * K * F
+    return {"op": "mlp fwd" if a.forward_only else "mlp fwd+bwd", "T": T, "features": K, "hidden": F, "act": a.act, "round": a.round,
+            "graph": bool(a.graph), "ms": med, "ms_best": best, "TOPS": ops / med / 1e9}
+
+
 # ---------------------------------------------------------------------------------------------
 # workload families
 # ---------------------------------------------------------------------------------------------
@@ -262,7 +293,7 @@ def case_sweep(a):
 def main(argv=None):
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     sub = ap.add_subparsers(dest="op", required=True)
-    for name in ("quantize", "gemm", "layer", "sweep", "mma-peak"):
+    for name in ("quantize", "gemm", "layer", "sweep", "mma-peak", "mlp"):
         p = sub.add_parser(name)
         p.add_argument("--iters", type=int, default=20)
         p.add_argument("--warmup", type=int, default=3)
@@ -290,14 +321,22 @@ def main(argv=None):
         if name == "mma-peak":
             p.add_argument("--k-blocks", dest="k_blocks", type=int, default=2048, help="128-byte blocks of contraction per CTA pair")
             p.add_argument("--seconds", type=float, default=0.0, help="also repeat the launch back to back for this long")
-        if name not in ("gemm", "sweep", "mma-peak"):
+        if name == "mlp":
+            p.add_argument("--T", type=int, default=16384, help="tokens")
+            p.add_argument("--K", type=int, default=2048, help="features")
+            p.add_argument("--N", type=int, default=5632, help="hidden features (a multiple of 128)")
+            p.add_argument("--act", default="silu", choices=["silu", "gelu"])
+            p.add_argument("--round", default="rne", choices=["rne", "sr"], help="rounding of the gradients")
+            p.add_argument("--forward-only", dest="forward_only", action="store_true")
+            p.add_argument("--graph", action="store_true", help="record the step in a CUDA graph and time its replay")
+        if name not in ("gemm", "sweep", "mma-peak", "mlp"):
             p.add_argument("--dtype", default="f32", choices=["f32", "bf16"])
             p.add_argument("--scale", default="tensor", choices=["tensor", "row"])
             p.add_argument("--round", default="sr", choices=["sr", "rtn", "sr8"])
     a = ap.parse_args(argv)
     if not torch.cuda.is_available():
         raise SystemExit("a CUDA device is required (there is no CPU fallback)")
-    res = {"quantize": case_quantize, "gemm": case_gemm, "layer": case_layer, "sweep": case_sweep, "mma-peak": case_mma_peak}[a.op](a)
+    res = {"quantize": case_quantize, "gemm": case_gemm, "layer": case_layer, "sweep": case_sweep, "mma-peak": case_mma_peak, "mlp": case_mlp}[a.op](a)
     if res is not None:
         print(json.dumps(res))
 
