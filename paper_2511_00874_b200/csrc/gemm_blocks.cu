@@ -555,6 +555,12 @@ struct SmallCfg {
     static constexpr int BUFS = 512 / COLS > 4 ? 4 : 512 / COLS;
     static constexpr int TMEM = BUFS * COLS < 32 ? 32 : BUFS * COLS;
     static_assert((size_t)STAGES * STAGE_BYTES >= (size_t)COLS * 128 * 4, "the ring holds the partial sums afterwards");
+    // Warps that add up: four, or eight that share the columns (the gated block: one half the gate, the other the up
+    // projection).  With four a k-block of 128 tokens took 0.83 us, with eight 0.5.
+    static constexpr int GROUPS = COLS >= 64 ? 2 : 1;
+    static constexpr int EW = 4 * GROUPS, THREADS = 64 + 32 * EW;
+    static constexpr int MY_COLS = COLS / GROUPS;                           // sums per thread
+    static constexpr int MY_TOKENS = GLU ? BN : BN / GROUPS;                // tokens whose step sizes a warp needs
 };
 template <int BN, bool GLU>
 struct SmallTail {
@@ -562,9 +568,8 @@ struct SmallTail {
     uint64_t full[C::STAGES], empty[C::STAGES], tmem_full[C::BUFS], tmem_empty[C::BUFS], drain;
     uint32_t tmem_base;
     volatile uint32_t abort_flag;
-    alignas(16) float token_scale[4][4][BN];           // [warp][k-block of the chunk][token]
+    alignas(16) float token_scale[C::EW][4][C::MY_TOKENS];           // [warp][k-block of the chunk][token]
 };
-constexpr int SMALL_THREADS = 192;
 template <int BN, bool GLU>
 constexpr size_t small_smem() { return 1024 + (size_t)SmallCfg<BN, GLU>::STAGES * SmallCfg<BN, GLU>::STAGE_BYTES + sizeof(SmallTail<BN, GLU>); }
 
@@ -581,7 +586,7 @@ __device__ __forceinline__ uint32_t cluster_nctarank() {
 
 // a: tokens [M], b (and b2): weights [N].  Cluster of S CTAs along x: CTA r takes k-blocks [r per, (r + 1) per).
 template <int BN, bool GLU>
-__global__ void __launch_bounds__(SMALL_THREADS, 1)
+__global__ void __launch_bounds__(SmallCfg<BN, GLU>::THREADS, 1)
 gemm_blocks_small_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                          const __grid_constant__ CUtensorMap map_b2, const __grid_constant__ GemmBlocksParams P) {
     pdl_trigger();                       // the wait follows the set-up below, which touches only shared memory and TMEM
@@ -594,7 +599,7 @@ gemm_blocks_small_kernel(const __grid_constant__ CUtensorMap map_a, const __grid
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) { mbar_init(&T->full[s], 1); mbar_init(&T->empty[s], 1); }
-        for (int b = 0; b < BUFS; ++b) { mbar_init(&T->tmem_full[b], 1); mbar_init(&T->tmem_empty[b], 4); }
+        for (int b = 0; b < BUFS; ++b) { mbar_init(&T->tmem_full[b], 1); mbar_init(&T->tmem_empty[b], C::EW); }
         mbar_init(&T->drain, 1);
         T->abort_flag = 0u;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -672,31 +677,36 @@ gemm_blocks_small_kernel(const __grid_constant__ CUtensorMap map_a, const __grid
             while (!mbar_try_wait(&T->drain, 0u) && global_ns() - w0 < WAIT_LIMIT_NS) {}
         }
     } else {
-        const int quarter = warp & 3, ew = warp - 2;
+        const int quarter = warp & 3, ew = warp - 2, grp = ew >> 2;
         const int wrow = quarter * 32 + lane;              // weight row within the tile = TMEM lane
         const int64_t n = n0 + wrow;
-        const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16);
-        const float* rw = n < P.N ? P.b.scale + (P.b.tile_rows > 1 ? tn : n) * P.b.ld_scale : nullptr;
-        const float* rw2 = GLU && n < P.N ? P.b2.scale + (P.b2.tile_rows > 1 ? tn : n) * P.b2.ld_scale : nullptr;
-        constexpr int TPL = (BN + 31) / 32;                // tokens whose step sizes this lane fetches
+        const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + grp * C::MY_COLS;
+        // one projection per thread, or both (gate columns, then up columns)
+        constexpr bool BOTH = GLU && C::GROUPS == 1;
+        const Blocks& wb = GLU && C::GROUPS == 2 && grp == 1 ? P.b2 : P.b;
+        const int64_t wr = wb.tile_rows > 1 ? tn : n;
+        const float* rw = n < P.N ? wb.scale + wr * wb.ld_scale : nullptr;
+        const float* rw2 = BOTH && n < P.N ? P.b2.scale + wr * P.b2.ld_scale : nullptr;
+        const int tok0 = GLU ? 0 : grp * C::MY_TOKENS;     // first of this warp's tokens
+        constexpr int TPL = (C::MY_TOKENS + 31) / 32;      // tokens whose step sizes this lane fetches
         const float* rt[TPL];
 #pragma unroll
         for (int i = 0; i < TPL; ++i) {
-            const int64_t t = t0 + lane + 32 * i;
-            rt[i] = (lane + 32 * i < BN && t < P.M) ? P.a.scale + (P.a.tile_rows > 1 ? t / QBLK : t) * P.a.ld_scale : nullptr;
+            const int64_t t = t0 + tok0 + lane + 32 * i;
+            rt[i] = (lane + 32 * i < C::MY_TOKENS && t < P.M) ? P.a.scale + (P.a.tile_rows > 1 ? t / QBLK : t) * P.a.ld_scale : nullptr;
         }
-        float (*ts)[BN] = T->token_scale[ew];
-        float acc[C::COLS];
+        float (*ts)[C::MY_TOKENS] = T->token_scale[ew];
+        float2 acc[C::MY_COLS / 2];
 #pragma unroll
-        for (int i = 0; i < C::COLS; ++i) acc[i] = 0.0f;
+        for (int i = 0; i < C::MY_COLS / 2; ++i) acc[i] = make_float2(0.0f, 0.0f);
         float4 nw = scales4(rw, kb0 >> 2, P.num_kb, P.b_vec), nw2 = scales4(rw2, kb0 >> 2, P.num_kb, P.b_vec);
         float4 nt[TPL];
 #pragma unroll
         for (int i = 0; i < TPL; ++i) nt[i] = scales4(rt[i], kb0 >> 2, P.num_kb, P.a_vec);
         float4 cw = nw, cw2 = nw2;
-        uint32_t it = 0;
+        uint32_t buf = 0, buf_ph = 0;
 #pragma unroll 1
-        for (int32_t kb = kb0; kb < kb1; ++kb, ++it) {
+        for (int32_t kb = kb0; kb < kb1; ++kb) {
             const int32_t in4 = kb & 3;
             if (in4 == 0 || kb == kb0) {
                 cw = nw; cw2 = nw2;
@@ -704,101 +714,137 @@ gemm_blocks_small_kernel(const __grid_constant__ CUtensorMap map_a, const __grid
 #pragma unroll
                 for (int i = 0; i < TPL; ++i) {
                     const int t = lane + 32 * i;
-                    if (t < BN) { ts[0][t] = nt[i].x; ts[1][t] = nt[i].y; ts[2][t] = nt[i].z; ts[3][t] = nt[i].w; }
+                    if (t < C::MY_TOKENS) { ts[0][t] = nt[i].x; ts[1][t] = nt[i].y; ts[2][t] = nt[i].z; ts[3][t] = nt[i].w; }
                 }
                 __syncwarp();
                 const int32_t next = (kb >> 2) + 1;
                 nw = scales4(rw, next, P.num_kb, P.b_vec);
-                if constexpr (GLU) nw2 = scales4(rw2, next, P.num_kb, P.b_vec);
+                if constexpr (BOTH) nw2 = scales4(rw2, next, P.num_kb, P.b_vec);
 #pragma unroll
                 for (int i = 0; i < TPL; ++i) nt[i] = scales4(rt[i], next, P.num_kb, P.a_vec);
             }
             const float sw = pick4(cw, in4), sw2 = pick4(cw2, in4);
-            const uint32_t buf = it % BUFS, use = it / BUFS;
-            wait_or_abort(smem_u32(&T->tmem_full[0]) + 8 * buf, use & 1u, &T->abort_flag, P.status);
+            wait_or_abort(smem_u32(&T->tmem_full[0]) + 8 * buf, buf_ph, &T->abort_flag, P.status);
             tc_fence_after();
 #pragma unroll
-            for (int c = 0; c < C::COLS / 16; ++c) {
+            for (int c = 0; c < C::MY_COLS / 16; ++c) {
                 uint32_t v[16];
                 tmem_ld16(taddr + buf * C::COLS + 16 * c, v);
                 tmem_ld_wait();
-                const float s = GLU && c >= BN / 16 ? sw2 : sw;
-                const float* tk = &ts[in4][(16 * c) % BN];
+                const float s = BOTH && c >= BN / 16 ? sw2 : sw;
+                const float2 s2 = make_float2(s, s);
+                const float* tk = &ts[in4][(16 * c) % C::MY_TOKENS];
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     const float4 f = *reinterpret_cast<const float4*>(tk + 4 * q);
-                    acc[16 * c + 4 * q + 0] = fmaf(__uint_as_float(v[4 * q + 0]), s * f.x, acc[16 * c + 4 * q + 0]);
-                    acc[16 * c + 4 * q + 1] = fmaf(__uint_as_float(v[4 * q + 1]), s * f.y, acc[16 * c + 4 * q + 1]);
-                    acc[16 * c + 4 * q + 2] = fmaf(__uint_as_float(v[4 * q + 2]), s * f.z, acc[16 * c + 4 * q + 2]);
-                    acc[16 * c + 4 * q + 3] = fmaf(__uint_as_float(v[4 * q + 3]), s * f.w, acc[16 * c + 4 * q + 3]);
+                    float2& x = acc[8 * c + 2 * q];
+                    float2& y = acc[8 * c + 2 * q + 1];
+                    x = __ffma2_rn(pair(v[4 * q], v[4 * q + 1]), __fmul2_rn(make_float2(f.x, f.y), s2), x);
+                    y = __ffma2_rn(pair(v[4 * q + 2], v[4 * q + 3]), __fmul2_rn(make_float2(f.z, f.w), s2), y);
                 }
             }
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(&T->tmem_empty[buf]);
+            buf = buf + 1 == (uint32_t)BUFS ? 0u : buf + 1;
+            buf_ph ^= buf == 0u ? 1u : 0u;
         }
         // this CTA's part of every sum: [token (gate, then up)][weight row], in the ring, which nothing uses any more
-        float* part = reinterpret_cast<float*>(smem);
+        float* part = reinterpret_cast<float*>(smem) + grp * C::MY_COLS * 128;
 #pragma unroll
-        for (int i = 0; i < C::COLS; ++i) part[i * 128 + wrow] = acc[i];
+        for (int i = 0; i < C::MY_COLS / 2; ++i) { part[2 * i * 128 + wrow] = acc[i].x; part[(2 * i + 1) * 128 + wrow] = acc[i].y; }
     }
 
     __syncwarp();
     tc_fence_before();
     cluster_sync();                      // all parts are there
     if (warp >= 2) {
-        // token t of the tile belongs to CTA t % parts and to one of its warps; a lane takes four columns
+        // token t of the tile belongs to CTA t % parts and to one of its warps; a lane takes four columns.  A warp works on
+        // several tokens at a time: each is a chain of dependent steps (loads, maxima, quotients) of over a thousand cycles.
+        // (With sixteen tokens at most there is little to overlap, and the longer code costs more: 8.4 us became 10.1.)
+        constexpr int U = BN == 16 ? 1 : GLU ? 4 : 2;
         const int64_t c = n0 + 4 * lane;
         const uint32_t base = smem_u32(smem) + (uint32_t)lane * 16u;
-        for (int t = (int)rank + (int)parts * (warp - 2); t < BN && t0 + t < P.M; t += (int)parts * 4) {
-            float x[4] = {0.0f, 0.0f, 0.0f, 0.0f}, y[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-            for (uint32_t r = 0; r < parts; ++r) {
-                const float4 f = ld_cluster_f4(map_to_cta(base + (uint32_t)t * 512u, r));
-                x[0] += f.x; x[1] += f.y; x[2] += f.z; x[3] += f.w;
-                if constexpr (GLU) {
-                    const float4 h = ld_cluster_f4(map_to_cta(base + (uint32_t)(BN + t) * 512u, r));
-                    y[0] += h.x; y[1] += h.y; y[2] += h.z; y[3] += h.w;
-                }
-            }
-            const int64_t row = t0 + t;
-            if constexpr (GLU) {
-                auto emit = [&](const Blocks& o, const float (&val)[4]) {
-                    uint32_t m = abs_word(absmax3(absmax3(val[0], val[1], val[2]), val[3], 0.0f));
-                    m = __reduce_max_sync(0xFFFFFFFFu, m);
-                    float step, inv;
-                    block_step(m, &step, &inv);
-                    if (lane == 0) {
-                        o.scale[row * o.ld_scale + tn] = step;
-                        if (block_nonfinite(m)) note(P.status, SRQ_ERR_NONFINITE);
-                    }
-                    const uint32_t w = e4m3x4(__fmul_rn(val[0], inv), __fmul_rn(val[1], inv), __fmul_rn(val[2], inv), __fmul_rn(val[3], inv));
-                    uint8_t* dst = o.codes + row * o.ld + c;
-                    if (c + 4 <= P.N) *reinterpret_cast<uint32_t*>(dst) = w;
-                    else
-                        for (int e = 0; e < 4; ++e) if (c + e < P.N) dst[e] = (uint8_t)(w >> (8 * e));
-                };
-                if (P.gate.codes) emit(P.gate, x);
-                if (P.up.codes) emit(P.up, y);
+        const int64_t tokens = P.M - t0 < BN ? P.M - t0 : BN;
+        const int stride = (int)parts * C::EW;
+        for (int t = (int)rank + (int)parts * (warp - 2); t < tokens; t += U * stride) {
+            float x[U][4], y[U][4];
+            auto gather = [&](float (&sum)[4], uint32_t addr) {            // all parts' loads are in flight before the first addition
+                float4 f[8];
 #pragma unroll
-                for (int e = 0; e < 4; e += 2) {
-                    const float2 g2 = make_float2(x[e], x[e + 1]), u2 = make_float2(y[e], y[e + 1]), h2 = P.gelu ? gated2<true>(g2, u2) : gated2<false>(g2, u2);
-                    x[e] = h2.x; x[e + 1] = h2.y;
+                for (uint32_t i = 0; i < 8; ++i)
+                    if (i < parts) f[i] = ld_cluster_f4(map_to_cta(addr, i));
+                sum[0] = sum[1] = sum[2] = sum[3] = 0.0f;
+#pragma unroll
+                for (uint32_t i = 0; i < 8; ++i)
+                    if (i < parts) { sum[0] += f[i].x; sum[1] += f[i].y; sum[2] += f[i].z; sum[3] += f[i].w; }
+            };
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                const int ti = t + i * stride < tokens ? t + i * stride : t;       // past the end: a token done already, not stored
+                gather(x[i], base + (uint32_t)ti * 512u);
+                if constexpr (GLU) gather(y[i], base + (uint32_t)(BN + ti) * 512u);
+            }
+            if constexpr (GLU) {
+                auto emit = [&](const Blocks& o, const float (&val)[U][4]) {
+                    if (!o.codes) return;
+                    uint32_t m[U];
+#pragma unroll
+                    for (int i = 0; i < U; ++i)
+                        m[i] = __reduce_max_sync(0xFFFFFFFFu, abs_word(absmax3(absmax3(val[i][0], val[i][1], val[i][2]), val[i][3], 0.0f)));
+                    // lane i has the divisions of token i
+                    uint32_t mine = m[0];
+#pragma unroll
+                    for (int i = 1; i < U; ++i) mine = lane == i ? m[i] : mine;
+                    const float inv = block_inv(mine);
+                    const int t_mine = t + lane * stride;
+                    if (lane < U && t_mine < tokens) {
+                        o.scale[(t0 + t_mine) * o.ld_scale + tn] = block_size(mine);
+                        if (block_nonfinite(mine)) note(P.status, SRQ_ERR_NONFINITE);
+                    }
+#pragma unroll
+                    for (int i = 0; i < U; ++i) {
+                        const float f = __shfl_sync(0xFFFFFFFFu, inv, i);
+                        const uint32_t w = encode4<false>(val[i][0], val[i][1], val[i][2], val[i][3], f, f, f, f, 0, 0, 0, 0);
+                        if (t + i * stride >= tokens) continue;
+                        uint8_t* dst = o.codes + (t0 + t + i * stride) * o.ld + c;
+                        if (c + 4 <= P.N) *reinterpret_cast<uint32_t*>(dst) = w;
+                        else
+                            for (int e = 0; e < 4; ++e) if (c + e < P.N) dst[e] = (uint8_t)(w >> (8 * e));
+                    }
+                };
+                emit(P.gate, x);
+                emit(P.up, y);
+#pragma unroll
+                for (int i = 0; i < U; ++i) {
+#pragma unroll
+                    for (int e = 0; e < 4; e += 2) {
+                        const float2 g2 = make_float2(x[i][e], x[i][e + 1]), u2 = make_float2(y[i][e], y[i][e + 1]);
+                        const float2 h2 = P.gelu ? gated2<true>(g2, u2) : gated2<false>(g2, u2);
+                        x[i][e] = h2.x; x[i][e + 1] = h2.y;
+                    }
                 }
-                if (P.h.codes) emit(P.h, x);
+                emit(P.h, x);
             }
             if (P.out) {
-                if (P.out_bf16) {
-                    __nv_bfloat16* dst = (__nv_bfloat16*)P.out + row * P.ldo + c;
-                    if (P.h_vec && c + 4 <= P.N) *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
-                    else
-                        for (int e = 0; e < 4; ++e) if (c + e < P.N) dst[e] = __float2bfloat16_rn(x[e]);
-                } else {
-                    float* dst = (float*)P.out + row * P.ldo + c;
-                    if (P.accumulate)
-                        for (int e = 0; e < 4; ++e) if (c + e < P.N) x[e] = __fadd_rn(dst[e], x[e]);
-                    if (P.h_vec && c + 4 <= P.N) *reinterpret_cast<float4*>(dst) = make_float4(x[0], x[1], x[2], x[3]);
-                    else
-                        for (int e = 0; e < 4; ++e) if (c + e < P.N) dst[e] = x[e];
+#pragma unroll
+                for (int i = 0; i < U; ++i) {
+                    const int64_t row = t0 + t + i * stride;
+                    if (t + i * stride >= tokens) continue;
+                    float (&v)[4] = x[i];
+                    if (P.out_bf16) {
+                        __nv_bfloat16* dst = (__nv_bfloat16*)P.out + row * P.ldo + c;
+                        if (P.h_vec && c + 4 <= P.N) *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+                        else
+                            for (int e = 0; e < 4; ++e) if (c + e < P.N) dst[e] = __float2bfloat16_rn(v[e]);
+                    } else {
+                        float* dst = (float*)P.out + row * P.ldo + c;
+                        if (P.accumulate)
+                            for (int e = 0; e < 4; ++e) if (c + e < P.N) v[e] = __fadd_rn(dst[e], v[e]);
+                        if (P.h_vec && c + 4 <= P.N) *reinterpret_cast<float4*>(dst) = make_float4(v[0], v[1], v[2], v[3]);
+                        else
+                            for (int e = 0; e < 4; ++e) if (c + e < P.N) dst[e] = v[e];
+                    }
                 }
             }
         }
@@ -875,7 +921,7 @@ static bool blocks_device(BlocksDevice** out) {
         d.pairs = n < d.sms / 2 ? n : d.sms / 2;
         for (int s = 1; s <= 8; ++s) {
             at.val.clusterDim.x = (unsigned)s;
-            cfg.gridDim = dim3((unsigned)(d.sms / s * s)); cfg.blockDim = dim3(SMALL_THREADS); cfg.dynamicSmemBytes = small_smem<16, false>();
+            cfg.gridDim = dim3((unsigned)(d.sms / s * s)); cfg.blockDim = dim3(SmallCfg<16, false>::THREADS); cfg.dynamicSmemBytes = small_smem<16, false>();
             if (cudaOccupancyMaxActiveClusters(&n, gemm_blocks_small_kernel<16, false>, &cfg) != cudaSuccess) { cudaGetLastError(); n = 0; }
             d.clusters[s] = n;
         }
@@ -888,18 +934,19 @@ static bool blocks_device(BlocksDevice** out) {
 // Which kernel, and how its tiles are cut.  Both kernels' time is modelled in units of 10 ns from measurements (N and K of 512
 // to 4096; the products of a whole family of sizes are within a fifth of it):
 //   few tokens   rounds (k-blocks of a part x cost(bn) + 300 + cost(part) (parts - 1)), where a k-block costs a CTA 28 / 38 /
-//                55 / 90 with tiles of 16 / 32 / 64 / 128 tokens (gated: 50 / 73 / 115, it adds up two projections), a further
-//                part of the contraction 20 (gated: 100) for the exchange, and a round is what is resident at a time
+//                42 / 62 with tiles of 16 / 32 / 64 / 128 tokens (gated: 45 / 48 / 67, and 4 per token of its share for
+//                the epilogue), a further part of the contraction 20 (gated: 50) for the exchange, and a round is what is
+//                resident at a time
 //   CTA pairs    rounds x k-blocks x 55 + 400 (gated: + 250 per round for its longer epilogue)
-// 333 tokens, 2048 -> 2560: pairs 13.7 us on 20 of 74 pairs, tiles of 64 tokens 12.6; 512 tokens, 512 outputs: 12.8 and 9;
-// 1024 tokens, 2048 -> 2560: 14.3 and 35.
+// 333 tokens, 2048 -> 2560: pairs 13.7 us on 20 of 74 pairs, tiles of 64 tokens 11.0; 1024 tokens, 512 outputs: 12.9 and 7.8;
+// 1024 tokens, 2048 -> 2560: 14.3 and 35; gated, 64 tokens, 2048 -> 5632: 16.3 and 13.3, 128 tokens: 16.8 and 20.6.
 struct Plan { bool pairs; int bn, parts; };
 static Plan plan_product(const BlocksDevice& d, int64_t M, int64_t N, int32_t num_kb, bool glu) {
     Plan best = {true, 0, 0};
     const int64_t cols = glu ? 128 : GB_N, tiles = ((M + 2 * GB_M - 1) / (2 * GB_M)) * ((N + cols - 1) / cols);
     const int64_t per_round = (int64_t)num_kb * 55 + (glu ? 250 : 0);
     int64_t cost = d.pairs > 0 ? (tiles + d.pairs - 1) / d.pairs * per_round + 400 : INT64_MAX;
-    static const int kCost[2][4] = {{28, 38, 55, 90}, {50, 73, 115, 0}};
+    static const int kCost[2][4] = {{28, 38, 42, 62}, {45, 48, 67, 0}};
     for (int i = 0; i < (glu ? 3 : 4); ++i) {
         const int bn = 16 << i;
         if (i > 0 && bn / 2 >= M) break;                             // half as many would do
@@ -909,7 +956,7 @@ static Plan plan_product(const BlocksDevice& d, int64_t M, int64_t N, int32_t nu
             if (d.clusters[s] <= 0) continue;
             const int32_t per = (num_kb + s - 1) / s;
             if ((num_kb + per - 1) / per != s) continue;             // a part would be empty
-            const int64_t c = (n + d.clusters[s] - 1) / d.clusters[s] * ((int64_t)per * kCost[glu][i] + 300 + (glu ? 100 : 20) * (s - 1));
+            const int64_t c = (n + d.clusters[s] - 1) / d.clusters[s] * ((int64_t)per * kCost[glu][i] + 300 + (glu ? 50 : 20) * (s - 1) + (glu ? 4 * (M < bn ? M : bn) / s : 0));
             if (c < cost) { cost = c; best = {false, bn, s}; }
         }
     }
@@ -922,7 +969,7 @@ template <int BN, bool GLU>
 static cudaError_t launch_small_bn(const CUtensorMap& ma, const CUtensorMap& mb, const CUtensorMap& mb2, const GemmBlocksParams& P,
                                    int parts, int64_t tiles_n, int64_t tiles_t, cudaStream_t stream) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(tiles_n * parts), (unsigned)tiles_t); cfg.blockDim = dim3(SMALL_THREADS);
+    cfg.gridDim = dim3((unsigned)(tiles_n * parts), (unsigned)tiles_t); cfg.blockDim = dim3(SmallCfg<BN, GLU>::THREADS);
     cfg.dynamicSmemBytes = small_smem<BN, GLU>(); cfg.stream = stream;
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeClusterDimension; at[0].val.clusterDim.x = (unsigned)parts; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
