@@ -5,11 +5,15 @@
 // row is read once: sum of squares (binary32, a fixed tree), then the norm, then the absmax of each
 // 128-column block, which sits in 16 neighbouring lanes, then the codes.  Both passes are bound by HBM.
 //
-// Two forms of each kernel.  The streaming one (whole groups of eight, 16-byte aligned rows of at most 16384 elements (8192 backward),
-// rounding to nearest) walks rows with a grid of resident CTAs, keeps the weight in registers, has the next row's
-// loads in flight while a row is worked on, and works on two values per instruction.  The general one takes any
-// extent, pitch and rounding, element by element where it must; rows too long for the registers (V = 0) it
-// reads twice.
+// Three forms of each kernel.
+//   stream   whole groups of eight columns, 16-byte aligned rows of at most 16384 elements (8192 backward), rounding to
+//            nearest: walks rows with a grid of resident CTAs, keeps the weight in registers, has the next row's loads
+//            in flight while a row is worked on, and works on two values per instruction
+//   any      any extent up to 8192 and any pitch, rounding to nearest: a warp takes 128 columns at a time, a lane every 32nd of
+//            them, so that rows that start anywhere are read in whole lines; the number of threads per row is a
+//            compile-time constant, so that a lane's columns are immediate offsets (with eight neighbouring columns
+//            per thread and bounds in 64 bits a value took 106 instructions and 2.5 times as long)
+//   long     what is left: longer rows (V = 0: read twice), stochastic rounding
 #include <mutex>
 
 #include "blocks.cuh"
@@ -178,6 +182,85 @@ __global__ void __launch_bounds__(V == 1 ? 1024 : 512) rmsnorm_fwd_stream_kernel
 
 template <typename W>
 __device__ __forceinline__ void load_w8(const void* w, int64_t c, int64_t cols, bool vec, float v[8]) { load8((const W*)w, c, cols, vec, v); }
+
+// The columns of lane `lane` of warp `warp` of a row in the any form: first + column_offset<TPR>(e), e = 0 .. 4 KB - 1.
+template <int TPR> __device__ __forceinline__ constexpr int column_offset(int e) { return (e >> 2) * (TPR * 4) + (e & 3) * 32; }
+
+template <typename T, typename W, int TPR, int KB>
+__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) rmsnorm_fwd_any_kernel(const __grid_constant__ NormFwdParams P) {
+    pdl_enter();
+    __shared__ float red[2][32];
+    constexpr int E = 4 * KB;
+    const NormFwdArgs& a = P.a;
+    const int t = threadIdx.x & (TPR - 1), slot = threadIdx.x / TPR, lane = threadIdx.x & 31;
+    const int32_t first = (t >> 5) * QBLK + lane, left = (int32_t)a.cols - first;      // column e exists: column_offset(e) < left
+    const int64_t step = (int64_t)gridDim.x * P.rows_per_cta;
+    float w[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) w[e] = column_offset<TPR>(e) < left ? (float)((const W*)a.w)[first + column_offset<TPR>(e)] : 0.0f;
+    T nx[E], nq[E];
+    auto fetch = [&](int64_t row) {
+        const T* x = (const T*)a.x + row * a.ldx + first;
+        const T* q = (const T*)a.residual + row * a.ld_residual + first;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const bool in = row < a.rows && column_offset<TPR>(e) < left;
+            nx[e] = in ? x[column_offset<TPR>(e)] : (T)0.0f;
+            nq[e] = in && a.residual ? q[column_offset<TPR>(e)] : (T)0.0f;
+        }
+    };
+    int64_t row = (int64_t)blockIdx.x * P.rows_per_cta + slot;
+    fetch(row);
+    const int64_t rounds = (a.rows + step - 1) / step;
+#pragma unroll 1
+    for (int64_t it = 0; it < rounds; ++it, row += step) {
+        const bool live = row < a.rows;
+        float v[E], s = 0.0f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            v[e] = __fadd_rn((float)nx[e], (float)nq[e]);
+            s = fmaf(v[e], v[e], s);
+        }
+        if (it + 1 < rounds) fetch(row + step);
+        const float rstd = rstd_of(row_sum(s, TPR, red[it & 1]), P.inv_cols, a.eps);
+        if (!live) continue;                               // whole warps; the next barrier is the next row's
+        if (t == 0 && a.rstd) a.rstd[row] = rstd;
+        if (a.r_out) {
+            T* o = (T*)a.r_out + row * a.ld_r + first;
+#pragma unroll
+            for (int e = 0; e < E; ++e) if (column_offset<TPR>(e) < left) o[column_offset<TPR>(e)] = (T)v[e];
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] = v[e] * rstd * w[e];
+        if (a.y_out) {
+            T* o = (T*)a.y_out + row * a.ld_y + first;
+#pragma unroll
+            for (int e = 0; e < E; ++e) if (column_offset<TPR>(e) < left) o[column_offset<TPR>(e)] = (T)v[e];
+        }
+        if (!a.y.codes) continue;
+        uint32_t m[KB], mine = 0u;
+#pragma unroll
+        for (int k = 0; k < KB; ++k) {
+            m[k] = __reduce_max_sync(0xFFFFFFFFu, abs_word(absmax3(absmax3(v[4 * k], v[4 * k + 1], v[4 * k + 2]), v[4 * k + 3], 0.0f)));
+            mine = (lane & (KB - 1)) == k ? m[k] : mine;   // lane k has the divisions of block k
+        }
+        const float inv = block_inv(mine);
+        const int32_t block = (t >> 5) + lane * (TPR / 32);
+        if (lane < KB && (int64_t)block * QBLK < a.cols) {
+            a.y.scale[row * a.y.ld_scale + block] = block_size(mine);
+            if (block_nonfinite(mine)) note(a.status, SRQ_ERR_NONFINITE);
+        }
+        uint8_t* codes = a.y.codes + row * a.y.ld + first;
+#pragma unroll
+        for (int k = 0; k < KB; ++k) {
+            const float f = __shfl_sync(0xFFFFFFFFu, inv, k);
+            const uint32_t c = encode4<false>(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3], f, f, f, f, 0, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (column_offset<TPR>(4 * k + i) < left) codes[column_offset<TPR>(4 * k + i)] = (uint8_t)(c >> (8 * i));
+        }
+    }
+}
 
 // One group of eight of y: block codes and / or y itself.  All 32 lanes of the warp call it together; the
 // sixteen lanes of a block have the same row and neighbouring groups.
@@ -385,130 +468,139 @@ __global__ void __launch_bounds__(512) rmsnorm_bwd_stream_kernel(const __grid_co
     }
 }
 
-// Row `first`, first + step, ... of one slot: every thread keeps its columns, so that the weight's gradient adds
-// up in its registers (or, for LONG rows, in its own words of the partial row) and leaves as one partial row
-// per slot.
-template <typename T, typename W, int V>
-__global__ void __launch_bounds__(512) rmsnorm_bwd_kernel(const __grid_constant__ NormBwdParams P) {
+template <typename T, typename W, int TPR, int KB>
+__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) rmsnorm_bwd_any_kernel(const __grid_constant__ NormBwdParams P) {
+    pdl_enter();
+    constexpr int E = 4 * KB, SLOTS = TPR < 256 ? 256 / TPR : 1;
+    __shared__ float red[2][32];
+    __shared__ float share[SLOTS > 1 ? SLOTS - 1 : 1][SLOTS > 1 ? E * TPR : 1];
+    const NormBwdArgs& a = P.a;
+    const int t = threadIdx.x & (TPR - 1), slot = threadIdx.x / TPR, lane = threadIdx.x & 31;
+    const int32_t first = (t >> 5) * QBLK + lane, left = (int32_t)a.cols - first;
+    const int64_t step = (int64_t)gridDim.x * SLOTS;
+    float w[E], dw[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        w[e] = column_offset<TPR>(e) < left ? (float)((const W*)a.w)[first + column_offset<TPR>(e)] : 0.0f;
+        dw[e] = 0.0f;
+    }
+    T ny[E], nr[E];
+    float next_rstd = 0.0f;
+    auto fetch = [&](int64_t row) {
+        const T* y = (const T*)a.dy + row * a.ld_dy + first;
+        const T* r = (const T*)a.r + row * a.ld_r + first;
+        next_rstd = row < a.rows ? __ldg(a.rstd + row) : 0.0f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const bool in = row < a.rows && column_offset<TPR>(e) < left;
+            ny[e] = in ? y[column_offset<TPR>(e)] : (T)0.0f;
+            nr[e] = in ? r[column_offset<TPR>(e)] : (T)0.0f;
+        }
+    };
+    int64_t row = (int64_t)blockIdx.x * SLOTS + slot;
+    fetch(row);
+    const int64_t rounds = (a.rows + step - 1) / step;
+#pragma unroll 1
+    for (int64_t it = 0; it < rounds; ++it, row += step) {
+        const bool live = row < a.rows;
+        const float rstd = next_rstd;
+        float g[E], n[E], s = 0.0f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            n[e] = (float)nr[e] * rstd;
+            g[e] = (float)ny[e];
+            dw[e] = fmaf(g[e], n[e], dw[e]);
+            g[e] *= w[e];
+            s = fmaf(g[e], n[e], s);
+        }
+        T q[E];
+        if (a.dx && a.d_residual) {
+            const T* d = (const T*)a.d_residual + row * a.ld_dres + first;
+#pragma unroll
+            for (int e = 0; e < E; ++e) q[e] = live && column_offset<TPR>(e) < left ? d[column_offset<TPR>(e)] : (T)0.0f;
+        }
+        if (it + 1 < rounds) fetch(row + step);
+        s = -row_sum(s, TPR, red[it & 1]) * P.inv_cols;
+        if (!a.dx || !live) continue;
+        T* o = (T*)a.dx + row * a.ld_dx + first;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            float x = rstd * fmaf(n[e], s, g[e]);
+            if (a.d_residual) x += (float)q[e];
+            if (column_offset<TPR>(e) < left) o[column_offset<TPR>(e)] = (T)x;
+        }
+    }
+    if (!a.dw) return;
+    // slots 1, 2, ... hand their sums to slot 0, in this order
+    if constexpr (SLOTS > 1) {
+        if (slot > 0) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) share[slot - 1][e * TPR + t] = dw[e];
+        }
+        __syncthreads();
+        if (slot > 0) return;
+        for (int o = 0; o + 1 < SLOTS; ++o) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) dw[e] += share[o][e * TPR + t];
+        }
+    }
+    float* part = a.partial + (int64_t)blockIdx.x * P.partial_ld + first;
+#pragma unroll
+    for (int e = 0; e < E; ++e) if (column_offset<TPR>(e) < left) part[column_offset<TPR>(e)] = dw[e];
+}
+
+// Rows too long for the registers: read twice, one CTA of 512 threads per row at a time; the weight's gradient adds up in the
+// CTA's own partial row.
+template <typename T, typename W>
+__global__ void __launch_bounds__(512) rmsnorm_bwd_long_kernel(const __grid_constant__ NormBwdParams P) {
     pdl_enter();
     __shared__ float red[2][32];
     const NormBwdArgs& a = P.a;
-    const int tpr = P.tpr, t = threadIdx.x & (tpr - 1), slot = threadIdx.x / tpr;
-    const int64_t first = (int64_t)blockIdx.x * P.slots + slot, step = (int64_t)gridDim.x * P.slots;
-    float* part = a.dw ? a.partial + first * P.partial_ld : nullptr;
-    const float inv_cols = P.inv_cols;
-    float w[V ? V : 1][8], dw[V ? V : 1][8];
-    if constexpr (V > 0) {
-#pragma unroll
-        for (int k = 0; k < V; ++k) {
-            load8((const W*)a.w, ((int64_t)k * tpr + t) * 8, a.cols, P.vec & 8, w[k]);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) dw[k][e] = 0.0f;
-        }
-    } else if (part) {
-        for (int64_t c = (int64_t)t * 8; c < a.cols; c += (int64_t)tpr * 8)
-            for (int e = 0; e < 8; ++e) part[c + e] = 0.0f;            // partial rows are padded to whole groups
-    }
-    const int64_t rounds = (a.rows + step - 1) / step;                  // the same for every slot: barriers inside
-    for (int64_t it = 0; it < rounds; ++it) {
-        const int64_t row = first + it * step;
-        const bool live = row < a.rows;
+    const W* w = (const W*)a.w;
+    float* part = a.dw ? a.partial + (int64_t)blockIdx.x * P.partial_ld : nullptr;
+    if (part)
+        for (int64_t c = threadIdx.x; c < a.cols; c += 512) part[c] = 0.0f;
+    int use = 0;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, use ^= 1) {
         const T* dy = (const T*)a.dy + row * a.ld_dy;
         const T* r = (const T*)a.r + row * a.ld_r;
-        const float rstd = live ? a.rstd[row] : 0.0f;
-        float g[V ? V : 1][8], n[V ? V : 1][8];
-        auto load_row = [&](int64_t c, float gy[8], float nn[8]) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) gy[e] = nn[e] = 0.0f;
-            if (!live || c >= a.cols) return;
-            load8(dy, c, a.cols, P.vec & 1, gy);
-            load8(r, c, a.cols, P.vec & 2, nn);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) nn[e] *= rstd;
-        };
+        const float rstd = a.rstd[row];
         float s = 0.0f;
-        if constexpr (V > 0) {
-#pragma unroll
-            for (int k = 0; k < V; ++k) load_row(((int64_t)k * tpr + t) * 8, g[k], n[k]);
-#pragma unroll
-            for (int k = 0; k < V; ++k) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    dw[k][e] = fmaf(g[k][e], n[k][e], dw[k][e]);
-                    g[k][e] *= w[k][e];
-                    s = fmaf(g[k][e], n[k][e], s);
-                }
-            }
-        } else {
-            for (int64_t c = (int64_t)t * 8; c < a.cols; c += (int64_t)tpr * 8) {
-                load_row(c, g[0], n[0]);
-                load8((const W*)a.w, c, a.cols, P.vec & 8, w[0]);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    if (part) part[c + e] = fmaf(g[0][e], n[0][e], part[c + e]);
-                    s = fmaf(g[0][e] * w[0][e], n[0][e], s);
-                }
-            }
+        for (int64_t c = threadIdx.x; c < a.cols; c += 512) {
+            const float gy = (float)dy[c], nn = (float)r[c] * rstd;
+            if (part) part[c] = fmaf(gy, nn, part[c]);
+            s = fmaf(gy * (float)w[c], nn, s);
         }
-        s = row_sum(s, tpr, red[it & 1]) * inv_cols;
-        if (a.dx && live) {
-            auto finish = [&](int64_t c, const float gw[8], const float nn[8]) {
-                if (c >= a.cols) return;
-                float o[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) o[e] = rstd * fmaf(-nn[e], s, gw[e]);
-                if (a.d_residual) {
-                    float q[8];
-                    load8((const T*)a.d_residual + row * a.ld_dres, c, a.cols, P.vec & 4, q);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) o[e] += q[e];
-                }
-                store8((T*)a.dx + row * a.ld_dx, c, a.cols, P.vec & 16, o);
-            };
-            if constexpr (V > 0) {
-#pragma unroll
-                for (int k = 0; k < V; ++k) finish(((int64_t)k * tpr + t) * 8, g[k], n[k]);
-            } else {
-                for (int64_t c = (int64_t)t * 8; c < a.cols; c += (int64_t)tpr * 8) {
-                    load_row(c, g[0], n[0]);
-                    load8((const W*)a.w, c, a.cols, P.vec & 8, w[0]);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) g[0][e] *= w[0][e];
-                    finish(c, g[0], n[0]);
-                }
-            }
-        }
-    }
-    if constexpr (V > 0) {
-        if (part) {
-#pragma unroll
-            for (int k = 0; k < V; ++k) {
-                const int64_t c = ((int64_t)k * tpr + t) * 8;
-                if (c < P.partial_ld) {
-                    *reinterpret_cast<float4*>(part + c) = make_float4(dw[k][0], dw[k][1], dw[k][2], dw[k][3]);
-                    *reinterpret_cast<float4*>(part + c + 4) = make_float4(dw[k][4], dw[k][5], dw[k][6], dw[k][7]);
-                }
-            }
+        s = row_sum(s, 512, red[use]) * P.inv_cols;
+        if (!a.dx) continue;
+        for (int64_t c = threadIdx.x; c < a.cols; c += 512) {
+            const float d = a.d_residual ? (float)((const T*)a.d_residual)[row * a.ld_dres + c] : 0.0f;
+            ((T*)a.dx)[row * a.ld_dx + c] = (T)(rstd * fmaf(-(float)r[c] * rstd, s, (float)dy[c] * (float)w[c]) + d);
         }
     }
 }
 
-// dw[c] = sum of the partial rows, in a fixed order: 8 warps take every eighth row of 32 columns, then one adds up.
-__global__ void __launch_bounds__(256) rmsnorm_dw_kernel(const float* __restrict__ partial, int64_t n, int64_t ld, int64_t cols,
-                                                         float* __restrict__ dw) {
+// dw[c] = sum of the partial rows, in a fixed order: 32 warps take every 32nd row of 32 columns (at most sixteen rows each, all
+// loads in flight at once), then one adds up.
+__global__ void __launch_bounds__(1024) rmsnorm_dw_kernel(const float* __restrict__ partial, int64_t n, int64_t ld, int64_t cols,
+                                                          float* __restrict__ dw) {
     pdl_enter();
-    __shared__ float part[8][32];
+    __shared__ float part[32][33];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int64_t c = (int64_t)blockIdx.x * 32 + lane;
-    float s = 0.0f;
-    if (c < cols)
-        for (int64_t r = warp; r < n; r += 8) s += partial[r * ld + c];
+    float v[NORM_MAX_PARTIALS / 32], s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NORM_MAX_PARTIALS / 32; ++i) v[i] = (c < cols && warp + 32 * i < n) ? __ldcg(partial + (int64_t)(warp + 32 * i) * ld + c) : 0.0f;
+#pragma unroll
+    for (int i = 0; i < NORM_MAX_PARTIALS / 32; ++i) s += v[i];
     part[warp][lane] = s;
     __syncthreads();
-    if (warp == 0 && c < cols) {
-        for (int i = 1; i < 8; ++i) s += part[i][lane];
-        dw[c] = s;
-    }
+    // warp w adds up column w
+    s = part[lane][warp];
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
+    const int64_t cw = (int64_t)blockIdx.x * 32 + warp;
+    if (lane == 0 && cw < cols) dw[cw] = s;
 }
 
 // ------------------------------------------------------------------------------------------
@@ -559,10 +651,46 @@ static cudaError_t launch_fwd_stream(const NormFwdParams& P, int v, dim3 grid, d
     }
 }
 
+// The any form: threads per row and blocks of 128 columns per warp for `cols` columns (at most 8192).
+template <template <int, int> class Launch, typename... A>
+static cudaError_t any_form(int64_t cols, A&&... args) {
+    if (cols <= 256) return Launch<32, 2>::go(args...);
+    if (cols <= 512) return Launch<32, 4>::go(args...);
+    if (cols <= 1024) return Launch<128, 2>::go(args...);
+    if (cols <= 2048) return Launch<128, 4>::go(args...);
+    if (cols <= 4096) return Launch<512, 2>::go(args...);
+    return Launch<512, 4>::go(args...);
+}
+// Resident CTAs of `threads` threads and at most 128 registers, or one per group of rows.
+static unsigned any_grid(int64_t rows, int slots, int threads, int sms) {
+    const int64_t want = (rows + slots - 1) / slots, most = (int64_t)sms * (threads <= 256 ? 2 : 1);
+    return (unsigned)(want < most ? want : most);
+}
+template <typename T, typename W> struct FwdAny {
+    template <int TPR, int KB> struct L {
+        static cudaError_t go(NormFwdParams& P, int sms, cudaStream_t st) {
+            constexpr int threads = TPR < 256 ? 256 : TPR;
+            P.tpr = TPR; P.rows_per_cta = threads / TPR;
+            return launch_pdl(rmsnorm_fwd_any_kernel<T, W, TPR, KB>, dim3(any_grid(P.a.rows, threads / TPR, threads, sms)), dim3(threads), 0, st, P);
+        }
+    };
+};
+template <typename T, typename W> struct BwdAny {
+    template <int TPR, int KB> struct L {
+        static cudaError_t go(NormBwdParams& P, int sms, unsigned* grid, cudaStream_t st) {
+            constexpr int threads = TPR < 256 ? 256 : TPR;
+            const unsigned n = any_grid(P.a.rows, threads / TPR, threads, sms);
+            *grid = n < NORM_MAX_PARTIALS ? n : NORM_MAX_PARTIALS;
+            return launch_pdl(rmsnorm_bwd_any_kernel<T, W, TPR, KB>, dim3(*grid), dim3(threads), 0, st, P);
+        }
+    };
+};
+
 template <typename T, typename W, bool SR>
 static cudaError_t launch_fwd(const NormFwdParams& P, int v, dim3 grid, dim3 block, cudaStream_t st) {
+    if constexpr (SR)                                          // rounded to nearest such short rows take the any form
+        if (v == 1) return launch_pdl(rmsnorm_fwd_kernel<T, W, 1, SR>, grid, block, 0, st, P);
     switch (v) {
-        case 1: return launch_pdl(rmsnorm_fwd_kernel<T, W, 1, SR>, grid, block, 0, st, P);
         case 2: return launch_pdl(rmsnorm_fwd_kernel<T, W, 2, SR>, grid, block, 0, st, P);
         case 4: return launch_pdl(rmsnorm_fwd_kernel<T, W, 4, SR>, grid, block, 0, st, P);
         default: return launch_pdl(rmsnorm_fwd_kernel<T, W, 0, SR>, grid, block, 0, st, P);
@@ -598,6 +726,12 @@ cudaError_t launch_rmsnorm_fwd(const NormFwdArgs& a, cudaStream_t stream) {
             return e;
         }
     }
+    if (a.cols <= 8192 && !a.rnd.sr) {
+        if (f) e = wf ? any_form<FwdAny<float, float>::L>(a.cols, P, sms, stream) : any_form<FwdAny<float, __nv_bfloat16>::L>(a.cols, P, sms, stream);
+        else e = wf ? any_form<FwdAny<__nv_bfloat16, float>::L>(a.cols, P, sms, stream) : any_form<FwdAny<__nv_bfloat16, __nv_bfloat16>::L>(a.cols, P, sms, stream);
+        count_launch();
+        return e;
+    }
     row_shape((a.cols + 7) / 8, a.rows < 512, 1024, &P.tpr, &v);
     const int threads = P.tpr < 256 ? 256 : P.tpr;
     P.rows_per_cta = threads / P.tpr;
@@ -621,20 +755,10 @@ static cudaError_t launch_bwd_stream(const NormBwdParams& P, int v, dim3 grid, d
     return v == 1 ? launch_pdl(rmsnorm_bwd_stream_kernel<T, W, 1>, grid, block, smem, st, P) : launch_pdl(rmsnorm_bwd_stream_kernel<T, W, 2>, grid, block, smem, st, P);
 }
 static cudaError_t launch_dw(const NormBwdArgs& a, int64_t partial_ld, int64_t n, cudaStream_t stream) {
-    const cudaError_t e = launch_pdl(rmsnorm_dw_kernel, dim3((unsigned)((a.cols + 31) / 32)), dim3(256), 0, stream, (const float*)a.partial, n,
+    const cudaError_t e = launch_pdl(rmsnorm_dw_kernel, dim3((unsigned)((a.cols + 31) / 32)), dim3(1024), 0, stream, (const float*)a.partial, n,
                                      partial_ld, a.cols, a.dw);
     count_launch();
     return e;
-}
-
-template <typename T, typename W>
-static cudaError_t launch_bwd(const NormBwdParams& P, int v, dim3 grid, dim3 block, cudaStream_t st) {
-    switch (v) {
-        case 1: return launch_pdl(rmsnorm_bwd_kernel<T, W, 1>, grid, block, 0, st, P);
-        case 2: return launch_pdl(rmsnorm_bwd_kernel<T, W, 2>, grid, block, 0, st, P);
-        case 4: return launch_pdl(rmsnorm_bwd_kernel<T, W, 4>, grid, block, 0, st, P);
-        default: return launch_pdl(rmsnorm_bwd_kernel<T, W, 0>, grid, block, 0, st, P);
-    }
 }
 
 cudaError_t launch_rmsnorm_bwd(const NormBwdArgs& a, cudaStream_t stream) {
@@ -662,20 +786,18 @@ cudaError_t launch_rmsnorm_bwd(const NormBwdArgs& a, cudaStream_t stream) {
         if (e != cudaSuccess || !a.dw) return e;
         return launch_dw(a, P.partial_ld, grid.x, stream);
     }
-    row_shape((a.cols + 7) / 8, true, 512, &P.tpr, &v);
-    // every slot leaves a partial row: at most as many as the workspace holds
-    const int64_t n_max = a.rows < NORM_MAX_PARTIALS ? a.rows : NORM_MAX_PARTIALS;
-    int slots = 256 / P.tpr;
-    if (slots < 1) slots = 1;
-    while (slots > 1 && slots > n_max) slots >>= 1;
-    P.slots = slots;
-    const int64_t ctas = n_max / slots;
-    const dim3 grid((unsigned)ctas), block(slots * P.tpr);
-    if (f) e = wf ? launch_bwd<float, float>(P, v, grid, block, stream) : launch_bwd<float, __nv_bfloat16>(P, v, grid, block, stream);
-    else e = wf ? launch_bwd<__nv_bfloat16, float>(P, v, grid, block, stream) : launch_bwd<__nv_bfloat16, __nv_bfloat16>(P, v, grid, block, stream);
+    unsigned grid = 0;
+    if (a.cols <= 8192) {
+        if (f) e = wf ? any_form<BwdAny<float, float>::L>(a.cols, P, sms, &grid, stream) : any_form<BwdAny<float, __nv_bfloat16>::L>(a.cols, P, sms, &grid, stream);
+        else e = wf ? any_form<BwdAny<__nv_bfloat16, float>::L>(a.cols, P, sms, &grid, stream) : any_form<BwdAny<__nv_bfloat16, __nv_bfloat16>::L>(a.cols, P, sms, &grid, stream);
+    } else {
+        grid = (unsigned)(a.rows < NORM_MAX_PARTIALS ? a.rows : NORM_MAX_PARTIALS);
+        if (f) e = wf ? launch_pdl(rmsnorm_bwd_long_kernel<float, float>, dim3(grid), dim3(512), 0, stream, P) : launch_pdl(rmsnorm_bwd_long_kernel<float, __nv_bfloat16>, dim3(grid), dim3(512), 0, stream, P);
+        else e = wf ? launch_pdl(rmsnorm_bwd_long_kernel<__nv_bfloat16, float>, dim3(grid), dim3(512), 0, stream, P) : launch_pdl(rmsnorm_bwd_long_kernel<__nv_bfloat16, __nv_bfloat16>, dim3(grid), dim3(512), 0, stream, P);
+    }
     count_launch();
     if (e != cudaSuccess || !a.dw) return e;
-    return launch_dw(a, P.partial_ld, ctas * slots, stream);
+    return launch_dw(a, P.partial_ld, grid, stream);
 }
 
 }  // namespace srq
