@@ -402,8 +402,8 @@ srq_status_t srq_requantize_blocks(const srq_blocks_t *x, int64_t rows, int64_t 
  *   out[i, j] = sum over blocks k of  sA[i, k] * sB[j, k] * sum_{c in block k} a[i, c] * b[j, c]
  * in binary32, the inner sums on the tensor cores.  out is binary32 or bfloat16 (out_dt, rounded once, to
  * nearest even), pitch ldo elements.  accumulate = 1 adds to a binary32 out instead of overwriting it.  Any M
- * from one token up; the sum's order depends on the sizes only, so results repeat bit for bit (with
- * accumulate = 1 too: one addition per element). */
+ * from one token up; the sum's order depends on sizes, types, alignment and the device alone, so that the same
+ * call repeats bit for bit (with accumulate = 1 too: one addition per element). */
 srq_status_t srq_gemm_blocks(const srq_blocks_t *a, const srq_blocks_t *b, int64_t M, int64_t N, int64_t Kc,
                              void *out, srq_dtype_t out_dt, int64_t ldo, int32_t accumulate,
                              uint32_t *device_status, void *cuda_stream);

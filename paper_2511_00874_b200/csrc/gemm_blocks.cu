@@ -27,6 +27,7 @@
 // waiting any more, and TMEM is freed.
 #include <cuda.h>
 
+#include <climits>
 #include <mutex>
 #include <type_traits>
 
@@ -52,6 +53,7 @@ constexpr int GB_SCALE_SLOTS = 3;                      // chunks of four k-block
 struct GemmBlocksParams {
     int64_t M, N;                       // N: columns of out, or of h (the gated block's F)
     int32_t num_kb, tiles_m, tiles_n;
+    int32_t full_tiles, half_kb;        // pairs: tiles from full_tiles on are done in two parts, k-blocks [0, half_kb) and the rest
     Blocks a, b, b2;                    // b2: up projection of the gated block
     int32_t a_vec, b_vec;               // 16-byte loads of four step sizes allowed
     void* out; int64_t ldo; int32_t out_bf16, tma_out, accumulate;
@@ -193,9 +195,20 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     const uint32_t tmem_base = T->tmem_base;
     pdl_wait();
 
-    const int64_t groups = gridDim.x / 2, group = blockIdx.x / 2;
-    const int64_t tiles = (int64_t)P.tiles_m * P.tiles_n;
     constexpr int TILE_COLS = GLU ? 128 : GB_N;        // columns of the result a tile covers
+    // work units: whole tiles, then the halves of the tiles of a last, partly filled round
+    const int32_t groups = gridDim.x / 2, group = blockIdx.x / 2;
+    const int32_t units = P.full_tiles + 2 * (P.tiles_m * P.tiles_n - P.full_tiles);
+    struct Unit { int32_t tm, tn, kb0, kb1; bool half; };
+    auto unit = [&](int32_t u) {
+        Unit w;
+        w.half = !GLU && u >= P.full_tiles;
+        const int32_t v = u - P.full_tiles, tile = w.half ? P.full_tiles + (v >> 1) : u;
+        w.tm = tile / P.tiles_n; w.tn = tile - w.tm * P.tiles_n;
+        w.kb0 = w.half && (v & 1) ? P.half_kb : 0;
+        w.kb1 = w.half && !(v & 1) ? P.half_kb : P.num_kb;
+        return w;
+    };
 
     if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(GB_REGS_FEW));
@@ -207,12 +220,13 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
             asm volatile("prefetch.tensormap [%0];" ::"l"(mb) : "memory");
             uint32_t it = 0;
             bool ok = true;
-            for (int64_t u = group; u < tiles && ok; u += groups) {
-                const int32_t tn = (int32_t)(u % P.tiles_n), tm = (int32_t)(u / P.tiles_n);
+            for (int32_t u = group; u < units && ok; u += groups) {
+                const Unit w = unit(u);
+                const int32_t tn = w.tn, tm = w.tm;
                 const int32_t row_a = (tm * 2 + (int32_t)rank) * GB_M;
                 // b's rows so that the first 64 of both CTAs are one half of the tile's columns and the last 64 the other
                 const int32_t row_b = GLU ? tn * 128 : tn * GB_N + (int32_t)rank * 64;
-                for (int32_t kb = 0; kb < P.num_kb; ++kb, ++it) {
+                for (int32_t kb = w.kb0; kb < w.kb1; ++kb, ++it) {
                     const uint32_t s = it % GB_STAGES, ph = (it / GB_STAGES) & 1u;
                     if (!mbar_wait(&T->empty[s], ph ^ 1u, &T->abort_flag)) { gb_give_up(&T->abort_flag, P.status); ok = false; break; }
                     if (leader) mbar_expect_tx(&T->full[s], GB_STAGE_BYTES * 2);
@@ -249,8 +263,9 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
             bool ok = true;
             uint32_t s = 0, ph = 0, buf = 0, buf_ph = 1;
             const uint64_t desc0 = make_smem_desc(smem_u32(smem));
-            for (int64_t u = group; u < tiles && ok; u += groups) {
-                for (int32_t kb = 0; kb < P.num_kb; ++kb) {
+            for (int32_t u = group; u < units && ok; u += groups) {
+                const Unit w = unit(u);
+                for (int32_t kb = w.kb0; kb < w.kb1; ++kb) {
                     ok = mbar_wait(&T->full[s], ph, &T->abort_flag);
                     const uint64_t da = desc0 + (uint64_t)(s * (GB_STAGE_BYTES >> 4)), db = da + (uint64_t)((GB_M * GB_K) >> 4);
 #pragma unroll
@@ -294,10 +309,10 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
             const float4 f = scales4(row, chunk, P.num_kb, vec);
             dst[0] = f.x; dst[ld] = f.y; dst[2 * ld] = f.z; dst[3 * ld] = f.w;
         };
-        for (int64_t u = group; u < tiles && ok; u += groups) {
-            const int32_t tn = (int32_t)(u % P.tiles_n), tm = (int32_t)(u / P.tiles_n);
-            const int64_t row = ((int64_t)tm * 2 + rank) * GB_M + t, col = (int64_t)tn * TILE_COLS;
-            for (int32_t chunk = 0; 4 * chunk < P.num_kb; ++chunk) {
+        for (int32_t u = group; u < units && ok; u += groups) {
+            const Unit w = unit(u);
+            const int64_t row = ((int64_t)w.tm * 2 + rank) * GB_M + t, col = (int64_t)w.tn * TILE_COLS;
+            for (int32_t chunk = w.kb0 >> 2; 4 * chunk < w.kb1; ++chunk) {
                 if (!mbar_wait(&T->scale_empty[slot], ph ^ 1u, &T->abort_flag)) { gb_give_up(&T->abort_flag, P.status); ok = false; break; }
 #pragma unroll 1
                 for (int j = 0; j < 2; ++j) put(&T->row_scale[slot][0][t + 64 * j], GB_M, P.a, row + 64 * j, P.M, chunk, P.a_vec);
@@ -333,12 +348,12 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
         const uint32_t stage = smem_u32(out_stage + (warp - 4) * GB_OUT_BYTES);
         const uint32_t full0 = smem_u32(&T->tmem_full[half][0]);
         uint32_t buf = 0, buf_ph = 0, par = 0, slot = 0, slot_ph = 0;
-        for (int64_t u = group; u < tiles; u += groups) {
+        for (int32_t u = group; u < units; u += groups) {
             float2 sum[GB_COLS / 2];                       // two by two
 #pragma unroll
             for (int i = 0; i < GB_COLS / 2; ++i) sum[i] = make_float2(0.0f, 0.0f);
 #pragma unroll 1
-            for (int32_t left = P.num_kb; left > 0; left -= 4) {
+            for (int32_t left = unit(u).kb1 - unit(u).kb0; left > 0; left -= 4) {
                 wait_or_abort(smem_u32(&T->scale_full[0]) + 8 * slot, slot_ph, &T->abort_flag, P.status);
                 const float* rs = &T->row_scale[slot][0][trow];
                 const float* cs = T->col_scale[slot][0];
@@ -399,8 +414,9 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                 slot_ph ^= slot == 0u ? 1u : 0u;
             }
 
-            const int32_t tn = (int32_t)(u % P.tiles_n), tm = (int32_t)(u / P.tiles_n);
-            const int64_t row0 = ((int64_t)tm * 2 + rank) * GB_M, row = row0 + trow;
+            const Unit where = unit(u);
+            const int32_t tn = where.tn;
+            const int64_t row0 = ((int64_t)where.tm * 2 + rank) * GB_M, row = row0 + trow;
             const int64_t col0 = (int64_t)tn * TILE_COLS;
             float acc[GB_COLS];
 #pragma unroll
@@ -509,7 +525,8 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                         __syncwarp();
                         const int64_t c = c_first + (P.out_bf16 ? 32 : 16) * j;
                         if (lane == 0 && wrow < P.M && c < P.N) {
-                            if (P.accumulate) tma_reduce_add_2d(&map_out, stage, (int32_t)c, wrow);
+                            // two halves onto zeros: the same sum in either order
+                            if (P.accumulate || where.half) tma_reduce_add_2d(&map_out, stage, (int32_t)c, wrow);
                             else tma_store_2d(&map_out, stage, (int32_t)c, wrow);
                             bulk_commit();
                         }
@@ -940,12 +957,19 @@ static bool blocks_device(BlocksDevice** out) {
 //   CTA pairs    rounds x k-blocks x 55 + 400 (gated: + 250 per round for its longer epilogue)
 // 333 tokens, 2048 -> 2560: pairs 13.7 us on 20 of 74 pairs, tiles of 64 tokens 11.0; 1024 tokens, 512 outputs: 12.9 and 7.8;
 // 1024 tokens, 2048 -> 2560: 14.3 and 35; gated, 64 tokens, 2048 -> 5632: 16.3 and 13.3, 128 tokens: 16.8 and 20.6.
-struct Plan { bool pairs; int bn, parts; };
-static Plan plan_product(const BlocksDevice& d, int64_t M, int64_t N, int32_t num_kb, bool glu) {
-    Plan best = {true, 0, 0};
+// halve: the result may be added up from two parts (binary32, overwritten, stored in blocks): tiles of a last round that fills
+// at most half of the pairs are done in two halves of the contraction, at the cost of clearing their rows before.
+// 5632 x 2048 x 8192, 176 tiles on 74 pairs: two and a half rounds instead of three.
+struct Plan { bool pairs; int bn, parts; bool halves; };
+static Plan plan_product(const BlocksDevice& d, int64_t M, int64_t N, int32_t num_kb, bool glu, bool halve) {
+    Plan best = {true, 0, 0, false};
     const int64_t cols = glu ? 128 : GB_N, tiles = ((M + 2 * GB_M - 1) / (2 * GB_M)) * ((N + cols - 1) / cols);
     const int64_t per_round = (int64_t)num_kb * 55 + (glu ? 250 : 0);
     int64_t cost = d.pairs > 0 ? (tiles + d.pairs - 1) / d.pairs * per_round + 400 : INT64_MAX;
+    if (halve && d.pairs > 0 && num_kb >= 16 && tiles % d.pairs != 0 && 2 * (tiles % d.pairs) <= d.pairs) {
+        const int64_t c = tiles / d.pairs * per_round + per_round / 2 + 700;
+        if (c < cost) { cost = c; best.halves = true; }
+    }
     static const int kCost[2][4] = {{28, 38, 42, 62}, {45, 48, 67, 0}};
     for (int i = 0; i < (glu ? 3 : 4); ++i) {
         const int bn = 16 << i;
@@ -957,7 +981,7 @@ static Plan plan_product(const BlocksDevice& d, int64_t M, int64_t N, int32_t nu
             const int32_t per = (num_kb + s - 1) / s;
             if ((num_kb + per - 1) / per != s) continue;             // a part would be empty
             const int64_t c = (n + d.clusters[s] - 1) / d.clusters[s] * ((int64_t)per * kCost[glu][i] + 300 + (glu ? 50 : 20) * (s - 1) + (glu ? 4 * (M < bn ? M : bn) / s : 0));
-            if (c < cost) { cost = c; best = {false, bn, s}; }
+            if (c < cost) { cost = c; best = {false, bn, s, false}; }
         }
     }
     return best;
@@ -1014,7 +1038,14 @@ static srq_status_t run_small(const Plan& plan, GemmBlocksParams& P, bool glu, i
     return e == cudaSuccess ? SRQ_OK : SRQ_ERR_CUDA;
 }
 
-static srq_status_t run_pairs(const BlocksDevice& d, GemmBlocksParams& P, bool glu, int64_t Kc, cudaStream_t stream) {
+// The result leaves through block stores: 16-byte aligned rows that also end on a 16-byte boundary (a block store that reaches
+// over the map's edge may write the whole last 16-byte piece).
+static bool block_stores(const GemmBlocksParams& P) {
+    const int per16 = P.out_bf16 ? 8 : 4;
+    return P.out && (uintptr_t)P.out % 16 == 0 && P.ldo % per16 == 0 && P.N % per16 == 0;
+}
+
+static srq_status_t run_pairs(const BlocksDevice& d, const Plan& plan, GemmBlocksParams& P, bool glu, int64_t Kc, cudaStream_t stream) {
     if (d.pairs <= 0) return SRQ_ERR_UNSUPPORTED;
     P.tiles_m = (int32_t)((P.M + 2 * GB_M - 1) / (2 * GB_M));
     P.tiles_n = (int32_t)((P.N + (glu ? 128 : GB_N) - 1) / (glu ? 128 : GB_N));
@@ -1022,18 +1053,24 @@ static srq_status_t run_pairs(const BlocksDevice& d, GemmBlocksParams& P, bool g
     if (!encode_codes(&ma, P.a, P.M, Kc, GB_M) || !encode_codes(&mb, P.b, P.N, Kc, 64)) return SRQ_ERR_CUDA;
     mb2 = mb; mo = mb; mg = mb; mu = mb;
     if (glu && !encode_codes(&mb2, P.b2, P.N, Kc, 64)) return SRQ_ERR_CUDA;
-    const int per16 = P.out_bf16 ? 8 : 4;
-    const bool out16 = P.out && (uintptr_t)P.out % 16 == 0 && P.ldo % per16 == 0;
-    P.h_vec = out16;
-    // a row must also end on a 16-byte boundary: a block store that reaches over the map's edge may write the whole
-    // last 16-byte piece
-    if (!glu) P.tma_out = out16 && P.N % per16 == 0 && encode_result(&mo, P.out, P.out_bf16 ? 2 : 4, P.M, P.N, P.ldo);
+    P.h_vec = P.out && (uintptr_t)P.out % 16 == 0 && P.ldo % (P.out_bf16 ? 8 : 4) == 0;
+    if (!glu) P.tma_out = block_stores(P) && encode_result(&mo, P.out, P.out_bf16 ? 2 : 4, P.M, P.N, P.ldo);
     else
         P.tma_out = P.N % 16 == 0 && (!P.h.codes || encode_result(&mo, P.h.codes, 1, P.M, P.N, P.h.ld)) &&
                     (!P.gate.codes || encode_result(&mg, P.gate.codes, 1, P.M, P.N, P.gate.ld)) &&
                     (!P.up.codes || encode_result(&mu, P.up.codes, 1, P.M, P.N, P.up.ld));
     const int64_t tiles = (int64_t)P.tiles_m * P.tiles_n;
-    const unsigned pairs = (unsigned)(tiles < d.pairs ? tiles : d.pairs);
+    if (2 * tiles > INT32_MAX) return SRQ_ERR_UNSUPPORTED;
+    P.full_tiles = (int32_t)tiles;
+    if (plan.halves && P.tma_out) {
+        P.full_tiles = (int32_t)(tiles / d.pairs * d.pairs);
+        P.half_kb = (P.num_kb / 2 + 3) / 4 * 4;                  // step sizes come in chunks of four
+        const int64_t first = (int64_t)(P.full_tiles / P.tiles_n) * 2 * GB_M;      // whole tiles in these rows are overwritten
+        if (cudaMemset2DAsync((float*)P.out + first * P.ldo, (size_t)P.ldo * 4, 0, (size_t)P.N * 4, (size_t)(P.M - first), stream) != cudaSuccess)
+            return SRQ_ERR_CUDA;
+    }
+    const int64_t units = P.full_tiles + 2 * (tiles - P.full_tiles);
+    const unsigned pairs = (unsigned)(units < d.pairs ? units : d.pairs);
     const bool colv = P.b.tile_rows == 1;
     cudaError_t e;
     if (glu) e = colv ? launch_pair<true, true>(ma, mb, mb2, mo, mg, mu, P, pairs, stream) : launch_pair<true, false>(ma, mb, mb2, mo, mg, mu, P, pairs, stream);
@@ -1043,8 +1080,9 @@ static srq_status_t run_pairs(const BlocksDevice& d, GemmBlocksParams& P, bool g
 }
 
 static srq_status_t run_product(const BlocksDevice& d, GemmBlocksParams& P, bool glu, int64_t Kc, cudaStream_t stream) {
-    const Plan plan = plan_product(d, P.M, P.N, P.num_kb, glu);
-    return plan.pairs ? run_pairs(d, P, glu, Kc, stream) : run_small(plan, P, glu, Kc, stream);
+    const bool halve = !glu && !P.out_bf16 && !P.accumulate && block_stores(P);
+    const Plan plan = plan_product(d, P.M, P.N, P.num_kb, glu, halve);
+    return plan.pairs ? run_pairs(d, plan, P, glu, Kc, stream) : run_small(plan, P, glu, Kc, stream);
 }
 
 srq_status_t launch_gemm_blocks(const GemmBlocksArgs& g, uint32_t* status, cudaStream_t stream) {

@@ -256,6 +256,14 @@ def test_product_of_zero_blocks_and_of_an_empty_contraction():
     assert st == 0 and not out.any()
 
 
+@pytest.mark.parametrize("m,n,k", [(600, 1000, 2048), (1100, 4000, 2600), (5000, 1028, 2304), (300, 260, 20480)])
+def test_product_last_round_in_halves(m, n, k):
+    # tiles of a partly filled last round are added up from two halves of the contraction; pitches wider than the result
+    for tb in (1, 128):
+        check_product(m, n, k, 1, tb, "f32", seed=m, ldo_extra=4)
+        check_product(m, n, k, 1, tb, "f32", seed=m, accumulate=True)
+
+
 def test_product_long_contraction_and_many_tiles():
     check_product(300, 300, 20000, 1, 1, "f32")
     check_product(4, 256, 40000, 1, 128, "f32")
