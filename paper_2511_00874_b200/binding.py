@@ -182,9 +182,9 @@ def _ptr(t: Optional[torch.Tensor]):
 
 
 def _dtype_of(t: torch.Tensor) -> int:
-    if t.dtype == torch.float32:
+    if t.dtype is torch.float32:
         return F32
-    if t.dtype == torch.bfloat16:
+    if t.dtype is torch.bfloat16:
         return BF16
     raise TypeError(f"inputs must be float32 or bfloat16, got {t.dtype}")
 
@@ -569,14 +569,12 @@ class Blocks:
 
     def c(self) -> _Blocks:
         codes, scale, tile = self.codes, self.scale, self.tile_rows
-        rows, cols = codes.shape if codes.dim() == 2 else (-1, -1)
-        ld, unit = codes.stride() if rows >= 0 else (0, 0)
-        if unit != 1 and cols > 1 or rows < 0 or codes.element_size() != 1 or not codes.is_cuda:
+        ld, ld_scale = codes.stride(), scale.stride()
+        if len(ld) != 2 or ld[1] != 1 or codes.element_size() != 1 or not codes.is_cuda:
             raise ValueError("codes must be a 2-D CUDA tensor of bytes with unit inner stride")
-        nr, nb = scale.shape if scale.dim() == 2 else (-1, -1)
-        ld_scale, unit = scale.stride() if nr >= 0 else (0, 0)
-        if unit != 1 and nb > 1 or nr < 0 or scale.dtype != torch.float32 or not scale.is_cuda:
+        if len(ld_scale) != 2 or ld_scale[1] != 1 or scale.dtype is not torch.float32 or not scale.is_cuda:
             raise ValueError("step sizes must be a 2-D float32 CUDA tensor with unit inner stride")
+        (rows, cols), (nr, nb), ld, ld_scale = codes.shape, scale.shape, ld[0], ld_scale[0]
         if nr * tile < rows or nb * BLOCK < cols:
             raise ValueError(f"step sizes of shape {tuple(scale.shape)} do not cover a {rows} x {cols} matrix")
         # the pitch of a single row says nothing: torch is free to report any
@@ -617,12 +615,33 @@ def _status_word(device_status: Optional[torch.Tensor]):
     return device_status.data_ptr()
 
 
-def _pitch(t: Optional[torch.Tensor]) -> int:
+def _mat(t: Optional[torch.Tensor], name: str, shape=None, dtype=None):
+    """(pointer, pitch) of a 2-D CUDA tensor with unit inner stride; (None, 0) of None.  shape, dtype: what it has to be."""
     if t is None:
-        return 0
+        return None, 0
+    ld = t.stride()
+    if len(ld) != 2 or ld[1] != 1 or not t.is_cuda:
+        raise ValueError(f"{name} must be a 2-D CUDA tensor with unit inner stride")
+    if (shape is not None and t.shape != shape) or (dtype is not None and t.dtype is not dtype):
+        raise ValueError(f"{name} must be {tuple(shape or t.shape)} of {dtype or t.dtype}, got {tuple(t.shape)} of {t.dtype}")
+    ld = ld[0]
     rows, cols = t.shape
-    ld = t.stride(0)
-    return ld if rows > 1 or ld >= cols else cols
+    return t.data_ptr(), ld if rows > 1 or ld >= cols else cols
+
+
+def _vec(t: Optional[torch.Tensor], name: str, n: int) -> Optional[int]:
+    """Pointer of a contiguous float32 CUDA tensor of at least n values."""
+    if t is None:
+        return None
+    if t.dtype is not torch.float32 or t.numel() < n or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name} must hold {n} contiguous float32 values on the device")
+    return t.data_ptr()
+
+
+def _weight(w: torch.Tensor, cols: int):
+    if w.shape != (cols,) or not w.is_cuda or (cols > 1 and w.stride(0) != 1):
+        raise ValueError("w must be a contiguous CUDA tensor of cols values")
+    return w.data_ptr(), _dtype_of(w)
 
 
 def srq_quantize_blocks(x, q: QSpec, rm: Optional[Blocks] = None, tr: Optional[Blocks] = None,
@@ -635,9 +654,8 @@ def srq_quantize_blocks(x, q: QSpec, rm: Optional[Blocks] = None, tr: Optional[B
         st = lib().srq_requantize_blocks(x.c(), rows, cols, q.c(), r, t, _status_word(device_status), _stream())
         _check(st, "srq_requantize_blocks")
         return
-    _dev2d(x, "x")
-    st = lib().srq_quantize_blocks(x.data_ptr(), _dtype_of(x), rows, cols, _pitch(x), q.c(), r, t,
-                                   _status_word(device_status), _stream())
+    px, ldx = _mat(x, "x")
+    st = lib().srq_quantize_blocks(px, _dtype_of(x), rows, cols, ldx, q.c(), r, t, _status_word(device_status), _stream())
     _check(st, "srq_quantize_blocks")
 
 
@@ -645,11 +663,10 @@ def srq_gemm_blocks(a: Blocks, b: Blocks, out: torch.Tensor, accumulate: bool = 
                     device_status: Optional[torch.Tensor] = None) -> None:
     """out[M, N] (+)= a[M, Kc] b[N, Kc]^T over block codes; out is float32 or bfloat16."""
     (M, Kc), (N, Kb) = a.shape, b.shape
-    _dev2d(out, "out")
-    if Kc != Kb or tuple(out.shape) != (M, N):
+    if Kc != Kb:
         raise ValueError("srq_gemm_blocks: shapes must be a[M,Kc], b[N,Kc], out[M,N]")
-    st = lib().srq_gemm_blocks(a.c(), b.c(), M, N, Kc, out.data_ptr(), _dtype_of(out), _pitch(out),
-                               int(accumulate), _status_word(device_status), _stream())
+    po, ldo = _mat(out, "out", (M, N))
+    st = lib().srq_gemm_blocks(a.c(), b.c(), M, N, Kc, po, _dtype_of(out), ldo, int(accumulate), _status_word(device_status), _stream())
     _check(st, "srq_gemm_blocks")
 
 
@@ -657,21 +674,15 @@ def srq_rmsnorm_fwd(x: torch.Tensor, residual: Optional[torch.Tensor], w: torch.
                     r_out: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None, y_out: Optional[torch.Tensor] = None,
                     q: QSpec = BLOCK_RNE, device_status: Optional[torch.Tensor] = None) -> None:
     """r = x + residual, y = r / rms(r) * w: y as block codes and / or in ``y_out``, r in ``r_out``, 1 / rms in ``rstd``."""
-    _dev2d(x, "x")
-    rows, cols = x.shape
-    dt = _dtype_of(x)
-    for t, name in ((residual, "residual"), (r_out, "r_out"), (y_out, "y_out")):
-        if t is not None:
-            _dev2d(t, name)
-            if t.dtype != x.dtype or t.shape != x.shape:
-                raise ValueError(f"{name} must have the shape and type of x")
-    if not w.is_cuda or w.shape != (cols,) or (cols > 1 and w.stride(0) != 1):
-        raise ValueError("w must be a CUDA tensor of cols values")
-    if rstd is not None and (rstd.dtype != torch.float32 or rstd.numel() < rows or not rstd.is_contiguous()):
-        raise ValueError("rstd must hold rows float32 values")
-    st = lib().srq_rmsnorm_fwd(x.data_ptr(), _pitch(x), _ptr(residual), _pitch(residual), dt, w.data_ptr(), _dtype_of(w), rows, cols,
-                               eps, q.c(), _bref(y, (rows, cols), "y"), _ptr(y_out), _pitch(y_out), _ptr(r_out), _pitch(r_out),
-                               _ptr(rstd), _status_word(device_status), _stream())
+    shape, dtype = x.shape, x.dtype
+    px, ldx = _mat(x, "x")
+    rows, cols = shape
+    pres, ldres = _mat(residual, "residual", shape, dtype)
+    pr, ldr = _mat(r_out, "r_out", shape, dtype)
+    py, ldy = _mat(y_out, "y_out", shape, dtype)
+    pw, wdt = _weight(w, cols)
+    st = lib().srq_rmsnorm_fwd(px, ldx, pres, ldres, _dtype_of(x), pw, wdt, rows, cols, eps, q.c(), _bref(y, shape, "y"), py, ldy,
+                               pr, ldr, _vec(rstd, "rstd", rows), _status_word(device_status), _stream())
     _check(st, "srq_rmsnorm_fwd")
 
 
@@ -682,23 +693,17 @@ def srq_rmsnorm_workspace_bytes(rows: int, cols: int) -> int:
 def srq_rmsnorm_bwd(dy: torch.Tensor, r: torch.Tensor, w: torch.Tensor, rstd: torch.Tensor, d_residual: Optional[torch.Tensor] = None,
                     dx: Optional[torch.Tensor] = None, dw: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None) -> None:
     """dx = rstd (w dy - n mean(w dy n)) + d_residual and dw = sum over rows of dy n, with n = r rstd."""
-    _dev2d(dy, "dy")
-    rows, cols = dy.shape
-    for t, name in ((r, "r"), (d_residual, "d_residual"), (dx, "dx")):
-        if t is not None:
-            _dev2d(t, name)
-            if t.dtype != dy.dtype or t.shape != dy.shape:
-                raise ValueError(f"{name} must have the shape and type of dy")
-    if not w.is_cuda or w.shape != (cols,) or (cols > 1 and w.stride(0) != 1):
-        raise ValueError("w must be a CUDA tensor of cols values")
-    for t, n, name in ((rstd, rows, "rstd"), (dw, cols, "dw")):
-        if t is not None and (t.dtype != torch.float32 or t.numel() < n or not t.is_contiguous() or not t.is_cuda):
-            raise ValueError(f"{name} must hold {n} float32 values")
+    shape, dtype = dy.shape, dy.dtype
+    pdy, lddy = _mat(dy, "dy")
+    rows, cols = shape
+    pr, ldr = _mat(r, "r", shape, dtype)
+    pres, ldres = _mat(d_residual, "d_residual", shape, dtype)
+    pdx, lddx = _mat(dx, "dx", shape, dtype)
+    pw, wdt = _weight(w, cols)
     if ws is None and dw is not None:
         ws = new_workspace(srq_rmsnorm_workspace_bytes(rows, cols), dy.device)
-    st = lib().srq_rmsnorm_bwd(dy.data_ptr(), _pitch(dy), r.data_ptr(), _pitch(r), _ptr(d_residual), _pitch(d_residual), _dtype_of(dy),
-                               w.data_ptr(), _dtype_of(w), rstd.data_ptr(), rows, cols, _ptr(dx), _pitch(dx), _ptr(dw),
-                               _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size(), _stream())
+    st = lib().srq_rmsnorm_bwd(pdy, lddy, pr, ldr, pres, ldres, _dtype_of(dy), pw, wdt, _vec(rstd, "rstd", rows), rows, cols, pdx, lddx,
+                               _vec(dw, "dw", cols), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size(), _stream())
     _check(st, "srq_rmsnorm_bwd")
 
 
@@ -709,12 +714,8 @@ def srq_glu_fwd(x: Blocks, wg: Blocks, wu: Blocks, act: int, h: Optional[Blocks]
     (T, K), (F, Kg) = x.shape, wg.shape
     if Kg != K or tuple(wu.shape) != (F, K):
         raise ValueError("srq_glu_fwd: shapes must be x[T,K], wg[F,K], wu[F,K]")
-    if h_out is not None:
-        _dev2d(h_out, "h_out")
-        if tuple(h_out.shape) != (T, F):
-            raise ValueError("h_out must be [T, F]")
-    st = lib().srq_glu_fwd(x.c(), wg.c(), wu.c(), T, F, K, act, _bref(h, (T, F), "h"),
-                           _ptr(h_out), F32 if h_out is None else _dtype_of(h_out), _pitch(h_out),
+    ph, ldh = _mat(h_out, "h_out", (T, F))
+    st = lib().srq_glu_fwd(x.c(), wg.c(), wu.c(), T, F, K, act, _bref(h, (T, F), "h"), ph, F32 if h_out is None else _dtype_of(h_out), ldh,
                            _bref(gate, (T, F), "gate"), _bref(up, (T, F), "up"), _status_word(device_status), _stream())
     _check(st, "srq_glu_fwd")
 
@@ -724,9 +725,9 @@ def srq_glu_bwd(dh: torch.Tensor, gate: Blocks, up: Blocks, act: int, q: QSpec, 
                 device_status: Optional[torch.Tensor] = None) -> None:
     """Gradients of both projections from the 8-bit checkpoints, as block codes along the features (dg, du)
     and along the tokens (dg_t, du_t), and h itself along the tokens (h_t)."""
-    _dev2d(dh, "dh")
+    pdh, lddh = _mat(dh, "dh")
     T, F = dh.shape
-    st = lib().srq_glu_bwd(dh.data_ptr(), _dtype_of(dh), _pitch(dh), _bref(gate, (T, F), "gate"), _bref(up, (T, F), "up"), T, F, act,
+    st = lib().srq_glu_bwd(pdh, _dtype_of(dh), lddh, _bref(gate, (T, F), "gate"), _bref(up, (T, F), "up"), T, F, act,
                            q.c(), _bref(dg, (T, F), "dg"), _bref(du, (T, F), "du"), _bref(dg_t, (F, T), "dg_t"),
                            _bref(du_t, (F, T), "du_t"), _bref(h_t, (F, T), "h_t"), _status_word(device_status), _stream())
     _check(st, "srq_glu_bwd")
