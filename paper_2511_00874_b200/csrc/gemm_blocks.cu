@@ -456,13 +456,13 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                 T->amax[par][0][cg][trow] = abs_word(mh);
                 if (ckpt) { T->amax[par][1][cg][trow] = abs_word(mg); T->amax[par][2][cg][trow] = abs_word(mu); }
                 asm volatile("bar.sync 3, %0;" ::"n"(32 * GB_ADD_WARPS) : "memory");
-                float m_mine = 0.0f, inv_mine;
+                float m_mine = 0.0f;
                 if (cg < (ckpt ? 3 : 1)) {
                     uint32_t m = 0u;
 #pragma unroll
                     for (int i = 0; i < GB_CGROUPS; ++i) m = max(m, T->amax[par][cg][i][trow]);
                     m_mine = __uint_as_float(m);
-                    T->inv[par][cg][trow] = inv_mine = block_inv(m);
+                    T->inv[par][cg][trow] = block_inv(m);
                 }
                 asm volatile("bar.sync 3, %0;" ::"n"(32 * GB_ADD_WARPS) : "memory");
                 const int32_t wrow = (int32_t)(row0 + quarter * 32);
@@ -489,10 +489,7 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                 if (ckpt) {
                     emit(P.gate, &map_gate, 1, stage, acc);
                     emit(P.up, &map_up, 2, stage + 1024, acc + GH);
-                    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");      // the gate's
-                    __syncwarp();
                 }
-                emit(P.h, &map_out, 0, stage, h);
                 if (cg < (ckpt ? 3 : 1) && live) {
                     const Blocks& o = cg == 0 ? P.h : cg == 1 ? P.gate : P.up;
                     if (o.codes) {
@@ -500,6 +497,11 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                         o.scale[row * o.ld_scale + tn] = block_size(__float_as_uint(m_mine));
                     }
                 }
+                if (ckpt) {
+                    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");      // the gate's codes have left
+                    __syncwarp();
+                }
+                emit(P.h, &map_out, 0, stage, h);
                 par ^= 1;            // these words are written again two tiles on, a barrier after everyone has read them
             } else {
                 const int32_t wrow = (int32_t)(row0 + quarter * 32);
