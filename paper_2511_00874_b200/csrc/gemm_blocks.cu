@@ -106,6 +106,12 @@ __device__ __forceinline__ void wait_or_abort(uint32_t bar, uint32_t parity, vol
     }
 }
 
+// Bounded wait of a whole warp, with one vote: the usual case is that the phase has completed.
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, uint64_t* b, volatile uint32_t* abort_flag) {
+    if (__all_sync(0xFFFFFFFFu, try_wait_addr(bar, parity))) return true;
+    return __all_sync(0xFFFFFFFFu, mbar_wait(b, parity, abort_flag));
+}
+
 // 32 lanes x 16 columns of TMEM (in registers after tmem_ld_wait).
 __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&v)[16]) {
     asm volatile(
@@ -192,7 +198,9 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     tc_fence_before();
     cluster_sync();
     tc_fence_after();
-    const uint32_t tmem_base = T->tmem_base;
+    // All 512 columns are this CTA's, so they start at 0: as a constant the address needs no move into a uniform register
+    // before every MMA (40 cycles each).
+    constexpr uint32_t tmem_base = 0;
     pdl_wait();
 
     constexpr int TILE_COLS = GLU ? 128 : GB_N;        // columns of the result a tile covers
@@ -266,12 +274,11 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
             for (int32_t u = group; u < units && ok; u += groups) {
                 const Unit w = unit(u);
                 for (int32_t kb = w.kb0; kb < w.kb1; ++kb) {
-                    ok = mbar_wait(&T->full[s], ph, &T->abort_flag);
+                    ok = warp_wait(smem_u32(&T->full[0]) + 8 * s, ph, &T->full[s], &T->abort_flag);
                     const uint64_t da = desc0 + (uint64_t)(s * (GB_STAGE_BYTES >> 4)), db = da + (uint64_t)((GB_M * GB_K) >> 4);
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        ok = ok && mbar_wait(&T->tmem_empty[h][buf], buf_ph, &T->abort_flag);
-                        ok = !__any_sync(0xFFFFFFFFu, !ok);
+                        ok = ok && warp_wait(smem_u32(&T->tmem_empty[h][0]) + 8 * buf, buf_ph, &T->tmem_empty[h][buf], &T->abort_flag);
                         if (!ok) break;
                         tc_fence_after();
                         if (elected) {
