@@ -227,7 +227,7 @@ inline Blocks to_blocks(const srq_blocks_t* b) {
     return r;
 }
 
-// What is being quantized to blocks: a matrix, or the three gradients of a gated block.
+// What is being quantized to blocks: a matrix of values, or one that is block-coded already.
 struct BlockSource {
     const void* x = nullptr; int32_t dt = 0; int64_t ld = 0;   // SRQ_F32 / SRQ_BF16 matrix
     Blocks coded;                                              // or a block-coded one

@@ -5,23 +5,29 @@
 //
 // The step sizes change every 128 values of the contraction, so the tensor core cannot add up the whole sum:
 // each P_k is left in TMEM for itself (kind::f8f6f4, binary32), read back and added into binary32 registers
-// with its factor.  That takes one tcgen05.ld and one multiply-add per element and k-block, next to the 512
-// cycles the MMAs of a 128 x 256 x 128 piece take: the two run side by side, k-block by k-block, through
-// two TMEM buffers.
+// with its factor.  That takes one tcgen05.ld and one multiply-add per element and k-block (two where every row and
+// every column has a step size of its own), next to the 512 cycles the MMAs of a 128 x 256 x 128 piece take: the two run
+// side by side, k-block by k-block, through two TMEM buffers.
 //
-// gemm_blocks_kernel: 256 x 256 tiles on CTA pairs (tcgen05.mma.cta_group::2, M256 N256 K32), persistent.
+// gemm_blocks_kernel: 256 x 256 tiles on CTA pairs (tcgen05.mma.cta_group::2), persistent.
 //   warp 0      TMA producer (128-byte swizzled tiles, ring of 5 stages of 32 KB)
-//   warp 1      TMEM and MMA issue (leader CTA): one k-block into one TMEM buffer at a time, in turn
+//   warp 1      TMEM and MMA issue (leader CTA): a k-block goes into one TMEM buffer as two M256 N128 halves with barriers
+//               of their own, so that the first half's sums are added up while the second is multiplied
 //   warps 2-3   step sizes: four k-blocks at a time from global memory into a shared ring, so that the warps that
 //               add up hold no addresses and no prefetched values in their registers
-//   warps 4-11  two groups of four; a thread owns one row of the CTA's 128 and 128 of the 256 columns: group
-//               g columns 128 g .. in a plain product; in the gated block, whose 256 columns are 128 of the
-//               gate and 128 of the up projection (one CTA of the pair stages Wg, the other Wu), columns
-//               64 g .. 64 g + 63 of both, so that g and u of an element meet in one thread
+//   warps 4-19  four groups of four; a thread owns one row of the CTA's 128 and 64 of the 256 columns: group g columns
+//               64 g .. in a plain product; in the gated block, whose 256 columns are 128 of the gate and 128 of the up
+//               projection (one CTA of the pair stages Wg, the other Wu), columns 32 g .. 32 g + 31 of both, so that
+//               g and u of an element meet in one thread
+// Measured: 16384 x 4096 x 4096, 128 x 128 tiles on b, 257 to 282 us (2.1 PFLOP/s); 5632 x 2048 x 8192, 1 x 128 on both, 150 to
+// 165 us, 117 with tiles on b; gated 16384 x 2048 x 5632 with checkpoints 480 to 510 us.  Eight adding warps with 128
+// sums each: 322 us for the first; a second issuing warp, and 16 columns read while 16 are added: no difference.
+//
 // gemm_blocks_small_kernel: few tokens.  The roles turn around: 128 rows of the weights are the M of the MMA and
 // 16 to 128 tokens its N, the contraction is cut over a cluster of CTAs (as many as fill the machine), and the
 // parts are added through distributed shared memory in a fixed order.  Reading the weights once is all there
-// is to do, and every SM reads its share with up to 200 KB in flight.
+// is to do, and every SM reads its share with up to 200 KB in flight.  Warp 0 loads, warp 1 issues, four or eight warps
+// scale and add up.  1 x 4096 x 4096: 6.8 us, of which 2.6 are the weights at the copy rate.
 //
 // Every wait is bounded (2 s); on expiry SRQ_ERR_TIMEOUT is recorded, all roles run to their end without
 // waiting any more, and TMEM is freed.
@@ -168,8 +174,8 @@ __device__ __forceinline__ void stage_rows64(uint32_t stage, int lane, const uin
                      "r"(w[4 * q]), "r"(w[4 * q + 1]), "r"(w[4 * q + 2]), "r"(w[4 * q + 3]) : "memory");
 }
 
-// map_out: of out, or of h's codes.  GLU: the gated block's epilogue instead of the plain one.  COLV: b has a step size per row (per column of
-// out), not per 128 of them.
+// map_out: of out, or of h's codes.  GLU: the gated block's epilogue instead of the plain one.  COLV: b has a step size per
+// row (per column of out), not per 128 of them.
 template <bool GLU, bool COLV>
 __global__ void __launch_bounds__(GB_THREADS, 1)
 gemm_blocks_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
@@ -264,7 +270,8 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
         // ------------------------------------------------------------------ MMA issuer (leader CTA only)
         // The whole warp walks the loop and one elected lane issues: what the instructions take (descriptors, barrier
         // addresses) is then uniform to the compiler and stays in uniform registers.  With a single thread in the loop
-        // every MMA cost some 95 cycles and every commit 61 to issue, more than the MMAs themselves take.
+        // every MMA cost some 95 cycles and every commit 61 to issue, more than the MMAs themselves take; now the eight MMAs
+        // and three commits of a k-block take some 420 together.
         if (leader) {
             constexpr uint32_t idesc = make_idesc(1, GB_M * 2, GB_N / 2);
             const uint32_t elected = elect_one();
@@ -337,7 +344,7 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
         }
     }
     } else {
-        // ------------------------------------------------------------------ scaling and epilogue (warps 4..11)
+        // ------------------------------------------------------------------ scaling and epilogue (warps 4..19)
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(GB_REGS_MANY));
         const int quarter = warp & 3, cg = (warp - 4) >> 2;
         const int trow = quarter * 32 + lane;            // row within this CTA's 128
@@ -376,7 +383,7 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                     wait_or_abort(full0 + 8 * buf, buf_ph, &T->abort_flag, P.status);
                     tc_fence_after();
                     const uint32_t tb = taddr + buf * GB_N;
-// the buffer is handed back as soon as its last piece is in registers
+                    // the buffer is handed back as soon as its last piece is in registers
                     auto release = [&]() {
                         tc_fence_before();
                         __syncwarp();
@@ -582,7 +589,7 @@ struct SmallCfg {
     static constexpr int TMEM = BUFS * COLS < 32 ? 32 : BUFS * COLS;
     static_assert((size_t)STAGES * STAGE_BYTES >= (size_t)COLS * 128 * 4, "the ring holds the partial sums afterwards");
     // Warps that add up: four, or eight that share the columns (the gated block: one half the gate, the other the up
-    // projection).  With four a k-block of 128 tokens took 0.83 us, with eight 0.5.
+    // projection).  With four a k-block of 128 tokens took 0.83 us, with eight 0.62.
     static constexpr int GROUPS = COLS >= 64 ? 2 : 1;
     static constexpr int EW = 4 * GROUPS, THREADS = 64 + 32 * EW;
     static constexpr int MY_COLS = COLS / GROUPS;                           // sums per thread
