@@ -520,44 +520,56 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
             } else {
                 const int32_t wrow = (int32_t)(row0 + quarter * 32);
                 const int64_t c_first = col0 + GB_COLS * cg;
-                if (P.tma_out) {
-                    // 64 bytes of every row at a time through the warp's staging block
-                    constexpr int F32_BLOCKS = GB_COLS / 16;
+                // 64 bytes of every row at a time through the warp's staging block, and from there by a block store or, where rows
+                // are not aligned for one, row by row with neighbouring lanes on neighbouring columns.  (Straight from the
+                // registers every store touched 32 rows: 8191 x 2047 x 300 in bfloat16 169 us, now 25, in binary32 139 and 37.)
+                constexpr int F32_BLOCKS = GB_COLS / 16;
+                const uint8_t* staged = out_stage + (warp - 4) * GB_OUT_BYTES;
 #pragma unroll
-                    for (int j = 0; j < F32_BLOCKS; ++j) {
-                        uint32_t w[16];
-                        if (P.out_bf16) {
-                            if (j >= F32_BLOCKS / 2) break;
+                for (int j = 0; j < F32_BLOCKS; ++j) {
+                    uint32_t w[16];
+                    if (P.out_bf16) {
+                        if (j >= F32_BLOCKS / 2) break;
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) w[i] = j < F32_BLOCKS / 2 ? pack_bf16(acc[(32 * j + 2 * i) % GB_COLS], acc[(32 * j + 2 * i + 1) % GB_COLS]) : 0u;
-                        } else {
+                        for (int i = 0; i < 16; ++i) w[i] = j < F32_BLOCKS / 2 ? pack_bf16(acc[(32 * j + 2 * i) % GB_COLS], acc[(32 * j + 2 * i + 1) % GB_COLS]) : 0u;
+                    } else {
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(acc[16 * j + i]);
-                        }
-                        if (lane == 0) bulk_wait_read();
-                        __syncwarp();
-                        stage_rows64(stage, lane, w);
+                        for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(acc[16 * j + i]);
+                    }
+                    if (P.tma_out && lane == 0) bulk_wait_read();
+                    __syncwarp();
+                    stage_rows64(stage, lane, w);
+                    const int64_t c = c_first + (P.out_bf16 ? 32 : 16) * j;
+                    if (P.tma_out) {
                         fence_async_smem();
                         __syncwarp();
-                        const int64_t c = c_first + (P.out_bf16 ? 32 : 16) * j;
                         if (lane == 0 && wrow < P.M && c < P.N) {
                             // two halves onto zeros: the same sum in either order
                             if (P.accumulate || where.half) tma_reduce_add_2d(&map_out, stage, (int32_t)c, wrow);
                             else tma_store_2d(&map_out, stage, (int32_t)c, wrow);
                             bulk_commit();
                         }
-                    }
-                } else if (row < P.M) {
-                    if (P.out_bf16) {
-                        __nv_bfloat16* dst = (__nv_bfloat16*)P.out + row * P.ldo;
-#pragma unroll
-                        for (int i = 0; i < GB_COLS; ++i)
-                            if (c_first + i < P.N) dst[c_first + i] = __float2bfloat16_rn(acc[i]);
                     } else {
-                        float* dst = (float*)P.out + row * P.ldo;
-#pragma unroll
-                        for (int i = 0; i < GB_COLS; ++i)
-                            if (c_first + i < P.N) dst[c_first + i] = P.accumulate ? __fadd_rn(dst[c_first + i], acc[i]) : acc[i];
+                        __syncwarp();
+                        const int32_t rows = (int32_t)min((int64_t)32, P.M - wrow);
+                        if (P.out_bf16) {
+                            __nv_bfloat16* dst = (__nv_bfloat16*)P.out + (int64_t)wrow * P.ldo + c + lane;
+                            if (c + lane < P.N) {
+#pragma unroll 4
+                                for (int32_t r = 0; r < rows; ++r, dst += P.ldo)
+                                    *dst = *reinterpret_cast<const __nv_bfloat16*>(staged + r * 64 + (((lane >> 3) ^ ((r >> 1) & 3)) << 4) + 2 * (lane & 7));
+                            }
+                        } else {
+                            const int col = lane & 15;
+                            float* dst = (float*)P.out + (int64_t)(wrow + (lane >> 4)) * P.ldo + c + col;
+                            if (c + col < P.N) {
+#pragma unroll 4
+                                for (int32_t r = lane >> 4; r < rows; r += 2, dst += 2 * P.ldo) {
+                                    const float f = *reinterpret_cast<const float*>(staged + r * 64 + (((col >> 2) ^ ((r >> 1) & 3)) << 4) + 4 * (col & 3));
+                                    *dst = P.accumulate ? __fadd_rn(*dst, f) : f;
+                                }
+                            }
+                        }
                     }
                 }
             }

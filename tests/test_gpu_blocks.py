@@ -264,6 +264,15 @@ def test_product_last_round_in_halves(m, n, k):
         check_product(m, n, k, 1, tb, "f32", seed=m, accumulate=True)
 
 
+@pytest.mark.parametrize("n", [1027, 1100])
+def test_product_of_many_rows_without_aligned_rows(n):
+    # too many tiles for the few-token kernel; rows that no block store can take
+    for tb in (1, 128):
+        check_product(4099, n, 700, 1, tb, "bf16", ldo_extra=3)
+        check_product(4099, n, 700, 1, tb, "f32", ldo_extra=1)
+        check_product(4099, n, 700, 1, tb, "f32", accumulate=True, ldo_extra=1)
+
+
 def test_product_long_contraction_and_many_tiles():
     check_product(300, 300, 20000, 1, 1, "f32")
     check_product(4, 256, 40000, 1, 128, "f32")
