@@ -511,8 +511,13 @@ gemm_blocks_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                         o.scale[row * o.ld_scale + tn] = block_size(__float_as_uint(m_mine));
                     }
                 }
-                if (ckpt) {
-                    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");      // the gate's codes have left
+                if (P.gate.codes) {
+                    // the gate's codes have left the buffer h's take now: all but the newest group, which are the up projection's
+                    // where those are wanted, else every group
+                    if (lane == 0) {
+                        if (P.up.codes) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+                        else bulk_wait_read();
+                    }
                     __syncwarp();
                 }
                 emit(P.h, &map_out, 0, stage, h);

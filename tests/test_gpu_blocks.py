@@ -452,6 +452,26 @@ def test_glu_many_tiles():
     check_glu(2100, 2600, 256, "silu", tile_w=1)
 
 
+@pytest.mark.parametrize("t,f,k", [(5, 384, 512), (60, 400, 256), (400, 400, 256), (2100, 2608, 256), (2100, 2601, 256)])
+@pytest.mark.parametrize("kind", ["silu", "gelu"])
+def test_glu_each_checkpoint_on_its_own(t, f, k, kind):
+    # either checkpoint may be left out, and what is written does not depend on the other (few tokens and CTA pairs; codes
+    # through block stores and, where f is no multiple of 16, straight from registers)
+    x = coded(synth.normal((t, k), 1.0, 1, torch.float32, "cuda"))
+    wg, wu = (coded(synth.normal((f, k), 2.0 * k ** -0.5, i, torch.float32, "cuda"), 128) for i in (2, 3))
+
+    def run(names):
+        out = {n: blocks(t, f) for n in names}
+        srq.srq_glu_fwd(x, wg, wu, KINDS[kind], out.get("h"), out.get("gate"), out.get("up"), None if "h" in out else torch.empty((t, f), device="cuda"))
+        for b in out.values():
+            padding_is_untouched(b)
+        return out
+    both = run(("h", "gate", "up"))
+    for names in (("h", "gate"), ("h", "up"), ("gate",), ("up",), ("gate", "up"), ("h",)):
+        for n, b in run(names).items():
+            assert torch.equal(b.codes, both[n].codes) and torch.equal(b.scale, both[n].scale), (names, n)
+
+
 def test_glu_saturated_gates():
     # gates far out on both sides: the logistic function reaches 0 and 1
     t, f, k = 150, 256, 128
