@@ -94,6 +94,7 @@ __device__ __forceinline__ uint32_t elect_one() {
 // Bounded wait of the warps that add up, on a barrier's shared address.  The usual case is one try; when the limit has
 // passed or another role has given up it returns all the same, so that the caller needs no second path: its
 // results are then garbage, the status says so, and every wait after it returns as soon.
+// The lanes may leave the loop at different times; they meet before they return, because a tcgen05.ld.sync.aligned follows.
 __device__ __forceinline__ bool try_wait_addr(uint32_t bar, uint32_t parity) {
     uint32_t ok;
     asm volatile(
@@ -104,12 +105,14 @@ __device__ __forceinline__ bool try_wait_addr(uint32_t bar, uint32_t parity) {
     return ok != 0;
 }
 __device__ __forceinline__ void wait_or_abort(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag, uint32_t* status) {
-    if (try_wait_addr(bar, parity)) return;
-    const uint64_t t0 = global_ns();
-    while (!try_wait_addr(bar, parity)) {
-        if (*abort_flag) break;
-        if (global_ns() - t0 > WAIT_LIMIT_NS) { gb_give_up(abort_flag, status); break; }
+    if (!try_wait_addr(bar, parity)) {
+        const uint64_t t0 = global_ns();
+        while (!try_wait_addr(bar, parity)) {
+            if (*abort_flag) break;
+            if (global_ns() - t0 > WAIT_LIMIT_NS) { gb_give_up(abort_flag, status); break; }
+        }
     }
+    __syncwarp();
 }
 
 // Bounded wait of a whole warp, with one vote: the usual case is that the phase has completed.

@@ -2,6 +2,8 @@
 differences, the quantizer against the other quantizers' oracle), and the host-side refusals of the
 block-scaled entry points."""
 import ctypes
+import os
+import re
 
 import numpy as np
 import pytest
@@ -190,3 +192,18 @@ def test_binding_checks_shapes_before_the_call():
         binding.Blocks(cpu, torch.zeros((4, 1))).c()
     with pytest.raises(ValueError):
         binding.srq_gemm_blocks(binding.Blocks(cpu, torch.zeros((4, 1))), binding.Blocks(cpu, torch.zeros((4, 1))), torch.zeros((4, 5)))
+
+
+def test_the_adding_warps_meet_after_a_wait():
+    """Their waits are loops that a lane leaves by itself, and what follows is tcgen05.ld.sync.aligned, which takes a
+    converged warp.  The wait must therefore end by bringing the lanes together, on every path through it."""
+    text = open(os.path.join(os.path.dirname(binding.__file__), "csrc", "gemm_blocks.cu")).read()
+    start = text.index("void wait_or_abort(")
+    body = text[text.index("{", start) + 1:text.index("\n}\n", start)]
+    assert "return" not in body and body.rstrip().endswith("__syncwarp();")
+    # and they have no other way to wait: what lies between a wait and the loads after it
+    calls = [m.start() for m in re.finditer(r"wait_or_abort\((?!uint32_t)", text)]
+    assert len(calls) == 3                       # step sizes and sums (CTA pairs), sums (few tokens)
+    for load in re.finditer(r"tmem_ld(?:16|32)\((?:tb|taddr)", text):
+        before = text[max(c for c in calls if c < load.start()):load.start()]
+        assert "mbar_wait(" not in before and "try_wait" not in before
