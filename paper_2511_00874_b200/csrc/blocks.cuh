@@ -103,7 +103,10 @@ __device__ __forceinline__ float2 logistic2(float2 g, float2* dz) {
         const float c = 1.5957691216057308f, k = 0.044715f;      // 2 sqrt(2 / pi)
         const float2 c2 = make_float2(c, c), gg = __fmul2_rn(g, g);
         z = __fmul2_rn(__fmul2_rn(c2, g), __ffma2_rn(make_float2(k, k), gg, one));
-        *dz = __fmul2_rn(c2, __ffma2_rn(make_float2(3.0f * k, 3.0f * k), gg, one));
+        // where g^2 is out of range g p (1 - p) is exactly 0: a finite slope keeps 0 times infinity out of the gradient.
+        // (z' passes 1e30 from |g| = 2e15 on, and p is exactly 0 or 1 from |g| = 12 on.)
+        const float2 d = __fmul2_rn(c2, __ffma2_rn(make_float2(3.0f * k, 3.0f * k), gg, one));
+        *dz = make_float2(fminf(d.x, 1e30f), fminf(d.y, 1e30f));
     }
     const float2 e = __fmul2_rn(z, minus_log2e);
     const float2 d = __fadd2_rn(make_float2(exp2_fast(e.x), exp2_fast(e.y)), one);

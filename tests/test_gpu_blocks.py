@@ -523,6 +523,28 @@ def test_glu_backward_strided_gradient(pad):
         check_glu_bwd(150, 256, dtype, "gelu", pad=pad)
 
 
+@pytest.mark.parametrize("kind", ["silu", "gelu"])
+def test_glu_backward_saturated_gates(kind):
+    # gates far out on both sides, up to where their squares leave binary32: the slope is 0 or 1 there, not infinity times 0
+    t, f = 140, 260
+    mag = torch.tensor([3.0, 50.0, 1e4, 1e12, 1.5e19, 2e19, 3e38], device="cuda")
+    sign = torch.where(synth.normal((t, f), 1.0, 1, torch.float32, "cuda") > 0, 1.0, -1.0)
+    gate = coded(sign * mag[torch.arange(t, device="cuda") % 7][:, None])
+    up = coded(synth.normal((t, f), 1.0, 2, torch.float32, "cuda").clamp(-0.9, 0.9))
+    dh = synth.normal((t, f), 1.0, 3, torch.float32, "cuda").clamp(-0.9, 0.9)
+    out = {n: (blocks(f, t) if n.endswith("_t") else blocks(t, f)) for n in ("dg", "du", "dg_t", "du_t", "h_t")}
+    s = status()
+    srq.srq_glu_bwd(dh, gate, up, KINDS[kind], srq.BLOCK_RNE, **out, device_status=s)
+    assert s.item() == 0
+    (dg, edg), (du, edu), (h, eh) = ref.glu_bwd(dh.double(), numbers(gate), numbers(up), kind)
+    for n, b in out.items():
+        v, e = {"dg": (dg, edg), "du": (du, edu), "h_": (h, eh)}[n[:2]]
+        e = e + 8 * ref.ULP * v.abs()
+        if n.endswith("_t"):
+            v, e = v.t().contiguous(), e.t().contiguous()
+        ref.check_coded(b.codes, b.scale, v, e, n)
+
+
 def test_glu_backward_stochastic_rounding_streams():
     t, f = 140, 264
     gate, up = coded(skewed(t, f, 1)), coded(skewed(t, f, 2))
