@@ -373,6 +373,9 @@ srq_status_t srq_dequant_i32(const int32_t *acc, int64_t ld_acc, int64_t M, int6
  *     thresholds of the flat index in the matrix that is being quantized, the source's own for both
  *     layouts).  q->bits must be 8, q->format SRQ_GRID_E4M3, q->scale SRQ_PER_BLOCK; q->absmax is ignored.
  *   - The last block of a row may be shorter than 128.
+ *   - Extents may be 0.  An operand without elements may have null pointers, and a call whose result has none does
+ *     nothing; sums over nothing (Kc = 0, a weight's gradient over no rows) are written as zero.  srq_glu_fwd wants
+ *     K >= 1.
  */
 
 /* A matrix of E4M3 codes [rows, cols] with its step sizes, on the device: element (r, c) stands for

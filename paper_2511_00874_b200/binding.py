@@ -577,8 +577,8 @@ class Blocks:
         (rows, cols), (nr, nb), ld, ld_scale = codes.shape, scale.shape, ld[0], ld_scale[0]
         if nr * tile < rows or nb * BLOCK < cols:
             raise ValueError(f"step sizes of shape {tuple(scale.shape)} do not cover a {rows} x {cols} matrix")
-        # the pitch of a single row says nothing: torch is free to report any
-        if rows <= 1:
+        # the pitch of a single row, or of a matrix without elements, says nothing: torch is free to report any
+        if rows <= 1 or cols == 0:
             ld = -(-max(ld, cols) // 16) * 16
         if nr <= 1 and ld_scale < nb:
             ld_scale = nb

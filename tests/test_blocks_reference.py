@@ -181,6 +181,26 @@ def test_glu_refusals(L):
     assert b(t=0) == OK and b(n=0) == OK
 
 
+def test_null_pointers_are_for_operands_without_elements(L):
+    none = lambda tile=1: ctypes.byref(binding._Blocks(None, 208, None, 2, tile))  # noqa: E731
+    for r, c in ((0, 200), (8, 0), (0, 0)):
+        assert int(L.srq_quantize_blocks(None, 0, r, c, 200, RNE, none(), none(128), None, None)) == OK
+        assert int(L.srq_requantize_blocks(none(), r, c, RNE, none(), none(), None, None)) == OK
+        assert int(L.srq_gemm_blocks(none(), none(), r, c, 0, None, 0, 200, 0, None, None)) == OK
+        assert int(L.srq_rmsnorm_fwd(None, 200, None, 200, 1, None, 1, r, c, 1e-5, RNE, none(), None, 200, None, 200, None, None, None)) == OK
+        assert int(L.srq_rmsnorm_bwd(None, 200, None, 200, None, 200, 0, None, 0, None, r, c, None, 200, None, None, 0, None)) == OK
+        assert int(L.srq_glu_fwd(none() if r == 0 else blk(), none() if c == 0 else blk(), none() if c == 0 else blk(), r, c, 200, 0, none(), None, 0, 200, none(), none(), None, None)) == OK
+        assert int(L.srq_glu_bwd(None, 0, 200, none(), none(), r, c, 0, RNE, none(), none(), none(), none(), none(), None, None)) == OK
+        # the rest of the arguments is checked as ever
+        assert int(L.srq_quantize_blocks(None, 7, r, c, 200, RNE, none(), None, None, None)) == INVALID
+        assert int(L.srq_quantize_blocks(None, 0, r, c, 200, RNE, None, None, None, None)) == INVALID
+        assert int(L.srq_gemm_blocks(none(), none(64), r, c, 0, None, 0, 200, 0, None, None)) == INVALID
+        assert int(L.srq_glu_bwd(None, 0, 200, none(), none(128), r, c, 0, RNE, none(), None, None, None, None, None, None)) == UNSUPPORTED
+    # an operand that has elements needs its pointers even where the result has none, or where the contraction is empty
+    assert int(L.srq_gemm_blocks(none(), none(), 0, 8, 200, None, 0, 200, 0, None, None)) == INVALID
+    assert int(L.srq_gemm_blocks(none(), none(), 8, 8, 0, None, 0, 200, 0, None, None)) == INVALID
+
+
 def test_block_modes_stay_out_of_the_other_entry_points(L):
     for q in (binding.QSpec(scale=binding.PER_BLOCK), binding.QSpec(round=binding.RNE)):
         assert int(L.sr_quantize(P, 0, 8, 8, 8, ctypes.byref(q.c()), P, 8, P, None, 0, None, P, 1 << 20, None)) == INVALID

@@ -630,3 +630,65 @@ def test_operators_run_on_the_current_stream_and_in_a_graph():
     step()
     torch.cuda.synchronize()
     assert torch.equal(out, replayed)
+
+
+# --------------------------------------------------------------------------------------------
+# nothing to do: torch gives a null pointer for a tensor without elements
+# --------------------------------------------------------------------------------------------
+NONE = [(0, 200), (5, 0), (0, 0)]
+
+
+@pytest.mark.parametrize("r,c", NONE)
+def test_quantizer_without_elements(r, c):
+    for x in (torch.empty((r, c), device="cuda"), torch.empty((r, c), dtype=torch.bfloat16, device="cuda"), srq.new_blocks(r, c), srq.new_blocks(r, c, 128)):
+        for q in (srq.BLOCK_RNE, srq.block_sr(1, 2)):
+            for tile in (1, 128):
+                rm, tr = srq.new_blocks(r, c, tile), srq.new_blocks(c, r, tile)
+                srq.srq_quantize_blocks(x, q, rm, tr, device_status=status())
+                srq.srq_quantize_blocks(x, q, rm)
+                srq.srq_quantize_blocks(x, q, None, tr)
+    with pytest.raises(binding.SrqError):                            # a call that asks for nothing stays an error
+        srq.srq_quantize_blocks(torch.empty((r, c), device="cuda"), srq.BLOCK_RNE)
+
+
+@pytest.mark.parametrize("m,n,k", [(0, 200, 256), (200, 0, 256), (0, 0, 0), (0, 10, 0), (3, 200, 0), (300, 40, 0), (1, 1, 0)])
+def test_product_without_elements(m, n, k):
+    for tile in (1, 128):
+        for dtype in (torch.float32, torch.bfloat16):
+            whole = torch.full((m, n + 3), 5.0, dtype=dtype, device="cuda")
+            out = whole[:, :n]
+            srq.srq_gemm_blocks(srq.new_blocks(m, k), srq.new_blocks(n, k, tile), out, device_status=status())
+            assert not out.any() and bool((whole[:, n:] == 5.0).all())               # an empty contraction is zero
+    out = torch.full((m, n), 5.0, device="cuda")
+    srq.srq_gemm_blocks(srq.new_blocks(m, k), srq.new_blocks(n, k), out, accumulate=True)
+    assert bool((out == 5.0).all())
+
+
+@pytest.mark.parametrize("r,c", NONE)
+def test_norm_without_elements(r, c):
+    for dtype in (torch.float32, torch.bfloat16):
+        e = lambda: torch.empty((r, c), dtype=dtype, device="cuda")  # noqa: E731
+        w, rstd = torch.ones(c, dtype=dtype, device="cuda"), torch.empty(r, device="cuda")
+        srq.srq_rmsnorm_fwd(e(), e(), w, EPS, srq.new_blocks(r, c), e(), rstd, e(), device_status=status())
+        srq.srq_rmsnorm_fwd(e(), None, w, EPS, None, y_out=e())
+        dw = torch.full((c,), 5.0, device="cuda")
+        srq.srq_rmsnorm_bwd(e(), e(), w, rstd, e(), e(), dw)
+        assert not dw.any()                                           # a sum over no rows
+        srq.srq_rmsnorm_bwd(e(), e(), w, rstd, None, e())
+        dw.fill_(5.0)
+        srq.srq_rmsnorm_bwd(e(), e(), w, rstd, None, None, dw)
+        assert not dw.any()
+
+
+@pytest.mark.parametrize("t,f", NONE)
+@pytest.mark.parametrize("act", [srq.SILU, srq.GELU])
+def test_glu_without_elements(t, f, act):
+    k = 256
+    nb = srq.new_blocks
+    h_out = torch.empty((t, f), device="cuda")
+    for tile in (1, 128):
+        srq.srq_glu_fwd(nb(t, k), nb(f, k, tile), nb(f, k, tile), act, nb(t, f), nb(t, f), nb(t, f), h_out, device_status=status())
+        srq.srq_glu_fwd(nb(t, k), nb(f, k, tile), nb(f, k, tile), act, None, h_out=h_out)
+    for dtype in (torch.float32, torch.bfloat16):
+        dh = torch.empty((t, f), dtype=dtype, device="cuda")
+        srq.srq_glu_bwd(dh, nb(t, f), nb(t, f), act, srq.BLOCK_RNE, nb(t, f), nb(t, f), nb(f, t), nb(f, t), nb(f, t), device_status=status())

@@ -60,3 +60,16 @@ def test_mlp_forward_and_backward_against_autograd(T, K, F, act, dtype, sr):
 def test_mlp_refuses_hidden_sizes_that_do_not_fill_blocks():
     with pytest.raises(ValueError, match="multiple of 128"):
         mlp.GatedMLP(4, 128, 200)
+
+
+def test_mlp_of_no_tokens_has_zero_gradients():
+    K, F = 256, 384
+    m = mlp.GatedMLP(0, K, F)
+    w = torch.ones(K, dtype=torch.bfloat16, device="cuda")
+    wg, wu, wd = (synth.normal(s, 0.05, i, torch.bfloat16, "cuda") for i, s in enumerate([(F, K), (F, K), (K, F)]))
+    m.load(w, wg, wu, wd)
+    e = torch.empty((0, K), dtype=torch.bfloat16, device="cuda")
+    assert m.forward(e, e).shape == (0, K) and m.backward(e, e).shape == (0, K)
+    assert m.status.item() == 0
+    for g in (m.dw, m.dwg, m.dwu, m.dwd):
+        assert not g.any()
