@@ -365,7 +365,10 @@ srq_status_t srq_dequant_i32(const int32_t *acc, int64_t ld_acc, int64_t M, int6
  * Conventions, where they differ from the calls above
  *   - No workspace and no header: `device_status` is an optional caller-owned device word (4-byte aligned).
  *     A call does not clear it; it receives SRQ_ERR_NONFINITE or SRQ_ERR_TIMEOUT if the device meets such a
- *     condition and it holds zero.  Zero it once, read it after as many calls as you like.
+ *     condition and it holds zero.  Zero it once, read it after as many calls as you like.  Values that are not
+ *     finite are looked for where step sizes are formed (every block that is coded) and in the norm's forward pass,
+ *     which also reports rows of finite values whose mean square is not finite in binary32 (or zero with eps = 0);
+ *     what leaves in 16 or 32 bits only is not searched.
  *   - Step size of a block: D = absmax / 448, the quotient is x * inv with inv = 448 / absmax rounded toward
  *     zero; a block whose absmax is 0 or at most 7 * 2^-122 (the reciprocal would overflow) has D = 0 and
  *     codes 0.

@@ -49,6 +49,13 @@ __device__ __forceinline__ float rstd_of(float sum, float inv_cols, float eps) {
     return fmaf(x * 0.5f, fmaf(-m * x, x, 1.0f), x);
 }
 
+// One thread per row: stores 1 / rms and reports a row for which it is no positive finite number (the mean square is NaN or
+// overflows binary32, or is 0 where eps is), since a row of finite values would leave as zeros without a trace.
+__device__ __forceinline__ void finish_rstd(const NormFwdArgs& a, int64_t row, float rstd) {
+    if (a.rstd) a.rstd[row] = rstd;
+    if (!(rstd > 0.0f && rstd < __int_as_float(0x7F800000))) note(a.status, SRQ_ERR_NONFINITE);
+}
+
 // Eight values of a row as they lie in memory.
 template <typename T> struct Raw8;
 template <> struct Raw8<float> { uint4 a, b; };
@@ -133,7 +140,7 @@ __global__ void __launch_bounds__(V == 1 ? 1024 : 512) rmsnorm_fwd_stream_kernel
         }
         if (it + 1 < rounds) fetch(row + step);
         const float rstd = rstd_of(row_sum(s2.x + s2.y, tpr, red[it & 1]), P.inv_cols, a.eps);
-        if (live && t == 0 && a.rstd) a.rstd[row] = rstd;
+        if (live && t == 0) finish_rstd(a, row, rstd);
         const float2 rs2 = make_float2(rstd, rstd);
         uint32_t m[V];
 #pragma unroll
@@ -224,7 +231,7 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) rmsnorm_fwd_any_kernel(
         if (it + 1 < rounds) fetch(row + step);
         const float rstd = rstd_of(row_sum(s, TPR, red[it & 1]), P.inv_cols, a.eps);
         if (!live) continue;                               // whole warps; the next barrier is the next row's
-        if (t == 0 && a.rstd) a.rstd[row] = rstd;
+        if (t == 0) finish_rstd(a, row, rstd);
         if (a.r_out) {
             T* o = (T*)a.r_out + row * a.ld_r + first;
 #pragma unroll
@@ -329,7 +336,7 @@ __global__ void __launch_bounds__(1024) rmsnorm_fwd_kernel(const __grid_constant
     }
     s = row_sum(s, tpr, S.red);
     const float rstd = rstd_of(s, P.inv_cols, a.eps);
-    if (live && t == 0 && a.rstd) a.rstd[row] = rstd;
+    if (live && t == 0) finish_rstd(a, row, rstd);
     auto finish = [&](int64_t c, const float r[8]) {
         if (live && a.r_out) store8((T*)a.r_out + row * a.ld_r, c, a.cols, P.vec & 8, r);
         float w[8], y[8];

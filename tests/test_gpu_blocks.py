@@ -354,6 +354,23 @@ def test_norm_of_zero_rows_and_of_rows_that_are_not_finite():
     assert s.item() == binding.ERR_NONFINITE
 
 
+@pytest.mark.parametrize("cols,sr", [(512, False), (4096, False), (131, False), (40001, False), (640, True)])
+def test_norm_reports_rows_whose_mean_square_leaves_binary32(cols, sr):
+    # every value is finite, their squares are not: 1 / rms is 0 then, and so are the row's codes, which must not pass unnoticed
+    q, w = srq.block_sr(1, 2) if sr else srq.BLOCK_RNE, torch.ones(cols, device="cuda")
+    for rows in (3, 400):
+        for big, want in ((1e15, 0), (3e19, binding.ERR_NONFINITE)):
+            x = skewed(rows, cols, 1)
+            x[rows - 1] = big
+            s = status()
+            srq.srq_rmsnorm_fwd(x, None, w, EPS, blocks(rows, cols), device_status=s, q=q)
+            assert s.item() == want
+            s = status()
+            srq.srq_rmsnorm_fwd(x, None, w, EPS, None, y_out=torch.empty_like(x), device_status=s)
+            assert s.item() == want
+            srq.srq_rmsnorm_fwd(x, None, w, EPS, blocks(rows, cols), q=q)                  # no word: no report
+
+
 def check_norm_bwd(rows, cols, dtype, wdtype="f32", residual=True, seed=0, pad=0):
     r, dres, w = norm_inputs(rows, cols, dtype, wdtype, residual, seed, pad)
     dy = skewed(rows, cols + pad, seed + 5, DTYPES[dtype])[:, :cols]
