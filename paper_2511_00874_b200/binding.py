@@ -702,6 +702,8 @@ def srq_rmsnorm_bwd(dy: torch.Tensor, r: torch.Tensor, w: torch.Tensor, rstd: to
     pw, wdt = _weight(w, cols)
     if ws is None and dw is not None:
         ws = new_workspace(srq_rmsnorm_workspace_bytes(rows, cols), dy.device)
+    if ws is not None and (not ws.is_cuda or not ws.is_contiguous()):
+        raise ValueError("ws must be contiguous memory on the device")
     st = lib().srq_rmsnorm_bwd(pdy, lddy, pr, ldr, pres, ldres, _dtype_of(dy), pw, wdt, _vec(rstd, "rstd", rows), rows, cols, pdx, lddx,
                                _vec(dw, "dw", cols), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size(), _stream())
     _check(st, "srq_rmsnorm_bwd")

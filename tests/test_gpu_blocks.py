@@ -414,6 +414,18 @@ def test_norm_backward_strides(pad):
         check_norm_bwd(40, 520, dtype, "bf16", pad=pad)
 
 
+def test_norm_backward_refuses_workspaces_that_are_not_device_memory():
+    x, w, rstd, dw = skewed(600, 256, 1), torch.ones(256, device="cuda"), torch.ones(600, device="cuda"), torch.empty(256, device="cuda")
+    n = srq.srq_rmsnorm_workspace_bytes(600, 256)
+    for ws in (torch.empty(n, dtype=torch.uint8), torch.empty(n, dtype=torch.uint8).pin_memory(),
+               torch.empty((1, 256), dtype=torch.uint8, device="cuda").expand(n // 256, 256)):
+        with pytest.raises(ValueError, match="ws"):
+            srq.srq_rmsnorm_bwd(x, x, w, rstd, None, None, dw, ws)
+    with pytest.raises(binding.SrqError, match="workspace"):
+        srq.srq_rmsnorm_bwd(x, x, w, rstd, None, None, dw, srq.new_workspace(n - 4))
+    srq.srq_rmsnorm_bwd(x, x, w, rstd, None, None, dw, srq.new_workspace(n))
+
+
 # --------------------------------------------------------------------------------------------
 # gated block
 # --------------------------------------------------------------------------------------------
