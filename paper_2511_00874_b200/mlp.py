@@ -47,13 +47,19 @@ class GatedMLP:
     def _columns(b: B.Blocks, first: int, n: int) -> B.Blocks:
         return B.Blocks(b.codes[:, first:first + n], b.scale[:, first // B.BLOCK:(first + n + B.BLOCK - 1) // B.BLOCK], b.tile_rows)
 
+    @staticmethod
+    def _stream(q: B.QSpec, i: int) -> B.QSpec:
+        """q with the thresholds of the i-th stream after its own."""
+        return B.QSpec(q.bits, q.scale, q.round, q.seed, q.tensor_id + i, q.index_offset, q.format)
+
     def load(self, w: torch.Tensor, wg: torch.Tensor, wu: torch.Tensor, wd: torch.Tensor, q: B.QSpec = B.BLOCK_RNE) -> None:
-        """Codes the weights once per step: wg, wu [hidden, features], wd [features, hidden]; w is the norm's."""
+        """Codes the weights once per step: wg, wu [hidden, features], wd [features, hidden]; w is the norm's.  Under
+        stochastic rounding each weight has a threshold stream of its own: q.tensor_id, + 1 and + 2."""
         _, K, F = self.shape
         self.w = w
         B.srq_quantize_blocks(wg, q, self.wg, self._columns(self.wgu_t, 0, F), self.status)
-        B.srq_quantize_blocks(wu, q, self.wu, self._columns(self.wgu_t, F, F), self.status)
-        B.srq_quantize_blocks(wd, q, self.wd, self.wd_t, self.status)
+        B.srq_quantize_blocks(wu, self._stream(q, 1), self.wu, self._columns(self.wgu_t, F, F), self.status)
+        B.srq_quantize_blocks(wd, self._stream(q, 2), self.wd, self.wd_t, self.status)
 
     def forward(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None) -> torch.Tensor:
         """out = MLP(norm(x + residual)); ``self.r`` holds x + residual."""
@@ -70,8 +76,7 @@ class GatedMLP:
         s = self.status
         B.srq_quantize_blocks(dout, q, self.dout, self.dout_t, s)
         B.srq_gemm_blocks(self.dout, self.wd_t, self.dh, device_status=s)
-        qg = B.QSpec(q.bits, q.scale, q.round, q.seed, q.tensor_id + 1, q.index_offset, q.format)
-        B.srq_glu_bwd(self.dh, self.gate, self.up, self.act, qg, self._columns(self.dgu, 0, F), self._columns(self.dgu, F, F),
+        B.srq_glu_bwd(self.dh, self.gate, self.up, self.act, self._stream(q, 1), self._columns(self.dgu, 0, F), self._columns(self.dgu, F, F),
                       self.dg_t, self.du_t, self.h_t, s)
         B.srq_gemm_blocks(self.dout_t, self.h_t, self.dwd, device_status=s)
         B.srq_quantize_blocks(self.y, B.BLOCK_RNE, None, self.y_t, s)              # the norm's codes, turned over

@@ -73,3 +73,20 @@ def test_mlp_of_no_tokens_has_zero_gradients():
     assert m.status.item() == 0
     for g in (m.dw, m.dwg, m.dwu, m.dwd):
         assert not g.any()
+
+
+def test_mlp_rounds_each_weight_with_thresholds_of_its_own():
+    K, F = 256, 256
+    m = mlp.GatedMLP(4, K, F)
+    one = synth.normal((F, K), 0.05, 1, torch.float32, "cuda")
+    w = torch.ones(K, dtype=torch.bfloat16, device="cuda")
+    m.load(w, one, one, one, srq.block_sr(3, 50))
+    codes = [b.codes for b in (m.wg, m.wu, m.wd)]
+    for i in range(3):
+        want = srq.new_blocks(F, K, 128)
+        srq.srq_quantize_blocks(one, srq.block_sr(3, 50 + i), want)
+        assert torch.equal(codes[i], want.codes)
+    for a, b in ((0, 1), (0, 2), (1, 2)):
+        assert (codes[a] != codes[b]).double().mean() > 0.1           # the same numbers, rounded independently
+    m.load(w, one, one, one)                                          # to nearest there is nothing to choose
+    assert torch.equal(m.wg.codes, m.wu.codes) and torch.equal(m.wg.codes, m.wd.codes)
