@@ -325,6 +325,14 @@ def test_norm_long_rows(cols):
     check_norm(2, cols, "bf16", "f32", residual=False)
 
 
+@pytest.mark.parametrize("cols", [8193, 8200, 12288, 12290, 16384])
+def test_norm_many_long_rows(cols):
+    # more rows than SMs, whole groups of eight columns and others
+    check_norm(300, cols, "f32")
+    check_norm(300, cols, "f32", residual=False)
+    check_norm(300, cols, "bf16", "f32", residual=False)
+
+
 @pytest.mark.parametrize("pad", [1, 8])
 @pytest.mark.parametrize("wdtype", ["f32", "bf16"])
 def test_norm_strides_and_types(pad, wdtype):
