@@ -524,6 +524,23 @@ def test_glu_saturated_gates():
             assert not ((h_out.double() - hh).abs() > eh + 1e-30).any()
 
 
+@pytest.mark.parametrize("t", [20, 300])
+def test_glu_reports_values_that_are_not_finite(t):
+    f, k = 300, 256
+    x = coded(synth.normal((t, k), 1.0, 1, torch.float32, "cuda"))
+    wg, wu = (coded(synth.normal((f, k), 1.0, i, torch.float32, "cuda"), 128) for i in (2, 3))
+    bad_row = srq.Blocks(x.codes, x.scale.clone(), 1)
+    bad_row.scale[t - 1, 1] = float("inf")
+    bad_code = srq.Blocks(x.codes.clone(), x.scale, 1)
+    bad_code.codes[3, 7] = 0x7F
+    for src, want in ((x, 0), (bad_row, binding.ERR_NONFINITE), (bad_code, binding.ERR_NONFINITE)):
+        for names in (("h",), ("gate",), ("up",), ("h", "gate", "up")):
+            s = status()
+            srq.srq_glu_fwd(src, wg, wu, srq.SILU, **{"h": None, **{n: blocks(t, f) for n in names}}, h_out=torch.empty((t, f), device="cuda"), device_status=s)
+            assert s.item() == want, names
+            srq.srq_glu_fwd(src, wg, wu, srq.GELU, **{"h": None, **{n: blocks(t, f) for n in names}}, h_out=torch.empty((t, f), device="cuda"))
+
+
 def check_glu_bwd(t, f, dtype, kind, which=("dg", "du", "dg_t", "du_t", "h_t"), pad=0, seed=0):
     gate, up = coded(synth.normal((t, f), 1.5, seed, torch.float32, "cuda")), coded(skewed(t, f, seed + 1))
     dh = (1e-3 * skewed(t, f + pad, seed + 2)).to(DTYPES[dtype])[:, :f]
