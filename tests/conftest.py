@@ -1,3 +1,4 @@
+import gc
 import os
 import sys
 
@@ -25,3 +26,10 @@ def pytest_collection_modifyitems(config, items):
     for item in items:
         if "gpu" in item.keywords:
             item.add_marker(skip)
+
+
+def pytest_runtest_setup(item):
+    # Caught exceptions keep their frames, and the frames their tensors, in cycles until Python's collector comes by.  The tests
+    # that compare the device memory held before and after a call must not have it come by in between.
+    if item.path.name == "test_zz_no_alloc.py":
+        gc.collect()
