@@ -406,7 +406,8 @@ srq_status_t srq_requantize_blocks(const srq_blocks_t *x, int64_t rows, int64_t 
 
 /* out[M, N] (+)= A B^T, A[M, Kc] and B[N, Kc] block-coded with the contracted axis contiguous:
  *   out[i, j] = sum over blocks k of  sA[i, k] * sB[j, k] * sum_{c in block k} a[i, c] * b[j, c]
- * in binary32, the inner sums on the tensor cores.  out is binary32 or bfloat16 (out_dt, rounded once, to
+ * in binary32, the inner sums on the tensor cores; sA * sB is formed first, so that it has to stay within binary32's
+ * normal range for a result of full precision.  out is binary32 or bfloat16 (out_dt, rounded once, to
  * nearest even), pitch ldo elements.  accumulate = 1 adds to a binary32 out instead of overwriting it.  Any M
  * from one token up; the sum's order depends on sizes, types, alignment and the device alone, so that the same
  * call repeats bit for bit (with accumulate = 1 too: one addition per element). */

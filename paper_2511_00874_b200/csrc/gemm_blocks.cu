@@ -19,9 +19,11 @@
 //               64 g .. in a plain product; in the gated block, whose 256 columns are 128 of the gate and 128 of the up
 //               projection (one CTA of the pair stages Wg, the other Wu), columns 32 g .. 32 g + 31 of both, so that
 //               g and u of an element meet in one thread
-// Measured: 16384 x 4096 x 4096, 128 x 128 tiles on b, 257 to 282 us (2.1 PFLOP/s); 5632 x 2048 x 8192, 1 x 128 on both, 150 to
-// 165 us, 117 with tiles on b; gated 16384 x 2048 x 5632 with checkpoints 480 to 510 us.  Eight adding warps with 128
-// sums each: 322 us for the first; a second issuing warp, and 16 columns read while 16 are added: no difference.
+// Measured, by machine and clock: 16384 x 4096 x 4096, 128 x 128 tiles on b, 257 to 300 us (2.1 to 1.8 PFLOP/s); 5632 x 2048 x
+// 8192, 1 x 128 on both, 150 to 169 us, 95 to 117 with tiles on b, 178 accumulating; gated 16384 x 2048 x 5632 with checkpoints
+// 453 to 515 us.  No pipe is at its limit (tensor 56 % of the cycles, issue 58 %): the MMAs, the reads of their sums and the
+// additions wait for one another.  Eight adding warps with 128 sums each: 322 us for the first; a second issuing warp, and
+// 16 columns read while 16 are added: no difference.
 //
 // gemm_blocks_small_kernel: few tokens.  The roles turn around: 128 rows of the weights are the M of the MMA and
 // 16 to 128 tokens its N, the contraction is cut over a cluster of CTAs (as many as fill the machine), and the

@@ -8,6 +8,11 @@
 Every product reads 8-bit codes and every tensor kept for the backward pass but r is 8 bits wide.  The class holds
 what a training program holds between steps: the coded weights (row-major for the forward pass, transposed for the
 input gradients) and the activations' and gradients' buffers.  The calls only enqueue work on the current stream.
+
+An object is one block of one training step: it takes one number of tokens, allocates every buffer of both passes when it is
+built, and each ``forward`` writes the results and checkpoints of the one before it over, so that ``backward`` belongs to the
+latest ``forward`` (copy what has to outlive the next call; one object per micro-batch in flight).  ``forward`` always
+writes the checkpoints; a program that only generates calls the operators itself and leaves them out of srq_glu_fwd.
 """
 from __future__ import annotations
 
