@@ -131,15 +131,16 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&v)[16]) {
           "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
         : "r"(taddr) : "memory");
 }
-// Step sizes of k-blocks 4 c .. 4 c + 3 of one scale row (zeros past num_kb).
+// Step sizes of k-blocks 4 c .. 4 c + 3 of one scale row (zeros past num_kb).  Ordinary loads: the kernel may have been launched
+// while its predecessor was still writing them, and the read-only path is for data that nobody writes while a kernel runs.
 __device__ __forceinline__ float4 scales4(const float* row, int32_t c, int32_t num_kb, bool vec) {
     const int32_t k = 4 * c;
     if (row == nullptr || k >= num_kb) return make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    if (vec && k + 4 <= num_kb) return __ldg(reinterpret_cast<const float4*>(row + k));
-    float4 f = make_float4(__ldg(row + k), 0.0f, 0.0f, 0.0f);
-    if (k + 1 < num_kb) f.y = __ldg(row + k + 1);
-    if (k + 2 < num_kb) f.z = __ldg(row + k + 2);
-    if (k + 3 < num_kb) f.w = __ldg(row + k + 3);
+    if (vec && k + 4 <= num_kb) return *reinterpret_cast<const float4*>(row + k);
+    float4 f = make_float4(row[k], 0.0f, 0.0f, 0.0f);
+    if (k + 1 < num_kb) f.y = row[k + 1];
+    if (k + 2 < num_kb) f.z = row[k + 2];
+    if (k + 3 < num_kb) f.w = row[k + 3];
     return f;
 }
 __device__ __forceinline__ float pick4(const float4& f, int32_t i) { return i == 0 ? f.x : i == 1 ? f.y : i == 2 ? f.z : f.w; }

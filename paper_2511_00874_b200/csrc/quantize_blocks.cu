@@ -115,7 +115,7 @@ __device__ __forceinline__ void fetch_coded(uint8_t* slot, const Blocks& b, cons
 }
 // The step size of row `row` of a tile, on its way to coded_scales() of its buffer.
 __device__ __forceinline__ float fetch_scale(const Blocks& b, const TilePos& p, int row) {
-    return __ldg(b.scale + (b.tile_rows > 1 ? p.r0 / QBLK : p.r0 + row) * b.ld_scale + p.c0 / QBLK);
+    return b.scale[(b.tile_rows > 1 ? p.r0 / QBLK : p.r0 + row) * b.ld_scale + p.c0 / QBLK];
 }
 __device__ __forceinline__ uint8_t* coded_codes(uint8_t* slot, int par) { return slot + par * CODED_TILE; }
 __device__ __forceinline__ float* coded_scales(uint8_t* slot, int par) { return reinterpret_cast<float*>(slot + 2 * CODED_TILE) + par * QBLK; }

@@ -390,7 +390,7 @@ __global__ void __launch_bounds__(512) rmsnorm_bwd_stream_kernel(const __grid_co
     auto fetch = [&](int64_t row) {
         const T* y = (const T*)a.dy + row * a.ld_dy + c0;
         const T* r = (const T*)a.r + row * a.ld_r + c0;
-        next_rstd = row < a.rows ? __ldg(a.rstd + row) : 0.0f;
+        next_rstd = row < a.rows ? a.rstd[row] : 0.0f;
 #pragma unroll
         for (int k = 0; k < V; ++k) {
             zero_raw(ny[k]); zero_raw(nr[k]);
@@ -496,7 +496,7 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) rmsnorm_bwd_any_kernel(
     auto fetch = [&](int64_t row) {
         const T* y = (const T*)a.dy + row * a.ld_dy + first;
         const T* r = (const T*)a.r + row * a.ld_r + first;
-        next_rstd = row < a.rows ? __ldg(a.rstd + row) : 0.0f;
+        next_rstd = row < a.rows ? a.rstd[row] : 0.0f;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             const bool in = row < a.rows && column_offset<TPR>(e) < left;

@@ -227,3 +227,12 @@ def test_the_adding_warps_meet_after_a_wait():
     for load in re.finditer(r"tmem_ld(?:16|32)\((?:tb|taddr)", text):
         before = text[max(c for c in calls if c < load.start()):load.start()]
         assert "mbar_wait(" not in before and "try_wait" not in before
+
+
+def test_kernels_launched_early_do_not_read_through_the_read_only_path():
+    """A programmatic dependent is running while its predecessor writes what it will read after its wait, so those reads
+    must be ordinary ones: ld.global.nc (__ldg) takes data that nobody writes for as long as the kernel runs."""
+    src = os.path.join(os.path.dirname(binding.__file__), "csrc")
+    for name in ("blocks.cuh", "gemm_blocks.cu", "quantize_blocks.cu", "rmsnorm.cu"):
+        text = re.sub(r"//[^\n]*", "", open(os.path.join(src, name)).read())
+        assert not re.search(r"__ldg\s*\(|ld\.global\.nc", text), name
