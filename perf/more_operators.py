@@ -292,10 +292,10 @@ def _moments(s):
 
 
 # ----------------------------------------------------------------- in plain torch operations
-def _words(n, first, seed, tensor_id, device):
+def _words(n, seed, tensor_id, device):
     """Philox4x32-10 words of the flat indices 0 .. n - 1 of a tensor."""
     low = 0xFFFFFFFF
-    j = torch.arange(first, first + (n + 3) // 4, dtype=torch.int64, device=device)
+    j = torch.arange((n + 3) // 4, dtype=torch.int64, device=device)
     c0, c1, c2, c3 = j & low, j >> 32, torch.full_like(j, tensor_id & low), torch.full_like(j, tensor_id >> 32)
     k0, k1 = seed & low, seed >> 32
     for _ in range(10):
@@ -337,7 +337,7 @@ def _plain_adamw(s):
     if case["bits"] == 8 or case["dtype"] == "bf16":
         word = torch.zeros(starts[-1], dtype=torch.int64, device=s["p"].device)
         for i, (n, a) in enumerate(zip(sizes, starts)):
-            word[a:a + n] = _words(n, 0, SEED + h["step"], TENSOR_ID + i, s["p"].device)
+            word[a:a + n] = _words(n, SEED, TENSOR_ID + i + (h["step"] << 32), s["p"].device)
         lo, hi = word & 0xFFFF, word >> 16
         del word
     p, g = s["p"].float(), s["g"].float()
