@@ -464,6 +464,151 @@ srq_status_t srq_glu_bwd(const void *dh, srq_dtype_t dt, int64_t ld_dh, const sr
                          const srq_blocks_t *dg, const srq_blocks_t *du, const srq_blocks_t *dg_t, const srq_blocks_t *du_t,
                          const srq_blocks_t *h_t, uint32_t *device_status, void *cuda_stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * The two ends of a language model's training step, and its update: the embedding of the tokens and its gradient, the losses
+ * on the logits, the AdamW step.
+ *
+ * Conventions are those of the block-scaled operators (device_status is an optional sticky word, extents may be 0, operands
+ * without elements may have null pointers), and
+ *   - Token ids, targets and offsets are whole numbers of type srq_index_t on the device.  The host does not see them: one that
+ *     is out of range is reported as SRQ_ERR_INVALID_ARG in device_status, nothing is read or written through it, and
+ *     the call goes on as is said at each operator.
+ *   - Sums over tokens, rows and classes are in binary32 or more and have an order that depends on sizes, ids and the device
+ *     alone: the same call repeats bit for bit.
+ *   - Base pointers of matrices and of AdamW's tensors are 16-byte aligned; pitches are in elements and may be odd.
+ */
+typedef enum { SRQ_I32 = 0, SRQ_I64 = 1 } srq_index_t;
+
+/* out[t, :] = scale * table[ids[t], :], table[rows, cols], out[tokens, cols], each result rounded once.  An id below zero is
+ * padding: its row of out is zero.  So is the row of an id that is not below `rows`, which is reported. */
+srq_status_t srq_embedding_fwd(const void *table, srq_dtype_t dt, int64_t rows, int64_t cols, int64_t ld,
+                               const void *ids, srq_index_t id_t, int64_t tokens, float scale,
+                               void *out, srq_dtype_t out_dt, int64_t ld_out, uint32_t *device_status, void *cuda_stream);
+
+/* Bytes of workspace srq_embedding_bwd needs (the sorted tokens, and the partial sums of ids whose tokens are many). */
+size_t srq_embedding_workspace_bytes(int64_t tokens, int64_t rows, int64_t cols);
+
+/* Its gradient: dtable[v, :] = scale * sum of dout[t, :] over the tokens t with ids[t] = v, added in the order of the tokens (in
+ * parts where they are many) in binary32 and rounded once.  Rows of ids without a token become zero.  accumulate = 1 adds to a
+ * binary32 dtable instead, and leaves the rows of ids without a token as they are.  Padding and ids out of range (reported)
+ * have no gradient.  tokens and rows are at most 2^31 - 2. */
+srq_status_t srq_embedding_bwd(const void *dout, srq_dtype_t dt, int64_t tokens, int64_t cols, int64_t ld,
+                               const void *ids, srq_index_t id_t, int64_t rows, float scale,
+                               void *dtable, srq_dtype_t dtable_dt, int64_t ld_dtable, int32_t accumulate,
+                               void *ws, size_t ws_bytes, uint32_t *device_status, void *cuda_stream);
+
+/* Log-probabilities of given classes: with z = logits / temperature, row by row,
+ *   lse = log(sum over j of e^(z_j)),  logp = z_target - lse.
+ * logits[rows, classes] has type dt and pitch ld; logits of minus infinity (masked classes) have probability 0.  A target
+ * below zero marks a row that does not count (padding, a prompt): its logits are not read, its logp and lse are 0.  A target
+ * that is not below `classes` is treated the same and reported.  A logp that is not finite is reported (SRQ_ERR_NONFINITE).
+ * lse may be NULL. */
+srq_status_t srq_logprob_fwd(const void *logits, srq_dtype_t dt, int64_t rows, int64_t classes, int64_t ld,
+                             const void *targets, srq_index_t target_t, float temperature,
+                             float *logp, float *lse, uint32_t *device_status, void *cuda_stream);
+
+/* Their gradient at the logits: dlogits_j = dlogp / temperature * ([j = target] - e^(z_j - lse)), type dt, from lse as
+ * srq_logprob_fwd gave it and the gradient dlogp[rows] at logp (supervised training: minus each token's weight).  Rows that do
+ * not count (target below zero or out of range, dlogp zero) become zero and their logits are not read.  dlogits may be
+ * the logits themselves (same pointer and pitch). */
+srq_status_t srq_logprob_bwd(const void *logits, srq_dtype_t dt, int64_t rows, int64_t classes, int64_t ld,
+                             const void *targets, srq_index_t target_t, float temperature, const float *lse, const float *dlogp,
+                             void *dlogits, int64_t ld_dlogits, uint32_t *device_status, void *cuda_stream);
+
+/* Clipped policy loss with a KL term, and its gradient at the logits, in one pass over them.  With logp as above and
+ * rho = e^(logp - logp_old), row r has the loss
+ *   row_loss = weight * ( -min(rho A, clip(rho, 1 - clip_low, 1 + clip_high) A)  +  kl_coef * (e^d - d - 1) ),  d = logp_ref - logp
+ * (A = advantage; the last term estimates the divergence from the reference policy without bias and is never negative), and
+ *   dlogp = weight * ( -(rho A where it is the smaller of the two, else 0)  +  kl_coef * (1 - e^d) ),
+ * from which dlogits follows as in srq_logprob_bwd.  weight[rows] holds what the caller's mean asks for (1 / number of tokens,
+ * or per sequence).  A row with weight zero, or with a target as above, does not count: its logits and its other inputs are
+ * not read, its logp, row_loss and dlogits are 0.  logp_ref may be NULL: no KL term (kl_coef is then ignored).  row_loss [rows],
+ * loss [1] (the sum of row_loss; needs row_loss), logp [rows] and dlogits may each be NULL, but not all of them.  dlogits may be
+ * the logits themselves. */
+typedef struct {
+    float temperature;           /* > 0 */
+    float clip_low, clip_high;   /* >= 0; clip_low = 0.2: ratios below 0.8 are clipped.  Infinity: not clipped on that side */
+    float kl_coef;               /* >= 0 */
+} srq_policy_t;
+srq_status_t srq_policy_loss(const void *logits, srq_dtype_t dt, int64_t rows, int64_t classes, int64_t ld,
+                             const void *targets, srq_index_t target_t, const float *logp_old, const float *advantage,
+                             const float *weight, const float *logp_ref, const srq_policy_t *policy,
+                             float *row_loss, float *loss, float *logp, void *dlogits, int64_t ld_dlogits,
+                             uint32_t *device_status, void *cuda_stream);
+
+/* Bytes of workspace srq_preference_loss needs for `rows` rows of logits. */
+size_t srq_preference_workspace_bytes(int64_t rows);
+
+/* Preference loss on pairs of answers, and its gradient at the logits.  The rows of the logits are the tokens of 2 * pairs
+ * answers one after the other: offsets[0 .. 2 * pairs], not falling, between 0 and rows; answer 2 i is the chosen and 2 i + 1 the
+ * rejected one of pair i.  With the sums over an answer's rows that count
+ *   h = beta * ( sum over the chosen of (logp - logp_ref)  -  sum over the rejected of (logp - logp_ref) ),
+ *   pair_loss = -(1 - label_smoothing) log sigma(h) - label_smoothing log sigma(-h),    loss = mean of pair_loss,
+ * and dlogits is the gradient of loss.  logp_ref[rows] comes from srq_logprob_fwd on the reference model's logits.  Rows whose
+ * target is below zero or out of range (reported) do not count: logp and dlogits are 0, logp_ref is not read.  Rows before
+ * offsets[0] and from offsets[2 * pairs] on belong to no answer: their logits are not read, and logp and dlogits are left as
+ * they were.  Offsets that fall, or lie outside, are reported, and what the call then writes within its arrays is unspecified.
+ * pair_loss [pairs] and logp [rows] are required; loss [1] and dlogits may be NULL.  dlogits may be
+ * the logits themselves. */
+typedef struct {
+    float temperature;       /* > 0 */
+    float beta;              /* finite */
+    float label_smoothing;   /* 0 .. 1 */
+} srq_preference_t;
+srq_status_t srq_preference_loss(const void *logits, srq_dtype_t dt, int64_t rows, int64_t classes, int64_t ld,
+                                 const void *targets, srq_index_t target_t, const float *logp_ref,
+                                 const void *offsets, srq_index_t offset_t, int64_t pairs, const srq_preference_t *preference,
+                                 float *pair_loss, float *loss, float *logp, void *dlogits, int64_t ld_dlogits,
+                                 void *ws, size_t ws_bytes, uint32_t *device_status, void *cuda_stream);
+
+/* AdamW step (decoupled weight decay) over many tensors at once, in place.  Per element, in binary32, with t the number of the step:
+ *   g <- g * grad_scale,   m <- beta1 m + (1 - beta1) g,   v <- beta2 v + (1 - beta2) g^2,
+ *   p <- (1 - lr weight_decay) p - lr / (1 - beta1^t) * m / ( sqrt(v / (1 - beta2^t)) + eps )
+ * (products and sums of m and v each rounded once, in this order; second moments below 2^-126 count as 0 under the root).
+ *
+ * param_dt: type of p.  bfloat16 weights are rounded to the nearest (SRQ_RNE) or stochastically (SRQ_SR), so that updates smaller
+ * than half a unit are not lost but taken with the right probability: the low 16 bits of the binary32 result are cut off
+ * after a 16-bit threshold was added.  grad_dt: type of g.
+ *
+ * state_bits 32: m and v are binary32.  state_bits 8: one byte per element and one binary32 step size per 128 elements (flat
+ * index / 128; the last block may be shorter), always rounded stochastically.
+ *   m   E4M3 codes, step D = max |m| * fl(1 / 448): |m| / D is cut to three bits of mantissa after a 16-bit threshold was added
+ *   v   codes without a sign, four bits of exponent (bias 7) and four of mantissa, no special values, largest number 496;
+ *       step max v * fl(1 / 496).  v itself is coded, not its root, so that the rounding has no bias; the noise of a step, 1.8 % of v on
+ *       average, adds up over the moment's memory to 1.8 % / sqrt(1 - beta2^2) (6 % at 0.95, 40 % at 0.999).  (Rounded to nearest
+ *       the moment would stand still: a step changes it by less than half a unit.)  A positive v does not get code 0, which
+ *       would make the next m / (sqrt(v) + eps) as large as m / eps.
+ *   x / D is x * inv as elsewhere, inv = 448 / max |m| or 496 / max v rounded toward zero; blocks where it overflows are zero.
+ *   m and v as zero bytes and step sizes 0 are the state before the first step.
+ * Thresholds: element i of tensor k uses word w = (i & 3) of the Philox block of counter {lo(i>>2), hi(i>>2), lo(id), hi(id)},
+ * id = tensor_id + k + t * 2^32, key seed: the low half of w for p, the high half for v, their exclusive-or for m (any two of
+ * the three are independent).
+ *
+ * A gradient that is not finite, or a moment that leaves binary32, is reported (SRQ_ERR_NONFINITE).  With 32-bit states the
+ * element follows the formula; with 8-bit states the block of 128 that has it is left as it was, weights and moments.
+ * If *grad_scale is not finite, nothing is changed at all and that is reported (a step whose gradient norm overflowed).
+ *
+ * tensors is a HOST array, read before the call returns; no pointer in it may overlap another tensor's. */
+typedef struct {
+    void *param; const void *grad;     /* [n] of param_dt, [n] of grad_dt; 16-byte aligned */
+    void *m, *v;                       /* [n] floats or bytes; 16-byte aligned */
+    float *m_step, *v_step;            /* [ceil(n / 128)], 8-bit states only (else ignored); 4-byte aligned */
+    int64_t n;
+} srq_adamw_tensor_t;
+typedef struct {
+    double lr, beta1, beta2;           /* lr finite; betas in [0, 1) */
+    double eps, weight_decay;          /* eps > 0, finite; weight_decay finite */
+    int64_t step;                      /* t, from 1 */
+    int32_t round;                     /* srq_round_t: SRQ_SR or SRQ_RNE, of bfloat16 weights */
+    uint64_t seed, tensor_id;
+    /* Device scalars for steps that are recorded in a CUDA graph and for clipping; each may be NULL. */
+    const float *lr_device;            /* read instead of lr */
+    const int64_t *step_device;        /* read instead of step; the caller raises it before the call */
+    const float *grad_scale;           /* factor on every gradient */
+} srq_adamw_t;
+srq_status_t srq_adamw_step(const srq_adamw_tensor_t *tensors, int64_t count, srq_dtype_t param_dt, srq_dtype_t grad_dt,
+                            int32_t state_bits, const srq_adamw_t *adamw, uint32_t *device_status, void *cuda_stream);
+
 /* Waits for the stream, then returns the device status word of the workspace: SRQ_OK, or the
  * first device-side condition recorded by the calls that used this workspace since its header
  * was last cleared (every entry point clears it when it starts). */

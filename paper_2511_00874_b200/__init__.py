@@ -14,3 +14,6 @@ from .binding import (Output, qlinear_bwd_ex, qlinear_fwd_ex, srq_gemm_i8_ex,  #
                       status_string)
 from .binding import (BLOCK_RNE, GELU, PER_BLOCK, RNE, SILU, Blocks, block_sr, new_blocks, srq_gemm_blocks,  # noqa: F401
                       srq_glu_bwd, srq_glu_fwd, srq_quantize_blocks, srq_rmsnorm_bwd, srq_rmsnorm_fwd, srq_rmsnorm_workspace_bytes)
+from .binding import (AdamTensor, AdamTensors, new_adam_state, srq_adamw_step, srq_embedding_bwd, srq_embedding_fwd,  # noqa: F401
+                      srq_embedding_workspace_bytes, srq_logprob_bwd, srq_logprob_fwd, srq_policy_loss, srq_preference_loss,
+                      srq_preference_workspace_bytes)

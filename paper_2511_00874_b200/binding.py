@@ -31,7 +31,9 @@ EXPORTS = ["srq_quantize_workspace_bytes", "srq_gemm_workspace_bytes", "srq_work
            "srq_gemm_i8_ex", "qlinear_fwd_ex", "qlinear_bwd_ex", "srq_dequant_i32",
            "srq_poll_status", "srq_status_string", "srq_launch_count", "srq_selftest_bounded_wait", "srq_selftest_mma_rate", "srq_set_product_timer", "srq_plan_splits",
            "srq_quantize_blocks", "srq_requantize_blocks", "srq_gemm_blocks", "srq_rmsnorm_fwd", "srq_rmsnorm_workspace_bytes",
-           "srq_rmsnorm_bwd", "srq_glu_fwd", "srq_glu_bwd"]
+           "srq_rmsnorm_bwd", "srq_glu_fwd", "srq_glu_bwd",
+           "srq_embedding_fwd", "srq_embedding_workspace_bytes", "srq_embedding_bwd", "srq_logprob_fwd", "srq_logprob_bwd", "srq_policy_loss",
+           "srq_preference_workspace_bytes", "srq_preference_loss", "srq_adamw_step"]
 
 
 class SrqError(RuntimeError):
@@ -79,6 +81,24 @@ class QSpec:
 class _Blocks(ctypes.Structure):
     _fields_ = [("codes", ctypes.c_void_p), ("ld", ctypes.c_int64), ("scale", ctypes.c_void_p), ("ld_scale", ctypes.c_int64),
                 ("tile_rows", ctypes.c_int32)]
+
+
+class _Policy(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_float) for n in ("temperature", "clip_low", "clip_high", "kl_coef")]
+
+
+class _Preference(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_float) for n in ("temperature", "beta", "label_smoothing")]
+
+
+class _AdamTensor(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("param", "grad", "m", "v", "m_step", "v_step")] + [("n", ctypes.c_int64)]
+
+
+class _AdamW(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_double) for n in ("lr", "beta1", "beta2", "eps", "weight_decay")] + \
+               [("step", ctypes.c_int64), ("round", ctypes.c_int32), ("seed", ctypes.c_uint64), ("tensor_id", ctypes.c_uint64),
+                ("lr_device", ctypes.c_void_p), ("step_device", ctypes.c_void_p), ("grad_scale", ctypes.c_void_p)]
 
 
 _lib: Optional[ctypes.CDLL] = None
@@ -148,6 +168,19 @@ def lib() -> ctypes.CDLL:
     L.srq_glu_fwd.argtypes = [bp, bp, bp, i64, i64, i64, i, bp, vp, i, i64, bp, bp, vp, vp]
     L.srq_glu_bwd.argtypes = [vp, i, i64, bp, bp, i64, i64, i, qp, bp, bp, bp, bp, bp, vp, vp]
     for name in ("srq_quantize_blocks", "srq_requantize_blocks", "srq_gemm_blocks", "srq_rmsnorm_fwd", "srq_rmsnorm_bwd", "srq_glu_fwd", "srq_glu_bwd"):
+        getattr(L, name).restype = ctypes.c_int
+    L.srq_embedding_fwd.argtypes = [vp, i, i64, i64, i64, vp, i, i64, f, vp, i, i64, vp, vp]
+    L.srq_embedding_workspace_bytes.argtypes = [i64, i64, i64]
+    L.srq_embedding_workspace_bytes.restype = sz
+    L.srq_embedding_bwd.argtypes = [vp, i, i64, i64, i64, vp, i, i64, f, vp, i, i64, i32, vp, sz, vp, vp]
+    L.srq_logprob_fwd.argtypes = [vp, i, i64, i64, i64, vp, i, f, vp, vp, vp, vp]
+    L.srq_logprob_bwd.argtypes = [vp, i, i64, i64, i64, vp, i, f, vp, vp, vp, i64, vp, vp]
+    L.srq_policy_loss.argtypes = [vp, i, i64, i64, i64, vp, i, vp, vp, vp, vp, ctypes.POINTER(_Policy), vp, vp, vp, vp, i64, vp, vp]
+    L.srq_preference_workspace_bytes.argtypes = [i64]
+    L.srq_preference_workspace_bytes.restype = sz
+    L.srq_preference_loss.argtypes = [vp, i, i64, i64, i64, vp, i, vp, vp, i, i64, ctypes.POINTER(_Preference), vp, vp, vp, vp, i64, vp, sz, vp, vp]
+    L.srq_adamw_step.argtypes = [ctypes.POINTER(_AdamTensor), i64, i, i, i32, ctypes.POINTER(_AdamW), vp, vp]
+    for name in ("srq_embedding_fwd", "srq_embedding_bwd", "srq_logprob_fwd", "srq_logprob_bwd", "srq_policy_loss", "srq_preference_loss", "srq_adamw_step"):
         getattr(L, name).restype = ctypes.c_int
     L.srq_poll_status.argtypes = [vp, vp]
     L.srq_poll_status.restype = ctypes.c_int
@@ -733,3 +766,199 @@ def srq_glu_bwd(dh: torch.Tensor, gate: Blocks, up: Blocks, act: int, q: QSpec, 
                            q.c(), _bref(dg, (T, F), "dg"), _bref(du, (T, F), "du"), _bref(dg_t, (F, T), "dg_t"),
                            _bref(du_t, (F, T), "du_t"), _bref(h_t, (F, T), "h_t"), _status_word(device_status), _stream())
     _check(st, "srq_glu_bwd")
+
+
+# ---------------------------------------------------------------------------------------------
+# the ends of a training step: embedding, losses on the logits, AdamW
+# ---------------------------------------------------------------------------------------------
+I32, I64 = 0, 1
+
+
+def _whole(t: torch.Tensor, name: str, n: Optional[int] = None):
+    """(pointer, type) of a contiguous vector of int32 or int64 on the device."""
+    if t.dtype is torch.int64:
+        wide = I64
+    elif t.dtype is torch.int32:
+        wide = I32
+    else:
+        raise TypeError(f"{name} must be int32 or int64, got {t.dtype}")
+    if t.dim() != 1 or not t.is_cuda or not t.is_contiguous() or (n is not None and t.numel() != n):
+        raise ValueError(f"{name} must be a contiguous CUDA vector" + ("" if n is None else f" of {n} whole numbers"))
+    return t.data_ptr(), wide
+
+
+def _workspace(ws: Optional[torch.Tensor], need: int, device):
+    """(pointer, bytes, tensor) of the caller's workspace, or of a new one."""
+    if ws is None:
+        ws = new_workspace(need, device)
+    if not ws.is_cuda or not ws.is_contiguous():
+        raise ValueError("ws must be contiguous memory on the device")
+    return ws.data_ptr(), ws.numel() * ws.element_size(), ws
+
+
+def srq_embedding_fwd(table: torch.Tensor, ids: torch.Tensor, out: torch.Tensor, scale: float = 1.0,
+                      device_status: Optional[torch.Tensor] = None) -> None:
+    """out[t] = scale * table[ids[t]]; an id below zero is padding and gives a row of zeros."""
+    pi, wide = _whole(ids, "ids")
+    T, (rows, cols) = ids.numel(), table.shape
+    pt, ldt = _mat(table, "table")
+    po, ldo = _mat(out, "out", (T, cols))
+    st = lib().srq_embedding_fwd(pt, _dtype_of(table), rows, cols, ldt, pi, wide, T, scale, po, _dtype_of(out), ldo, _status_word(device_status), _stream())
+    _check(st, "srq_embedding_fwd")
+
+
+def srq_embedding_workspace_bytes(tokens: int, rows: int, cols: int) -> int:
+    return int(lib().srq_embedding_workspace_bytes(tokens, rows, cols))
+
+
+def srq_embedding_bwd(dout: torch.Tensor, ids: torch.Tensor, dtable: torch.Tensor, scale: float = 1.0, accumulate: bool = False,
+                      ws: Optional[torch.Tensor] = None, device_status: Optional[torch.Tensor] = None) -> None:
+    """dtable[v] (+)= scale * sum of dout[t] over the tokens with ids[t] = v; rows without a token become zero, or stay as they
+    are where it accumulates."""
+    T, cols = dout.shape
+    rows = dtable.shape[0]
+    pi, wide = _whole(ids, "ids", T)
+    pd, ldd = _mat(dout, "dout")
+    pt, ldt = _mat(dtable, "dtable", (rows, cols))
+    pw, nb, ws = _workspace(ws, srq_embedding_workspace_bytes(T, rows, cols) if ws is None else 0, dout.device)
+    st = lib().srq_embedding_bwd(pd, _dtype_of(dout), T, cols, ldd, pi, wide, rows, scale, pt, _dtype_of(dtable), ldt, int(accumulate), pw, nb,
+                                 _status_word(device_status), _stream())
+    _check(st, "srq_embedding_bwd")
+
+
+def _logits(logits: torch.Tensor, targets: torch.Tensor):
+    """The arguments every call on logits begins with: pointer, type, rows, classes, pitch, targets, their type."""
+    rows, classes = logits.shape
+    px, ld = _mat(logits, "logits")
+    pt, wide = _whole(targets, "targets", rows)
+    return px, _dtype_of(logits), rows, classes, ld, pt, wide
+
+
+def srq_logprob_fwd(logits: torch.Tensor, targets: torch.Tensor, logp: torch.Tensor, lse: Optional[torch.Tensor] = None, temperature: float = 1.0,
+                    device_status: Optional[torch.Tensor] = None) -> None:
+    """logp[r] = log softmax(logits[r] / temperature)[targets[r]] and lse[r]; 0 for rows whose target is below zero."""
+    x = _logits(logits, targets)
+    st = lib().srq_logprob_fwd(*x, temperature, _vec(logp, "logp", x[2]), _vec(lse, "lse", x[2]), _status_word(device_status), _stream())
+    _check(st, "srq_logprob_fwd")
+
+
+def srq_logprob_bwd(logits: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor, dlogp: torch.Tensor, dlogits: torch.Tensor,
+                    temperature: float = 1.0, device_status: Optional[torch.Tensor] = None) -> None:
+    """Gradient at the logits from the gradient at logp; ``dlogits`` may be ``logits``."""
+    x = _logits(logits, targets)
+    pd, ldd = _mat(dlogits, "dlogits", logits.shape, logits.dtype)
+    st = lib().srq_logprob_bwd(*x, temperature, _vec(lse, "lse", x[2]), _vec(dlogp, "dlogp", x[2]), pd, ldd, _status_word(device_status), _stream())
+    _check(st, "srq_logprob_bwd")
+
+
+def srq_policy_loss(logits: torch.Tensor, targets: torch.Tensor, logp_old: torch.Tensor, advantage: torch.Tensor, weight: torch.Tensor,
+                    logp_ref: Optional[torch.Tensor] = None, row_loss: Optional[torch.Tensor] = None, loss: Optional[torch.Tensor] = None,
+                    logp: Optional[torch.Tensor] = None, dlogits: Optional[torch.Tensor] = None, temperature: float = 1.0, clip_low: float = 0.2,
+                    clip_high: float = 0.2, kl_coef: float = 0.0, device_status: Optional[torch.Tensor] = None) -> None:
+    """Clipped policy loss with a KL term to ``logp_ref`` and its gradient at the logits, in one pass; rows of weight zero do not
+    count.  ``loss`` needs ``row_loss``; ``dlogits`` may be ``logits``."""
+    x = _logits(logits, targets)
+    n = x[2]
+    pd, ldd = _mat(dlogits, "dlogits", logits.shape, logits.dtype)
+    st = lib().srq_policy_loss(*x, _vec(logp_old, "logp_old", n), _vec(advantage, "advantage", n), _vec(weight, "weight", n), _vec(logp_ref, "logp_ref", n),
+                               _Policy(temperature, clip_low, clip_high, kl_coef), _vec(row_loss, "row_loss", n), _vec(loss, "loss", 1),
+                               _vec(logp, "logp", n), pd, ldd, _status_word(device_status), _stream())
+    _check(st, "srq_policy_loss")
+
+
+def srq_preference_workspace_bytes(rows: int) -> int:
+    return int(lib().srq_preference_workspace_bytes(rows))
+
+
+def srq_preference_loss(logits: torch.Tensor, targets: torch.Tensor, logp_ref: torch.Tensor, offsets: torch.Tensor, pair_loss: torch.Tensor,
+                        loss: Optional[torch.Tensor], logp: torch.Tensor, dlogits: Optional[torch.Tensor] = None, beta: float = 0.1,
+                        label_smoothing: float = 0.0, temperature: float = 1.0, ws: Optional[torch.Tensor] = None,
+                        device_status: Optional[torch.Tensor] = None) -> None:
+    """Preference loss over pairs of answers (rows offsets[2 i] .. of the chosen, offsets[2 i + 1] .. of the rejected one) and its
+    gradient at the logits; ``dlogits`` may be ``logits``."""
+    x = _logits(logits, targets)
+    n = x[2]
+    po, wide = _whole(offsets, "offsets")
+    if offsets.numel() % 2 != 1:
+        raise ValueError("offsets must hold 2 * pairs + 1 whole numbers")
+    pairs = offsets.numel() // 2
+    pd, ldd = _mat(dlogits, "dlogits", logits.shape, logits.dtype)
+    pw, nb, ws = _workspace(ws, srq_preference_workspace_bytes(n) if ws is None else 0, logits.device)
+    st = lib().srq_preference_loss(*x, _vec(logp_ref, "logp_ref", n), po, wide, pairs, _Preference(temperature, beta, label_smoothing),
+                                   _vec(pair_loss, "pair_loss", pairs), _vec(loss, "loss", 1), _vec(logp, "logp", n), pd, ldd, pw, nb,
+                                   _status_word(device_status), _stream())
+    _check(st, "srq_preference_loss")
+
+
+@dataclass
+class AdamTensor:
+    """One tensor of an AdamW step: weight, gradient and moments of the same number of elements (any shape, contiguous); moments
+    are float32, or uint8 with their step sizes, one float32 per 128 elements (new_adam_state)."""
+    param: torch.Tensor
+    grad: torch.Tensor
+    m: torch.Tensor
+    v: torch.Tensor
+    m_step: Optional[torch.Tensor] = None
+    v_step: Optional[torch.Tensor] = None
+
+
+def new_adam_state(param: torch.Tensor, bits: int = 32):
+    """(m, v, m_step, v_step) before the first step, for a weight; bits is 32 or 8."""
+    if bits not in (8, 32):
+        raise ValueError("moments have 8 or 32 bits")
+    new = lambda n, dt: torch.zeros(n, dtype=dt, device=param.device)  # noqa: E731
+    n = param.numel()
+    if bits == 32:
+        return new(n, torch.float32), new(n, torch.float32), None, None
+    nb = -(-n // BLOCK)
+    return new(n, torch.uint8), new(n, torch.uint8), new(nb, torch.float32), new(nb, torch.float32)
+
+
+class AdamTensors:
+    """The tensors of a group of an AdamW step, listed once: all weights have one type, all gradients one, all moments 8 or 32
+    bits.  Holds the tensors, whose memory must stay where it is; a gradient that moves is given anew with ``set_grad``."""
+
+    def __init__(self, tensors):
+        self.tensors = list(tensors)
+        t0 = self.tensors[0] if self.tensors else None
+        self.param_dtype, self.grad_dtype = (F32, F32) if t0 is None else (_dtype_of(t0.param), _dtype_of(t0.grad))
+        self.bits = 32 if t0 is None or t0.m.dtype is torch.float32 else 8
+        self.c = (_AdamTensor * max(1, len(self.tensors)))()
+        for i, t in enumerate(self.tensors):
+            n, state = t.param.numel(), torch.float32 if self.bits == 32 else torch.uint8
+            for name, x, dtype, size in (("param", t.param, t0.param.dtype, n), ("m", t.m, state, n), ("v", t.v, state, n)):
+                self._check(i, name, x, dtype, size)
+            for name, x in (("m_step", t.m_step), ("v_step", t.v_step)):
+                if self.bits == 8:
+                    self._check(i, name, x, torch.float32, -(-n // BLOCK))
+            self.c[i] = _AdamTensor(t.param.data_ptr(), None, t.m.data_ptr(), t.v.data_ptr(), _ptr(t.m_step) if self.bits == 8 else None,
+                                    _ptr(t.v_step) if self.bits == 8 else None, n)
+            self.set_grad(i, t.grad)
+
+    @staticmethod
+    def _check(i, name, x, dtype, size):
+        if x is None or x.dtype is not dtype or x.numel() != size or not x.is_cuda or not x.is_contiguous():
+            raise ValueError(f"tensor {i}: {name} must hold {size} contiguous values of {dtype} on the device")
+
+    def set_grad(self, i: int, grad: torch.Tensor) -> None:
+        """The gradient of tensor i from now on."""
+        self._check(i, "grad", grad, torch.float32 if self.grad_dtype == F32 else torch.bfloat16, self.tensors[i].param.numel())
+        self.tensors[i].grad = grad
+        self.c[i].grad = grad.data_ptr()
+
+    def __len__(self):
+        return len(self.tensors)
+
+
+def srq_adamw_step(tensors: AdamTensors, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.0,
+                   step: int = 1, round: int = SR, seed: int = 0, tensor_id: int = 0, lr_device: Optional[torch.Tensor] = None,
+                   step_device: Optional[torch.Tensor] = None, grad_scale: Optional[torch.Tensor] = None,
+                   device_status: Optional[torch.Tensor] = None) -> None:
+    """One AdamW step in place over all tensors; ``round``: SR or RNE, of bfloat16 weights.  ``lr_device`` (float32),
+    ``step_device`` (int64) and ``grad_scale`` (float32) are device scalars that are read when the step runs."""
+    if step_device is not None and (step_device.dtype is not torch.int64 or not step_device.is_cuda):
+        raise ValueError("step_device must be an int64 CUDA tensor of one element")
+    h = _AdamW(lr, beta1, beta2, eps, weight_decay, step, round, seed, tensor_id, _vec(lr_device, "lr_device", 1), _ptr(step_device),
+               _vec(grad_scale, "grad_scale", 1))
+    st = lib().srq_adamw_step(tensors.c, len(tensors.tensors), tensors.param_dtype, tensors.grad_dtype, tensors.bits, h, _status_word(device_status), _stream())
+    _check(st, "srq_adamw_step")

@@ -11,7 +11,8 @@ _ROOT = os.path.dirname(_PKG)
 CSRC = os.path.join(_PKG, "csrc")
 INCLUDE = os.path.join(_ROOT, "include")
 LIB = os.path.join(_PKG, "libsrq.so")
-SOURCES = ["api.cu", "api_blocks.cu", "quantize.cu", "quantize_blocks.cu", "rmsnorm.cu", "gemm_i8.cu", "gemm_blocks.cu", "noalloc.cu"]
+SOURCES = ["api.cu", "api_blocks.cu", "quantize.cu", "quantize_blocks.cu", "rmsnorm.cu", "gemm_i8.cu", "gemm_blocks.cu", "noalloc.cu",
+           "api_train.cu", "embedding.cu", "losses.cu", "adamw.cu"]
 
 
 def _nvcc() -> str:

@@ -265,4 +265,42 @@ struct GluArgs {
 };
 srq_status_t launch_glu_fwd(const GluArgs& g, uint32_t* status, cudaStream_t stream);
 
+// ------------------------------------------------------------------------------------------
+// The ends of a training step (embedding.cu, losses.cu, adamw.cu)
+// ------------------------------------------------------------------------------------------
+struct EmbedFwdArgs {
+    const void* table; int32_t dt; int64_t rows, cols, ld; const void* ids; int32_t id_t; int64_t tokens; float scale;
+    void* out; int32_t out_dt; int64_t ld_out; uint32_t* status;
+};
+cudaError_t launch_embedding_fwd(const EmbedFwdArgs& a, cudaStream_t stream);
+struct EmbedBwdArgs {
+    const void* dout; int32_t dt; int64_t tokens, cols, ld; const void* ids; int32_t id_t; int64_t rows; float scale;
+    void* out; int32_t out_dt; int64_t ld_out; int32_t accumulate; void* ws; uint32_t* status;
+};
+size_t embedding_bytes(int64_t tokens, int64_t rows, int64_t cols);
+cudaError_t launch_embedding_bwd(const EmbedBwdArgs& a, cudaStream_t stream);
+
+struct LogitsArgs {
+    const void* x; int32_t dt; int64_t rows, classes, ld; const void* targets; int32_t target_t; float temperature; uint32_t* status;
+};
+cudaError_t launch_logprob_fwd(const LogitsArgs& a, float* logp, float* lse, cudaStream_t stream);
+cudaError_t launch_logprob_bwd(const LogitsArgs& a, const float* lse, const float* dlogp, void* dx, int64_t ldx, cudaStream_t stream);
+struct PolicyArgs {
+    const float* old; const float* advantage; const float* weight; const float* ref; srq_policy_t h;
+    float* row_loss; float* loss; float* logp; void* dx; int64_t ldx;
+};
+cudaError_t launch_policy(const LogitsArgs& a, const PolicyArgs& p, cudaStream_t stream);
+struct PreferenceArgs {
+    const float* ref; const void* offsets; int32_t offset_t; int64_t pairs; srq_preference_t h;
+    float* pair_loss; float* loss; float* logp; void* dx; int64_t ldx;
+};
+size_t preference_bytes(int64_t rows);
+cudaError_t launch_preference(const LogitsArgs& a, const PreferenceArgs& p, void* ws, cudaStream_t stream);
+
+struct AdamwArgs {
+    const srq_adamw_tensor_t* tensors; int64_t count; int32_t param_dt, grad_dt; bool state8, sr;
+    const srq_adamw_t* h; uint32_t* status;
+};
+cudaError_t launch_adamw(const AdamwArgs& a, cudaStream_t stream);
+
 }  // namespace srq
