@@ -1,17 +1,21 @@
 // AdamW step over many tensors at once (the formula and the formats of the 8-bit moments are in srq.h).
 //
 // The list of tensors travels in the kernel's parameters, so that a call needs no table on the device and can be recorded as it
-// is.  Work is cut into groups of 256 elements of one tensor; a warp takes a group, a lane eight neighbouring elements of it, so
-// that a block of 128 (the unit of an 8-bit moment's step size) is the sixteen lanes of half a warp: everything is read once,
-// the block's new moments stay in registers between their absmax and their codes, and what is written is written once.
-// 32-bit states are bound by HBM.  With 8-bit states and bfloat16 weights 10 bytes move per element while Philox takes about 20
-// issue slots per 32 elements and the arithmetic and the packing about 40, which is near what HBM allows.
+// is.  Everything is read once and written once.
+//   32-bit states: a warp takes groups of 256 elements, a lane eight neighbouring ones.  Bound by HBM.
+//   8-bit states: a warp takes groups of 512, a lane sixteen neighbouring ones, so that a block of 128 (the unit of a step size) is eight
+//   lanes, whose new moments stay in registers between their absmax and their codes.  With bfloat16 weights and gradients 10 bytes
+//   move per element while Philox takes about 20 issue slots per 32 elements and the rest about 40, so that issue is the bound
+//   as much as HBM: the arithmetic is on pairs, thresholds and codes are put together byte-wise.
 #include "train.cuh"
 
 namespace srq {
 
-constexpr int ADAM_GROUP = 256;                 // elements a warp takes at a time
-constexpr int ADAM_THREADS = 256;
+// 8-bit states: 96 registers, five CTAs of four warps per SM (256 threads at 80 registers spill, at 128 there are too few warps:
+// 907 and 940 us against 843 for eight layers).
+template <bool STATE8> constexpr int ADAM_THREADS = STATE8 ? 128 : 256;
+constexpr int ADAM_RUN = 4;                     // groups a warp takes before it looks for its tensor again, where there are many
+template <bool STATE8> constexpr int ADAM_GROUP = STATE8 ? 512 : 256;      // elements a warp takes at a time
 
 struct AdamEntry {
     void* p; const void* g; void* m; void* v; float* m_step; float* v_step;
@@ -31,7 +35,7 @@ struct AdamScalars {
 template <int CAP>
 struct AdamParams {
     AdamScalars s;
-    int32_t count;
+    int32_t count, run;
     int64_t groups;
     AdamEntry e[CAP];
 };
@@ -61,21 +65,6 @@ __device__ __forceinline__ float sqrt_fast(float x) {
     float r;
     asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
-}
-
-// 8-bit codes of the second moment (E4M4 without a sign).  Shifted to binary32's place of the exponent and multiplied by 2^120 a
-// code is the number it stands for, subnormal ones included.
-__device__ __forceinline__ float2 e4m4_pair(uint32_t a, uint32_t b) {
-    const float2 up = make_float2(0x1p120f, 0x1p120f);
-    return __fmul2_rn(make_float2(__uint_as_float(a & 0x07F80000u), __uint_as_float(b & 0x07F80000u)), up);
-}
-__device__ __forceinline__ void e4m4x8_to_f32(uint2 w, float2 v[4]) {
-    v[0] = e4m4_pair(w.x << 19, w.x << 11); v[1] = e4m4_pair(w.x << 3, w.x >> 5);
-    v[2] = e4m4_pair(w.y << 19, w.y << 11); v[3] = e4m4_pair(w.y << 3, w.y >> 5);
-}
-// |x| / D as a binary32 pattern whose exponent field is the code's (times 2^-120), plus the threshold below the code's last bit.
-__device__ __forceinline__ uint32_t threshold_sum(float quotient, uint32_t threshold) {
-    return (__float_as_uint(__fmul_rn(quotient, 0x1p-120f)) & 0x7FFFFFFFu) + threshold;
 }
 
 // Reciprocal step of a block of second moments, whose largest number is 496: block_inv (blocks.cuh) with another constant.
@@ -132,186 +121,357 @@ __device__ __forceinline__ float2 adam_weight(const AdamScalars& s, const AdamNo
     const float2 u = __fmul2_rn(m, make_float2(rcp_fast(d.x), rcp_fast(d.y)));
     return __ffma2_rn(u, make_float2(-n.rate, -n.rate), __fmul2_rn(p, make_float2(n.decay, n.decay)));
 }
-// bfloat16 by cutting off 16 bits after the threshold was added.  What is not finite stays so (a NaN keeps a payload bit).
-__device__ __forceinline__ uint32_t bf16_sr_bits(float x, uint32_t u16) {
-    const uint32_t b = __float_as_uint(x);
-    return (b & 0x7FFFFFFFu) >= 0x7F800000u ? ((b & 0x7FFFFFFFu) > 0x7F800000u ? b | 0x00400000u : b) : b + u16;
+// Two bfloat16 numbers by cutting off 16 bits after a threshold was added to them: the low halves of w0 (for x.x) and w1.  The
+// conversion instruction does just that with the halves of its random operand (checked against the bits of a million numbers of every
+// kind; infinities stay, a NaN becomes 0x7FFF).
+__device__ __forceinline__ uint32_t bf16_pair_sr(float2 x, uint32_t w0, uint32_t w1) {
+    uint32_t r;
+    asm("cvt.rs.bf16x2.f32 %0, %1, %2, %3;" : "=r"(r) : "f"(x.y), "f"(x.x), "r"(__byte_perm(w0, w1, 0x5410)));
+    return r;
 }
 __device__ __forceinline__ uint32_t bf16_pair(float2 x) {
     const __nv_bfloat162 p = __floats2bfloat162_rn(x.x, x.y);
     return *reinterpret_cast<const uint32_t*>(&p);
 }
 
-// Philox words of the eight elements whose first has the flat index i (a multiple of 8).
-__device__ __forceinline__ void adam_words(const AdamScalars& s, int64_t i, uint32_t c2, uint32_t c3, uint32_t w[8]) {
+// Philox words of the four elements of block j.
+__device__ __forceinline__ void adam_words(const AdamScalars& s, uint64_t j, uint32_t c2, uint32_t c3, uint32_t w[4]) {
+    uint32_t x0 = (uint32_t)j, x1 = (uint32_t)(j >> 32), x2 = c2, x3 = c3;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const uint64_t j = ((uint64_t)i >> 2) + h;
-        uint32_t x0 = (uint32_t)j, x1 = (uint32_t)(j >> 32), x2 = c2, x3 = c3;
-#pragma unroll
-        for (int r = 0; r < 10; ++r) {
-            const uint64_t p0 = (uint64_t)0xD2511F53u * x0, p1 = (uint64_t)0xCD9E8D57u * x2;
-            x0 = (uint32_t)(p1 >> 32) ^ x1 ^ s.k0[r];
-            x1 = (uint32_t)p1;
-            x2 = (uint32_t)(p0 >> 32) ^ x3 ^ s.k1[r];
-            x3 = (uint32_t)p0;
+    for (int r = 0; r < 10; ++r) {
+        const uint64_t p0 = (uint64_t)0xD2511F53u * x0, p1 = (uint64_t)0xCD9E8D57u * x2;
+        x0 = (uint32_t)(p1 >> 32) ^ x1 ^ s.k0[r];
+        x1 = (uint32_t)p1;
+        x2 = (uint32_t)(p0 >> 32) ^ x3 ^ s.k1[r];
+        x3 = (uint32_t)p0;
+    }
+    w[0] = x0; w[1] = x1; w[2] = x2; w[3] = x3;
+}
+
+// The tensor of group u: the last one that begins at or before it (empty tensors begin where the next one does).
+template <int CAP>
+__device__ __forceinline__ int adam_find(const AdamParams<CAP>& a, int64_t u) {
+    int k = 0;
+    for (int hi = a.count; hi - k > 1;) {
+        const int mid = (k + hi) >> 1;
+        if (a.e[mid].first <= u) k = mid; else hi = mid;
+    }
+    return k;
+}
+
+// What both kernels walk: CTAs take chunks of run * WARPS groups, warp w the groups w, w + WARPS, ... of a chunk.
+template <int WARPS, int CAP, typename F>
+__device__ __forceinline__ void adam_walk(const AdamParams<CAP>& a, F&& body) {
+    const int warp = __shfl_sync(0xFFFFFFFFu, (int)threadIdx.x >> 5, 0);       // so that the compiler knows it to be the same for the warp
+    const int64_t size = (int64_t)a.run * WARPS;
+    for (int64_t chunk = blockIdx.x * size; chunk < a.groups; chunk += gridDim.x * size) {
+        int k = -1;
+        int64_t end = 0;                                       // groups before the tensor after tensor k
+#pragma unroll 1
+        for (int r = 0; r < a.run; ++r) {
+            const int64_t u = chunk + r * WARPS + warp;
+            if (u >= a.groups) break;
+            if (k < 0 || u >= end) {
+                k = adam_find(a, u);
+                end = k + 1 < a.count ? a.e[k + 1].first : a.groups;
+            }
+            body(u, k);
         }
-        w[4 * h] = x0; w[4 * h + 1] = x1; w[4 * h + 2] = x2; w[4 * h + 3] = x3;
     }
 }
 
-// P, G: types of weights and gradients.  SR: bfloat16 weights are rounded stochastically (8-bit moments always are).
-template <typename P, typename G, bool STATE8, bool SR, int CAP>
-__global__ void __launch_bounds__(ADAM_THREADS) adamw_kernel(const __grid_constant__ AdamParams<CAP> a) {
+// P, G: types of weights and gradients.  SR: bfloat16 weights are rounded stochastically.
+template <typename P, typename G, bool SR, int CAP>
+__global__ void __launch_bounds__(ADAM_THREADS<false>) adamw_kernel(const __grid_constant__ AdamParams<CAP> a) {
     pdl_enter();
-    constexpr bool WORDS = STATE8 || (SR && sizeof(P) == 2);
+    constexpr bool WORDS = SR && sizeof(P) == 2;
     const AdamScalars& s = a.s;
     const AdamNow now = adam_now(s);
     if (!now.go) {
         if (threadIdx.x == 0 && blockIdx.x == 0) note(s.status, SRQ_ERR_NONFINITE);
         return;
     }
-    const int lane = threadIdx.x & 31;
-    const int64_t warps = (int64_t)gridDim.x * (ADAM_THREADS / 32);
-    for (int64_t u = (int64_t)blockIdx.x * (ADAM_THREADS / 32) + (threadIdx.x >> 5); u < a.groups; u += warps) {
-        int k = 0;                                             // last tensor that begins at or before group u
-        for (int hi = a.count; hi - k > 1;) {
-            const int mid = (k + hi) >> 1;
-            if (a.e[mid].first <= u) k = mid; else hi = mid;
-        }
+    adam_walk<ADAM_THREADS<false> / 32>(a, [&](int64_t group, int k) {
         const AdamEntry& e = a.e[k];
-        const int64_t i = (u - e.first) * ADAM_GROUP + lane * 8;
+        const int64_t i = (group - e.first) * ADAM_GROUP<false> + (threadIdx.x & 31) * 8;
         const int64_t left = e.n - i;                          // elements of this lane: min(left, 8), none or less: none
+        if (left <= 0) return;
         float2 p[4], g[4], m[4], v[4];
-        uint2 mc, vc;
         if (left >= 8) {
             read8<G>(e.g, i, g);
             read8<P>(e.p, i, p);
-            if constexpr (STATE8) {
-                mc = *reinterpret_cast<const uint2*>(reinterpret_cast<const uint8_t*>(e.m) + i);
-                vc = *reinterpret_cast<const uint2*>(reinterpret_cast<const uint8_t*>(e.v) + i);
-            } else {
-                read8<float>(e.m, i, m);
-                read8<float>(e.v, i, v);
-            }
+            read8<float>(e.m, i, m);
+            read8<float>(e.v, i, v);
         } else {
-            mc = make_uint2(0, 0); vc = make_uint2(0, 0);
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
-                float pp = 0.0f, gg = 0.0f, mm = 0.0f, vv = 0.0f;
-                if (q < left) {
-                    gg = read1<G>(e.g, i + q);
-                    pp = read1<P>(e.p, i + q);
-                    if constexpr (STATE8) {
-                        const uint32_t cm = reinterpret_cast<const uint8_t*>(e.m)[i + q], cv = reinterpret_cast<const uint8_t*>(e.v)[i + q];
-                        if (q < 4) { mc.x |= cm << (8 * q); vc.x |= cv << (8 * q); }
-                        else { mc.y |= cm << (8 * q - 32); vc.y |= cv << (8 * q - 32); }
-                    } else {
-                        mm = read1<float>(e.m, i + q);
-                        vv = read1<float>(e.v, i + q);
-                    }
-                }
-                if (q & 1) { p[q >> 1].y = pp; g[q >> 1].y = gg; if constexpr (!STATE8) { m[q >> 1].y = mm; v[q >> 1].y = vv; } }
-                else { p[q >> 1].x = pp; g[q >> 1].x = gg; if constexpr (!STATE8) { m[q >> 1].x = mm; v[q >> 1].x = vv; } }
+                const bool in = q < left;
+                const float gg = in ? read1<G>(e.g, i + q) : 0.0f, pp = in ? read1<P>(e.p, i + q) : 0.0f;
+                const float mm = in ? read1<float>(e.m, i + q) : 0.0f, vv = in ? read1<float>(e.v, i + q) : 0.0f;
+                if (q & 1) { p[q >> 1].y = pp; g[q >> 1].y = gg; m[q >> 1].y = mm; v[q >> 1].y = vv; }
+                else { p[q >> 1].x = pp; g[q >> 1].x = gg; m[q >> 1].x = mm; v[q >> 1].x = vv; }
             }
-        }
-        if constexpr (STATE8) {
-            float sm = 0.0f, sv = 0.0f;
-            if (left > 0) { sm = e.m_step[i / QBLK]; sv = e.v_step[i / QBLK]; }
-            float t[4];
-            e4m3x4_to_f32(mc.x, t); m[0] = make_float2(t[0], t[1]); m[1] = make_float2(t[2], t[3]);
-            e4m3x4_to_f32(mc.y, t); m[2] = make_float2(t[0], t[1]); m[3] = make_float2(t[2], t[3]);
-            e4m4x8_to_f32(vc, v);
-#pragma unroll
-            for (int q = 0; q < 4; ++q) { m[q] = __fmul2_rn(m[q], make_float2(sm, sm)); v[q] = __fmul2_rn(v[q], make_float2(sv, sv)); }
         }
         uint32_t w[8];
         if constexpr (WORDS) {
             const uint64_t id = (((uint64_t)s.id_hi << 32) | s.id_lo) + (uint64_t)k + ((uint64_t)now.t << 32);
-            adam_words(s, i, (uint32_t)id, (uint32_t)(id >> 32), w);
+            adam_words(s, (uint64_t)i >> 2, (uint32_t)id, (uint32_t)(id >> 32), w);
+            adam_words(s, ((uint64_t)i >> 2) + 1, (uint32_t)id, (uint32_t)(id >> 32), w + 4);
         }
         float mmax = 0.0f, vmax = 0.0f;
+        uint32_t pb[8];                                        // weights: bits of binary32 numbers, or in the first four of bfloat16 pairs
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             g[q] = __fmul2_rn(g[q], make_float2(now.gscale, now.gscale));
             adam_moments(s, g[q], m[q], v[q]);
             mmax = absmax3(mmax, m[q].x, m[q].y);
             vmax = absmax3(vmax, v[q].x, v[q].y);
-        }
-        bool keep = true;
-        if constexpr (STATE8) {
-#pragma unroll
-            for (int d = 8; d > 0; d >>= 1) {                  // the block's sixteen lanes
-                mmax = absmax3(mmax, mmax, __shfl_xor_sync(0xFFFFFFFFu, mmax, d));
-                vmax = absmax3(vmax, vmax, __shfl_xor_sync(0xFFFFFFFFu, vmax, d));
-            }
-        }
-        if (block_nonfinite(abs_word(mmax)) || block_nonfinite(abs_word(vmax))) {
-            note(s.status, SRQ_ERR_NONFINITE);
-            keep = !STATE8;
-        }
-        if (!keep || left <= 0) continue;
-        uint32_t pb[8];                                        // weights: binary32 bits, or bfloat16 ones in the upper half
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
             const float2 x = adam_weight(s, now, p[q], m[q], v[q]);
-            if constexpr (sizeof(P) == 2 && SR) {
-                pb[2 * q] = bf16_sr_bits(x.x, w[2 * q] & 0xFFFFu);
-                pb[2 * q + 1] = bf16_sr_bits(x.y, w[2 * q + 1] & 0xFFFFu);
-            } else if constexpr (sizeof(P) == 2) {
-                const uint32_t b = bf16_pair(x);
-                pb[2 * q] = b << 16; pb[2 * q + 1] = b & 0xFFFF0000u;
+            if constexpr (sizeof(P) == 2) {
+                pb[q] = WORDS ? bf16_pair_sr(x, w[2 * q], w[2 * q + 1]) : bf16_pair(x);
             } else {
                 pb[2 * q] = __float_as_uint(x.x); pb[2 * q + 1] = __float_as_uint(x.y);
             }
         }
-        if constexpr (STATE8) {
-            const float im = block_inv(abs_word(mmax)), iv = e4m4_inv(vmax);
-            uint32_t cm[8], cv[8];
-#pragma unroll
-            for (int q = 0; q < 8; ++q) {
-                const float mm = q & 1 ? m[q >> 1].y : m[q >> 1].x, vv = q & 1 ? v[q >> 1].y : v[q >> 1].x;
-                const uint32_t hi = w[q] >> 16, lo = w[q] & 0xFFFFu;
-                cm[q] = (threshold_sum(__fmul_rn(mm, im), ((lo ^ hi) << 4) + 8u) >> 20) | ((__float_as_uint(mm) >> 24) & 0x80u);
-                cv[q] = threshold_sum(__fmul_rn(vv, iv), (hi << 3) + 4u) >> 19;
-                if (cv[q] == 0 && vv > 0.0f && iv > 0.0f) cv[q] = 1;
-            }
-            mc = make_uint2(cm[0] | cm[1] << 8 | cm[2] << 16 | cm[3] << 24, cm[4] | cm[5] << 8 | cm[6] << 16 | cm[7] << 24);
-            vc = make_uint2(cv[0] | cv[1] << 8 | cv[2] << 16 | cv[3] << 24, cv[4] | cv[5] << 8 | cv[6] << 16 | cv[7] << 24);
-            if ((lane & 15) == 0) { e.m_step[i / QBLK] = moment_step(mmax, im, 1.0f / E4M3_MAX); e.v_step[i / QBLK] = moment_step(vmax, iv, 1.0f / E4M4_MAX); }
-        }
+        if (block_nonfinite(abs_word(mmax)) || block_nonfinite(abs_word(vmax))) note(s.status, SRQ_ERR_NONFINITE);
         if (left >= 8) {
             if constexpr (sizeof(P) == 2) {
-                *reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(e.p) + i) =
-                    make_uint4(__byte_perm(pb[0], pb[1], 0x7632), __byte_perm(pb[2], pb[3], 0x7632), __byte_perm(pb[4], pb[5], 0x7632), __byte_perm(pb[6], pb[7], 0x7632));
+                *reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(e.p) + i) = make_uint4(pb[0], pb[1], pb[2], pb[3]);
             } else {
                 uint4* o = reinterpret_cast<uint4*>(reinterpret_cast<float*>(e.p) + i);
                 o[0] = make_uint4(pb[0], pb[1], pb[2], pb[3]);
                 o[1] = make_uint4(pb[4], pb[5], pb[6], pb[7]);
             }
-            if constexpr (STATE8) {
-                *reinterpret_cast<uint2*>(reinterpret_cast<uint8_t*>(e.m) + i) = mc;
-                *reinterpret_cast<uint2*>(reinterpret_cast<uint8_t*>(e.v) + i) = vc;
-            } else {
-                write8(e.m, i, m);
-                write8(e.v, i, v);
-            }
+            write8(e.m, i, m);
+            write8(e.v, i, v);
         } else {
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
                 if (q >= left) continue;
-                if constexpr (sizeof(P) == 2) reinterpret_cast<uint16_t*>(e.p)[i + q] = (uint16_t)(pb[q] >> 16);
+                if constexpr (sizeof(P) == 2) reinterpret_cast<uint16_t*>(e.p)[i + q] = (uint16_t)(pb[q >> 1] >> (16 * (q & 1)));
                 else reinterpret_cast<uint32_t*>(e.p)[i + q] = pb[q];
-                if constexpr (STATE8) {
-                    reinterpret_cast<uint8_t*>(e.m)[i + q] = (uint8_t)((q < 4 ? mc.x : mc.y) >> (8 * (q & 3)));
-                    reinterpret_cast<uint8_t*>(e.v)[i + q] = (uint8_t)((q < 4 ? vc.x : vc.y) >> (8 * (q & 3)));
-                } else {
-                    reinterpret_cast<float*>(e.m)[i + q] = q & 1 ? m[q >> 1].y : m[q >> 1].x;
-                    reinterpret_cast<float*>(e.v)[i + q] = q & 1 ? v[q >> 1].y : v[q >> 1].x;
-                }
+                reinterpret_cast<float*>(e.m)[i + q] = q & 1 ? m[q >> 1].y : m[q >> 1].x;
+                reinterpret_cast<float*>(e.v)[i + q] = q & 1 ? v[q >> 1].y : v[q >> 1].x;
             }
         }
+    });
+}
+
+// Sixteen elements of type T as they lie in memory: 8 words (bfloat16) or 16 (binary32).  wide: 32-byte aligned.
+template <typename T> struct Raw16 { uint32_t w[4 * sizeof(T)]; };
+template <typename T>
+__device__ __forceinline__ Raw16<T> read16(const void* base, int64_t i, bool wide) {
+    Raw16<T> r;
+    const char* p = reinterpret_cast<const char*>(base) + i * (int64_t)sizeof(T);
+#pragma unroll
+    for (int h = 0; h < (int)sizeof(T) / 2; ++h) {
+        if (wide) {
+            const Word8 x = load32(p + 32 * h);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) r.w[8 * h + q] = x.w[q];
+        } else {
+            const uint4 x = *reinterpret_cast<const uint4*>(p + 32 * h), y = *reinterpret_cast<const uint4*>(p + 32 * h + 16);
+            r.w[8 * h] = x.x; r.w[8 * h + 1] = x.y; r.w[8 * h + 2] = x.z; r.w[8 * h + 3] = x.w;
+            r.w[8 * h + 4] = y.x; r.w[8 * h + 5] = y.y; r.w[8 * h + 6] = y.z; r.w[8 * h + 7] = y.w;
+        }
     }
+    return r;
+}
+template <typename T>
+__device__ __forceinline__ void write16(void* base, int64_t i, const Raw16<T>& r, bool wide) {
+    char* p = reinterpret_cast<char*>(base) + i * (int64_t)sizeof(T);
+#pragma unroll
+    for (int h = 0; h < (int)sizeof(T) / 2; ++h) {
+        if (wide) {
+            Word8 x;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) x.w[q] = r.w[8 * h + q];
+            store32(p + 32 * h, x);
+        } else {
+            *reinterpret_cast<uint4*>(p + 32 * h) = make_uint4(r.w[8 * h], r.w[8 * h + 1], r.w[8 * h + 2], r.w[8 * h + 3]);
+            *reinterpret_cast<uint4*>(p + 32 * h + 16) = make_uint4(r.w[8 * h + 4], r.w[8 * h + 5], r.w[8 * h + 6], r.w[8 * h + 7]);
+        }
+    }
+}
+// Pair q (elements 2 q and 2 q + 1).
+template <typename T>
+__device__ __forceinline__ float2 pair_of(const Raw16<T>& r, int q) {
+    if constexpr (sizeof(T) == 4) return make_float2(__uint_as_float(r.w[2 * q]), __uint_as_float(r.w[2 * q + 1]));
+    else return make_float2(bf16_lo(r.w[q]), bf16_hi(r.w[q]));
+}
+// The first `left` of sixteen elements, one by one; the others are zero.
+template <typename T>
+__device__ __forceinline__ Raw16<T> read_some(const void* base, int64_t i, int64_t left) {
+    Raw16<T> r;
+#pragma unroll
+    for (int q = 0; q < (int)(4 * sizeof(T)); ++q) r.w[q] = 0;
+#pragma unroll
+    for (int q = 0; q < 16; ++q) {
+        if (q >= left) continue;
+        if constexpr (sizeof(T) == 4) r.w[q] = reinterpret_cast<const uint32_t*>(base)[i + q];
+        else r.w[q >> 1] |= (uint32_t)reinterpret_cast<const uint16_t*>(base)[i + q] << (16 * (q & 1));
+    }
+    return r;
+}
+template <typename T>
+__device__ __forceinline__ void write_some(void* base, int64_t i, const Raw16<T>& r, int64_t left) {
+#pragma unroll
+    for (int q = 0; q < 16; ++q) {
+        if (q >= left) continue;
+        if constexpr (sizeof(T) == 4) reinterpret_cast<uint32_t*>(base)[i + q] = r.w[q];
+        else reinterpret_cast<uint16_t*>(base)[i + q] = (uint16_t)(r.w[q >> 1] >> (16 * (q & 1)));
+    }
+}
+__device__ __forceinline__ uint4 read_codes(const void* base, int64_t i, int64_t left) {
+    const uint8_t* p = reinterpret_cast<const uint8_t*>(base) + i;
+    if (left >= 16) return *reinterpret_cast<const uint4*>(p);
+    uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int q = 0; q < 16; ++q) if (q < left) w[q >> 2] |= (uint32_t)p[q] << (8 * (q & 3));
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ void write_codes(void* base, int64_t i, const uint32_t w[4], int64_t left) {
+    uint8_t* p = reinterpret_cast<uint8_t*>(base) + i;
+    if (left >= 16) { *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]); return; }
+#pragma unroll
+    for (int q = 0; q < 16; ++q) if (q < left) p[q] = (uint8_t)(w[q >> 2] >> (8 * (q & 3)));
+}
+
+// Four codes of the second moment (E4M4 without a sign) as numbers times 2^-8: shifted into place they are binary16 numbers, the
+// grid's subnormal ones included.
+__device__ __forceinline__ void e4m4x4_to_f32(uint32_t w, float2 v[2]) {
+    const uint32_t a = __byte_perm(w, 0, 0x4140) << 6, b = __byte_perm(w, 0, 0x4342) << 6;
+    v[0] = __half22float2(*reinterpret_cast<const __half2*>(&a));
+    v[1] = __half22float2(*reinterpret_cast<const __half2*>(&b));
+}
+// The top bytes of four words.
+__device__ __forceinline__ uint32_t top_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    return __byte_perm(__byte_perm(a, b, 0x0073), __byte_perm(c, d, 0x0073), 0x5410);
+}
+
+// Two codes' worth of a pair of moments: quotients x * inv, times 2^-120, where binary32's exponent field is the grid's, subnormal
+// numbers included, as bits.
+__device__ __forceinline__ uint2 code_bits(float2 x, float inv) {
+    const float2 t = __fmul2_rn(__fmul2_rn(x, make_float2(inv, inv)), make_float2(0x1p-120f, 0x1p-120f));
+    return make_uint2(__float_as_uint(t.x), __float_as_uint(t.y));
+}
+
+// One group of 512 elements of tensor e, sixteen per lane.  FULL: all of them are there and 32-byte aligned.
+template <typename P, typename G, bool SR, bool FULL>
+__device__ __forceinline__ void adam8_group(const AdamScalars& s, const AdamNow& now, const AdamEntry& e, int64_t i, uint64_t id) {
+    const int64_t left = FULL ? 16 : e.n - i;                  // elements of this lane: min(left, 16), none or less: none
+    Raw16<P> p;
+    Raw16<G> g;
+    uint4 mc = make_uint4(0, 0, 0, 0), vc = make_uint4(0, 0, 0, 0);
+    float sm = 0.0f, sv = 0.0f;
+    if (FULL || left >= 16) { g = read16<G>(e.g, i, FULL); p = read16<P>(e.p, i, FULL); }
+    else { g = read_some<G>(e.g, i, left); p = read_some<P>(e.p, i, left); }
+    if (FULL || left > 0) {
+        mc = read_codes(e.m, i, left);
+        vc = read_codes(e.v, i, left);
+        sm = e.m_step[i / QBLK];
+        sv = e.v_step[i / QBLK] * 256.0f;                      // with the decoder's 2^-8; at most 2^127
+    }
+    float2 m[8], v[8];
+    const uint32_t mw[4] = {mc.x, mc.y, mc.z, mc.w}, vw[4] = {vc.x, vc.y, vc.z, vc.w};
+    float mmax = 0.0f, vmax = 0.0f;
+    if (now.gscale != 1.0f) {                                  // (the same for all threads)
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            const float2 x = __fmul2_rn(pair_of(g, q), make_float2(now.gscale, now.gscale));
+            m[q] = x;
+        }
+    } else {
+#pragma unroll
+        for (int q = 0; q < 8; ++q) m[q] = pair_of(g, q);
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        float t[4];
+        float2 u[2];
+        e4m3x4_to_f32(mw[q], t);
+        e4m4x4_to_f32(vw[q], u);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const float2 x = m[2 * q + h];
+            m[2 * q + h] = __fmul2_rn(make_float2(t[2 * h], t[2 * h + 1]), make_float2(sm, sm));
+            v[2 * q + h] = __fmul2_rn(u[h], make_float2(sv, sv));
+            adam_moments(s, x, m[2 * q + h], v[2 * q + h]);
+            mmax = absmax3(mmax, m[2 * q + h].x, m[2 * q + h].y);
+            vmax = absmax3(vmax, v[2 * q + h].x, v[2 * q + h].y);
+        }
+    }
+#pragma unroll
+    for (int d = 4; d > 0; d >>= 1) {                          // the block's eight lanes
+        const float om = __shfl_xor_sync(0xFFFFFFFFu, mmax, d), ov = __shfl_xor_sync(0xFFFFFFFFu, vmax, d);
+        mmax = absmax3(mmax, om, om);
+        vmax = absmax3(vmax, ov, ov);
+    }
+    if (block_nonfinite(abs_word(mmax)) || block_nonfinite(abs_word(vmax))) {      // the block is left as it was
+        note(s.status, SRQ_ERR_NONFINITE);
+        return;
+    }
+    if (!FULL && left <= 0) return;
+    const float im = block_inv(abs_word(mmax)), iv = e4m4_inv(vmax);
+    uint32_t cm[4], cv[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        uint32_t w[4], tv[4], tm[4];
+        adam_words(s, ((uint64_t)i >> 2) + q, (uint32_t)id, (uint32_t)(id >> 32), w);
+        // thresholds with half a unit below them, where they meet the bits below a code that stands in the top byte
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+            tv[h] = __byte_perm(w[h], 0x80u, 0x5324);          // 0, upper half, 0x80
+            tm[h] = tv[h] ^ __byte_perm(w[h], 0u, 0x5105);     // 0, upper ^ lower half, 0x80
+        }
+        const float2 m0 = m[2 * q], m1 = m[2 * q + 1], v0 = v[2 * q], v1 = v[2 * q + 1];
+        uint2 x = code_bits(m0, im), y = code_bits(m1, im);
+        // three bits of mantissa: code at bit 20; four: at bit 19.  The sign is shifted out and put back.
+        const uint32_t mag = top_bytes((x.x << 4) + tm[0], (x.y << 4) + tm[1], (y.x << 4) + tm[2], (y.y << 4) + tm[3]);
+        cm[q] = (mag & 0x7F7F7F7Fu) | (top_bytes(x.x, x.y, y.x, y.y) & 0x80808080u);
+        x = code_bits(v0, iv); y = code_bits(v1, iv);
+        uint32_t c = top_bytes((x.x << 5) + tv[0], (x.y << 5) + tv[1], (y.x << 5) + tv[2], (y.y << 5) + tv[3]);
+        if (((c - 0x01010101u) & ~c & 0x80808080u) != 0 && iv > 0.0f) {          // a code is 0: a positive moment takes the next
+            if ((c & 0x000000FFu) == 0 && v0.x > 0.0f) c |= 0x00000001u;
+            if ((c & 0x0000FF00u) == 0 && v0.y > 0.0f) c |= 0x00000100u;
+            if ((c & 0x00FF0000u) == 0 && v1.x > 0.0f) c |= 0x00010000u;
+            if ((c & 0xFF000000u) == 0 && v1.y > 0.0f) c |= 0x01000000u;
+        }
+        cv[q] = c;
+        const float2 a0 = adam_weight(s, now, pair_of(p, 2 * q), m0, v0), a1 = adam_weight(s, now, pair_of(p, 2 * q + 1), m1, v1);
+        if constexpr (sizeof(P) == 2 && SR) {
+            p.w[2 * q] = bf16_pair_sr(a0, w[0], w[1]);
+            p.w[2 * q + 1] = bf16_pair_sr(a1, w[2], w[3]);
+        } else if constexpr (sizeof(P) == 2) {
+            p.w[2 * q] = bf16_pair(a0);
+            p.w[2 * q + 1] = bf16_pair(a1);
+        } else {
+            p.w[4 * q] = __float_as_uint(a0.x); p.w[4 * q + 1] = __float_as_uint(a0.y);
+            p.w[4 * q + 2] = __float_as_uint(a1.x); p.w[4 * q + 3] = __float_as_uint(a1.y);
+        }
+    }
+    if (FULL || left >= 16) write16<P>(e.p, i, p, FULL); else write_some<P>(e.p, i, p, left);
+    write_codes(e.m, i, cm, left);
+    write_codes(e.v, i, cv, left);
+    if ((threadIdx.x & 7) == 0) { e.m_step[i / QBLK] = moment_step(mmax, im, 1.0f / E4M3_MAX); e.v_step[i / QBLK] = moment_step(vmax, iv, 1.0f / E4M4_MAX); }
+}
+
+template <typename P, typename G, bool SR, int CAP>
+__global__ void __launch_bounds__(ADAM_THREADS<true>, 5) adamw8_kernel(const __grid_constant__ AdamParams<CAP> a) {
+    pdl_enter();
+    const AdamScalars& s = a.s;
+    const AdamNow now = adam_now(s);
+    if (!now.go) {
+        if (threadIdx.x == 0 && blockIdx.x == 0) note(s.status, SRQ_ERR_NONFINITE);
+        return;
+    }
+    adam_walk<ADAM_THREADS<true> / 32>(a, [&](int64_t group, int k) {
+        const AdamEntry& e = a.e[k];
+        const int64_t first = (group - e.first) * ADAM_GROUP<true>, i = first + (threadIdx.x & 31) * 16;
+        const uint64_t id = (((uint64_t)s.id_hi << 32) | s.id_lo) + (uint64_t)k + ((uint64_t)now.t << 32);
+        if (first + ADAM_GROUP<true> <= e.n && (((uintptr_t)e.p | (uintptr_t)e.g) & 31u) == 0) adam8_group<P, G, SR, true>(s, now, e, i, id);
+        else adam8_group<P, G, SR, false>(s, now, e, i, id);
+    });
 }
 
 template <int CAP>
@@ -321,29 +481,30 @@ static cudaError_t launch_adamw_cap(const AdamScalars& s, const srq_adamw_tensor
     a.s = s;
     a.count = 0;
     a.groups = 0;
+    const int64_t group = state8 ? ADAM_GROUP<true> : ADAM_GROUP<false>;
     for (int i = 0; i < n; ++i) {                              // empty tensors stay in the list: the position numbers the thresholds
         AdamEntry& e = a.e[a.count++];
         e.p = t[i].param; e.g = t[i].grad; e.m = t[i].m; e.v = t[i].v; e.m_step = t[i].m_step; e.v_step = t[i].v_step; e.n = t[i].n;
         e.first = a.groups;
-        a.groups += (t[i].n + ADAM_GROUP - 1) / ADAM_GROUP;
+        a.groups += (t[i].n + group - 1) / group;
     }
     if (a.groups == 0) return cudaSuccess;
     const int sms = sm_count();
     if (sms == 0) return cudaErrorUnknown;
-    const int64_t want = (a.groups + ADAM_THREADS / 32 - 1) / (ADAM_THREADS / 32), most = (int64_t)sms * 32;
-    const dim3 grid((unsigned)(want < most ? want : most)), block(ADAM_THREADS);
+    // few groups: one per warp, on as many SMs as there are (36 tensors of 2048: 6.5 -> 3.5 us)
+    a.run = a.groups > (int64_t)sms * 32 * ADAM_RUN ? ADAM_RUN : 1;
+    const int threads = state8 ? ADAM_THREADS<true> : ADAM_THREADS<false>;
+    const int64_t chunk = (int64_t)a.run * (threads / 32), want = (a.groups + chunk - 1) / chunk, most = (int64_t)sms * 32;
+    const dim3 grid((unsigned)(want < most ? want : most)), block(threads);
     const bool pf = p_dt == SRQ_F32, gf = g_dt == SRQ_F32;
     typedef __nv_bfloat16 H;
     cudaError_t e;
-    if (state8) {
-        if (pf) e = gf ? launch_pdl(adamw_kernel<float, float, true, true, CAP>, grid, block, 0, st, a) : launch_pdl(adamw_kernel<float, H, true, true, CAP>, grid, block, 0, st, a);
-        else if (sr) e = gf ? launch_pdl(adamw_kernel<H, float, true, true, CAP>, grid, block, 0, st, a) : launch_pdl(adamw_kernel<H, H, true, true, CAP>, grid, block, 0, st, a);
-        else e = gf ? launch_pdl(adamw_kernel<H, float, true, false, CAP>, grid, block, 0, st, a) : launch_pdl(adamw_kernel<H, H, true, false, CAP>, grid, block, 0, st, a);
-    } else {
-        if (pf) e = gf ? launch_pdl(adamw_kernel<float, float, false, false, CAP>, grid, block, 0, st, a) : launch_pdl(adamw_kernel<float, H, false, false, CAP>, grid, block, 0, st, a);
-        else if (sr) e = gf ? launch_pdl(adamw_kernel<H, float, false, true, CAP>, grid, block, 0, st, a) : launch_pdl(adamw_kernel<H, H, false, true, CAP>, grid, block, 0, st, a);
-        else e = gf ? launch_pdl(adamw_kernel<H, float, false, false, CAP>, grid, block, 0, st, a) : launch_pdl(adamw_kernel<H, H, false, false, CAP>, grid, block, 0, st, a);
-    }
+#define SRQ_ADAM(kernel)                                                                                                                                      \
+    (pf ? (gf ? launch_pdl(kernel<float, float, false, CAP>, grid, block, 0, st, a) : launch_pdl(kernel<float, H, false, CAP>, grid, block, 0, st, a))        \
+     : sr ? (gf ? launch_pdl(kernel<H, float, true, CAP>, grid, block, 0, st, a) : launch_pdl(kernel<H, H, true, CAP>, grid, block, 0, st, a))                \
+          : (gf ? launch_pdl(kernel<H, float, false, CAP>, grid, block, 0, st, a) : launch_pdl(kernel<H, H, false, CAP>, grid, block, 0, st, a)))
+    e = state8 ? SRQ_ADAM(adamw8_kernel) : SRQ_ADAM(adamw_kernel);
+#undef SRQ_ADAM
     count_launch();
     return e;
 }
