@@ -14,7 +14,7 @@ namespace srq {
 // 8-bit states: 96 registers, five CTAs of four warps per SM (256 threads at 80 registers spill, at 128 there are too few warps:
 // 907 and 940 us against 843 for eight layers).
 template <bool STATE8> constexpr int ADAM_THREADS = STATE8 ? 128 : 256;
-constexpr int ADAM_RUN = 4;                     // groups a warp takes before it looks for its tensor again, where there are many
+template <bool STATE8> constexpr int ADAM_RUN = STATE8 ? 16 : 4;   // groups a warp takes in a row, where there are many
 template <bool STATE8> constexpr int ADAM_GROUP = STATE8 ? 512 : 256;      // elements a warp takes at a time
 
 struct AdamEntry {
@@ -159,26 +159,34 @@ __device__ __forceinline__ int adam_find(const AdamParams<CAP>& a, int64_t u) {
     return k;
 }
 
-// What both kernels walk: CTAs take chunks of run * WARPS groups, warp w the groups w, w + WARPS, ... of a chunk.
-template <int WARPS, int CAP, typename F>
-__device__ __forceinline__ void adam_walk(const AdamParams<CAP>& a, F&& body) {
-    const int warp = __shfl_sync(0xFFFFFFFFu, (int)threadIdx.x >> 5, 0);       // so that the compiler knows it to be the same for the warp
-    const int64_t size = (int64_t)a.run * WARPS;
-    for (int64_t chunk = blockIdx.x * size; chunk < a.groups; chunk += gridDim.x * size) {
-        int k = -1;
-        int64_t end = 0;                                       // groups before the tensor after tensor k
-#pragma unroll 1
-        for (int r = 0; r < a.run; ++r) {
-            const int64_t u = chunk + r * WARPS + warp;
-            if (u >= a.groups) break;
-            if (k < 0 || u >= end) {
-                k = adam_find(a, u);
+// What both kernels walk: CTAs take chunks of run * WARPS groups, warp w the groups w, w + WARPS, ... of a chunk.  All of it is the
+// same for the lanes of a warp.
+template <int WARPS, int CAP>
+struct AdamCursor {
+    const AdamParams<CAP>& a;
+    int warp, r = 0, k = -1;
+    int64_t chunk, size, end = 0;                              // end: groups before the tensor after tensor k
+    __device__ __forceinline__ explicit AdamCursor(const AdamParams<CAP>& params) : a(params) {
+        warp = __shfl_sync(0xFFFFFFFFu, (int)threadIdx.x >> 5, 0);
+        size = (int64_t)a.run * WARPS;
+        chunk = blockIdx.x * size;
+    }
+    // The next group and its tensor; false: there is none.
+    __device__ __forceinline__ bool next(int64_t& group, int& tensor) {
+        for (; chunk < a.groups; chunk += gridDim.x * size, r = 0) {
+            group = chunk + r * WARPS + warp;
+            if (r == a.run || group >= a.groups) continue;
+            ++r;
+            if (k < 0 || group >= end) {
+                k = adam_find(a, group);
                 end = k + 1 < a.count ? a.e[k + 1].first : a.groups;
             }
-            body(u, k);
+            tensor = k;
+            return true;
         }
+        return false;
     }
-}
+};
 
 // P, G: types of weights and gradients.  SR: bfloat16 weights are rounded stochastically.
 template <typename P, typename G, bool SR, int CAP>
@@ -191,11 +199,14 @@ __global__ void __launch_bounds__(ADAM_THREADS<false>) adamw_kernel(const __grid
         if (threadIdx.x == 0 && blockIdx.x == 0) note(s.status, SRQ_ERR_NONFINITE);
         return;
     }
-    adam_walk<ADAM_THREADS<false> / 32>(a, [&](int64_t group, int k) {
+    AdamCursor<ADAM_THREADS<false> / 32, CAP> at(a);
+    int64_t group;
+    int k;
+    while (at.next(group, k)) {
         const AdamEntry& e = a.e[k];
         const int64_t i = (group - e.first) * ADAM_GROUP<false> + (threadIdx.x & 31) * 8;
         const int64_t left = e.n - i;                          // elements of this lane: min(left, 8), none or less: none
-        if (left <= 0) return;
+        if (left <= 0) continue;
         float2 p[4], g[4], m[4], v[4];
         if (left >= 8) {
             read8<G>(e.g, i, g);
@@ -254,29 +265,11 @@ __global__ void __launch_bounds__(ADAM_THREADS<false>) adamw_kernel(const __grid
                 reinterpret_cast<float*>(e.v)[i + q] = q & 1 ? v[q >> 1].y : v[q >> 1].x;
             }
         }
-    });
+    }
 }
 
 // Sixteen elements of type T as they lie in memory: 8 words (bfloat16) or 16 (binary32).  wide: 32-byte aligned.
 template <typename T> struct Raw16 { uint32_t w[4 * sizeof(T)]; };
-template <typename T>
-__device__ __forceinline__ Raw16<T> read16(const void* base, int64_t i, bool wide) {
-    Raw16<T> r;
-    const char* p = reinterpret_cast<const char*>(base) + i * (int64_t)sizeof(T);
-#pragma unroll
-    for (int h = 0; h < (int)sizeof(T) / 2; ++h) {
-        if (wide) {
-            const Word8 x = load32(p + 32 * h);
-#pragma unroll
-            for (int q = 0; q < 8; ++q) r.w[8 * h + q] = x.w[q];
-        } else {
-            const uint4 x = *reinterpret_cast<const uint4*>(p + 32 * h), y = *reinterpret_cast<const uint4*>(p + 32 * h + 16);
-            r.w[8 * h] = x.x; r.w[8 * h + 1] = x.y; r.w[8 * h + 2] = x.z; r.w[8 * h + 3] = x.w;
-            r.w[8 * h + 4] = y.x; r.w[8 * h + 5] = y.y; r.w[8 * h + 6] = y.z; r.w[8 * h + 7] = y.w;
-        }
-    }
-    return r;
-}
 template <typename T>
 __device__ __forceinline__ void write16(void* base, int64_t i, const Raw16<T>& r, bool wide) {
     char* p = reinterpret_cast<char*>(base) + i * (int64_t)sizeof(T);
@@ -356,22 +349,56 @@ __device__ __forceinline__ uint2 code_bits(float2 x, float inv) {
     return make_uint2(__float_as_uint(t.x), __float_as_uint(t.y));
 }
 
-// One group of 512 elements of tensor e, sixteen per lane.  FULL: all of them are there and 32-byte aligned.
+// What a lane has of a whole group on its way through shared memory, in pieces of 16 bytes: weights, gradients, codes.  Piece j of
+// lane l lies at [j][l], so that neighbouring lanes' pieces are neighbours.  A lane reads only what it has copied itself.
+template <typename P, typename G>
+struct Staged {
+    static constexpr int PP = sizeof(P), GP = sizeof(G), PIECES = PP + GP + 2;      // sixteen elements of n bytes: n pieces
+    uint4 piece[PIECES][32];
+};
+__device__ __forceinline__ void copy16(uint4* dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src) : "memory");
+}
+template <typename P, typename G>
+__device__ __forceinline__ void stage(Staged<P, G>& b, const AdamEntry& e, int64_t i, int lane) {
+    typedef Staged<P, G> S;
+    const char* p = reinterpret_cast<const char*>(e.p) + i * (int64_t)sizeof(P);
+    const char* g = reinterpret_cast<const char*>(e.g) + i * (int64_t)sizeof(G);
+#pragma unroll
+    for (int j = 0; j < S::PP; ++j) copy16(&b.piece[j][lane], p + 16 * j);
+#pragma unroll
+    for (int j = 0; j < S::GP; ++j) copy16(&b.piece[S::PP + j][lane], g + 16 * j);
+    copy16(&b.piece[S::PP + S::GP][lane], reinterpret_cast<const char*>(e.m) + i);
+    copy16(&b.piece[S::PP + S::GP + 1][lane], reinterpret_cast<const char*>(e.v) + i);
+}
+
+// One group of 512 elements of tensor e, sixteen per lane, with the step sizes sm and sv.  FULL: all of them are there, and staged.
 template <typename P, typename G, bool SR, bool FULL>
-__device__ __forceinline__ void adam8_group(const AdamScalars& s, const AdamNow& now, const AdamEntry& e, int64_t i, uint64_t id) {
+__device__ __forceinline__ void adam8_group(const AdamScalars& s, const AdamNow& now, const AdamEntry& e, int64_t i, uint64_t id, float sm, float sv,
+                                            const Staged<P, G>* b) {
+    typedef Staged<P, G> S;
+    const int lane = threadIdx.x & 31;
     const int64_t left = FULL ? 16 : e.n - i;                  // elements of this lane: min(left, 16), none or less: none
     Raw16<P> p;
     Raw16<G> g;
     uint4 mc = make_uint4(0, 0, 0, 0), vc = make_uint4(0, 0, 0, 0);
-    float sm = 0.0f, sv = 0.0f;
-    if (FULL || left >= 16) { g = read16<G>(e.g, i, FULL); p = read16<P>(e.p, i, FULL); }
-    else { g = read_some<G>(e.g, i, left); p = read_some<P>(e.p, i, left); }
-    if (FULL || left > 0) {
-        mc = read_codes(e.m, i, left);
-        vc = read_codes(e.v, i, left);
-        sm = e.m_step[i / QBLK];
-        sv = e.v_step[i / QBLK] * 256.0f;                      // with the decoder's 2^-8; at most 2^127
+    if constexpr (FULL) {
+#pragma unroll
+        for (int j = 0; j < S::GP; ++j) {
+            const uint4 x = b->piece[S::PP + j][lane];
+            g.w[4 * j] = x.x; g.w[4 * j + 1] = x.y; g.w[4 * j + 2] = x.z; g.w[4 * j + 3] = x.w;
+        }
+        mc = b->piece[S::PP + S::GP][lane];
+        vc = b->piece[S::PP + S::GP + 1][lane];
+    } else {
+        g = read_some<G>(e.g, i, left);
+        p = read_some<P>(e.p, i, left);
+        if (left > 0) {
+            mc = read_codes(e.m, i, left);
+            vc = read_codes(e.v, i, left);
+        }
     }
+    sv *= 256.0f;                                              // with the decoder's 2^-8; at most 2^127
     float2 m[8], v[8];
     const uint32_t mw[4] = {mc.x, mc.y, mc.z, mc.w}, vw[4] = {vc.x, vc.y, vc.z, vc.w};
     float mmax = 0.0f, vmax = 0.0f;
@@ -416,6 +443,13 @@ __device__ __forceinline__ void adam8_group(const AdamScalars& s, const AdamNow&
     uint32_t cm[4], cv[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
+        if constexpr (FULL) {                                  // the weights leave shared memory when they are due
+            if (sizeof(P) == 4 || (q & 1) == 0) {
+                constexpr int words = sizeof(P) == 4 ? 4 : 2;
+                const uint4 x = b->piece[q * words / 4][lane];
+                p.w[q * words] = x.x; p.w[q * words + 1] = x.y; p.w[q * words + 2] = x.z; p.w[q * words + 3] = x.w;
+            }
+        }
         uint32_t w[4], tv[4], tm[4];
         adam_words(s, ((uint64_t)i >> 2) + q, (uint32_t)id, (uint32_t)(id >> 32), w);
         // thresholds with half a unit below them, where they meet the bits below a code that stands in the top byte
@@ -450,7 +484,7 @@ __device__ __forceinline__ void adam8_group(const AdamScalars& s, const AdamNow&
             p.w[4 * q + 2] = __float_as_uint(a1.x); p.w[4 * q + 3] = __float_as_uint(a1.y);
         }
     }
-    if (FULL || left >= 16) write16<P>(e.p, i, p, FULL); else write_some<P>(e.p, i, p, left);
+    if (FULL) write16<P>(e.p, i, p, ((uintptr_t)e.p & 31u) == 0); else write_some<P>(e.p, i, p, left);
     write_codes(e.m, i, cm, left);
     write_codes(e.v, i, cv, left);
     if ((threadIdx.x & 7) == 0) { e.m_step[i / QBLK] = moment_step(mmax, im, 1.0f / E4M3_MAX); e.v_step[i / QBLK] = moment_step(vmax, iv, 1.0f / E4M4_MAX); }
@@ -459,19 +493,56 @@ __device__ __forceinline__ void adam8_group(const AdamScalars& s, const AdamNow&
 template <typename P, typename G, bool SR, int CAP>
 __global__ void __launch_bounds__(ADAM_THREADS<true>, 5) adamw8_kernel(const __grid_constant__ AdamParams<CAP> a) {
     pdl_enter();
+    constexpr int WARPS = ADAM_THREADS<true> / 32, GROUP = ADAM_GROUP<true>;
+    __shared__ Staged<P, G> buffers[WARPS][2];
     const AdamScalars& s = a.s;
     const AdamNow now = adam_now(s);
     if (!now.go) {
         if (threadIdx.x == 0 && blockIdx.x == 0) note(s.status, SRQ_ERR_NONFINITE);
         return;
     }
-    adam_walk<ADAM_THREADS<true> / 32>(a, [&](int64_t group, int k) {
-        const AdamEntry& e = a.e[k];
-        const int64_t first = (group - e.first) * ADAM_GROUP<true>, i = first + (threadIdx.x & 31) * 16;
-        const uint64_t id = (((uint64_t)s.id_hi << 32) | s.id_lo) + (uint64_t)k + ((uint64_t)now.t << 32);
-        if (first + ADAM_GROUP<true> <= e.n && (((uintptr_t)e.p | (uintptr_t)e.g) & 31u) == 0) adam8_group<P, G, SR, true>(s, now, e, i, id);
-        else adam8_group<P, G, SR, false>(s, now, e, i, id);
-    });
+    const int lane = threadIdx.x & 31, warp = __shfl_sync(0xFFFFFFFFu, (int)threadIdx.x >> 5, 0);
+    Staged<P, G>* b = buffers[warp];
+    const int64_t size = (int64_t)a.run * WARPS;
+    for (int64_t chunk = blockIdx.x * size; chunk < a.groups; chunk += gridDim.x * size) {
+        const int64_t chunk_end = chunk + size < a.groups ? chunk + size : a.groups;
+        // the chunk's groups, tensor by tensor: whole groups, the next one's bytes on their way while one is worked on, then the rest
+        for (int64_t u = chunk; u < chunk_end;) {
+            const int k = adam_find(a, u);
+            const AdamEntry& e = a.e[k];
+            const int64_t tensor_end = k + 1 < a.count ? a.e[k + 1].first : a.groups, end = tensor_end < chunk_end ? tensor_end : chunk_end;
+            const int64_t whole = e.first + e.n / GROUP, whole_end = whole < end ? whole : end;
+            const int mine = (int)(whole_end - u) - warp, turns = mine > 0 ? (mine + WARPS - 1) / WARPS : 0;
+            const uint64_t id = (((uint64_t)s.id_hi << 32) | s.id_lo) + (uint64_t)k + ((uint64_t)now.t << 32);
+            int64_t i = (u + warp - e.first) * GROUP + lane * 16;
+            float sm = 0.0f, sv = 0.0f, next_sm = 0.0f, next_sv = 0.0f;
+            if (turns > 0) {
+                stage<P, G>(b[0], e, i, lane);
+                sm = e.m_step[i / QBLK];
+                sv = e.v_step[i / QBLK];
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+#pragma unroll 1
+            for (int t = 0; t < turns; ++t) {
+                if (t + 1 < turns) {
+                    const int64_t n = i + WARPS * GROUP;
+                    stage<P, G>(b[(t + 1) & 1], e, n, lane);
+                    next_sm = e.m_step[n / QBLK];
+                    next_sv = e.v_step[n / QBLK];
+                }
+                asm volatile("cp.async.commit_group;\ncp.async.wait_group 1;" ::: "memory");
+                adam8_group<P, G, SR, true>(s, now, e, i, id, sm, sv, &b[t & 1]);
+                i += WARPS * GROUP;
+                sm = next_sm; sv = next_sv;
+            }
+            if (whole_end < end && (int)(whole_end - u) % WARPS == warp) {     // the tensor's last group
+                i = (whole_end - e.first) * GROUP + lane * 16;
+                if (i < e.n) { sm = e.m_step[i / QBLK]; sv = e.v_step[i / QBLK]; }
+                adam8_group<P, G, SR, false>(s, now, e, i, id, sm, sv, nullptr);
+            }
+            u = end;
+        }
+    }
 }
 
 template <int CAP>
@@ -492,8 +563,9 @@ static cudaError_t launch_adamw_cap(const AdamScalars& s, const srq_adamw_tensor
     const int sms = sm_count();
     if (sms == 0) return cudaErrorUnknown;
     // few groups: one per warp, on as many SMs as there are (36 tensors of 2048: 6.5 -> 3.5 us)
-    a.run = a.groups > (int64_t)sms * 32 * ADAM_RUN ? ADAM_RUN : 1;
     const int threads = state8 ? ADAM_THREADS<true> : ADAM_THREADS<false>;
+    const int64_t warps = (int64_t)sms * (state8 ? 20 : 32);   // that run at a time
+    a.run = a.groups >= 4 * warps * ADAM_RUN<true> && state8 ? ADAM_RUN<true> : a.groups > warps * ADAM_RUN<false> ? ADAM_RUN<false> : 1;
     const int64_t chunk = (int64_t)a.run * (threads / 32), want = (a.groups + chunk - 1) / chunk, most = (int64_t)sms * 32;
     const dim3 grid((unsigned)(want < most ? want : most)), block(threads);
     const bool pf = p_dt == SRQ_F32, gf = g_dt == SRQ_F32;
