@@ -1,26 +1,31 @@
 // Losses on the logits: log-probabilities of the targets, the clipped policy loss and the preference loss, and their gradients.
 //
-// One kernel walks the rows.  A row belongs to one CTA, or to a cluster of up to eight where rows are few.  First walk: running
-// maximum m and sum s of e^(z - m) in every thread, joined over the CTA and, through distributed shared memory, over the
-// cluster.  Then every thread knows logp, and with it the row's gradient at logp (policy), so that the second walk writes the
-// logits' gradient at once; the row is re-read from L2, where the first walk has just brought it, so that HBM sees every logit
-// once and its gradient once.  The preference loss needs the log-probabilities of whole answers before its first gradient,
-// so there the two walks are two launches with a small kernel over the pairs between them.
+// One kernel walks the rows.  A row belongs to one CTA, or to a cluster of up to eight that shares it.  Every thread copies its
+// vectors of the row into shared memory, several groups ahead of the one it works on (cp.async; a thread reads only what it has copied
+// itself, so that nothing but its own copies is waited for).  First walk: running maximum and sum of the exponentials, joined
+// over the CTA and, through distributed shared memory, over the cluster.  Then every thread knows logp, and with it the row's gradient at logp
+// (policy), so that the second walk writes the logits' gradient at once, from shared memory where the row's share fits there (up to 64 KB
+// per CTA, 512 KB per row), else by copying it once more, mostly out of L2: HBM sees every logit once and its gradient once.  The
+// preference loss needs the log-probabilities of whole answers before its first gradient, so there the two walks are two
+// launches with a small kernel over the pairs between them.
 //
-// Exponentials: e^((x - m) / T) = 2^((x - m) log2(e) / T), the difference first (exact for neighbours, so that large logits cost no
-// precision), by the hardware's approximation (2 units); sums in binary32 per thread, at most 16384 terms of 32 partial sums.
+// Exponentials: e^((x - m) / T) = 2^((x - m) k) with k = log2(e) / T, the difference first, so that large logits cost no precision
+// and the range is binary32's.  k is a sum of two numbers where probabilities are added up (one alone would shift every log-probability
+// of a row the same way, which shows in sums over rows).  2^y is the hardware's approximation (2 units); sums are binary32, of at
+// most 16384 terms in 64 partial sums per warp.
+#include <math.h>
+
 #include "train.cuh"
 
 namespace srq {
 
 enum RowMode { ROW_LOGP = 0, ROW_GRAD = 1, ROW_POLICY = 2 };
-constexpr float LOG2E = 1.4426950408889634f;
 #define SRQ_INF __int_as_float(0x7F800000)
 
 struct RowParams {
     const void* x; int64_t rows, classes, ld;
     const void* targets; int32_t wide;
-    float k, inv_t, t;                          // log2(e) / T, 1 / T, T
+    float k, k_low, inv_t, t;                   // log2(e) / T and what it lacks, 1 / T, T
     int32_t parts;                              // CTAs per row
     uint32_t* status;
     float* logp; float* lse;
@@ -38,13 +43,18 @@ template <typename T>
 struct RowSpan {
     static constexpr int N = 16 / (int)sizeof(T);
     const T* first;                             // aligned address of vector 0
-    int skip;                                   // elements of vector 0 before the row
-    int64_t vectors;
-    __device__ __forceinline__ RowSpan(const T* row, int64_t n) {
+    int skip, n;                                // elements of vector 0 before the row, classes
+    int vectors, lo, hi;                        // vectors; those that lie wholly inside: lo .. hi - 1
+    __device__ __forceinline__ RowSpan(const T* row, int64_t classes) {
+        n = (int)classes;
         skip = (int)(((uintptr_t)row & 15u) / sizeof(T));
         first = row - skip;
-        vectors = (n + skip + N - 1) / N;
+        vectors = (int)((classes + skip + N - 1) / N);
+        lo = skip ? 1 : 0;
+        hi = (int)((classes + skip) / N);
     }
+    __device__ __forceinline__ bool inside(int j) const { return j >= lo && j < hi; }
+    __device__ __forceinline__ int64_t element(int j) const { return (int64_t)j * N - skip; }      // class of vector j's first element
 };
 
 template <typename T>
@@ -56,34 +66,111 @@ __device__ __forceinline__ void unpack(const uint4& w, float v[16 / sizeof(T)]) 
         v[4] = bf16_lo(w.z); v[5] = bf16_hi(w.z); v[6] = bf16_lo(w.w); v[7] = bf16_hi(w.w);
     }
 }
-// Vector j of a row of n elements; what lies outside the row reads as minus infinity.
+// Copies vector j of a row to dst; what lies outside the row becomes minus infinity.
 template <typename T>
-__device__ __forceinline__ void load_vec(const RowSpan<T>& r, int64_t j, int64_t n, float* v) {
+__device__ __forceinline__ void copy_vec(const RowSpan<T>& r, int j, uint4* dst) {
     constexpr int N = RowSpan<T>::N;
-    const int64_t c = j * N - r.skip;           // class of the vector's first element
-    if (c >= 0 && c + N <= n) {
-        unpack<T>(*reinterpret_cast<const uint4*>(r.first + j * N), v);
+    const T* src = r.first + (int64_t)j * N;
+    if (r.inside(j)) {
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src) : "memory");
     } else {
+        const int64_t c = r.element(j);
+        T* d = reinterpret_cast<T*>(dst);
 #pragma unroll
-        for (int e = 0; e < N; ++e) v[e] = c + e >= 0 && c + e < n ? (float)r.first[j * N + e] : -SRQ_INF;
+        for (int e = 0; e < N; ++e) d[e] = c + e >= 0 && c + e < r.n ? src[e] : (T)-SRQ_INF;
     }
 }
 
-// (m, s) of two sets joined: s counts in units of e^m.
-__device__ __forceinline__ float2 join(float2 a, float2 b, float k) {
-    const float m = fmaxf(a.x, b.x), r = m == -SRQ_INF ? 0.0f : m;
-    return make_float2(m, a.y * exp2_fast((a.x - r) * k) + b.y * exp2_fast((b.x - r) * k));
+// 2^(d k) of two differences.
+__device__ __forceinline__ float2 powers(float2 d, float2 k, float2 k_low) {
+    const float2 t = __ffma2_rn(d, k_low, __fmul2_rn(d, k));
+    return make_float2(exp2_fast(t.x), exp2_fast(t.y));
+}
+// The cluster's barrier without an order of memory: whoever has written for others fences first.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
+// A thread's vectors j0 + tid, j0 + tid + threads, ... of a row, by way of shared memory: the thread's i-th in its slot i % ROW_SLOTS (as many slots as
+// it has vectors, if these are fewer).  ROW_GROUP vectors are copied and waited for together, ROW_AHEAD groups ahead.
+constexpr int ROW_THREADS = 256, ROW_GROUP = 4, ROW_AHEAD = 4, ROW_SLOTS = ROW_GROUP * ROW_AHEAD;
+template <typename T>
+struct RowStream {
+    const RowSpan<T>& span;
+    int first, step, count;                     // the thread's first vector, the distance to its next, how many
+    uint4* buffer;                              // the thread's first slot
+    __device__ __forceinline__ int vector(int i) const { return first + i * step; }
+    __device__ __forceinline__ uint4* slot(int i) const { return buffer + (i & (ROW_SLOTS - 1)) * step; }
+    // whether vectors i .. i + ROW_GROUP - 1 are there and lie wholly inside the row
+    __device__ __forceinline__ bool plain(int i) const {
+        return i + ROW_GROUP <= count && vector(i) >= span.lo && vector(i + ROW_GROUP - 1) < span.hi;
+    }
+    __device__ __forceinline__ void copy_group(int i) const {          // vectors i .. i + ROW_GROUP - 1, as far as there are such; closes the group
+        if (plain(i)) {
+            const T* src = span.first + (int64_t)vector(i) * RowSpan<T>::N;
+            const uint32_t dst = (uint32_t)__cvta_generic_to_shared(slot(i));
+#pragma unroll
+            for (int u = 0; u < ROW_GROUP; ++u)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + u * step * 16), "l"(src + (int64_t)u * step * RowSpan<T>::N) : "memory");
+        } else {
+#pragma unroll 1
+            for (int u = 0; u < ROW_GROUP; ++u)
+                if (i + u < count) copy_vec<T>(span, vector(i + u), slot(i + u));
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    __device__ __forceinline__ bool resident() const { return count <= ROW_SLOTS; }
+    // body(i): vectors i .. i + ROW_GROUP - 1 are in their slots.  copy: they have to be brought there.
+    template <typename F>
+    __device__ __forceinline__ void walk(bool copy, F&& body) const {
+        if (copy) {
+#pragma unroll
+            for (int g = 0; g < ROW_AHEAD; ++g) copy_group(g * ROW_GROUP);
+        }
+#pragma unroll 1
+        for (int i = 0; i < count; i += ROW_GROUP) {
+            if (copy) asm volatile("cp.async.wait_group %0;" ::"n"(ROW_AHEAD - 1) : "memory");
+            body(i);
+            if (copy) copy_group(i + ROW_SLOTS);
+        }
+    }
+};
+
+// One vector's gradient: f 2^((x - m) k).
+template <typename T>
+__device__ __forceinline__ void gradient(const uint4& raw, float m, float2 k2, float2 low2, float f, float w[16 / sizeof(T)]) {
+    unpack<T>(raw, w);
+#pragma unroll
+    for (int e = 0; e < 16 / (int)sizeof(T); e += 2) {
+        const float2 d = __fadd2_rn(make_float2(w[e], w[e + 1]), make_float2(-m, -m));
+        const float2 z = sizeof(T) == 4 ? __ffma2_rn(d, low2, __fmul2_rn(d, k2)) : __fmul2_rn(d, k2);   // (k_low: lost in a bfloat16 result's rounding)
+        const float2 p = __fmul2_rn(make_float2(exp2_fast(z.x), exp2_fast(z.y)), make_float2(f, f));
+        w[e] = p.x; w[e + 1] = p.y;
+    }
+}
+template <typename T>
+__device__ __forceinline__ uint4 pack(const float w[16 / sizeof(T)]) {
+    if constexpr (sizeof(T) == 4) return make_uint4(__float_as_uint(w[0]), __float_as_uint(w[1]), __float_as_uint(w[2]), __float_as_uint(w[3]));
+    else {
+        uint32_t q[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const __nv_bfloat162 b = __floats2bfloat162_rn(w[2 * e], w[2 * e + 1]);
+            q[e] = *reinterpret_cast<const uint32_t*>(&b);
+        }
+        return make_uint4(q[0], q[1], q[2], q[3]);
+    }
 }
 
-__device__ __forceinline__ void cluster_sync() {
-    asm volatile("barrier.cluster.arrive.aligned;\nbarrier.cluster.wait.aligned;" ::: "memory");
-}
+// What the second walk needs of a row: the maximum, 1 / sum, the gradient at logp.
+struct RowResult { float m, inv, c; };
 
 template <typename T, int MODE>
-__global__ void __launch_bounds__(512) row_kernel(const RowParams P) {
+__global__ void __launch_bounds__(ROW_THREADS) row_kernel(const RowParams P) {
     pdl_enter();
-    constexpr int N = RowSpan<T>::N, U = 32 / N;               // vectors in flight per thread and turn
-    __shared__ float2 part[17];
+    constexpr int N = RowSpan<T>::N;
+    extern __shared__ uint4 staged[];
+    __shared__ float2 part[ROW_THREADS / 32], mine;
+    __shared__ RowResult shared_result;
     const int64_t row = blockIdx.x / P.parts;
     const int rank = (int)(blockIdx.x - row * P.parts), tid = threadIdx.x, nt = blockDim.x;
     if (P.offsets) {
@@ -92,149 +179,176 @@ __global__ void __launch_bounds__(512) row_kernel(const RowParams P) {
     const int64_t target = whole_at(P.targets, P.wide, row);
     bool counts = target >= 0 && target < P.classes;
     if (target >= P.classes && tid == 0 && rank == 0) note(P.status, SRQ_ERR_INVALID_ARG);
-    float weight = 1.0f, old = 0.0f, adv = 0.0f, ref = 0.0f, c = 0.0f;
+    float weight = 1.0f;
     if constexpr (MODE == ROW_POLICY) {
         weight = P.weight[row];
         counts = counts && weight != 0.0f;
-        if (counts) { old = P.old[row]; adv = P.advantage[row]; if (P.ref) ref = P.ref[row]; }
     }
     const T* x = reinterpret_cast<const T*>(P.x) + row * P.ld;
     const RowSpan<T> span(x, P.classes);
-    const int64_t share = (span.vectors + P.parts - 1) / P.parts, j0 = rank * share, j1 = j0 + share < span.vectors ? j0 + share : span.vectors;
-    float m = -SRQ_INF, inv = 0.0f;
+    const int share = (span.vectors + P.parts - 1) / P.parts, j0 = rank * share, j1 = j0 + share < span.vectors ? j0 + share : span.vectors;
+    const RowStream<T> stream = {span, j0 + tid, nt, j0 + tid < j1 ? (j1 - j0 - tid + nt - 1) / nt : 0, staged + tid};
+    const float2 k2 = make_float2(P.k, P.k), low2 = make_float2(P.k_low, P.k_low);
+    RowResult r = {0.0f, 0.0f, 0.0f};
     if constexpr (MODE == ROW_GRAD) {
-        c = counts ? P.dlogp[row] : 0.0f;
-        if (c != 0.0f) {
-            if (P.stat) { const float2 q = P.stat[row]; m = q.x; inv = q.y; }
-            else { m = P.lse[row] * P.t; inv = 1.0f; }
+        r.c = counts ? P.dlogp[row] : 0.0f;
+        if (r.c != 0.0f) {
+            if (P.stat) { const float2 q = P.stat[row]; r.m = q.x; r.inv = q.y; }
+            else { r.m = P.lse[row] * P.t; r.inv = 1.0f; }
         }
     } else {
-        const float xt = counts ? (float)x[target] : 0.0f;
-        float2 all = make_float2(0.0f, 1.0f);
+        // what the row's first warp will need, requested before the walk
+        float xt = 0.0f, old = 0.0f, adv = 0.0f, ref = 0.0f;
+        if (counts && tid < 32) {
+            xt = (float)x[target];
+            if constexpr (MODE == ROW_POLICY) { old = P.old[row]; adv = P.advantage[row]; if (P.ref) ref = P.ref[row]; }
+        }
+        float m = -SRQ_INF;
+        float2 sum = make_float2(0.0f, 0.0f);
         if (counts) {
-            float s0 = 0.0f, s1 = 0.0f;
-            for (int64_t j = j0 + tid; j < j1; j += (int64_t)nt * U) {
-                float v[U * N];
+            stream.walk(true, [&](int i) {
+                float v[ROW_GROUP * N];
+                if (i + ROW_GROUP <= stream.count) {
+                    const uint4* q = stream.slot(i);
 #pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    if (j + (int64_t)u * nt < j1) load_vec<T>(span, j + (int64_t)u * nt, P.classes, v + u * N);
-                    else
+                    for (int u = 0; u < ROW_GROUP; ++u) unpack<T>(q[u * nt], v + u * N);
+                } else {
 #pragma unroll
-                        for (int e = 0; e < N; ++e) v[u * N + e] = -SRQ_INF;
+                    for (int u = 0; u < ROW_GROUP; ++u) {
+                        if (i + u < stream.count) unpack<T>(*stream.slot(i + u), v + u * N);
+                        else
+#pragma unroll
+                            for (int e = 0; e < N; ++e) v[u * N + e] = -SRQ_INF;
+                    }
                 }
                 float top = m;
 #pragma unroll
-                for (int e = 0; e < U * N; ++e) top = fmaxf(top, v[e]);
-                const float r = top == -SRQ_INF ? 0.0f : top, f = exp2_fast((m - r) * P.k);
-                s0 *= f; s1 *= f; m = top;
+                for (int e = 0; e < ROW_GROUP * N; ++e) top = fmaxf(top, v[e]);
+                const float to = top == -SRQ_INF ? 0.0f : top, f = exp2_fast((m - to) * P.k);
+                sum = __fmul2_rn(sum, make_float2(f, f));
+                m = top;
 #pragma unroll
-                for (int e = 0; e < U * N; e += 2) {
-                    const float2 d = __fmul2_rn(__fadd2_rn(make_float2(v[e], v[e + 1]), make_float2(-r, -r)), make_float2(P.k, P.k));
-                    s0 += exp2_fast(d.x); s1 += exp2_fast(d.y);
-                }
+                for (int e = 0; e < ROW_GROUP * N; e += 2)
+                    sum = __fadd2_rn(sum, powers(__fadd2_rn(make_float2(v[e], v[e + 1]), make_float2(-to, -to)), k2, low2));
+            });
+        }
+        // (m, s) of the warp, the CTA and the cluster: the largest m first, then the sums in its units
+        float s = sum.x + sum.y;
+        const auto reduce = [&](int lanes) {
+            float top = m;
+            for (int d = lanes / 2; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+            s *= exp2_fast((m - (top == -SRQ_INF ? 0.0f : top)) * P.k);
+            m = top;
+            for (int d = lanes / 2; d > 0; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
+        };
+        reduce(32);
+        if (nt > 32) {
+            if ((tid & 31) == 0) part[tid >> 5] = make_float2(m, s);
+            __syncthreads();
+            if (tid < 32) {
+                const float2 o = tid < nt / 32 ? part[tid] : make_float2(-SRQ_INF, 0.0f);
+                m = o.x; s = o.y;
+                reduce(ROW_THREADS / 32);
             }
-            all = make_float2(m, s0 + s1);
         }
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) {
-            const float2 o = make_float2(__shfl_xor_sync(0xFFFFFFFFu, all.x, d), __shfl_xor_sync(0xFFFFFFFFu, all.y, d));
-            all = join(all, o, P.k);
-        }
-        if ((tid & 31) == 0) part[tid >> 5] = all;
-        __syncthreads();
-        all = part[0];
-        for (int w = 1; w < nt / 32; ++w) all = join(all, part[w], P.k);
         if (P.parts > 1) {
-            if (tid == 0) part[16] = all;
-            cluster_sync();
-            float2 sum = make_float2(-SRQ_INF, 0.0f);
-            for (int q = 0; q < P.parts; ++q) {
-                float2 o;
-                asm volatile("{\n.reg .u32 a;\nmapa.shared::cluster.u32 a, %2, %3;\nld.shared::cluster.v2.f32 {%0, %1}, [a];\n}"
-                             : "=f"(o.x), "=f"(o.y) : "r"((uint32_t)__cvta_generic_to_shared(&part[16])), "r"(q) : "memory");
-                sum = join(sum, o, P.k);
+            if (tid == 0) {
+                mine = make_float2(m, s);
+                asm volatile("fence.acq_rel.cluster;" ::: "memory");
             }
-            all = sum;
-            cluster_sync();                                    // nobody leaves while its sums are being read
+            cluster_arrive();
+            cluster_wait();
+            if (tid < 32) {
+                m = -SRQ_INF; s = 0.0f;
+                if (tid < P.parts)
+                    asm volatile("{\n.reg .u32 a;\nmapa.shared::cluster.u32 a, %2, %3;\nld.shared::cluster.v2.f32 {%0, %1}, [a];\n}"
+                                 : "=f"(m), "=f"(s) : "r"((uint32_t)__cvta_generic_to_shared(&mine)), "r"(tid) : "memory");
+                reduce(8);
+            }
         }
-        m = all.x; inv = 1.0f / all.y;
-        const float log_s = logf(all.y), logp = counts ? (xt - m) * P.inv_t - log_s : 0.0f;
-        float loss = 0.0f;
-        if constexpr (MODE == ROW_POLICY) {
-            if (counts) {
-                const float rho = expf(logp - old), a = rho * adv, b = fminf(fmaxf(rho, P.clip_lo), P.clip_hi) * adv;
-                loss = a <= b ? -a : -b;
-                c = a <= b ? -a : 0.0f;
-                if (a != a) loss = c = a;                      // NaN stays NaN
-                if (P.ref) {
-                    const float d = ref - logp, g = expm1f(d);
-                    loss += P.kl * (g - d);
-                    c -= P.kl * g;
+        if (tid < 32) {                                        // (lanes 0 .. 7 hold the sums)
+            r.m = m; r.inv = 1.0f / s;
+            const float log_s = logf(s), logp = counts ? (xt - m) * P.inv_t - log_s : 0.0f;
+            float loss = 0.0f;
+            if constexpr (MODE == ROW_POLICY) {
+                if (counts) {
+                    const float rho = expf(logp - old), a = rho * adv, b = fminf(fmaxf(rho, P.clip_lo), P.clip_hi) * adv;
+                    loss = a <= b ? -a : -b;
+                    r.c = a <= b ? -a : 0.0f;
+                    if (a != a) loss = r.c = a;                // NaN stays NaN
+                    if (P.ref) {
+                        const float d = ref - logp, g = expm1f(d);
+                        loss += P.kl * (g - d);
+                        r.c -= P.kl * g;
+                    }
+                    loss *= weight; r.c *= weight;
                 }
-                loss *= weight; c *= weight;
+            }
+            if (tid == 0) {
+                shared_result = r;
+                if (rank == 0) {
+                    if (P.logp) P.logp[row] = logp;
+                    if (P.lse) P.lse[row] = counts ? m * P.inv_t + log_s : 0.0f;
+                    if (P.stat) P.stat[row] = make_float2(m, r.inv);
+                    if constexpr (MODE == ROW_POLICY) if (P.row_loss) P.row_loss[row] = loss;
+                    if (abs_word(logp) >= 0x7F800000u || abs_word(r.c) >= 0x7F800000u) note(P.status, SRQ_ERR_NONFINITE);
+                }
             }
         }
-        if (tid == 0 && rank == 0) {
-            if (P.logp) P.logp[row] = logp;
-            if (P.lse) P.lse[row] = counts ? m * P.inv_t + log_s : 0.0f;
-            if (P.stat) P.stat[row] = make_float2(m, inv);
-            if constexpr (MODE == ROW_POLICY) if (P.row_loss) P.row_loss[row] = loss;
-            if (abs_word(logp) >= 0x7F800000u || abs_word(c) >= 0x7F800000u) note(P.status, SRQ_ERR_NONFINITE);
-        }
+        __syncthreads();
+        if (P.parts > 1) cluster_arrive();                     // no CTA leaves while its sums are being read: the wait is at the end
+        r = shared_result;
     }
     if constexpr (MODE != ROW_LOGP) {
-        if (!P.dx) return;
-        T* y = reinterpret_cast<T*>(P.dx) + row * P.ldx;
-        c *= P.inv_t;
-        const float f = -c * inv;
-        const bool same = (((uintptr_t)y ^ (uintptr_t)x) & 15u) == 0;
-        T* y0 = y - span.skip;                                 // where vector 0 would begin
-        for (int64_t j = j0 + tid; j < j1; j += (int64_t)nt * U) {
-            float v[U * N];
+        if (P.dx) {
+            T* y = reinterpret_cast<T*>(P.dx) + row * P.ldx;
+            const float c = r.c * P.inv_t, f = -c * r.inv;
+            const bool same = (((uintptr_t)y ^ (uintptr_t)x) & 15u) == 0, zero = c == 0.0f;
+            T* y0 = y - span.skip;                             // where vector 0 would begin
+            // the target's place among this thread's vectors
+            const int away = counts ? (int)((target + span.skip) / N) - stream.first : -1, target_i = away >= 0 && away % nt == 0 ? away / nt : -1;
+            stream.walk(!zero && !(MODE == ROW_POLICY && stream.resident()), [&](int i) {
+                const bool has_target = (unsigned)(target_i - i) < (unsigned)ROW_GROUP;
+                if (same && !has_target && stream.plain(i)) {
+                    const uint4* q = stream.slot(i);
+                    uint4* out = reinterpret_cast<uint4*>(y0 + (int64_t)stream.vector(i) * N);
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int64_t i = j + (int64_t)u * nt;
-                if (c != 0.0f && i < j1) load_vec<T>(span, i, P.classes, v + u * N);
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int64_t i = j + (int64_t)u * nt;
-                if (i >= j1) break;
-                float* w = v + u * N;
-                const int64_t first = i * N - span.skip;
-#pragma unroll
-                for (int e = 0; e < N; e += 2) {
-                    if (c != 0.0f) {
-                        const float2 d = __fmul2_rn(__fadd2_rn(make_float2(w[e], w[e + 1]), make_float2(-m, -m)), make_float2(P.k, P.k));
-                        const float2 p = __fmul2_rn(make_float2(exp2_fast(d.x), exp2_fast(d.y)), make_float2(f, f));
-                        w[e] = p.x; w[e + 1] = p.y;
-                    } else { w[e] = 0.0f; w[e + 1] = 0.0f; }
-                }
-                if (target >= first && target < first + N) {
-#pragma unroll
-                    for (int e = 0; e < N; ++e) if (first + e == target) w[e] += c;
-                }
-                if (same && first >= 0 && first + N <= P.classes) {
-                    uint4 o;
-                    if constexpr (sizeof(T) == 4) {
-                        o = make_uint4(__float_as_uint(w[0]), __float_as_uint(w[1]), __float_as_uint(w[2]), __float_as_uint(w[3]));
-                    } else {
-                        uint32_t q[4];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const __nv_bfloat162 b = __floats2bfloat162_rn(w[2 * e], w[2 * e + 1]);
-                            q[e] = *reinterpret_cast<const uint32_t*>(&b);
+                    for (int u = 0; u < ROW_GROUP; ++u) {
+                        float w[N];
+                        uint4 o = make_uint4(0, 0, 0, 0);
+                        if (!zero) {
+                            gradient<T>(q[u * nt], r.m, k2, low2, f, w);
+                            o = pack<T>(w);
                         }
-                        o = make_uint4(q[0], q[1], q[2], q[3]);
+                        out[u * nt] = o;
                     }
-                    *reinterpret_cast<uint4*>(y0 + i * N) = o;
                 } else {
+#pragma unroll 1
+                    for (int u = 0; u < ROW_GROUP && i + u < stream.count; ++u) {
+                        const int j = stream.vector(i + u);
+                        float w[N];
 #pragma unroll
-                    for (int e = 0; e < N; ++e) if (first + e >= 0 && first + e < P.classes) y0[i * N + e] = (T)w[e];
+                        for (int e = 0; e < N; ++e) w[e] = 0.0f;
+                        if (!zero) gradient<T>(*stream.slot(i + u), r.m, k2, low2, f, w);
+                        if (i + u == target_i) {
+#pragma unroll
+                            for (int e = 0; e < N; ++e) if (span.element(j) + e == target) w[e] += c;
+                        }
+                        if (same && span.inside(j)) {
+                            *reinterpret_cast<uint4*>(y0 + (int64_t)j * N) = pack<T>(w);
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < N; ++e) {
+                                const int64_t col = span.element(j) + e;
+                                if (col >= 0 && col < P.classes) y[col] = (T)w[e];
+                            }
+                        }
+                    }
                 }
-            }
+            });
         }
     }
+    if (MODE != ROW_GRAD && P.parts > 1) cluster_wait();
 }
 
 // out[0] = scale * sum of x[0 .. n): one CTA, binary64, a fixed order.
@@ -301,23 +415,34 @@ __global__ void __launch_bounds__(256) pair_kernel(const PairParams P) {
     for (int64_t r = a + tid; r < e; r += 256) P.dlogp[r] = r < b ? c : -c;
 }
 
-// CTAs per row and threads per CTA: one CTA a row where rows fill the device, up to a cluster of eight where they do not and
-// the row is long enough to share.
-static void row_shape(int64_t rows, int64_t vectors, int* parts, int* threads) {
+// CTAs per row, threads per CTA and vectors per thread in shared memory.  A thread gets at least a group of vectors, a CTA at most 256
+// threads with sixteen vectors each (64 KB, three CTAs per SM); rows beyond that are shared by more CTAs, as are long rows where
+// there are too few to fill the device.
+static size_t row_shape(int64_t rows, int64_t vectors, int32_t* parts, int* threads) {
     const int sms = sm_count();
     int p = 1;
-    while (p < 8 && rows * p < 2 * (int64_t)sms && vectors >= 512 * (int64_t)p) p <<= 1;
-    const int64_t share = vectors / p;
+    while (p < 8 && (vectors > (int64_t)p * ROW_THREADS * ROW_SLOTS || (rows * p < 2 * (int64_t)sms && vectors >= 512 * (int64_t)p))) p <<= 1;
+    const int64_t share = (vectors + p - 1) / p;
+    int t = 32;
+    while (t < ROW_THREADS && share > (int64_t)t * ROW_SLOTS) t <<= 1;
+    const int64_t each = (share + t - 1) / t;
     *parts = p;
-    *threads = share >= 1024 ? 512 : share >= 512 ? 256 : 128;
+    *threads = t;
+    return (size_t)(each < ROW_SLOTS ? each : ROW_SLOTS) * t * 16;
 }
 
 template <typename T, int MODE>
 static cudaError_t launch_rows(RowParams P, cudaStream_t st) {
     int threads;
-    row_shape(P.rows, (P.classes * (int64_t)sizeof(T) + 15) / 16, &P.parts, &threads);
+    const int64_t bytes = P.classes * (int64_t)sizeof(T);
+    // rows that do not begin at 16-byte boundaries have a vector more
+    const size_t smem = row_shape(P.rows, bytes / 16 + (bytes % 16 || P.ld * (int64_t)sizeof(T) % 16 ? 2 : 0), &P.parts, &threads);
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(P.rows * P.parts)); cfg.blockDim = dim3(threads); cfg.stream = st;
+    if (smem > 40 * 1024) {                                    // (48 KB are to be had without asking, static shared memory included)
+        const cudaError_t e = cudaFuncSetAttribute(row_kernel<T, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, ROW_THREADS * ROW_SLOTS * 16);
+        if (e != cudaSuccess) return e;
+    }
+    cfg.gridDim = dim3((unsigned)(P.rows * P.parts)); cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
     cudaLaunchAttribute at[2];
     int n = 0;
     if (P.parts > 1 && MODE != ROW_GRAD) {                     // the gradient's walk exchanges nothing
@@ -343,7 +468,10 @@ static RowParams row_params(const LogitsArgs& a) {
     RowParams P = {};
     P.x = a.x; P.rows = a.rows; P.classes = a.classes; P.ld = a.ld;
     P.targets = a.targets; P.wide = a.target_t == SRQ_I64;
-    P.k = LOG2E / a.temperature; P.inv_t = 1.0f / a.temperature; P.t = a.temperature;
+    const double k = 1.4426950408889634074 / (double)a.temperature;
+    P.k = (float)k;
+    while ((double)P.k >= k) P.k = nextafterf(P.k, 0.0f);      // what is lacking is positive: minus infinity times it is no NaN
+    P.k_low = (float)(k - (double)P.k); P.inv_t = 1.0f / a.temperature; P.t = a.temperature;
     P.status = a.status;
     return P;
 }
