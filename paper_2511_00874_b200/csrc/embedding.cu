@@ -25,7 +25,15 @@ struct EmbedFwdParams {
 };
 constexpr int EMBED_U = 4;                      // vectors in flight per lane
 
-// Eight elements of a row (VEC: whole, 16-byte aligned), else one.
+// N elements of a row as they lie in memory (eight: 16-byte aligned).
+template <typename T, int N> struct alignas(N == 8 ? 16 : sizeof(T)) Raw { T e[N]; };
+template <typename T, int N>
+__device__ __forceinline__ void values(const Raw<T, N>& r, float v[N]) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] = (float)r.e[e];
+}
+
+// VEC: eight elements of a row at a time, else one.
 template <typename I, typename O, bool VEC>
 __global__ void __launch_bounds__(256) embedding_fwd_kernel(const EmbedFwdParams P) {
     pdl_enter();
@@ -40,25 +48,22 @@ __global__ void __launch_bounds__(256) embedding_fwd_kernel(const EmbedFwdParams
     const I* src = reinterpret_cast<const I*>(P.table) + (valid ? id : 0) * P.ld;
     O* dst = reinterpret_cast<O*>(P.out) + token * P.ld_out;
     const int64_t c0 = (turn * EMBED_U * P.lanes + lane) * N, step = (int64_t)P.lanes * N;
-    float v[EMBED_U][N];
+    Raw<I, N> raw[EMBED_U];
 #pragma unroll
     for (int u = 0; u < EMBED_U; ++u) {
-        const int64_t c = c0 + u * step;
-#pragma unroll
-        for (int e = 0; e < N; ++e) v[u][e] = 0.0f;
-        if (valid && c < P.cols) {
-            if constexpr (VEC) load8<I>(src, c, P.cols, true, v[u]);
-            else v[u][0] = (float)src[c];
-        }
+        raw[u] = {};
+        if (valid && c0 + u * step < P.cols) raw[u] = *reinterpret_cast<const Raw<I, N>*>(src + c0 + u * step);
     }
 #pragma unroll
     for (int u = 0; u < EMBED_U; ++u) {
         const int64_t c = c0 + u * step;
         if (c >= P.cols) break;
+        float v[N];
+        values<I, N>(raw[u], v);
 #pragma unroll
-        for (int e = 0; e < N; ++e) v[u][e] *= P.scale;
-        if constexpr (VEC) store8<O>(dst, c, P.cols, true, v[u]);
-        else dst[c] = (O)v[u][0];
+        for (int e = 0; e < N; ++e) v[e] *= P.scale;
+        if constexpr (VEC) store8<O>(dst, c, P.cols, true, v);
+        else dst[c] = (O)v[0];
     }
 }
 
@@ -111,16 +116,19 @@ __device__ __forceinline__ uint32_t key_of(const void* ids, int wide, int64_t i,
 }
 
 // Ranks a warp's keys, 32 at a time in their order: place among the warp's keys of the same digit so far.  counts: the warp's own.
-__device__ __forceinline__ uint32_t rank_in_warp(uint32_t digit, bool active, uint16_t* counts, int lane) {
-    const uint32_t who = __ballot_sync(0xFFFFFFFFu, active);
-    uint32_t rank = 0;
-    if (active) {
-        const uint32_t same = __match_any_sync(who, digit), before = same & ((1u << lane) - 1u);
-        rank = counts[digit] + __popc(before);
-        __syncwarp(who);
-        if (before == 0) counts[digit] = (uint16_t)(counts[digit] + __popc(same));
-        __syncwarp(who);
+// Who has the same digit is found by a ballot per bit (the instruction that matches whole words is an order slower: 16384 tokens 41 us).
+__device__ __forceinline__ uint32_t rank_in_warp(uint32_t digit, int bits, bool active, uint16_t* counts, int lane) {
+    uint32_t same = __ballot_sync(0xFFFFFFFFu, active);
+    for (int b = 0; b < bits; ++b) {
+        const uint32_t set = __ballot_sync(0xFFFFFFFFu, (digit >> b) & 1u);
+        same &= (digit >> b) & 1u ? set : ~set;
     }
+    uint32_t rank = 0;
+    const uint32_t before = same & ((1u << lane) - 1u);
+    if (active) rank = counts[digit] + __popc(before);
+    __syncwarp();
+    if (active && before == 0) counts[digit] = (uint16_t)(counts[digit] + __popc(same));
+    __syncwarp();
     return rank;
 }
 
@@ -172,7 +180,7 @@ __global__ void __launch_bounds__(SORT_ONE_THREADS) sort_one_kernel(const void* 
             const bool active = i < n;
             key[t] = active ? S.key[i] : 0u;
             rank[t] = active ? (uint32_t)S.place[i] << 16 : 0u;
-            rank[t] |= rank_in_warp((key[t] >> shift) & mask, active, S.count[warp], lane);
+            rank[t] |= rank_in_warp((key[t] >> shift) & mask, plan.bits, active, S.count[warp], lane);
         }
         __syncthreads();
         uint32_t total = 0;
@@ -243,7 +251,7 @@ __global__ void __launch_bounds__(SORT_THREADS) sort_scatter_kernel(const SortPa
             const int64_t i = tile + (warp * TURNS + t) * 32 + lane;
             const bool active = i < end;
             key[t] = !active ? 0u : P.ids ? key_of(P.ids, P.wide, i, P.rows, nullptr) : P.key_in[i];
-            rank[t] = rank_in_warp((key[t] >> P.shift) & mask, active, count[warp], lane);
+            rank[t] = rank_in_warp((key[t] >> P.shift) & mask, P.bits, active, count[warp], lane);
         }
         __syncthreads();
         uint32_t here = 0;
@@ -408,18 +416,21 @@ __global__ void __launch_bounds__(ROWS_THREADS) embedding_join_kernel(const Embe
     const int64_t piece = blockIdx.x;
     const PieceInfo me = P.info[piece];
     if (!me.opened || !me.closed) return;
-    int64_t first = piece - 1;                                 // where the row begins: the pieces between hold nothing else
-    while (first > 0) {
-        const PieceInfo p = P.info[first];
-        if (!(p.row == me.row && p.opened)) break;
-        --first;
+    // Where the row begins: the last piece before this one that did not find it open.  Those between hold nothing else.  A warp looks
+    // at 32 pieces at a time.
+    int64_t first = piece - 1;
+    for (;; first -= 32) {
+        const int64_t p = first - (threadIdx.x & 31);
+        const bool begins = p <= 0 || !(P.info[p].row == me.row && P.info[p].opened);
+        const uint32_t who = __ballot_sync(0xFFFFFFFFu, begins);
+        if (who) { first -= __ffs(who) - 1; break; }
     }
     const int64_t c = ((int64_t)blockIdx.y * blockDim.x + threadIdx.x) * N;
     if (c >= P.cols) return;
     float acc[N], v[N];
 #pragma unroll
     for (int e = 0; e < N; ++e) acc[e] = 0.0f;
-#pragma unroll 4
+#pragma unroll 8
     for (int64_t p = first; p < piece; ++p) {
         load_cols<float, N>(P.carry + p * P.ld_part, c, v);
 #pragma unroll

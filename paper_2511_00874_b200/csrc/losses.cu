@@ -4,8 +4,8 @@
 // vectors of the row into shared memory, several groups ahead of the one it works on (cp.async; a thread reads only what it has copied
 // itself, so that nothing but its own copies is waited for).  First walk: running maximum and sum of the exponentials, joined
 // over the CTA and, through distributed shared memory, over the cluster.  Then every thread knows logp, and with it the row's gradient at logp
-// (policy), so that the second walk writes the logits' gradient at once, from shared memory where the row's share fits there (up to 64 KB
-// per CTA, 512 KB per row), else by copying it once more, mostly out of L2: HBM sees every logit once and its gradient once.  The
+// (policy), so that the second walk writes the logits' gradient at once, from shared memory where the row's share fits there (up to 32 KB
+// per CTA, 256 KB per row), else by copying it once more, mostly out of L2: HBM sees every logit once and its gradient once.  The
 // preference loss needs the log-probabilities of whole answers before its first gradient, so there the two walks are two
 // launches with a small kernel over the pairs between them.
 //
@@ -90,47 +90,53 @@ __device__ __forceinline__ float2 powers(float2 d, float2 k, float2 k_low) {
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
-// A thread's vectors j0 + tid, j0 + tid + threads, ... of a row, by way of shared memory: the thread's i-th in its slot i % ROW_SLOTS (as many slots as
-// it has vectors, if these are fewer).  ROW_GROUP vectors are copied and waited for together, ROW_AHEAD groups ahead.
-constexpr int ROW_THREADS = 256, ROW_GROUP = 4, ROW_AHEAD = 4, ROW_SLOTS = ROW_GROUP * ROW_AHEAD;
-template <typename T>
+// A thread's vectors first, first + NT, ... of a row (NT: threads of the CTA), by way of shared memory: the thread's i-th in its slot i % ROW_SLOTS.
+// ROW_GROUP vectors are copied and waited for together, ROW_AHEAD groups ahead.
+constexpr int ROW_GROUP = 2, ROW_AHEAD = 8, ROW_SLOTS = ROW_GROUP * ROW_AHEAD;
+template <typename T, int NT>
 struct RowStream {
     const RowSpan<T>& span;
-    int first, step, count;                     // the thread's first vector, the distance to its next, how many
+    int first, count;                           // the thread's first vector, how many
     uint4* buffer;                              // the thread's first slot
-    __device__ __forceinline__ int vector(int i) const { return first + i * step; }
-    __device__ __forceinline__ uint4* slot(int i) const { return buffer + (i & (ROW_SLOTS - 1)) * step; }
-    // whether vectors i .. i + ROW_GROUP - 1 are there and lie wholly inside the row
-    __device__ __forceinline__ bool plain(int i) const {
-        return i + ROW_GROUP <= count && vector(i) >= span.lo && vector(i + ROW_GROUP - 1) < span.hi;
+    int plain_lo, plain_hi;                     // groups that begin at vectors plain_lo .. plain_hi - 1 are complete and wholly inside the row
+    __device__ __forceinline__ RowStream(const RowSpan<T>& s, int j0, int j1, uint4* staged) : span(s) {
+        first = j0 + (int)threadIdx.x;
+        count = first < j1 ? (j1 - first + NT - 1) / NT : 0;
+        buffer = staged + threadIdx.x;
+        plain_lo = first >= s.lo ? 0 : 1;
+        const int in = first < s.hi ? (s.hi - first + NT - 1) / NT : 0;        // vectors before the end of those inside
+        plain_hi = (in < count ? in : count) - (ROW_GROUP - 1);
     }
-    __device__ __forceinline__ void copy_group(int i) const {          // vectors i .. i + ROW_GROUP - 1, as far as there are such; closes the group
+    __device__ __forceinline__ int vector(int i) const { return first + i * NT; }
+    __device__ __forceinline__ bool plain(int i) const { return i >= plain_lo && i < plain_hi; }
+    __device__ __forceinline__ void copy_group(int i, uint4* slot) const {     // vectors i .. i + ROW_GROUP - 1, as far as there are such; closes the group
         if (plain(i)) {
             const T* src = span.first + (int64_t)vector(i) * RowSpan<T>::N;
-            const uint32_t dst = (uint32_t)__cvta_generic_to_shared(slot(i));
+            const uint32_t dst = (uint32_t)__cvta_generic_to_shared(slot);
 #pragma unroll
             for (int u = 0; u < ROW_GROUP; ++u)
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + u * step * 16), "l"(src + (int64_t)u * step * RowSpan<T>::N) : "memory");
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + u * NT * 16), "l"(src + u * NT * RowSpan<T>::N) : "memory");
         } else {
 #pragma unroll 1
-            for (int u = 0; u < ROW_GROUP; ++u)
-                if (i + u < count) copy_vec<T>(span, vector(i + u), slot(i + u));
+            for (int u = 0; u < ROW_GROUP && i + u < count; ++u) copy_vec<T>(span, vector(i + u), slot + u * NT);
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     }
     __device__ __forceinline__ bool resident() const { return count <= ROW_SLOTS; }
-    // body(i): vectors i .. i + ROW_GROUP - 1 are in their slots.  copy: they have to be brought there.
+    // body(i, slot): vectors i .. i + ROW_GROUP - 1 are in slot[0], slot[NT], ...  copy: they have to be brought there.
     template <typename F>
     __device__ __forceinline__ void walk(bool copy, F&& body) const {
         if (copy) {
 #pragma unroll
-            for (int g = 0; g < ROW_AHEAD; ++g) copy_group(g * ROW_GROUP);
+            for (int g = 0; g < ROW_AHEAD; ++g) copy_group(g * ROW_GROUP, buffer + g * ROW_GROUP * NT);
         }
 #pragma unroll 1
-        for (int i = 0; i < count; i += ROW_GROUP) {
+        for (int i = 0, at = 0; i < count; i += ROW_GROUP) {
+            uint4* slot = buffer + at;
+            at = at == (ROW_AHEAD - 1) * ROW_GROUP * NT ? 0 : at + ROW_GROUP * NT;
             if (copy) asm volatile("cp.async.wait_group %0;" ::"n"(ROW_AHEAD - 1) : "memory");
-            body(i);
-            if (copy) copy_group(i + ROW_SLOTS);
+            body(i, slot);
+            if (copy) copy_group(i + ROW_SLOTS, slot);
         }
     }
 };
@@ -161,18 +167,21 @@ __device__ __forceinline__ uint4 pack(const float w[16 / sizeof(T)]) {
     }
 }
 
+// CTAs of NT threads per SM that registers are kept for: what shared memory allows with 32 KB each, and sixteen of a warp.
+template <int NT> constexpr int ROW_CTAS = NT == 128 ? 6 : 16;
+
 // What the second walk needs of a row: the maximum, 1 / sum, the gradient at logp.
 struct RowResult { float m, inv, c; };
 
-template <typename T, int MODE>
-__global__ void __launch_bounds__(ROW_THREADS) row_kernel(const RowParams P) {
+template <typename T, int MODE, int NT>
+__global__ void __launch_bounds__(NT, ROW_CTAS<NT>) row_kernel(const RowParams P) {
     pdl_enter();
     constexpr int N = RowSpan<T>::N;
     extern __shared__ uint4 staged[];
-    __shared__ float2 part[ROW_THREADS / 32], mine;
+    __shared__ float2 part[NT / 32], mine;
     __shared__ RowResult shared_result;
     const int64_t row = blockIdx.x / P.parts;
-    const int rank = (int)(blockIdx.x - row * P.parts), tid = threadIdx.x, nt = blockDim.x;
+    const int rank = (int)(blockIdx.x - row * P.parts), tid = threadIdx.x;
     if (P.offsets) {
         if (row < whole_at(P.offsets, P.off_wide, 0) || row >= whole_at(P.offsets, P.off_wide, P.last)) return;     // the whole cluster
     }
@@ -187,7 +196,7 @@ __global__ void __launch_bounds__(ROW_THREADS) row_kernel(const RowParams P) {
     const T* x = reinterpret_cast<const T*>(P.x) + row * P.ld;
     const RowSpan<T> span(x, P.classes);
     const int share = (span.vectors + P.parts - 1) / P.parts, j0 = rank * share, j1 = j0 + share < span.vectors ? j0 + share : span.vectors;
-    const RowStream<T> stream = {span, j0 + tid, nt, j0 + tid < j1 ? (j1 - j0 - tid + nt - 1) / nt : 0, staged + tid};
+    const RowStream<T, NT> stream(span, j0, j1, staged);
     const float2 k2 = make_float2(P.k, P.k), low2 = make_float2(P.k_low, P.k_low);
     RowResult r = {0.0f, 0.0f, 0.0f};
     if constexpr (MODE == ROW_GRAD) {
@@ -206,16 +215,15 @@ __global__ void __launch_bounds__(ROW_THREADS) row_kernel(const RowParams P) {
         float m = -SRQ_INF;
         float2 sum = make_float2(0.0f, 0.0f);
         if (counts) {
-            stream.walk(true, [&](int i) {
+            stream.walk(true, [&](int i, const uint4* slot) {
                 float v[ROW_GROUP * N];
                 if (i + ROW_GROUP <= stream.count) {
-                    const uint4* q = stream.slot(i);
 #pragma unroll
-                    for (int u = 0; u < ROW_GROUP; ++u) unpack<T>(q[u * nt], v + u * N);
+                    for (int u = 0; u < ROW_GROUP; ++u) unpack<T>(slot[u * NT], v + u * N);
                 } else {
 #pragma unroll
                     for (int u = 0; u < ROW_GROUP; ++u) {
-                        if (i + u < stream.count) unpack<T>(*stream.slot(i + u), v + u * N);
+                        if (i + u < stream.count) unpack<T>(slot[u * NT], v + u * N);
                         else
 #pragma unroll
                             for (int e = 0; e < N; ++e) v[u * N + e] = -SRQ_INF;
@@ -242,13 +250,13 @@ __global__ void __launch_bounds__(ROW_THREADS) row_kernel(const RowParams P) {
             for (int d = lanes / 2; d > 0; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
         };
         reduce(32);
-        if (nt > 32) {
+        if constexpr (NT > 32) {
             if ((tid & 31) == 0) part[tid >> 5] = make_float2(m, s);
             __syncthreads();
             if (tid < 32) {
-                const float2 o = tid < nt / 32 ? part[tid] : make_float2(-SRQ_INF, 0.0f);
+                const float2 o = tid < NT / 32 ? part[tid] : make_float2(-SRQ_INF, 0.0f);
                 m = o.x; s = o.y;
-                reduce(ROW_THREADS / 32);
+                reduce(NT / 32);
             }
         }
         if (P.parts > 1) {
@@ -266,7 +274,7 @@ __global__ void __launch_bounds__(ROW_THREADS) row_kernel(const RowParams P) {
                 reduce(8);
             }
         }
-        if (tid < 32) {                                        // (lanes 0 .. 7 hold the sums)
+        if (tid < 32) {                                        // (lane 0 holds the sums)
             r.m = m; r.inv = 1.0f / s;
             const float log_s = logf(s), logp = counts ? (xt - m) * P.inv_t - log_s : 0.0f;
             float loss = 0.0f;
@@ -306,21 +314,20 @@ __global__ void __launch_bounds__(ROW_THREADS) row_kernel(const RowParams P) {
             const bool same = (((uintptr_t)y ^ (uintptr_t)x) & 15u) == 0, zero = c == 0.0f;
             T* y0 = y - span.skip;                             // where vector 0 would begin
             // the target's place among this thread's vectors
-            const int away = counts ? (int)((target + span.skip) / N) - stream.first : -1, target_i = away >= 0 && away % nt == 0 ? away / nt : -1;
-            stream.walk(!zero && !(MODE == ROW_POLICY && stream.resident()), [&](int i) {
+            const int away = counts ? (int)((target + span.skip) / N) - stream.first : -1, target_i = away >= 0 && away % NT == 0 ? away / NT : -1;
+            stream.walk(!zero && !(MODE == ROW_POLICY && stream.resident()), [&](int i, const uint4* slot) {
                 const bool has_target = (unsigned)(target_i - i) < (unsigned)ROW_GROUP;
                 if (same && !has_target && stream.plain(i)) {
-                    const uint4* q = stream.slot(i);
                     uint4* out = reinterpret_cast<uint4*>(y0 + (int64_t)stream.vector(i) * N);
 #pragma unroll
                     for (int u = 0; u < ROW_GROUP; ++u) {
                         float w[N];
                         uint4 o = make_uint4(0, 0, 0, 0);
                         if (!zero) {
-                            gradient<T>(q[u * nt], r.m, k2, low2, f, w);
+                            gradient<T>(slot[u * NT], r.m, k2, low2, f, w);
                             o = pack<T>(w);
                         }
-                        out[u * nt] = o;
+                        out[u * NT] = o;
                     }
                 } else {
 #pragma unroll 1
@@ -329,7 +336,7 @@ __global__ void __launch_bounds__(ROW_THREADS) row_kernel(const RowParams P) {
                         float w[N];
 #pragma unroll
                         for (int e = 0; e < N; ++e) w[e] = 0.0f;
-                        if (!zero) gradient<T>(*stream.slot(i + u), r.m, k2, low2, f, w);
+                        if (!zero) gradient<T>(slot[u * NT], r.m, k2, low2, f, w);
                         if (i + u == target_i) {
 #pragma unroll
                             for (int e = 0; e < N; ++e) if (span.element(j) + e == target) w[e] += c;
@@ -415,34 +422,21 @@ __global__ void __launch_bounds__(256) pair_kernel(const PairParams P) {
     for (int64_t r = a + tid; r < e; r += 256) P.dlogp[r] = r < b ? c : -c;
 }
 
-// CTAs per row, threads per CTA and vectors per thread in shared memory.  A thread gets at least a group of vectors, a CTA at most 256
-// threads with sixteen vectors each (64 KB, three CTAs per SM); rows beyond that are shared by more CTAs, as are long rows where
-// there are too few to fill the device.
-static size_t row_shape(int64_t rows, int64_t vectors, int32_t* parts, int* threads) {
+// CTAs per row and threads per CTA.  A CTA of 128 threads holds 32 KB of a row in shared memory (six CTAs per SM), one of 32 threads 8 KB, which
+// is enough for short rows; longer rows are shared by more CTAs, as are long rows where there are too few to fill the device.
+static int row_parts(int64_t rows, int64_t vectors) {
     const int sms = sm_count();
     int p = 1;
-    while (p < 8 && (vectors > (int64_t)p * ROW_THREADS * ROW_SLOTS || (rows * p < 2 * (int64_t)sms && vectors >= 512 * (int64_t)p))) p <<= 1;
-    const int64_t share = (vectors + p - 1) / p;
-    int t = 32;
-    while (t < ROW_THREADS && share > (int64_t)t * ROW_SLOTS) t <<= 1;
-    const int64_t each = (share + t - 1) / t;
-    *parts = p;
-    *threads = t;
-    return (size_t)(each < ROW_SLOTS ? each : ROW_SLOTS) * t * 16;
+    while (p < 8 && (vectors > (int64_t)p * 128 * ROW_SLOTS || (rows * p < 4 * (int64_t)sms && vectors >= 512 * (int64_t)p))) p <<= 1;
+    return p;
 }
 
-template <typename T, int MODE>
-static cudaError_t launch_rows(RowParams P, cudaStream_t st) {
-    int threads;
-    const int64_t bytes = P.classes * (int64_t)sizeof(T);
-    // rows that do not begin at 16-byte boundaries have a vector more
-    const size_t smem = row_shape(P.rows, bytes / 16 + (bytes % 16 || P.ld * (int64_t)sizeof(T) % 16 ? 2 : 0), &P.parts, &threads);
+template <typename T, int MODE, int NT>
+static cudaError_t launch_rows_of(const RowParams& P, int64_t vectors, cudaStream_t st) {
+    const int64_t each = ((vectors + P.parts - 1) / P.parts + NT - 1) / NT;
     cudaLaunchConfig_t cfg = {};
-    if (smem > 40 * 1024) {                                    // (48 KB are to be had without asking, static shared memory included)
-        const cudaError_t e = cudaFuncSetAttribute(row_kernel<T, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, ROW_THREADS * ROW_SLOTS * 16);
-        if (e != cudaSuccess) return e;
-    }
-    cfg.gridDim = dim3((unsigned)(P.rows * P.parts)); cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+    cfg.gridDim = dim3((unsigned)(P.rows * P.parts)); cfg.blockDim = dim3(NT); cfg.stream = st;
+    cfg.dynamicSmemBytes = (size_t)(each < ROW_SLOTS ? each : ROW_SLOTS) * NT * 16;
     cudaLaunchAttribute at[2];
     int n = 0;
     if (P.parts > 1 && MODE != ROW_GRAD) {                     // the gradient's walk exchanges nothing
@@ -457,7 +451,14 @@ static cudaError_t launch_rows(RowParams P, cudaStream_t st) {
     }
     cfg.attrs = at; cfg.numAttrs = n;
     count_launch();
-    return cudaLaunchKernelEx(&cfg, row_kernel<T, MODE>, P);
+    return cudaLaunchKernelEx(&cfg, row_kernel<T, MODE, NT>, P);
+}
+template <typename T, int MODE>
+static cudaError_t launch_rows(RowParams P, cudaStream_t st) {
+    // rows that do not begin at 16-byte boundaries have a vector more
+    const int64_t bytes = P.classes * (int64_t)sizeof(T), vectors = bytes / 16 + (bytes % 16 || P.ld * (int64_t)sizeof(T) % 16 ? 2 : 0);
+    P.parts = row_parts(P.rows, vectors);
+    return (vectors + P.parts - 1) / P.parts <= 32 * ROW_SLOTS ? launch_rows_of<T, MODE, 32>(P, vectors, st) : launch_rows_of<T, MODE, 128>(P, vectors, st);
 }
 template <int MODE>
 static cudaError_t launch_rows(const RowParams& P, int32_t dt, cudaStream_t st) {
