@@ -115,7 +115,7 @@ cudaError_t launch_embedding_fwd(const EmbedFwdArgs& a, cudaStream_t st) {
 // sorting
 // ------------------------------------------------------------------------------------------------
 // Radix sort, lowest digits first (of at most 9 bits, where several CTAs take part).  Keys are ids; everything without a gradient has the key `rows`, which sorts last.
-constexpr int SORT_BINS = 512, SORT_ONE = 16384, SORT_ONE_THREADS = 1024, SORT_TILE = 4096, SORT_THREADS = 512, SORT_MAX_BLOCKS = 128;
+constexpr int SORT_BINS = 512, SORT_ONE = 65536, SORT_ONE_THREADS = 512, SORT_TILE = 4096, SORT_THREADS = 512, SORT_MAX_BLOCKS = 128;
 
 struct SortPlan { int total, passes, bits; };
 static SortPlan sort_plan(int64_t rows) {
@@ -180,74 +180,148 @@ __device__ __forceinline__ int64_t tokens_before(const uint32_t* keys, int64_t n
 // Where piece p begins in a list of `items`.
 __device__ __forceinline__ int64_t piece_begin(int64_t items, int64_t pieces, int64_t p) { return items / pieces * p + (items % pieces) * p / pieces; }
 
-// All passes in one CTA, for up to SORT_ONE tokens, and the pieces' first tokens (cuts; null: not wanted).  A thread has neighbouring tokens and
-// a counter of its own for each value of a digit, so that a token's rank is one addition; the counters' exclusive sums, digit
-// by digit and thread by thread, are the places.  (Ranking 32 tokens at a time by the warp's votes took 34 us for 16384 tokens.)
-constexpr int ONE_BITS = 5, ONE_BINS = 1 << ONE_BITS, ONE_MOST = SORT_ONE / SORT_ONE_THREADS;
+// All passes in one launch, for up to SORT_ONE tokens, by one CTA or a cluster of eight, and the pieces' first tokens (cuts; null: not
+// wanted).  CTA q holds places q * per .. (q + 1) * per - 1 in shared memory.  A thread has neighbouring tokens and a counter of its own
+// for each value of a digit, so that a token's rank is one addition; the counters' exclusive sums, digit by digit and thread by
+// thread, with the other CTAs' totals before them, are the places, and the tokens go there through distributed shared memory.
+// 16384 tokens, ids below 32000: 52 us with one CTA alone (its shared memory is the bound).
+constexpr int ONE_BITS = 6, ONE_BINS = 1 << ONE_BITS, ONE_PER = SORT_ONE / 8, ONE_MOST = ONE_PER / SORT_ONE_THREADS + 1;
 struct SortOneShared {
-    uint32_t key[SORT_ONE];
-    uint16_t place[SORT_ONE];
-    uint16_t count[ONE_BINS][SORT_ONE_THREADS];
+    uint32_t key[ONE_PER];
+    uint16_t place[ONE_PER];
+    uint4 count[ONE_BINS * SORT_ONE_THREADS / 8];              // 16-bit counters [digit][thread], eight to a unit
+    uint32_t totals[8][ONE_BINS], start[ONE_BINS], base[ONE_BINS];
     uint32_t sums[32];
 };
-__global__ void __launch_bounds__(SORT_ONE_THREADS) sort_one_kernel(const void* ids, int wide, int n, int64_t rows, int bits, uint32_t* keys, uint32_t* perm,
-                                                                    int64_t* cuts, int64_t pieces, uint32_t* status) {
+// Where unit u of the counters lies: threads that read eight units in a row each would meet in the same banks otherwise.
+__device__ __forceinline__ int unit_at(int u) { return (u & ~7) | ((u + (u >> 3)) & 7); }
+__device__ __forceinline__ uint16_t& counter(SortOneShared& S, uint32_t digit, int tid) {
+    const int e = (int)digit * SORT_ONE_THREADS + tid;
+    return reinterpret_cast<uint16_t*>(&S.count[unit_at(e >> 3)])[e & 7];
+}
+__device__ __forceinline__ uint32_t in_cta(const void* p, uint32_t cta) {      // the same shared variable of another CTA of the cluster
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(cta));
+    return a;
+}
+__device__ __forceinline__ void cluster_barrier(int parts) {
+    if (parts > 1) asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    else __syncthreads();
+}
+struct SortOneParams {
+    const void* ids; int32_t wide; int32_t n; int64_t rows; int32_t bits, parts, log_per;
+    uint32_t* keys; uint32_t* perm; int64_t* cuts; int64_t pieces; uint32_t* status;
+};
+__global__ void __launch_bounds__(SORT_ONE_THREADS) sort_one_kernel(const SortOneParams P) {
     pdl_enter();
-    extern __shared__ char raw[];
+    extern __shared__ uint4 raw[];
     SortOneShared& S = *reinterpret_cast<SortOneShared*>(raw);
-    const int tid = threadIdx.x, each = (n + SORT_ONE_THREADS - 1) / SORT_ONE_THREADS, first = tid * each;
+    const int tid = threadIdx.x, rank = blockIdx.x, per = 1 << P.log_per;
+    const int rest = P.n - rank * per, n = rest < 0 ? 0 : rest < per ? rest : per;
+    // an odd number of tokens per thread: neighbouring threads' tokens lie in different banks
+    const int each = ((n + SORT_ONE_THREADS - 1) / SORT_ONE_THREADS) | 1, first = tid * each;
     {
-        int64_t id[ONE_MOST];                                  // all loads first: one wait instead of sixteen
-#pragma unroll
-        for (int t = 0; t < ONE_MOST; ++t) id[t] = t * SORT_ONE_THREADS + tid < n ? whole_at(ids, wide, t * SORT_ONE_THREADS + tid) : -1;
+        int64_t id[ONE_MOST];                                  // all loads first: one wait
 #pragma unroll
         for (int t = 0; t < ONE_MOST; ++t) {
             const int i = t * SORT_ONE_THREADS + tid;
-            if (i < n) { S.key[i] = key_of(id[t], rows, status); S.place[i] = (uint16_t)i; }
+            id[t] = i < n ? whole_at(P.ids, P.wide, (int64_t)rank * per + i) : -1;
+        }
+#pragma unroll
+        for (int t = 0; t < ONE_MOST; ++t) {
+            const int i = t * SORT_ONE_THREADS + tid;
+            if (i < n) { S.key[i] = key_of(id[t], P.rows, P.status); S.place[i] = (uint16_t)(rank * per + i); }
         }
     }
-    for (int shift = 0; shift < bits; shift += ONE_BITS) {
-        uint4* mine = reinterpret_cast<uint4*>(&S.count[0][0]) + tid * 4;      // 32 counters in the order of the sums: 64 bytes
-#pragma unroll
-        for (int q = 0; q < 4; ++q) mine[q] = make_uint4(0, 0, 0, 0);
+    cluster_barrier(P.parts);                                  // every CTA of the cluster is there
+    for (int shift = 0; shift < P.bits; shift += ONE_BITS) {
+        for (int u = tid; u < ONE_BINS * SORT_ONE_THREADS / 8; u += SORT_ONE_THREADS) S.count[u] = make_uint4(0, 0, 0, 0);
         __syncthreads();
-        uint32_t key[ONE_MOST], rank[ONE_MOST];                // rank: the token in the upper half
+        uint32_t key[ONE_MOST], own[ONE_MOST];                 // own: the token in the upper half, its rank among the thread's
 #pragma unroll
         for (int t = 0; t < ONE_MOST; ++t) {
             if (t >= each || first + t >= n) break;
             key[t] = S.key[first + t];
-            uint16_t& c = S.count[(key[t] >> shift) & (ONE_BINS - 1)][tid];
-            rank[t] = (uint32_t)S.place[first + t] << 16 | c;
+            uint16_t& c = counter(S, (key[t] >> shift) & (ONE_BINS - 1), tid);
+            own[t] = (uint32_t)S.place[first + t] << 16 | c;
             c = (uint16_t)(c + 1);
         }
         __syncthreads();
-        uint32_t w[16], total = 0;                             // pairs of counters
+        // exclusive sums over this CTA's counters; a thread has ONE_BINS of them in a row, all of one digit
+        uint4 w[ONE_BINS / 8];
+        uint32_t total = 0;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) { const uint4 x = mine[q]; w[4 * q] = x.x; w[4 * q + 1] = x.y; w[4 * q + 2] = x.z; w[4 * q + 3] = x.w; }
-#pragma unroll
-        for (int q = 0; q < 16; ++q) total += (w[q] & 0xFFFFu) + (w[q] >> 16);
-        uint32_t at = exclusive_scan<SORT_ONE_THREADS>(total, S.sums);
-#pragma unroll
-        for (int q = 0; q < 16; ++q) {
-            const uint32_t lo = w[q] & 0xFFFFu, hi = w[q] >> 16;
-            w[q] = at | (at + lo) << 16;
-            at += lo + hi;
+        for (int q = 0; q < ONE_BINS / 8; ++q) {
+            w[q] = S.count[unit_at(tid * (ONE_BINS / 8) + q)];
+            const uint32_t pairs = w[q].x + w[q].y + w[q].z + w[q].w;           // two 16-bit sums: at most 8 * 17 each
+            total += (pairs & 0xFFFFu) + (pairs >> 16);
         }
+        uint32_t at = exclusive_scan<SORT_ONE_THREADS>(total, S.sums);
+        constexpr int PER_DIGIT = SORT_ONE_THREADS / ONE_BINS;                 // threads whose counters are one digit's
+        if (tid % PER_DIGIT == 0) S.start[tid / PER_DIGIT] = at;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) mine[q] = make_uint4(w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]);
+        for (int q = 0; q < ONE_BINS / 8; ++q) {
+            uint32_t* x = reinterpret_cast<uint32_t*>(&w[q]);
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+                const uint32_t lo = x[h] & 0xFFFFu, hi = x[h] >> 16;
+                x[h] = at | (at + lo) << 16;
+                at += lo + hi;
+            }
+            S.count[unit_at(tid * (ONE_BINS / 8) + q)] = w[q];
+        }
+        __syncthreads();
+        if (tid < ONE_BINS) {                                  // this CTA's totals, to every CTA
+            const uint32_t mine = (tid + 1 < ONE_BINS ? S.start[tid + 1] : (uint32_t)n) - S.start[tid];
+            for (int q = 0; q < P.parts; ++q)
+                asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(in_cta(&S.totals[rank][tid], q)), "r"(mine) : "memory");
+        }
+        cluster_barrier(P.parts);
+        if (tid < 32) {                                        // two digits per lane: tokens of smaller digits, and of these in the CTAs before
+            uint32_t all[2] = {0, 0}, before[2] = {0, 0};
+            for (int q = 0; q < P.parts; ++q)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t c = S.totals[q][2 * tid + h];
+                    all[h] += c;
+                    if (q < rank) before[h] += c;
+                }
+            uint32_t s = all[0] + all[1];
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const uint32_t o = __shfl_up_sync(0xFFFFFFFFu, s, d);
+                if (tid >= d) s += o;
+            }
+            s -= all[0] + all[1];
+            S.base[2 * tid] = s + before[0] - S.start[2 * tid];
+            S.base[2 * tid + 1] = s + all[0] + before[1] - S.start[2 * tid + 1];
+        }
         __syncthreads();
 #pragma unroll
         for (int t = 0; t < ONE_MOST; ++t) {
             if (t >= each || first + t >= n) break;
-            const uint32_t to = S.count[(key[t] >> shift) & (ONE_BINS - 1)][tid] + (rank[t] & 0xFFFFu);
-            S.key[to] = key[t];
-            S.place[to] = (uint16_t)(rank[t] >> 16);
+            const uint32_t d = (key[t] >> shift) & (ONE_BINS - 1), to = S.base[d] + counter(S, d, tid) + (own[t] & 0xFFFFu);
+            const uint32_t cta = to >> P.log_per, i = to & (uint32_t)(per - 1);
+            asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(in_cta(&S.key[i], cta)), "r"(key[t]) : "memory");
+            asm volatile("st.shared::cluster.u16 [%0], %1;" ::"r"(in_cta(&S.place[i], cta)), "h"((uint16_t)(own[t] >> 16)) : "memory");
         }
-        __syncthreads();
+        cluster_barrier(P.parts);
     }
-    for (int i = tid; i < n; i += SORT_ONE_THREADS) { keys[i] = S.key[i]; perm[i] = S.place[i]; }
-    if (cuts)
-        for (int64_t p = tid; p <= pieces; p += SORT_ONE_THREADS) cuts[p] = tokens_before(S.key, n, piece_begin(rows + n, pieces, p));
+    for (int i = tid; i < n; i += SORT_ONE_THREADS) { P.keys[rank * per + i] = S.key[i]; P.perm[rank * per + i] = S.place[i]; }
+    if (P.cuts) {
+        for (int64_t p = rank * SORT_ONE_THREADS + tid; p <= P.pieces; p += P.parts * SORT_ONE_THREADS) {
+            const int64_t d = piece_begin(P.rows + P.n, P.pieces, p);
+            int lo = 0, hi = P.n;
+            while (lo < hi) {                                  // as in tokens_before, over the cluster's shared memory
+                const int mid = (lo + hi) >> 1;
+                uint32_t k;
+                asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(k) : "r"(in_cta(&S.key[mid & (per - 1)], mid >> P.log_per)) : "memory");
+                if (mid + (int64_t)k < d) lo = mid + 1; else hi = mid;
+            }
+            P.cuts[p] = lo;
+        }
+        cluster_barrier(P.parts);                              // nobody leaves while its tokens are being looked at
+    }
 }
 // The same for tokens that are sorted already.
 __global__ void __launch_bounds__(256) cut_kernel(const uint32_t* keys, int64_t n, int64_t rows, int64_t* cuts, int64_t pieces) {
@@ -545,11 +619,22 @@ cudaError_t launch_embedding_bwd(const EmbedBwdArgs& a, cudaStream_t st) {
     const int wide = a.id_t == SRQ_I64;
     int last = 0;                                              // buffers that hold the sorted tokens
     if (a.tokens > 0 && a.tokens <= SORT_ONE) {
+        SortOneParams Q = {a.ids, wide, (int)a.tokens, a.rows, plan.total, 1, 0, s.key[0], s.place[0], a.accumulate ? nullptr : s.cuts, pieces, a.status};
+        // one CTA for what its threads hold in four tokens each (a cluster's barriers cost more than they save), else eight
+        Q.parts = a.tokens <= 4 * SORT_ONE_THREADS ? 1 : 8;
+        while ((int64_t)Q.parts << Q.log_per < a.tokens) ++Q.log_per;
         cudaError_t e = cudaFuncSetAttribute(sort_one_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(SortOneShared));
         if (e != cudaSuccess) return e;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(Q.parts); cfg.blockDim = dim3(SORT_ONE_THREADS); cfg.dynamicSmemBytes = sizeof(SortOneShared); cfg.stream = st;
+        cudaLaunchAttribute at[2];
+        at[0].id = cudaLaunchAttributeClusterDimension;
+        at[0].val.clusterDim.x = (unsigned)Q.parts; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+        at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        at[1].val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = at; cfg.numAttrs = pdl_allowed(st) ? 2 : 1;
         count_launch();
-        e = launch_pdl(sort_one_kernel, dim3(1), dim3(SORT_ONE_THREADS), sizeof(SortOneShared), st, a.ids, wide, (int)a.tokens, a.rows, plan.total, s.key[0], s.place[0],
-                       a.accumulate ? (int64_t*)nullptr : s.cuts, pieces, a.status);
+        e = cudaLaunchKernelEx(&cfg, sort_one_kernel, Q);
         if (e != cudaSuccess) return e;
     } else if (a.tokens > 0) {
         SortParams Q = {};

@@ -126,7 +126,7 @@ def test_embedding_gradient(t, v, d, kind):
     assert out[~seen].isnan().all()
 
 
-@pytest.mark.parametrize("t,v", [(16385, 40000), (70001, 300), (30000, 2 ** 19 + 3), (600000, 20)])
+@pytest.mark.parametrize("t,v", [(2049, 64), (16385, 40000), (65536, 4096), (65537, 5000), (70001, 300), (30000, 2 ** 19 + 3), (80001, 2 ** 19 + 3), (600000, 20)])
 def test_embedding_gradient_of_many_tokens(t, v):
     g = gen(t)
     for kind in ("few", "padded", "one"):
