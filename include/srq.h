@@ -491,7 +491,7 @@ size_t srq_embedding_workspace_bytes(int64_t tokens, int64_t rows, int64_t cols)
 /* Its gradient: dtable[v, :] = scale * sum of dout[t, :] over the tokens t with ids[t] = v, added in the order of the tokens (in
  * parts where they are many) in binary32 and rounded once.  Rows of ids without a token become zero.  accumulate = 1 adds to a
  * binary32 dtable instead, and leaves the rows of ids without a token as they are.  Padding and ids out of range (reported)
- * have no gradient.  tokens and rows are at most 2^31 - 2. */
+ * have no gradient.  tokens and rows are at most 2^31 - 2, cols 2^20 (in both directions). */
 srq_status_t srq_embedding_bwd(const void *dout, srq_dtype_t dt, int64_t tokens, int64_t cols, int64_t ld,
                                const void *ids, srq_index_t id_t, int64_t rows, float scale,
                                void *dtable, srq_dtype_t dtable_dt, int64_t ld_dtable, int32_t accumulate,

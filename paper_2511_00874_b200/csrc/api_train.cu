@@ -14,7 +14,7 @@ inline size_t index_bytes(srq_index_t t) { return t == SRQ_I64 ? 8 : 4; }
 inline bool empty(int64_t rows, int64_t cols) { return rows == 0 || cols == 0; }
 inline srq_status_t status_of(cudaError_t e) { return e == cudaSuccess ? SRQ_OK : SRQ_ERR_CUDA; }
 constexpr int64_t kMaxExtent = 0x7FFFFFFEll;           // rows, tokens and classes are counted in 32 bits
-constexpr int64_t kMaxColumns = 1ll << 23;             // of an embedding: a grid's second extent
+constexpr int64_t kMaxColumns = 1ll << 20;             // of an embedding: a grid's second extent
 
 #define SRQ_TRY(expr) do { const srq_status_t s_ = (expr); if (s_ != SRQ_OK) return s_; } while (0)
 
@@ -51,7 +51,7 @@ srq_status_t srq_embedding_fwd(const void* table, srq_dtype_t dt, int64_t rows, 
 
 size_t srq_embedding_workspace_bytes(int64_t tokens, int64_t rows, int64_t cols) {
     if (tokens < 0 || rows < 0 || cols < 0 || tokens > kMaxExtent || rows > kMaxExtent || cols > kMaxColumns) return 0;
-    return embedding_bytes(tokens, rows, cols);
+    return embedding_bytes(tokens, cols);
 }
 
 srq_status_t srq_embedding_bwd(const void* dout, srq_dtype_t dt, int64_t tokens, int64_t cols, int64_t ld, const void* ids, srq_index_t id_t, int64_t rows,
@@ -65,7 +65,7 @@ srq_status_t srq_embedding_bwd(const void* dout, srq_dtype_t dt, int64_t tokens,
     if (!aligned_to(dout, 16) || !aligned_to(dtable, 16) || !aligned_to(ids, index_bytes(id_t)) || !aligned_to(device_status, 4)) return SRQ_ERR_INVALID_ARG;
     if (rows > kMaxExtent || tokens > kMaxExtent || cols > kMaxColumns) return SRQ_ERR_UNSUPPORTED;
     if (!ws || !aligned_to(ws, 256)) return SRQ_ERR_INVALID_ARG;
-    if (ws_bytes < embedding_bytes(tokens, rows, cols)) return SRQ_ERR_WORKSPACE;
+    if (ws_bytes < embedding_bytes(tokens, cols)) return SRQ_ERR_WORKSPACE;
     if (empty(rows, cols) || (accumulate && tokens == 0)) return SRQ_OK;
     const EmbedBwdArgs a = {dout, dt, tokens, cols, ld, ids, id_t, rows, scale, dtable, dtable_dt, ld_dtable, accumulate, ws, device_status};
     return status_of(launch_embedding_bwd(a, (cudaStream_t)cuda_stream));

@@ -277,7 +277,7 @@ struct EmbedBwdArgs {
     const void* dout; int32_t dt; int64_t tokens, cols, ld; const void* ids; int32_t id_t; int64_t rows; float scale;
     void* out; int32_t out_dt; int64_t ld_out; int32_t accumulate; void* ws; uint32_t* status;
 };
-size_t embedding_bytes(int64_t tokens, int64_t rows, int64_t cols);
+size_t embedding_bytes(int64_t tokens, int64_t cols);
 cudaError_t launch_embedding_bwd(const EmbedBwdArgs& a, cudaStream_t stream);
 
 struct LogitsArgs {

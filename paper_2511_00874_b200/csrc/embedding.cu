@@ -3,12 +3,11 @@
 // Forward: a copy of rows; bound by HBM (rows that come up often are read from L2).
 //
 // Gradient.  The tokens are sorted by id (stable, radix), so that the tokens of one row of the table are neighbours, in the order
-// in which they came.  The rows of the table and the sorted tokens are then merged into one list (a row's tokens, then the row's end)
-// and cut into equal pieces, one per CTA: the merge path of sparse products (Merrill and Garland, SC'16), which gives
-// every CTA the same number of rows to write and tokens to add, however uneven the ids are.  Item j of the sorted tokens stands
-// at place j + id_j of the list, so that a cut is found by one search (in shared memory, where the sort ends there).  A CTA writes the rows that end in its piece, zero rows
-// included, once each; sums of a row that began in an earlier piece or goes on in the next one are kept aside as
-// partial rows (binary32) and joined by a second kernel in the order of the pieces.  No atomics: the result repeats bit for bit.
+// in which they came.  Most rows of a table have no token at all and are written as zeros, which is most of the traffic and needs no
+// sorted tokens: while one cluster of CTAs sorts, all others look through the ids for those of their own rows and clear the rest.
+// Then the sorted tokens are cut into equal pieces, one per CTA, however uneven the ids are.  A CTA writes the rows that begin and end in
+// its piece; sums of a row that began in an earlier piece or goes on in the next one are kept aside as partial rows (binary32) and
+// joined by a third kernel in the order of the pieces.  No atomics on sums: the result repeats bit for bit.
 #include "train.cuh"
 
 namespace srq {
@@ -168,20 +167,8 @@ __device__ __forceinline__ uint32_t exclusive_scan(uint32_t x, uint32_t* warp_su
     return before + s - x;
 }
 
-// Tokens before place d of the merged list: the first j with j + key_j >= d (one thread).
-__device__ __forceinline__ int64_t tokens_before(const uint32_t* keys, int64_t n, int64_t d) {
-    int64_t lo = 0, hi = n;
-    while (lo < hi) {
-        const int64_t mid = (lo + hi) >> 1;
-        if (mid + (int64_t)keys[mid] < d) lo = mid + 1; else hi = mid;
-    }
-    return lo;
-}
-// Where piece p begins in a list of `items`.
-__device__ __forceinline__ int64_t piece_begin(int64_t items, int64_t pieces, int64_t p) { return items / pieces * p + (items % pieces) * p / pieces; }
-
-// All passes in one launch, for up to SORT_ONE tokens, by one CTA or a cluster of eight, and the pieces' first tokens (cuts; null: not
-// wanted).  CTA q holds places q * per .. (q + 1) * per - 1 in shared memory.  A thread has neighbouring tokens and a counter of its own
+// All passes in one launch, for up to SORT_ONE tokens, by one CTA or a cluster of eight, the first of the grid; the others clear the rows
+// without a token.  CTA q holds places q * per .. (q + 1) * per - 1 in shared memory.  A thread has neighbouring tokens and a counter of its own
 // for each value of a digit, so that a token's rank is one addition; the counters' exclusive sums, digit by digit and thread by
 // thread, with the other CTAs' totals before them, are the places, and the tokens go there through distributed shared memory.
 // 16384 tokens, ids below 32000: 52 us with one CTA alone (its shared memory is the bound).
@@ -210,11 +197,51 @@ __device__ __forceinline__ void cluster_barrier(int parts) {
 }
 struct SortOneParams {
     const void* ids; int32_t wide; int32_t n; int64_t rows; int32_t bits, parts, log_per;
-    uint32_t* keys; uint32_t* perm; int64_t* cuts; int64_t pieces; uint32_t* status;
+    uint32_t* keys; uint32_t* perm; uint32_t* status;
+    char* out; int64_t pitch, bytes;            // rows to clear: distance and length in bytes
 };
+
+// Rows of this CTA's share that no token has become zero.  flags: shared memory, a byte per row.
+constexpr int CLEAR_ROWS = 65536;               // at a time
+__device__ __forceinline__ void clear_rows(const SortOneParams& P, uint8_t* flags) {
+    const int tid = threadIdx.x;
+    const int64_t share = blockIdx.x - P.parts, shares = gridDim.x - P.parts;
+    const int64_t a = P.rows / shares * share + P.rows % shares * share / shares, b = P.rows / shares * (share + 1) + P.rows % shares * (share + 1) / shares;
+    const bool vec = (((uintptr_t)P.out | (uintptr_t)P.pitch | (uintptr_t)P.bytes) & 15u) == 0;
+    for (int64_t r0 = a; r0 < b; r0 += CLEAR_ROWS) {
+        const int rows = (int)(b - r0 < CLEAR_ROWS ? b - r0 : CLEAR_ROWS);
+        __syncthreads();
+        for (int r = tid; r < rows; r += SORT_ONE_THREADS) flags[r] = 0;
+        __syncthreads();
+        for (int i = tid; i < P.n; i += 8 * SORT_ONE_THREADS) {
+            int64_t id[8];
+#pragma unroll
+            for (int t = 0; t < 8; ++t) id[t] = i + t * SORT_ONE_THREADS < P.n ? whole_at(P.ids, P.wide, i + t * SORT_ONE_THREADS) : -1;
+#pragma unroll
+            for (int t = 0; t < 8; ++t)
+                if (id[t] >= r0 && id[t] < r0 + rows) flags[id[t] - r0] = 1;
+        }
+        __syncthreads();
+        for (int r = tid >> 5; r < rows; r += SORT_ONE_THREADS / 32) {
+            if (flags[r]) continue;
+            char* p = P.out + (r0 + r) * P.pitch;
+            if (vec) {
+#pragma unroll 4
+                for (int64_t c = (tid & 31) * 16; c < P.bytes; c += 512) *reinterpret_cast<uint4*>(p + c) = make_uint4(0, 0, 0, 0);
+            } else {
+                for (int64_t c = (tid & 31) * 2; c < P.bytes; c += 64) *reinterpret_cast<uint16_t*>(p + c) = 0;
+            }
+        }
+    }
+}
+
 __global__ void __launch_bounds__(SORT_ONE_THREADS) sort_one_kernel(const SortOneParams P) {
     pdl_enter();
     extern __shared__ uint4 raw[];
+    if ((int)blockIdx.x >= P.parts) {                          // (whole clusters)
+        clear_rows(P, reinterpret_cast<uint8_t*>(raw));
+        return;
+    }
     SortOneShared& S = *reinterpret_cast<SortOneShared*>(raw);
     const int tid = threadIdx.x, rank = blockIdx.x, per = 1 << P.log_per;
     const int rest = P.n - rank * per, n = rest < 0 ? 0 : rest < per ? rest : per;
@@ -308,26 +335,6 @@ __global__ void __launch_bounds__(SORT_ONE_THREADS) sort_one_kernel(const SortOn
         cluster_barrier(P.parts);
     }
     for (int i = tid; i < n; i += SORT_ONE_THREADS) { P.keys[rank * per + i] = S.key[i]; P.perm[rank * per + i] = S.place[i]; }
-    if (P.cuts) {
-        for (int64_t p = rank * SORT_ONE_THREADS + tid; p <= P.pieces; p += P.parts * SORT_ONE_THREADS) {
-            const int64_t d = piece_begin(P.rows + P.n, P.pieces, p);
-            int lo = 0, hi = P.n;
-            while (lo < hi) {                                  // as in tokens_before, over the cluster's shared memory
-                const int mid = (lo + hi) >> 1;
-                uint32_t k;
-                asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(k) : "r"(in_cta(&S.key[mid & (per - 1)], mid >> P.log_per)) : "memory");
-                if (mid + (int64_t)k < d) lo = mid + 1; else hi = mid;
-            }
-            P.cuts[p] = lo;
-        }
-        cluster_barrier(P.parts);                              // nobody leaves while its tokens are being looked at
-    }
-}
-// The same for tokens that are sorted already.
-__global__ void __launch_bounds__(256) cut_kernel(const uint32_t* keys, int64_t n, int64_t rows, int64_t* cuts, int64_t pieces) {
-    pdl_enter();
-    const int64_t p = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (p <= pieces) cuts[p] = tokens_before(keys, n, piece_begin(rows + n, pieces, p));
 }
 
 // One pass over many CTAs: a CTA takes `per` neighbouring tokens (a multiple of SORT_TILE).  ids != nullptr: the first pass.
@@ -416,14 +423,13 @@ __global__ void __launch_bounds__(SORT_THREADS) sort_scatter_kernel(const SortPa
 // ------------------------------------------------------------------------------------------------
 constexpr int ROWS_THREADS = 256;
 
-struct PieceInfo { int64_t row; int32_t opened, closed; };     // first row of the piece; begun in an earlier piece; ends in this one
+struct alignas(8) PieceInfo { uint32_t row; uint16_t opened, closed; };     // first row of the piece; begun in an earlier piece; ends in this one
 
 struct EmbedBwdParams {
     const uint32_t* keys; const uint32_t* perm; int64_t tokens, rows, cols;
     const void* dout; int64_t ld; void* out; int64_t ld_out; float scale;
     int32_t accumulate;
     int64_t pieces;
-    const int64_t* cuts;                        // first token of each piece, [pieces + 1] (not where it accumulates)
     PieceInfo* info; float* carry; float* head; int64_t ld_part;   // partial rows [pieces, ld_part]: at the end, at the beginning
 };
 
@@ -445,50 +451,39 @@ __global__ void __launch_bounds__(ROWS_THREADS, 4) embedding_rows_kernel(const E
     constexpr int BATCH = sizeof(T) == 4 && N == 8 ? 4 : 8;    // tokens whose rows are on their way together
     __shared__ uint32_t skey[ROWS_THREADS], sperm[ROWS_THREADS];
     const int tid = threadIdx.x;
-    const int64_t piece = blockIdx.x, items = (P.accumulate ? 0 : P.rows) + P.tokens;
-    const int64_t d0 = piece_begin(items, P.pieces, piece), d1 = piece_begin(items, P.pieces, piece + 1);
-    const int64_t j0 = P.accumulate ? d0 : P.cuts[piece], j1 = P.accumulate ? d1 : P.cuts[piece + 1];
-    const int64_t before = j0 > 0 ? (int64_t)P.keys[j0 - 1] : -1;   // row of the token before the piece
-    int64_t r0, r1;                                            // rows that end in this piece: [r0, r1)
-    if (P.accumulate) {
-        r0 = j0 < j1 ? (int64_t)P.keys[j0] : P.rows;
-        const int64_t last = j0 < j1 ? (int64_t)P.keys[j1 - 1] : -1;
-        r1 = j1 < P.tokens && (int64_t)P.keys[j1] == last ? last : last + 1;
-    } else {
-        r0 = d0 - j0; r1 = d1 - j1;
-    }
-    r1 = r1 < P.rows ? r1 : P.rows;
-    const bool opened = j0 < j1 || !P.accumulate ? before == r0 && r0 < P.rows : false;
-    if (tid == 0 && blockIdx.y == 0) P.info[piece] = {r0, opened, r0 < r1};
+    const int64_t piece = blockIdx.x, each = P.tokens / P.pieces, more = P.tokens % P.pieces;
+    const int64_t j0 = each * piece + (more < piece ? more : piece), j1 = j0 + each + (piece < more ? 1 : 0);      // at least one token
+    const uint32_t rows = (uint32_t)P.rows;
+    const uint32_t r0 = P.keys[j0], before = j0 > 0 ? P.keys[j0 - 1] : ~0u, last = P.keys[j1 - 1], after = j1 < P.tokens ? P.keys[j1] : ~0u;
+    const bool opened = before == r0 && r0 < rows, goes_on = after == last && last < rows;     // the first row has begun, the last one goes on
+    if (tid == 0 && blockIdx.y == 0) P.info[piece] = PieceInfo{r0, (uint16_t)opened, (uint16_t)(r0 < rows && !(goes_on && last == r0))};
     const int64_t c = ((int64_t)blockIdx.y * blockDim.x + tid) * N;
     const bool mine = c < P.cols;                              // N == 8: whole vectors
-    const T* x = reinterpret_cast<const T*>(P.dout);
-    O* out = reinterpret_cast<O*>(P.out);
+    const T* x = reinterpret_cast<const T*>(P.dout) + c;
+    O* out = reinterpret_cast<O*>(P.out) + c;
     float acc[N];
 #pragma unroll
     for (int e = 0; e < N; ++e) acc[e] = 0.0f;
-    int64_t row = r0;                                          // the row being added up
-    bool any = false;                                          // it has tokens in this piece
-    auto close = [&]() {                                       // the row ends here
+    uint32_t row = r0;                                         // the row being added up
+    const auto close = [&]() {                                 // it ends here
         if (mine) {
             if (row == r0 && opened) {
                 store_cols<float, N>(P.head + piece * P.ld_part, c, acc);
-            } else if (!P.accumulate || any) {
+            } else {
                 float v[N];
 #pragma unroll
                 for (int e = 0; e < N; ++e) v[e] = acc[e] * P.scale;
                 if (P.accumulate) {
                     float o[N];
-                    load_cols<O, N>(out + row * P.ld_out, c, o);
+                    load_cols<O, N>(out + row * P.ld_out, 0, o);
 #pragma unroll
                     for (int e = 0; e < N; ++e) v[e] += o[e];
                 }
-                store_cols<O, N>(out + row * P.ld_out, c, v);
+                store_cols<O, N>(out + row * P.ld_out, 0, v);
             }
         }
 #pragma unroll
         for (int e = 0; e < N; ++e) acc[e] = 0.0f;
-        any = false;
     };
     for (int64_t base = j0; base < j1; base += blockDim.x) {
         const int here = (int)(j1 - base < (int64_t)blockDim.x ? j1 - base : (int64_t)blockDim.x);
@@ -500,86 +495,129 @@ __global__ void __launch_bounds__(ROWS_THREADS, 4) embedding_rows_kernel(const E
 #pragma unroll
             for (int b = 0; b < BATCH; ++b) {
                 raw[b].clear();
-                if (t + b < here && mine && skey[t + b] < P.rows) raw[b].load(x + (int64_t)sperm[t + b] * P.ld + c);
+                if (t + b < here && mine && skey[t + b] < rows) raw[b].load(x + sperm[t + b] * P.ld);
             }
 #pragma unroll
             for (int b = 0; b < BATCH; ++b) {
                 if (t + b >= here) break;
-                const int64_t key = (int64_t)skey[t + b];
-                if (key >= P.rows) break;                      // what has no gradient sorts last
-                if (key != row) {
-                    if (P.accumulate) { close(); row = key; }
-                    else
-                        for (; row < key; ++row) close();
-                }
+                const uint32_t key = skey[t + b];
+                if (key >= rows) break;                        // what has no gradient sorts last
+                if (key != row) { close(); row = key; }
                 float v[N];
                 raw[b].values(v);
 #pragma unroll
                 for (int e = 0; e < N; ++e) acc[e] += v[e];
-                any = true;
             }
         }
     }
-    if (P.accumulate) {
-        if (row < r1) { close(); row = P.rows; }
-    } else {
-        for (; row < r1; ++row) close();
-    }
-    if (any && mine) store_cols<float, N>(P.carry + piece * P.ld_part, c, acc);      // the row goes on in the next piece
+    if (row >= rows) return;                                   // no token of the piece has a gradient
+    if (!goes_on) close();
+    else if (mine) store_cols<float, N>(P.carry + piece * P.ld_part, c, acc);
 }
 
-// Rows that span pieces: the pieces' partial rows in order, by the CTA of the piece in which the row ends.
+// Rows that span pieces: the pieces' partial rows, joined where the row ends.  A warp takes a piece and adds up the row that ends there, if it
+// spans few; rows of more than JOIN_ALONE pieces are added up by all warps of the CTA together, one row after the other: warp g the partial
+// rows g, g + JOIN_GROUPS, ..., then the warps' sums in order.
+constexpr int JOIN_GROUPS = 8, JOIN_COLS = 32, JOIN_ALONE = 16;        // (threads: JOIN_GROUPS * JOIN_COLS, N columns each)
 template <typename O, int N>
-__global__ void __launch_bounds__(ROWS_THREADS) embedding_join_kernel(const EmbedBwdParams P) {
+__global__ void __launch_bounds__(JOIN_GROUPS * JOIN_COLS) embedding_join_kernel(const EmbedBwdParams P) {
     pdl_enter();
-    const int64_t piece = blockIdx.x;
-    const PieceInfo me = P.info[piece];
-    if (!me.opened || !me.closed) return;
-    // Where the row begins: the last piece before this one that did not find it open.  Those between hold nothing else.  A warp looks
-    // at 32 pieces at a time.
-    int64_t first = piece - 1;
-    for (;; first -= 32) {
-        const int64_t p = first - (threadIdx.x & 31);
-        const bool begins = p <= 0 || !(P.info[p].row == me.row && P.info[p].opened);
-        const uint32_t who = __ballot_sync(0xFFFFFFFFu, begins);
-        if (who) { first -= __ffs(who) - 1; break; }
-    }
-    const int64_t c = ((int64_t)blockIdx.y * blockDim.x + threadIdx.x) * N;
-    if (c >= P.cols) return;
-    float acc[N], v[N];
+    __shared__ int64_t first_of[JOIN_GROUPS];                  // of rows that are joined by all; -1: none
+    __shared__ float sums[JOIN_GROUPS][JOIN_COLS * N];
+    const int lane = threadIdx.x & 31, group = threadIdx.x >> 5;
+    const int64_t c = ((int64_t)blockIdx.y * JOIN_COLS + lane) * N;
+    const bool mine = c < P.cols;
+    const int64_t piece = (int64_t)blockIdx.x * JOIN_GROUPS + group;
+    int64_t first = -1;
+    PieceInfo me = {};
+    if (piece < P.pieces) me = P.info[piece];
+    if (me.opened && me.closed) {
+        // where the row begins: the last piece before this one that did not find it open.  Those between hold nothing else.
+        // 128 pieces are looked at together.
+        bool found = false;
+        for (first = piece - 1; !found;) {
+            PieceInfo p[4];
 #pragma unroll
-    for (int e = 0; e < N; ++e) acc[e] = 0.0f;
+            for (int q = 0; q < 4; ++q) {
+                p[q] = PieceInfo{};
+                if (first - 32 * q - lane > 0) p[q] = P.info[first - 32 * q - lane];
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                if (found) break;
+                const uint32_t who = __ballot_sync(0xFFFFFFFFu, !(p[q].row == me.row && p[q].opened));
+                found = who != 0;
+                first -= found ? __ffs(who) - 1 : 32;
+            }
+        }
+    }
+    // partial rows start, start + step, ... of the row that begins in piece `from` and ends in piece `to`, where its part is a head
+    const auto add_up = [&](int64_t from, int64_t to, int start, int step, float acc[N]) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) acc[e] = 0.0f;
+        if (!mine) return;
 #pragma unroll 8
-    for (int64_t p = first; p < piece; ++p) {
-        load_cols<float, N>(P.carry + p * P.ld_part, c, v);
+        for (int64_t p = from + start; p <= to; p += step) {
+            float v[N];
+            load_cols<float, N>((p < to ? P.carry : P.head) + p * P.ld_part, c, v);
 #pragma unroll
-        for (int e = 0; e < N; ++e) acc[e] += v[e];
+            for (int e = 0; e < N; ++e) acc[e] += v[e];
+        }
+    };
+    const auto finish = [&](uint32_t row, float acc[N]) {
+        if (!mine) return;
+        O* o = reinterpret_cast<O*>(P.out) + (int64_t)row * P.ld_out;
+        float v[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) acc[e] *= P.scale;
+        if (P.accumulate) {
+            load_cols<O, N>(o, c, v);
+#pragma unroll
+            for (int e = 0; e < N; ++e) acc[e] += v[e];
+        }
+        store_cols<O, N>(o, c, acc);
+    };
+    float acc[N];
+    if (first >= 0 && piece - first < JOIN_ALONE) {
+        add_up(first, piece, 0, 1, acc);
+        finish(me.row, acc);
+        first = -1;
     }
-    load_cols<float, N>(P.head + piece * P.ld_part, c, v);
-    O* o = reinterpret_cast<O*>(P.out) + me.row * P.ld_out;
+    if (lane == 0) first_of[group] = first;
+    __syncthreads();
+    for (int k = 0; k < JOIN_GROUPS; ++k) {
+        if (first_of[k] < 0) continue;                         // the same for the whole CTA
+        const int64_t last = (int64_t)blockIdx.x * JOIN_GROUPS + k;
+        add_up(first_of[k], last, group, JOIN_GROUPS, acc);
 #pragma unroll
-    for (int e = 0; e < N; ++e) acc[e] = (acc[e] + v[e]) * P.scale;
-    if (P.accumulate) {
-        load_cols<O, N>(o, c, v);
+        for (int e = 0; e < N; ++e) sums[group][lane * N + e] = acc[e];
+        __syncthreads();
+        if (group == 0) {
 #pragma unroll
-        for (int e = 0; e < N; ++e) acc[e] += v[e];
+            for (int e = 0; e < N; ++e) {
+                acc[e] = 0.0f;
+#pragma unroll
+                for (int g = 0; g < JOIN_GROUPS; ++g) acc[e] += sums[g][lane * N + e];
+            }
+            finish(P.info[last].row, acc);
+        }
+        __syncthreads();
     }
-    store_cols<O, N>(o, c, acc);
 }
 
 // ------------------------------------------------------------------------------------------------
 // workspace and launch
 // ------------------------------------------------------------------------------------------------
-// Pieces: enough for every SM to hold its share of CTAs, at least eight items each.  The bound does not ask the device, since the
+// Pieces: enough for every SM to hold its share of CTAs, at least four tokens each.  The bound does not ask the device, since the
 // workspace's size is the same for every one.
 constexpr int64_t MAX_PIECES = 1184;
-static int64_t piece_count(int64_t items) {
-    const int64_t n = (items + 7) / 8;
+static int64_t piece_count(int64_t tokens) {
+    const int64_t n = (tokens + 3) / 4;
     return n < 1 ? 1 : n < MAX_PIECES ? n : MAX_PIECES;
 }
 static int64_t part_pitch(int64_t cols) { return (cols + 63) / 64 * 64; }
-struct EmbedScratch { uint32_t* key[2]; uint32_t* place[2]; uint32_t* hist; int64_t* cuts; PieceInfo* info; float* carry; float* head; size_t bytes; };
-static EmbedScratch embed_scratch(void* ws, int64_t tokens, int64_t rows, int64_t cols) {
+struct EmbedScratch { uint32_t* key[2]; uint32_t* place[2]; uint32_t* hist; PieceInfo* info; float* carry; float* head; size_t bytes; };
+static EmbedScratch embed_scratch(void* ws, int64_t tokens, int64_t cols) {
     EmbedScratch s;
     char* p = (char*)ws;
     size_t at = 0;
@@ -590,15 +628,14 @@ static EmbedScratch embed_scratch(void* ws, int64_t tokens, int64_t rows, int64_
         s.place[i] = i < sets ? (uint32_t*)take((size_t)tokens * 4) : nullptr;
     }
     s.hist = sets == 2 ? (uint32_t*)take((size_t)SORT_MAX_BLOCKS * SORT_BINS * 4) : nullptr;
-    const int64_t pieces = piece_count(rows + tokens);
-    s.cuts = (int64_t*)take((size_t)(pieces + 1) * 8);
+    const int64_t pieces = piece_count(tokens);
     s.info = (PieceInfo*)take((size_t)pieces * sizeof(PieceInfo));
     s.carry = (float*)take((size_t)pieces * part_pitch(cols) * 4);
     s.head = (float*)take((size_t)pieces * part_pitch(cols) * 4);
     s.bytes = at;
     return s;
 }
-size_t embedding_bytes(int64_t tokens, int64_t rows, int64_t cols) { return embed_scratch(nullptr, tokens, rows, cols).bytes; }
+size_t embedding_bytes(int64_t tokens, int64_t cols) { return embed_scratch(nullptr, tokens, cols).bytes; }
 
 template <typename T, typename O>
 static cudaError_t launch_rows(const EmbedBwdParams& P, bool vec, cudaStream_t st) {
@@ -609,24 +646,32 @@ static cudaError_t launch_rows(const EmbedBwdParams& P, bool vec, cudaStream_t s
     cudaError_t e = vec ? launch_pdl(embedding_rows_kernel<T, O, 8>, grid, block, 0, st, P) : launch_pdl(embedding_rows_kernel<T, O, 1>, grid, block, 0, st, P);
     if (e != cudaSuccess || P.pieces == 1) return e;
     count_launch();
-    return vec ? launch_pdl(embedding_join_kernel<O, 8>, grid, block, 0, st, P) : launch_pdl(embedding_join_kernel<O, 1>, grid, block, 0, st, P);
+    const dim3 join((unsigned)((P.pieces + JOIN_GROUPS - 1) / JOIN_GROUPS), (unsigned)((n + JOIN_COLS - 1) / JOIN_COLS)), threads_of(JOIN_GROUPS * JOIN_COLS);
+    return vec ? launch_pdl(embedding_join_kernel<O, 8>, join, threads_of, 0, st, P) : launch_pdl(embedding_join_kernel<O, 1>, join, threads_of, 0, st, P);
 }
 
 cudaError_t launch_embedding_bwd(const EmbedBwdArgs& a, cudaStream_t st) {
-    const EmbedScratch s = embed_scratch(a.ws, a.tokens, a.rows, a.cols);
+    const size_t esize = a.out_dt == SRQ_F32 ? 4 : 2;
+    const auto clear_all = [&]() { return cudaMemset2DAsync(a.out, (size_t)a.ld_out * esize, 0, (size_t)a.cols * esize, (size_t)a.rows, st); };
+    if (a.tokens == 0) return a.accumulate ? cudaSuccess : clear_all();
+    const EmbedScratch s = embed_scratch(a.ws, a.tokens, a.cols);
     const SortPlan plan = sort_plan(a.rows);
-    const int64_t pieces = piece_count((a.accumulate ? 0 : a.rows) + a.tokens);
+    const int sms = sm_count();
+    if (sms == 0) return cudaErrorUnknown;
     const int wide = a.id_t == SRQ_I64;
     int last = 0;                                              // buffers that hold the sorted tokens
-    if (a.tokens > 0 && a.tokens <= SORT_ONE) {
-        SortOneParams Q = {a.ids, wide, (int)a.tokens, a.rows, plan.total, 1, 0, s.key[0], s.place[0], a.accumulate ? nullptr : s.cuts, pieces, a.status};
+    if (a.tokens <= SORT_ONE) {
+        SortOneParams Q = {a.ids, wide, (int)a.tokens, a.rows, plan.total, 1, 0, s.key[0], s.place[0], a.status,
+                           (char*)a.out, a.ld_out * (int64_t)esize, a.cols * (int64_t)esize};
         // one CTA for what its threads hold in four tokens each (a cluster's barriers cost more than they save), else eight
         Q.parts = a.tokens <= 4 * SORT_ONE_THREADS ? 1 : 8;
         while ((int64_t)Q.parts << Q.log_per < a.tokens) ++Q.log_per;
         cudaError_t e = cudaFuncSetAttribute(sort_one_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(SortOneShared));
         if (e != cudaSuccess) return e;
         cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3(Q.parts); cfg.blockDim = dim3(SORT_ONE_THREADS); cfg.dynamicSmemBytes = sizeof(SortOneShared); cfg.stream = st;
+        // two CTAs per SM have room; where it accumulates there is nothing to clear
+        const int resident = 2 * sms / Q.parts * Q.parts;
+        cfg.gridDim = dim3(a.accumulate ? Q.parts : resident > Q.parts ? resident : 2 * Q.parts); cfg.blockDim = dim3(SORT_ONE_THREADS); cfg.dynamicSmemBytes = sizeof(SortOneShared); cfg.stream = st;
         cudaLaunchAttribute at[2];
         at[0].id = cudaLaunchAttributeClusterDimension;
         at[0].val.clusterDim.x = (unsigned)Q.parts; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
@@ -636,7 +681,11 @@ cudaError_t launch_embedding_bwd(const EmbedBwdArgs& a, cudaStream_t st) {
         count_launch();
         e = cudaLaunchKernelEx(&cfg, sort_one_kernel, Q);
         if (e != cudaSuccess) return e;
-    } else if (a.tokens > 0) {
+    } else {
+        if (!a.accumulate) {                                   // here the ids are too many to be looked through by every CTA
+            const cudaError_t e = clear_all();
+            if (e != cudaSuccess) return e;
+        }
         SortParams Q = {};
         Q.wide = wide; Q.n = a.tokens; Q.rows = a.rows; Q.bits = plan.bits; Q.hist = s.hist; Q.status = a.status;
         Q.per = (a.tokens + SORT_MAX_BLOCKS - 1) / SORT_MAX_BLOCKS;
@@ -655,15 +704,10 @@ cudaError_t launch_embedding_bwd(const EmbedBwdArgs& a, cudaStream_t st) {
             if (e != cudaSuccess) return e;
         }
     }
-    if ((a.tokens == 0 || a.tokens > SORT_ONE) && !a.accumulate) {
-        count_launch();
-        const cudaError_t e = launch_pdl(cut_kernel, dim3((unsigned)(pieces / 256 + 1)), dim3(256), 0, st, (const uint32_t*)s.key[last], a.tokens, a.rows, s.cuts, pieces);
-        if (e != cudaSuccess) return e;
-    }
     EmbedBwdParams P;
     P.keys = s.key[last]; P.perm = s.place[last]; P.tokens = a.tokens; P.rows = a.rows; P.cols = a.cols;
     P.dout = a.dout; P.ld = a.ld; P.out = a.out; P.ld_out = a.ld_out; P.scale = a.scale; P.accumulate = a.accumulate;
-    P.pieces = pieces; P.cuts = s.cuts;
+    P.pieces = piece_count(a.tokens);
     P.info = s.info; P.carry = s.carry; P.head = s.head; P.ld_part = part_pitch(a.cols);
     const bool vec = whole_vectors(a.dout, a.ld, a.cols, a.dt) && whole_vectors(a.out, a.ld_out, a.cols, a.out_dt);
     typedef __nv_bfloat16 H;

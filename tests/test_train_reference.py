@@ -142,12 +142,12 @@ def test_embedding_refusals(L):
     for bad in (dict(table=None), dict(ids=None), dict(out=None), dict(dt=2), dict(odt=-1), dict(it=2), dict(rows=-1), dict(cols=-1), dict(t=-1), dict(ld=23),
                 dict(ldo=23), dict(table=P + 8), dict(out=P + 8), dict(ids=P + 4), dict(s=P + 2)):
         assert f(**bad) == INVALID, bad
-    for bad in (dict(rows=1 << 31), dict(t=1 << 31), dict(cols=(1 << 23) + 1, ld=1 << 24, ldo=1 << 24)):
+    for bad in (dict(rows=1 << 31), dict(t=1 << 31), dict(cols=(1 << 20) + 1, ld=1 << 24, ldo=1 << 24)):
         assert f(**bad) == UNSUPPORTED, bad
     assert f(t=0, ids=None, out=None) == OK and f(cols=0, table=None, out=None) == OK
 
     need = int(L.srq_embedding_workspace_bytes(5, 8, 24))
-    assert need > 0 and L.srq_embedding_workspace_bytes(-1, 8, 24) == 0 and L.srq_embedding_workspace_bytes(5, 8, (1 << 23) + 1) == 0
+    assert need > 0 and L.srq_embedding_workspace_bytes(-1, 8, 24) == 0 and L.srq_embedding_workspace_bytes(5, 8, (1 << 20) + 1) == 0
 
     def b(dout=P, dt=0, t=5, cols=24, ld=24, ids=P, it=0, rows=8, out=P, odt=0, ldo=24, acc=0, ws=P, nb=need, s=None):
         return int(L.srq_embedding_bwd(dout, dt, t, cols, ld, ids, it, rows, 1.0, out, odt, ldo, acc, ws, nb, s, None))
