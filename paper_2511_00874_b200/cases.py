@@ -5,6 +5,7 @@
     python -m paper_2511_00874_b200.cases layer --T 16384 --N 2304 --K 768
     python -m paper_2511_00874_b200.cases mma-peak --k-blocks 2048 --seconds 2
     python -m paper_2511_00874_b200.cases mlp --T 16384 --K 2048 --N 5632
+    python -m paper_2511_00874_b200.cases finetune --T 8192 --K 2048 --N 5632 --layers 2 --vocab 32000 --loss policy
 
     python -m paper_2511_00874_b200.cases sweep --config 3
 
@@ -190,6 +191,48 @@ def case_mlp(a):
             "graph": bool(a.graph), "ms": med, "ms_best": best, "TOPS": ops / med / 1e9}
 
 
+def case_finetune(a):
+    """One training step of lm.TokenModel: embedding, layers, logits, loss, backward pass and AdamW, with K features, N hidden
+    features, T tokens."""
+    from . import lm
+    T, V = a.T, a.vocab
+    m = lm.TokenModel(T, V, a.K, a.N, a.layers, state_bits=a.state_bits, seed=a.seed)
+    m.initialise()
+    m.lr.fill_(1e-4)
+    g = torch.Generator(device="cuda").manual_seed(a.seed)
+    pick = lambda: torch.randint(0, V, (T,), generator=g, device="cuda")  # noqa: E731
+    noise = lambda std: std * torch.randn(T, generator=g, device="cuda")  # noqa: E731
+    ids, targets, weight = pick(), pick(), torch.full((T,), 1.0 / T, device="cuda")
+    B.srq_logprob_fwd(m.forward(ids), targets, m.logp)
+    old, ref, adv = m.logp + noise(0.1), m.logp + noise(0.3), noise(1.0)
+    pairs = max(1, T // 512)
+    offsets = torch.arange(2 * pairs + 1, device="cuda") * T // (2 * pairs)
+    pair_loss = torch.empty(pairs, device="cuda")
+    q = B.block_sr(a.seed, 1) if a.round == "sr" else B.BLOCK_RNE
+
+    def fn():
+        m.forward(ids)
+        if a.loss == "policy":
+            m.policy(targets, old, adv, weight, ref, kl_coef=0.05)
+        elif a.loss == "preference":
+            m.preference(targets, ref, offsets, pair_loss)
+        else:
+            m.supervised(targets, weight)
+        m.backward(ids, q)
+        m.update()
+    if a.graph:
+        fn()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            fn()
+        fn = graph.replay
+    med, best = _time(fn, a.iters, a.warmup, flush=False)
+    assert m.status.item() == 0
+    return {"op": "finetune", "loss": a.loss, "T": T, "features": a.K, "hidden": a.N, "layers": a.layers, "vocab": V, "state_bits": a.state_bits,
+            "round": a.round, "graph": bool(a.graph), "ms": med, "ms_best": best, "tokens_per_s": T / med * 1e3}
+
+
 # ---------------------------------------------------------------------------------------------
 # workload families
 # ---------------------------------------------------------------------------------------------
@@ -293,7 +336,7 @@ def case_sweep(a):
 def main(argv=None):
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     sub = ap.add_subparsers(dest="op", required=True)
-    for name in ("quantize", "gemm", "layer", "sweep", "mma-peak", "mlp"):
+    for name in ("quantize", "gemm", "layer", "sweep", "mma-peak", "mlp", "finetune"):
         p = sub.add_parser(name)
         p.add_argument("--iters", type=int, default=20)
         p.add_argument("--warmup", type=int, default=3)
@@ -329,14 +372,25 @@ def main(argv=None):
             p.add_argument("--round", default="rne", choices=["rne", "sr"], help="rounding of the gradients")
             p.add_argument("--forward-only", dest="forward_only", action="store_true")
             p.add_argument("--graph", action="store_true", help="record the step in a CUDA graph and time its replay")
-        if name not in ("gemm", "sweep", "mma-peak", "mlp"):
+        if name == "finetune":
+            p.add_argument("--T", type=int, default=8192, help="tokens")
+            p.add_argument("--K", type=int, default=2048, help="features")
+            p.add_argument("--N", type=int, default=5632, help="hidden features (a multiple of 128)")
+            p.add_argument("--layers", type=int, default=2)
+            p.add_argument("--vocab", type=int, default=32000)
+            p.add_argument("--loss", default="policy", choices=["policy", "preference", "supervised"])
+            p.add_argument("--state-bits", dest="state_bits", type=int, default=8, choices=[8, 32])
+            p.add_argument("--round", default="rne", choices=["rne", "sr"], help="rounding of the gradients")
+            p.add_argument("--graph", action="store_true", help="record the step in a CUDA graph and time its replay")
+        if name not in ("gemm", "sweep", "mma-peak", "mlp", "finetune"):
             p.add_argument("--dtype", default="f32", choices=["f32", "bf16"])
             p.add_argument("--scale", default="tensor", choices=["tensor", "row"])
             p.add_argument("--round", default="sr", choices=["sr", "rtn", "sr8"])
     a = ap.parse_args(argv)
     if not torch.cuda.is_available():
         raise SystemExit("a CUDA device is required (there is no CPU fallback)")
-    res = {"quantize": case_quantize, "gemm": case_gemm, "layer": case_layer, "sweep": case_sweep, "mma-peak": case_mma_peak, "mlp": case_mlp}[a.op](a)
+    res = {"quantize": case_quantize, "gemm": case_gemm, "layer": case_layer, "sweep": case_sweep, "mma-peak": case_mma_peak, "mlp": case_mlp,
+           "finetune": case_finetune}[a.op](a)
     if res is not None:
         print(json.dumps(res))
 
