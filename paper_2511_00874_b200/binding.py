@@ -834,6 +834,20 @@ def _logits(logits: torch.Tensor, targets: torch.Tensor):
     return px, _dtype_of(logits), rows, classes, ld, pt, wide
 
 
+def _vecs(n: int, **vectors):
+    """Pointers of contiguous float32 CUDA tensors of at least n values each (None of None), by name."""
+    f = torch.float32
+    out = []
+    for name, t in vectors.items():
+        if t is None:
+            out.append(None)
+            continue
+        if t.dtype is not f or t.numel() < n or not t.is_cuda or not t.is_contiguous():
+            raise ValueError(f"{name} must hold {n} contiguous float32 values on the device")
+        out.append(t.data_ptr())
+    return out
+
+
 def srq_logprob_fwd(logits: torch.Tensor, targets: torch.Tensor, logp: torch.Tensor, lse: Optional[torch.Tensor] = None, temperature: float = 1.0,
                     device_status: Optional[torch.Tensor] = None) -> None:
     """logp[r] = log softmax(logits[r] / temperature)[targets[r]] and lse[r]; 0 for rows whose target is below zero."""
@@ -860,9 +874,9 @@ def srq_policy_loss(logits: torch.Tensor, targets: torch.Tensor, logp_old: torch
     x = _logits(logits, targets)
     n = x[2]
     pd, ldd = _mat(dlogits, "dlogits", logits.shape, logits.dtype)
-    st = lib().srq_policy_loss(*x, _vec(logp_old, "logp_old", n), _vec(advantage, "advantage", n), _vec(weight, "weight", n), _vec(logp_ref, "logp_ref", n),
-                               _Policy(temperature, clip_low, clip_high, kl_coef), _vec(row_loss, "row_loss", n), _vec(loss, "loss", 1),
-                               _vec(logp, "logp", n), pd, ldd, _status_word(device_status), _stream())
+    po, pa, pw, pr, prow, plogp = _vecs(n, logp_old=logp_old, advantage=advantage, weight=weight, logp_ref=logp_ref, row_loss=row_loss, logp=logp)
+    st = lib().srq_policy_loss(*x, po, pa, pw, pr, _Policy(temperature, clip_low, clip_high, kl_coef), prow, _vec(loss, "loss", 1), plogp, pd, ldd,
+                               _status_word(device_status), _stream())
     _check(st, "srq_policy_loss")
 
 

@@ -207,18 +207,23 @@ __device__ __forceinline__ void clear_rows(const SortOneParams& P, uint8_t* flag
     const int tid = threadIdx.x;
     const int64_t share = blockIdx.x - P.parts, shares = gridDim.x - P.parts;
     const int64_t a = P.rows / shares * share + P.rows % shares * share / shares, b = P.rows / shares * (share + 1) + P.rows % shares * (share + 1) / shares;
-    const bool vec = (((uintptr_t)P.out | (uintptr_t)P.pitch | (uintptr_t)P.bytes) & 15u) == 0;
+    const uintptr_t odd = (uintptr_t)P.out | (uintptr_t)P.pitch | (uintptr_t)P.bytes;
+    const bool vec = (odd & 31u) == 0;
+    Word8 zero;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) zero.w[q] = 0;
     for (int64_t r0 = a; r0 < b; r0 += CLEAR_ROWS) {
         const int rows = (int)(b - r0 < CLEAR_ROWS ? b - r0 : CLEAR_ROWS);
         __syncthreads();
         for (int r = tid; r < rows; r += SORT_ONE_THREADS) flags[r] = 0;
         __syncthreads();
-        for (int i = tid; i < P.n; i += 8 * SORT_ONE_THREADS) {
-            int64_t id[8];
+        constexpr int AHEAD = 16;
+        for (int i = tid; i < P.n; i += AHEAD * SORT_ONE_THREADS) {
+            int64_t id[AHEAD];
 #pragma unroll
-            for (int t = 0; t < 8; ++t) id[t] = i + t * SORT_ONE_THREADS < P.n ? whole_at(P.ids, P.wide, i + t * SORT_ONE_THREADS) : -1;
+            for (int t = 0; t < AHEAD; ++t) id[t] = i + t * SORT_ONE_THREADS < P.n ? whole_at(P.ids, P.wide, i + t * SORT_ONE_THREADS) : -1;
 #pragma unroll
-            for (int t = 0; t < 8; ++t)
+            for (int t = 0; t < AHEAD; ++t)
                 if (id[t] >= r0 && id[t] < r0 + rows) flags[id[t] - r0] = 1;
         }
         __syncthreads();
@@ -226,10 +231,9 @@ __device__ __forceinline__ void clear_rows(const SortOneParams& P, uint8_t* flag
             if (flags[r]) continue;
             char* p = P.out + (r0 + r) * P.pitch;
             if (vec) {
-#pragma unroll 4
-                for (int64_t c = (tid & 31) * 16; c < P.bytes; c += 512) *reinterpret_cast<uint4*>(p + c) = make_uint4(0, 0, 0, 0);
+                for (int c = (tid & 31) * 32; c < (int)P.bytes; c += 1024) store32(p + c, zero);
             } else {
-                for (int64_t c = (tid & 31) * 2; c < P.bytes; c += 64) *reinterpret_cast<uint16_t*>(p + c) = 0;
+                for (int c = (tid & 31) * 2; c < (int)P.bytes; c += 64) *reinterpret_cast<uint16_t*>(p + c) = 0;
             }
         }
     }
