@@ -93,50 +93,82 @@ __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.w
 // A thread's vectors first, first + NT, ... of a row (NT: threads of the CTA), by way of shared memory: the thread's i-th in its slot i % ROW_SLOTS.
 // ROW_GROUP vectors are copied and waited for together, ROW_AHEAD groups ahead.
 constexpr int ROW_GROUP = 2, ROW_AHEAD = 8, ROW_SLOTS = ROW_GROUP * ROW_AHEAD;
+// Waits until at most n groups of copies are on their way (n: a constant once loops are unrolled).
+__device__ __forceinline__ void wait_copies(int n) {
+    switch (n) {
+        case 0: asm volatile("cp.async.wait_group 0;" ::: "memory"); break;
+        case 1: asm volatile("cp.async.wait_group 1;" ::: "memory"); break;
+        case 2: asm volatile("cp.async.wait_group 2;" ::: "memory"); break;
+        case 3: asm volatile("cp.async.wait_group 3;" ::: "memory"); break;
+        case 4: asm volatile("cp.async.wait_group 4;" ::: "memory"); break;
+        case 5: asm volatile("cp.async.wait_group 5;" ::: "memory"); break;
+        case 6: asm volatile("cp.async.wait_group 6;" ::: "memory"); break;
+        default: asm volatile("cp.async.wait_group 7;" ::: "memory"); break;
+    }
+}
+static_assert(ROW_AHEAD <= 8, "wait_copies");
+
+// Groups that are complete and wholly inside the row for all lanes of a warp are plain: one comparison that is the same for the warp
+// decides, and nothing of a plain group is checked (with a check per vector and lane a third of all instructions were checks).
 template <typename T, int NT>
 struct RowStream {
+    static constexpr int GROUP_BYTES = ROW_GROUP * NT * 16;
     const RowSpan<T>& span;
     int first, count;                           // the thread's first vector, how many
+    int groups, plain_lo, plain_hi;             // of the warp: groups, the plain ones are plain_lo .. plain_hi - 1
     uint4* buffer;                              // the thread's first slot
-    int plain_lo, plain_hi;                     // groups that begin at vectors plain_lo .. plain_hi - 1 are complete and wholly inside the row
     __device__ __forceinline__ RowStream(const RowSpan<T>& s, int j0, int j1, uint4* staged) : span(s) {
         first = j0 + (int)threadIdx.x;
         count = first < j1 ? (j1 - first + NT - 1) / NT : 0;
         buffer = staged + threadIdx.x;
-        plain_lo = first >= s.lo ? 0 : 1;
         const int in = first < s.hi ? (s.hi - first + NT - 1) / NT : 0;        // vectors before the end of those inside
-        plain_hi = (in < count ? in : count) - (ROW_GROUP - 1);
+        groups = __reduce_max_sync(0xFFFFFFFFu, (count + ROW_GROUP - 1) / ROW_GROUP);
+        plain_lo = __reduce_max_sync(0xFFFFFFFFu, first >= s.lo ? 0 : 1);
+        plain_hi = __reduce_min_sync(0xFFFFFFFFu, (in < count ? in : count) / ROW_GROUP);
     }
     __device__ __forceinline__ int vector(int i) const { return first + i * NT; }
-    __device__ __forceinline__ bool plain(int i) const { return i >= plain_lo && i < plain_hi; }
-    __device__ __forceinline__ void copy_group(int i, uint4* slot) const {     // vectors i .. i + ROW_GROUP - 1, as far as there are such; closes the group
-        if (plain(i)) {
-            const T* src = span.first + (int64_t)vector(i) * RowSpan<T>::N;
+    __device__ __forceinline__ bool plain(int g) const { return g >= plain_lo && g < plain_hi; }
+    // group g of the row to the slots at `slot`, as far as there is such a group; closes the copies' group
+    __device__ __forceinline__ void copy_group(int g, uint4* slot) const {
+        if (plain(g)) {
+            const char* src = reinterpret_cast<const char*>(span.first) + (int64_t)first * 16 + (int64_t)g * GROUP_BYTES;
             const uint32_t dst = (uint32_t)__cvta_generic_to_shared(slot);
 #pragma unroll
             for (int u = 0; u < ROW_GROUP; ++u)
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + u * NT * 16), "l"(src + u * NT * RowSpan<T>::N) : "memory");
-        } else {
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + u * NT * 16), "l"(src + u * NT * 16) : "memory");
+        } else if (g < groups) {
 #pragma unroll 1
-            for (int u = 0; u < ROW_GROUP && i + u < count; ++u) copy_vec<T>(span, vector(i + u), slot + u * NT);
+            for (int u = 0; u < ROW_GROUP && g * ROW_GROUP + u < count; ++u) copy_vec<T>(span, vector(g * ROW_GROUP + u), slot + u * NT);
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     }
-    __device__ __forceinline__ bool resident() const { return count <= ROW_SLOTS; }
-    // body(i, slot): vectors i .. i + ROW_GROUP - 1 are in slot[0], slot[NT], ...  copy: they have to be brought there.
-    template <typename F>
-    __device__ __forceinline__ void walk(bool copy, F&& body) const {
+    __device__ __forceinline__ bool resident() const { return groups <= ROW_AHEAD; }
+    // fast(g, slot) for plain groups, slow(g, slot) for the others: the vectors of group g are in slot[0], slot[NT], ...  copy: they have to be
+    // brought there.  Where all groups have slots of their own the plain ones come first, in straight code.
+    template <typename Fast, typename Slow>
+    __device__ __forceinline__ void walk(bool copy, Fast&& fast, Slow&& slow) const {
         if (copy) {
 #pragma unroll
-            for (int g = 0; g < ROW_AHEAD; ++g) copy_group(g * ROW_GROUP, buffer + g * ROW_GROUP * NT);
+            for (int g = 0; g < ROW_AHEAD; ++g) copy_group(g, buffer + g * ROW_GROUP * NT);
+        }
+        if (resident()) {
+#pragma unroll
+            for (int g = 0; g < ROW_AHEAD; ++g) {
+                if (copy) wait_copies(ROW_AHEAD - 1 - g);
+                if (plain(g)) fast(g, buffer + g * ROW_GROUP * NT);
+            }
+#pragma unroll 1
+            for (int g = 0; g < groups; ++g)
+                if (!plain(g)) slow(g, buffer + g * ROW_GROUP * NT);
+            return;
         }
 #pragma unroll 1
-        for (int i = 0, at = 0; i < count; i += ROW_GROUP) {
+        for (int g = 0, at = 0; g < groups; ++g) {
             uint4* slot = buffer + at;
             at = at == (ROW_AHEAD - 1) * ROW_GROUP * NT ? 0 : at + ROW_GROUP * NT;
-            if (copy) asm volatile("cp.async.wait_group %0;" ::"n"(ROW_AHEAD - 1) : "memory");
-            body(i, slot);
-            if (copy) copy_group(i + ROW_SLOTS, slot);
+            if (copy) wait_copies(ROW_AHEAD - 1);
+            if (plain(g)) fast(g, slot); else slow(g, slot);
+            if (copy) copy_group(g + ROW_AHEAD, slot);
         }
     }
 };
@@ -215,20 +247,7 @@ __global__ void __launch_bounds__(NT, ROW_CTAS<NT>) row_kernel(const RowParams P
         float m = -SRQ_INF;
         float2 sum = make_float2(0.0f, 0.0f);
         if (counts) {
-            stream.walk(true, [&](int i, const uint4* slot) {
-                float v[ROW_GROUP * N];
-                if (i + ROW_GROUP <= stream.count) {
-#pragma unroll
-                    for (int u = 0; u < ROW_GROUP; ++u) unpack<T>(slot[u * NT], v + u * N);
-                } else {
-#pragma unroll
-                    for (int u = 0; u < ROW_GROUP; ++u) {
-                        if (i + u < stream.count) unpack<T>(slot[u * NT], v + u * N);
-                        else
-#pragma unroll
-                            for (int e = 0; e < N; ++e) v[u * N + e] = -SRQ_INF;
-                    }
-                }
+            const auto add = [&](const float v[ROW_GROUP * N]) {
                 float top = m;
 #pragma unroll
                 for (int e = 0; e < ROW_GROUP * N; ++e) top = fmaxf(top, v[e]);
@@ -238,6 +257,25 @@ __global__ void __launch_bounds__(NT, ROW_CTAS<NT>) row_kernel(const RowParams P
 #pragma unroll
                 for (int e = 0; e < ROW_GROUP * N; e += 2)
                     sum = __fadd2_rn(sum, powers(__fadd2_rn(make_float2(v[e], v[e + 1]), make_float2(-to, -to)), k2, low2));
+            };
+            stream.walk(true, [&](int, const uint4* slot) {
+                uint4 raw[ROW_GROUP];
+                float v[ROW_GROUP * N];
+#pragma unroll
+                for (int u = 0; u < ROW_GROUP; ++u) raw[u] = slot[u * NT];
+#pragma unroll
+                for (int u = 0; u < ROW_GROUP; ++u) unpack<T>(raw[u], v + u * N);
+                add(v);
+            }, [&](int g, const uint4* slot) {
+                float v[ROW_GROUP * N];
+#pragma unroll
+                for (int u = 0; u < ROW_GROUP; ++u) {
+                    if (g * ROW_GROUP + u < stream.count) unpack<T>(slot[u * NT], v + u * N);
+                    else
+#pragma unroll
+                        for (int e = 0; e < N; ++e) v[u * N + e] = -SRQ_INF;
+                }
+                add(v);
             });
         }
         // (m, s) of the warp, the CTA and the cluster: the largest m first, then the sums in its units
@@ -313,46 +351,54 @@ __global__ void __launch_bounds__(NT, ROW_CTAS<NT>) row_kernel(const RowParams P
             const float c = r.c * P.inv_t, f = -c * r.inv;
             const bool same = (((uintptr_t)y ^ (uintptr_t)x) & 15u) == 0, zero = c == 0.0f;
             T* y0 = y - span.skip;                             // where vector 0 would begin
-            // the target's place among this thread's vectors
+            // The target's vector is written like the others, and its thread writes the target's element once more, last.
             const int away = counts ? (int)((target + span.skip) / N) - stream.first : -1, target_i = away >= 0 && away % NT == 0 ? away / NT : -1;
-            stream.walk(!zero && !(MODE == ROW_POLICY && stream.resident()), [&](int i, const uint4* slot) {
-                const bool has_target = (unsigned)(target_i - i) < (unsigned)ROW_GROUP;
-                if (same && !has_target && stream.plain(i)) {
-                    uint4* out = reinterpret_cast<uint4*>(y0 + (int64_t)stream.vector(i) * N);
-#pragma unroll
-                    for (int u = 0; u < ROW_GROUP; ++u) {
-                        float w[N];
-                        uint4 o = make_uint4(0, 0, 0, 0);
-                        if (!zero) {
-                            gradient<T>(slot[u * NT], r.m, k2, low2, f, w);
-                            o = pack<T>(w);
-                        }
-                        out[u * NT] = o;
-                    }
-                } else {
+            const bool has_target = target_i >= 0 && target_i < stream.count;
+            float at_target = c;
+            if (has_target && !zero) at_target = c + f * powers(make_float2((float)x[target] - r.m, 0.0f), k2, low2).x;      // (before it is overwritten)
+            const auto some = [&](int g, const uint4* slot) {
 #pragma unroll 1
-                    for (int u = 0; u < ROW_GROUP && i + u < stream.count; ++u) {
-                        const int j = stream.vector(i + u);
-                        float w[N];
+                for (int u = 0; u < ROW_GROUP && g * ROW_GROUP + u < stream.count; ++u) {
+                    const int j = stream.vector(g * ROW_GROUP + u);
+                    float w[N];
 #pragma unroll
-                        for (int e = 0; e < N; ++e) w[e] = 0.0f;
-                        if (!zero) gradient<T>(slot[u * NT], r.m, k2, low2, f, w);
-                        if (i + u == target_i) {
+                    for (int e = 0; e < N; ++e) w[e] = 0.0f;
+                    if (!zero) gradient<T>(slot[u * NT], r.m, k2, low2, f, w);
+                    if (same && span.inside(j)) {
+                        *reinterpret_cast<uint4*>(y0 + (int64_t)j * N) = pack<T>(w);
+                    } else {
 #pragma unroll
-                            for (int e = 0; e < N; ++e) if (span.element(j) + e == target) w[e] += c;
-                        }
-                        if (same && span.inside(j)) {
-                            *reinterpret_cast<uint4*>(y0 + (int64_t)j * N) = pack<T>(w);
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < N; ++e) {
-                                const int64_t col = span.element(j) + e;
-                                if (col >= 0 && col < P.classes) y[col] = (T)w[e];
-                            }
+                        for (int e = 0; e < N; ++e) {
+                            const int64_t col = span.element(j) + e;
+                            if (col >= 0 && col < P.classes) y[col] = (T)w[e];
                         }
                     }
                 }
-            });
+            };
+            const bool copy = !zero && !(MODE == ROW_POLICY && stream.resident());
+            if (!same) {                                       // nothing of the gradient's row is aligned as the logits' is
+                stream.walk(copy, some, some);
+            } else if (zero) {
+                stream.walk(false, [&](int g, const uint4*) {
+                    uint4* out = reinterpret_cast<uint4*>(y0 + (int64_t)stream.first * N + (int64_t)g * (ROW_GROUP * NT * N));
+#pragma unroll
+                    for (int u = 0; u < ROW_GROUP; ++u) out[u * NT] = make_uint4(0, 0, 0, 0);
+                }, some);
+            } else {
+                stream.walk(copy, [&](int g, const uint4* slot) {
+                    uint4* out = reinterpret_cast<uint4*>(y0 + (int64_t)stream.first * N + (int64_t)g * (ROW_GROUP * NT * N));
+                    uint4 raw[ROW_GROUP];
+#pragma unroll
+                    for (int u = 0; u < ROW_GROUP; ++u) raw[u] = slot[u * NT];
+#pragma unroll
+                    for (int u = 0; u < ROW_GROUP; ++u) {
+                        float w[N];
+                        gradient<T>(raw[u], r.m, k2, low2, f, w);
+                        out[u * NT] = pack<T>(w);
+                    }
+                }, some);
+            }
+            if (has_target && !zero) y[target] = (T)at_target;
         }
     }
     if (MODE != ROW_GRAD && P.parts > 1) cluster_wait();
