@@ -502,7 +502,7 @@ srq_status_t srq_embedding_bwd(const void *dout, srq_dtype_t dt, int64_t tokens,
  * logits[rows, classes] has type dt and pitch ld; logits of minus infinity (masked classes) have probability 0.  A target
  * below zero marks a row that does not count (padding, a prompt): its logits are not read, its logp and lse are 0.  A target
  * that is not below `classes` is treated the same and reported.  A logp that is not finite is reported (SRQ_ERR_NONFINITE).
- * lse may be NULL. */
+ * lse may be NULL.  temperature lies between 2^-100 and 2^100. */
 srq_status_t srq_logprob_fwd(const void *logits, srq_dtype_t dt, int64_t rows, int64_t classes, int64_t ld,
                              const void *targets, srq_index_t target_t, float temperature,
                              float *logp, float *lse, uint32_t *device_status, void *cuda_stream);
@@ -526,7 +526,7 @@ srq_status_t srq_logprob_bwd(const void *logits, srq_dtype_t dt, int64_t rows, i
  * loss [1] (the sum of row_loss; needs row_loss), logp [rows] and dlogits may each be NULL, but not all of them.  dlogits may be
  * the logits themselves. */
 typedef struct {
-    float temperature;           /* > 0 */
+    float temperature;           /* 2^-100 .. 2^100 */
     float clip_low, clip_high;   /* >= 0; clip_low = 0.2: ratios below 0.8 are clipped.  Infinity: not clipped on that side */
     float kl_coef;               /* >= 0 */
 } srq_policy_t;
@@ -551,7 +551,7 @@ size_t srq_preference_workspace_bytes(int64_t rows);
  * pair_loss [pairs] and logp [rows] are required; loss [1] and dlogits may be NULL.  dlogits may be
  * the logits themselves. */
 typedef struct {
-    float temperature;       /* > 0 */
+    float temperature;       /* 2^-100 .. 2^100 */
     float beta;              /* finite */
     float label_smoothing;   /* 0 .. 1 */
 } srq_preference_t;

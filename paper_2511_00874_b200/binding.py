@@ -787,6 +787,12 @@ def _whole(t: torch.Tensor, name: str, n: Optional[int] = None):
     return t.data_ptr(), wide
 
 
+def _here(t: torch.Tensor, name: str) -> None:
+    """The calls go to the current device's current stream: their tensors have to live on that device."""
+    if t.get_device() != torch._C._cuda_getDevice():
+        raise ValueError(f"{name} is on another device than the current one")
+
+
 def _workspace(ws: Optional[torch.Tensor], need: int, device):
     """(pointer, bytes, tensor) of the caller's workspace, or of a new one."""
     if ws is None:
@@ -800,6 +806,7 @@ def srq_embedding_fwd(table: torch.Tensor, ids: torch.Tensor, out: torch.Tensor,
                       device_status: Optional[torch.Tensor] = None) -> None:
     """out[t] = scale * table[ids[t]]; an id below zero is padding and gives a row of zeros."""
     pi, wide = _whole(ids, "ids")
+    _here(ids, "ids")
     T, (rows, cols) = ids.numel(), table.shape
     pt, ldt = _mat(table, "table")
     po, ldo = _mat(out, "out", (T, cols))
@@ -818,6 +825,7 @@ def srq_embedding_bwd(dout: torch.Tensor, ids: torch.Tensor, dtable: torch.Tenso
     T, cols = dout.shape
     rows = dtable.shape[0]
     pi, wide = _whole(ids, "ids", T)
+    _here(ids, "ids")
     pd, ldd = _mat(dout, "dout")
     pt, ldt = _mat(dtable, "dtable", (rows, cols))
     pw, nb, ws = _workspace(ws, srq_embedding_workspace_bytes(T, rows, cols) if ws is None else 0, dout.device)
@@ -831,6 +839,7 @@ def _logits(logits: torch.Tensor, targets: torch.Tensor):
     rows, classes = logits.shape
     px, ld = _mat(logits, "logits")
     pt, wide = _whole(targets, "targets", rows)
+    _here(targets, "targets")
     return px, _dtype_of(logits), rows, classes, ld, pt, wide
 
 
@@ -972,6 +981,8 @@ def srq_adamw_step(tensors: AdamTensors, lr: float, beta1: float = 0.9, beta2: f
     ``step_device`` (int64) and ``grad_scale`` (float32) are device scalars that are read when the step runs."""
     if step_device is not None and (step_device.dtype is not torch.int64 or not step_device.is_cuda):
         raise ValueError("step_device must be an int64 CUDA tensor of one element")
+    if tensors.tensors:
+        _here(tensors.tensors[0].param, "param")
     h = _AdamW(lr, beta1, beta2, eps, weight_decay, step, round, seed, tensor_id, _vec(lr_device, "lr_device", 1), _ptr(step_device),
                _vec(grad_scale, "grad_scale", 1))
     st = lib().srq_adamw_step(tensors.c, len(tensors.tensors), tensors.param_dtype, tensors.grad_dtype, tensors.bits, h, _status_word(device_status), _stream())

@@ -21,7 +21,7 @@ constexpr int64_t kMaxColumns = 1ll << 20;             // of an embedding: a gri
 // A matrix of logits with its targets; one without elements may have null pointers.
 srq_status_t check_logits(const void* x, srq_dtype_t dt, int64_t rows, int64_t classes, int64_t ld, const void* targets, srq_index_t target_t,
                           float temperature, const uint32_t* status) {
-    if (rows < 0 || classes < 0 || !known_dtype(dt) || !known_index(target_t) || !(temperature > 0.0f) || !isfinite(temperature)) return SRQ_ERR_INVALID_ARG;
+    if (rows < 0 || classes < 0 || !known_dtype(dt) || !known_index(target_t) || !(temperature >= 0x1p-100f && temperature <= 0x1p100f)) return SRQ_ERR_INVALID_ARG;
     if ((!x && !empty(rows, classes)) || (!targets && rows)) return SRQ_ERR_INVALID_ARG;
     if (ld < classes || !aligned_to(x, 16) || !aligned_to(targets, index_bytes(target_t)) || !aligned_to(status, 4)) return SRQ_ERR_INVALID_ARG;
     if (rows > kMaxExtent || classes > kMaxExtent) return SRQ_ERR_UNSUPPORTED;

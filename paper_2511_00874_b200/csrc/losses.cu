@@ -505,6 +505,7 @@ static int row_parts(int64_t rows, int64_t vectors) {
 template <typename T, int MODE, int NT>
 static cudaError_t launch_rows_of(const RowParams& P, int64_t vectors, cudaStream_t st) {
     const int64_t each = ((vectors + P.parts - 1) / P.parts + NT - 1) / NT;
+    if (P.rows * P.parts > 0x7FFFFFFFll) return cudaErrorInvalidConfiguration;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(P.rows * P.parts)); cfg.blockDim = dim3(NT); cfg.stream = st;
     cfg.dynamicSmemBytes = (size_t)(each < ROW_SLOTS ? each : ROW_SLOTS) * NT * 16;

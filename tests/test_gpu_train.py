@@ -287,6 +287,21 @@ def test_policy_loss(rows, classes, extra, dt):
         assert torch.equal(row, row2)
 
 
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_gradients_whose_rows_are_aligned_otherwise_than_the_logits(dt):
+    g = gen(21)
+    x, targets = make_logits(g, 37, 5001, DT[dt], 0)
+    dlogp = randn(g, 37)
+    logp, lse = torch.empty(37, device="cuda"), torch.empty(37, device="cuda")
+    srq.srq_logprob_fwd(x, targets, logp, lse)
+    want = torch.empty_like(x)
+    srq.srq_logprob_bwd(x, targets, lse, dlogp, want)
+    for extra in (1, 7):
+        out = strided(torch.full_like(x, 5.0), extra)
+        srq.srq_logprob_bwd(x, targets, lse, dlogp, out)
+        assert torch.equal(out, want) and behind(out)
+
+
 def test_policy_loss_clips_where_it_should():
     # logits (0, log 3): logp = log 3/4.  ratios 0.5 .. 2 through logp_old, both signs of the advantage
     x = torch.tensor([[0.0, math.log(3.0)]], device="cuda").repeat(12, 1)
@@ -580,6 +595,34 @@ def test_adamw_leaves_what_lies_between_the_tensors_alone():
         assert f[~inside].eq(7).all()
     for f in (flat[0], flat[3]):                                            # (the first moment stays: 0.9 * 7 + 0.1 * 7)
         assert not f[inside].eq(7).any()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_on_views_that_begin_at_any_sixteen_bytes(bits):
+    for dt, off in ((torch.bfloat16, 8), (torch.float32, 4)):
+        t = group([700, 2048, 5001], dt, dt, bits, 31)
+        for x in t:
+            for name in ("param", "grad"):
+                old = getattr(x, name)
+                wide = torch.zeros(old.numel() + off, dtype=dt, device="cuda")
+                wide[off:] = old
+                setattr(x, name, wide[off:])
+            assert x.param.data_ptr() % 32 == 16
+        check_step(t, bits, H, 9, srq.SR, 5, 77)
+
+
+def test_adamw_gradients_that_move_are_given_anew():
+    t = group([300, 40], torch.float32, torch.float32, 32, 33)
+    a = srq.AdamTensors(t)
+    old = t[1].grad
+    a.set_grad(1, torch.full((40,), 2.0, device="cuda"))
+    old.fill_(math.nan)
+    m = t[1].m.clone()
+    s = status()
+    srq.srq_adamw_step(a, **H, step=1, device_status=s)
+    assert s.item() == 0 and torch.allclose(t[1].m, m * 0.9 + 0.2) and len(a) == 2
+    with pytest.raises(ValueError, match="grad"):
+        a.set_grad(1, torch.zeros(39, device="cuda"))
 
 
 # --------------------------------------------------------------------------------------------

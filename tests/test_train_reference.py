@@ -161,7 +161,7 @@ def test_embedding_refusals(L):
 
 def bad_logits():
     return (dict(x=None), dict(t=None), dict(dt=3), dict(it=2), dict(rows=-1), dict(c=-1), dict(ld=39), dict(x=P + 8), dict(t=P + 4), dict(temp=0.0),
-            dict(temp=-1.0), dict(temp=float("nan")), dict(temp=float("inf")), dict(s=P + 1))
+            dict(temp=-1.0), dict(temp=float("nan")), dict(temp=float("inf")), dict(temp=1e-31), dict(temp=2e30), dict(s=P + 1))
 
 
 def test_logprob_refusals(L):
