@@ -212,8 +212,10 @@ __global__ void __launch_bounds__(NT, ROW_CTAS<NT>) row_kernel(const RowParams P
     extern __shared__ uint4 staged[];
     __shared__ float2 part[NT / 32], mine;
     __shared__ RowResult shared_result;
-    const int64_t row = blockIdx.x / P.parts;
+    int64_t row = blockIdx.x / P.parts;
     const int rank = (int)(blockIdx.x - row * P.parts), tid = threadIdx.x;
+    // the second walk over the same logits begins with the rows that the first one read last: some are still in L2
+    if (MODE == ROW_GRAD && P.stat) row = P.rows - 1 - row;
     if (P.offsets) {
         if (row < whole_at(P.offsets, P.off_wide, 0) || row >= whole_at(P.offsets, P.off_wide, P.last)) return;     // the whole cluster
     }
@@ -493,12 +495,14 @@ __global__ void __launch_bounds__(PAIR_THREADS) pair_kernel(const PairParams P, 
     }
 }
 
-// CTAs per row and threads per CTA.  A CTA of 128 threads holds 32 KB of a row in shared memory (six CTAs per SM), one of 32 threads 8 KB, which
-// is enough for short rows; longer rows are shared by more CTAs, as are long rows where there are too few to fill the device.
-static int row_parts(int64_t rows, int64_t vectors) {
+// CTAs per row.  A CTA of 128 threads holds 32 KB of a row in shared memory (six CTAs per SM), one of 32 threads 8 KB, which is enough for short
+// rows.  A gradient's rows (keep) are shared by as many CTAs as hold them, up to eight; all long rows where there are too few to fill the
+// device.  Sums alone go through the row 32 KB at a time and share nothing (16 pairs of 256 on 50257 classes: sums with a cluster of four 180 us, one
+// CTA 140; gradients by one CTA a row 257, by four 242).
+static int row_parts(int64_t rows, int64_t vectors, bool keep) {
     const int sms = sm_count();
     int p = 1;
-    while (p < 8 && (vectors > (int64_t)p * 128 * ROW_SLOTS || (rows * p < 4 * (int64_t)sms && vectors >= 512 * (int64_t)p))) p <<= 1;
+    while (p < 8 && ((keep && vectors > (int64_t)p * 128 * ROW_SLOTS) || (rows * p < 4 * (int64_t)sms && vectors >= 512 * (int64_t)p))) p <<= 1;
     return p;
 }
 
@@ -529,7 +533,7 @@ template <typename T, int MODE>
 static cudaError_t launch_rows(RowParams P, cudaStream_t st) {
     // rows that do not begin at 16-byte boundaries have a vector more
     const int64_t bytes = P.classes * (int64_t)sizeof(T), vectors = bytes / 16 + (bytes % 16 || P.ld * (int64_t)sizeof(T) % 16 ? 2 : 0);
-    P.parts = row_parts(P.rows, vectors);
+    P.parts = row_parts(P.rows, vectors, MODE != ROW_LOGP);
     return (vectors + P.parts - 1) / P.parts <= 32 * ROW_SLOTS ? launch_rows_of<T, MODE, 32>(P, vectors, st) : launch_rows_of<T, MODE, 128>(P, vectors, st);
 }
 template <int MODE>

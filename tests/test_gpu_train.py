@@ -242,7 +242,7 @@ def test_log_probabilities_at_the_ends_of_the_range():
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
-@pytest.mark.parametrize("rows,classes,extra", SHAPES)
+@pytest.mark.parametrize("rows,classes,extra", SHAPES + [(1000, 20000, 0), (700, 16391, 5), (500, 50257, 0)])      # (the last ones: many long rows)
 def test_policy_loss(rows, classes, extra, dt):
     g = gen(rows * 3 + classes)
     x, targets = make_logits(g, rows, classes, DT[dt], extra, 1.5)
