@@ -586,7 +586,8 @@ srq_status_t srq_preference_loss(const void *logits, srq_dtype_t dt, int64_t row
  *
  * A gradient that is not finite, or a moment that leaves binary32, is reported (SRQ_ERR_NONFINITE).  With 32-bit states the
  * element follows the formula; with 8-bit states the block of 128 that has it is left as it was, weights and moments.
- * If *grad_scale is not finite, nothing is changed at all and that is reported (a step whose gradient norm overflowed).
+ * If *grad_scale or *lr_device is not finite, nothing is changed at all and that is reported (a step whose gradient norm overflowed);
+ * so is a *step_device below 1 (SRQ_ERR_INVALID_ARG).
  *
  * tensors is a HOST array, read before the call returns; no pointer in it may overlap another tensor's. */
 typedef struct {

@@ -86,15 +86,17 @@ __device__ __forceinline__ float moment_step(float m, float inv, float top_recip
 struct AdamNow {
     float rate, decay, root, gscale;            // lr / bias1, 1 - lr wd, 1 / sqrt(bias2), factor on gradients
     uint32_t t;                                 // number of the step, for the thresholds
-    bool go;
+    uint32_t refused;                           // why nothing is done, or 0
 };
 __device__ __forceinline__ AdamNow adam_now(const AdamScalars& s) {
     AdamNow n;
     float ib1 = s.inv_bias1, ib2 = s.inv_root_bias2;
     n.t = (uint32_t)s.step;
+    bool no_step = false;
     if (s.step_device) {
         const int64_t t = *s.step_device;
         n.t = (uint32_t)t;
+        no_step = t < 1;
         // 1 - beta^t = -(e^(t ln beta) - 1): no cancellation for betas near 1
         ib1 = 1.0f / -expm1f((float)t * ib1);
         ib2 = 1.0f / sqrtf(-expm1f((float)t * ib2));
@@ -104,7 +106,8 @@ __device__ __forceinline__ AdamNow adam_now(const AdamScalars& s) {
     n.decay = 1.0f - lr * s.weight_decay;
     n.root = ib2;
     n.gscale = s.grad_scale ? *s.grad_scale : 1.0f;
-    n.go = abs_word(n.gscale) < 0x7F800000u;
+    n.refused = block_nonfinite(abs_word(n.gscale)) || block_nonfinite(abs_word(lr)) ? SRQ_ERR_NONFINITE : 0u;
+    if (no_step) n.refused = SRQ_ERR_INVALID_ARG;
     return n;
 }
 
@@ -195,8 +198,8 @@ __global__ void __launch_bounds__(ADAM_THREADS<false>) adamw_kernel(const __grid
     constexpr bool WORDS = SR && sizeof(P) == 2;
     const AdamScalars& s = a.s;
     const AdamNow now = adam_now(s);
-    if (!now.go) {
-        if (threadIdx.x == 0 && blockIdx.x == 0) note(s.status, SRQ_ERR_NONFINITE);
+    if (now.refused) {
+        if (threadIdx.x == 0 && blockIdx.x == 0) note(s.status, now.refused);
         return;
     }
     AdamCursor<ADAM_THREADS<false> / 32, CAP> at(a);
@@ -497,8 +500,8 @@ __global__ void __launch_bounds__(ADAM_THREADS<true>, 5) adamw8_kernel(const __g
     __shared__ Staged<P, G> buffers[WARPS][2];
     const AdamScalars& s = a.s;
     const AdamNow now = adam_now(s);
-    if (!now.go) {
-        if (threadIdx.x == 0 && blockIdx.x == 0) note(s.status, SRQ_ERR_NONFINITE);
+    if (now.refused) {
+        if (threadIdx.x == 0 && blockIdx.x == 0) note(s.status, now.refused);
         return;
     }
     const int lane = threadIdx.x & 31, warp = __shfl_sync(0xFFFFFFFFu, (int)threadIdx.x >> 5, 0);

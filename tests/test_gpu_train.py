@@ -567,6 +567,11 @@ def test_adamw_reports_what_is_not_finite(what):
     s = status()
     srq.srq_adamw_step(srq.AdamTensors([t]), **H, step=3, grad_scale=torch.tensor([math.inf], device="cuda"), device_status=s)
     assert s.item() == binding.ERR_NONFINITE and all(torch.equal(a, b) for a, b in zip(old, (t.param, t.m, t.v)))
+    for kw, why in ((dict(lr_device=torch.tensor([math.nan], device="cuda")), binding.ERR_NONFINITE),
+                    (dict(step_device=torch.zeros(1, dtype=torch.int64, device="cuda")), binding.ERR_INVALID_ARG)):
+        s = status()
+        srq.srq_adamw_step(srq.AdamTensors([t]), **H, step=3, **kw, device_status=s)
+        assert s.item() == why and all(torch.equal(a, b) for a, b in zip(old, (t.param, t.m, t.v)))
 
 
 def test_adamw_rounds_small_updates_with_the_right_probability():
