@@ -173,9 +173,7 @@ __device__ __forceinline__ uint32_t exclusive_scan(uint32_t x, uint32_t* warp_su
 // thread, with the other CTAs' totals before them, are the places, and the tokens go there through distributed shared memory.
 // 16384 tokens, ids below 32000: 52 us with one CTA alone (its shared memory is the bound).
 constexpr int ONE_BITS = 6, ONE_BINS = 1 << ONE_BITS, ONE_PER = SORT_ONE / 8, ONE_MOST = ONE_PER / SORT_ONE_THREADS + 1;
-struct SortOneShared {
-    uint32_t key[ONE_PER];
-    uint16_t place[ONE_PER];
+struct SortOneShared {                          // then uint32_t key[per], uint16_t place[per]
     uint4 count[ONE_BINS * SORT_ONE_THREADS / 8];              // 16-bit counters [digit][thread], eight to a unit
     uint32_t totals[8][ONE_BINS], start[ONE_BINS], base[ONE_BINS];
     uint32_t sums[32];
@@ -202,7 +200,7 @@ struct SortOneParams {
 };
 
 // Rows of this CTA's share that no token has become zero.  flags: shared memory, a byte per row.
-constexpr int CLEAR_ROWS = 65536;               // at a time
+constexpr int CLEAR_ROWS = ONE_BINS * SORT_ONE_THREADS * 2;    // at a time: the memory of the counters
 __device__ __forceinline__ void clear_rows(const SortOneParams& P, uint8_t* flags) {
     const int tid = threadIdx.x;
     const int64_t share = blockIdx.x - P.parts, shares = gridDim.x - P.parts;
@@ -239,7 +237,7 @@ __device__ __forceinline__ void clear_rows(const SortOneParams& P, uint8_t* flag
     }
 }
 
-__global__ void __launch_bounds__(SORT_ONE_THREADS) sort_one_kernel(const SortOneParams P) {
+__global__ void __launch_bounds__(SORT_ONE_THREADS, 2) sort_one_kernel(const SortOneParams P) {
     pdl_enter();
     extern __shared__ uint4 raw[];
     if ((int)blockIdx.x >= P.parts) {                          // (whole clusters)
@@ -248,6 +246,8 @@ __global__ void __launch_bounds__(SORT_ONE_THREADS) sort_one_kernel(const SortOn
     }
     SortOneShared& S = *reinterpret_cast<SortOneShared*>(raw);
     const int tid = threadIdx.x, rank = blockIdx.x, per = 1 << P.log_per;
+    uint32_t* S_key = reinterpret_cast<uint32_t*>(&S + 1);
+    uint16_t* S_place = reinterpret_cast<uint16_t*>(S_key + per);
     const int rest = P.n - rank * per, n = rest < 0 ? 0 : rest < per ? rest : per;
     // an odd number of tokens per thread: neighbouring threads' tokens lie in different banks
     const int each = ((n + SORT_ONE_THREADS - 1) / SORT_ONE_THREADS) | 1, first = tid * each;
@@ -261,7 +261,7 @@ __global__ void __launch_bounds__(SORT_ONE_THREADS) sort_one_kernel(const SortOn
 #pragma unroll
         for (int t = 0; t < ONE_MOST; ++t) {
             const int i = t * SORT_ONE_THREADS + tid;
-            if (i < n) { S.key[i] = key_of(id[t], P.rows, P.status); S.place[i] = (uint16_t)(rank * per + i); }
+            if (i < n) { S_key[i] = key_of(id[t], P.rows, P.status); S_place[i] = (uint16_t)(rank * per + i); }
         }
     }
     cluster_barrier(P.parts);                                  // every CTA of the cluster is there
@@ -272,9 +272,9 @@ __global__ void __launch_bounds__(SORT_ONE_THREADS) sort_one_kernel(const SortOn
 #pragma unroll
         for (int t = 0; t < ONE_MOST; ++t) {
             if (t >= each || first + t >= n) break;
-            key[t] = S.key[first + t];
+            key[t] = S_key[first + t];
             uint16_t& c = counter(S, (key[t] >> shift) & (ONE_BINS - 1), tid);
-            own[t] = (uint32_t)S.place[first + t] << 16 | c;
+            own[t] = (uint32_t)S_place[first + t] << 16 | c;
             c = (uint16_t)(c + 1);
         }
         __syncthreads();
@@ -333,12 +333,12 @@ __global__ void __launch_bounds__(SORT_ONE_THREADS) sort_one_kernel(const SortOn
             if (t >= each || first + t >= n) break;
             const uint32_t d = (key[t] >> shift) & (ONE_BINS - 1), to = S.base[d] + counter(S, d, tid) + (own[t] & 0xFFFFu);
             const uint32_t cta = to >> P.log_per, i = to & (uint32_t)(per - 1);
-            asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(in_cta(&S.key[i], cta)), "r"(key[t]) : "memory");
-            asm volatile("st.shared::cluster.u16 [%0], %1;" ::"r"(in_cta(&S.place[i], cta)), "h"((uint16_t)(own[t] >> 16)) : "memory");
+            asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(in_cta(&S_key[i], cta)), "r"(key[t]) : "memory");
+            asm volatile("st.shared::cluster.u16 [%0], %1;" ::"r"(in_cta(&S_place[i], cta)), "h"((uint16_t)(own[t] >> 16)) : "memory");
         }
         cluster_barrier(P.parts);
     }
-    for (int i = tid; i < n; i += SORT_ONE_THREADS) { P.keys[rank * per + i] = S.key[i]; P.perm[rank * per + i] = S.place[i]; }
+    for (int i = tid; i < n; i += SORT_ONE_THREADS) { P.keys[rank * per + i] = S_key[i]; P.perm[rank * per + i] = S_place[i]; }
 }
 
 // One pass over many CTAs: a CTA takes `per` neighbouring tokens (a multiple of SORT_TILE).  ids != nullptr: the first pass.
@@ -670,12 +670,14 @@ cudaError_t launch_embedding_bwd(const EmbedBwdArgs& a, cudaStream_t st) {
         // one CTA for what its threads hold in four tokens each (a cluster's barriers cost more than they save), else eight
         Q.parts = a.tokens <= 4 * SORT_ONE_THREADS ? 1 : 8;
         while ((int64_t)Q.parts << Q.log_per < a.tokens) ++Q.log_per;
-        cudaError_t e = cudaFuncSetAttribute(sort_one_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(SortOneShared));
+        const size_t smem = sizeof(SortOneShared) + ((size_t)6 << Q.log_per);
+        cudaError_t e = cudaFuncSetAttribute(sort_one_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(sizeof(SortOneShared) + 6 * ONE_PER));
         if (e != cudaSuccess) return e;
         cudaLaunchConfig_t cfg = {};
-        // two CTAs per SM have room; where it accumulates there is nothing to clear
-        const int resident = 2 * sms / Q.parts * Q.parts;
-        cfg.gridDim = dim3(a.accumulate ? Q.parts : resident > Q.parts ? resident : 2 * Q.parts); cfg.blockDim = dim3(SORT_ONE_THREADS); cfg.dynamicSmemBytes = sizeof(SortOneShared); cfg.stream = st;
+        // as many CTAs as the SMs have room for (113 KB each for two); where it accumulates there is nothing to clear
+        const int resident = (smem <= 112 * 1024 ? 2 : 1) * sms / Q.parts * Q.parts;
+        cfg.gridDim = dim3(a.accumulate ? Q.parts : resident > Q.parts ? resident : 2 * Q.parts); cfg.blockDim = dim3(SORT_ONE_THREADS);
+        cfg.dynamicSmemBytes = smem; cfg.stream = st;
         cudaLaunchAttribute at[2];
         at[0].id = cudaLaunchAttributeClusterDimension;
         at[0].val.clusterDim.x = (unsigned)Q.parts; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
