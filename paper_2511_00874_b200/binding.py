@@ -947,27 +947,24 @@ class AdamTensors:
         self.param_dtype, self.grad_dtype = (F32, F32) if t0 is None else (_dtype_of(t0.param), _dtype_of(t0.grad))
         self.bits = 32 if t0 is None or t0.m.dtype is torch.float32 else 8
         self.c = (_AdamTensor * max(1, len(self.tensors)))()
+        state, coded, check = torch.float32 if self.bits == 32 else torch.uint8, self.bits == 8, self._check
         for i, t in enumerate(self.tensors):
-            n, state = t.param.numel(), torch.float32 if self.bits == 32 else torch.uint8
-            for name, x, dtype, size in (("param", t.param, t0.param.dtype, n), ("m", t.m, state, n), ("v", t.v, state, n)):
-                self._check(i, name, x, dtype, size)
-            for name, x in (("m_step", t.m_step), ("v_step", t.v_step)):
-                if self.bits == 8:
-                    self._check(i, name, x, torch.float32, -(-n // BLOCK))
-            self.c[i] = _AdamTensor(t.param.data_ptr(), None, t.m.data_ptr(), t.v.data_ptr(), _ptr(t.m_step) if self.bits == 8 else None,
-                                    _ptr(t.v_step) if self.bits == 8 else None, n)
+            n = t.param.numel()
+            param, m, v = check(i, "param", t.param, t0.param.dtype, n), check(i, "m", t.m, state, n), check(i, "v", t.v, state, n)
+            steps = [check(i, name, x, torch.float32, -(-n // BLOCK)) for name, x in (("m_step", t.m_step), ("v_step", t.v_step))] if coded else (None, None)
+            self.c[i] = _AdamTensor(param, None, m, v, *steps, n)
             self.set_grad(i, t.grad)
 
     @staticmethod
     def _check(i, name, x, dtype, size):
         if x is None or x.dtype is not dtype or x.numel() != size or not x.is_cuda or not x.is_contiguous():
             raise ValueError(f"tensor {i}: {name} must hold {size} contiguous values of {dtype} on the device")
+        return x.data_ptr()
 
     def set_grad(self, i: int, grad: torch.Tensor) -> None:
         """The gradient of tensor i from now on."""
-        self._check(i, "grad", grad, torch.float32 if self.grad_dtype == F32 else torch.bfloat16, self.tensors[i].param.numel())
+        self.c[i].grad = self._check(i, "grad", grad, torch.float32 if self.grad_dtype == F32 else torch.bfloat16, self.c[i].n)
         self.tensors[i].grad = grad
-        self.c[i].grad = grad.data_ptr()
 
     def __len__(self):
         return len(self.tensors)

@@ -195,6 +195,7 @@ __device__ __forceinline__ uint32_t in_cta(const void* p, uint32_t cta) {      /
     return a;
 }
 __device__ __forceinline__ void cluster_barrier(int parts) {
+    __syncwarp();                                              // the cluster's barrier takes converged warps
     if (parts > 1) asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
     else __syncthreads();
 }

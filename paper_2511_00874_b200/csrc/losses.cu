@@ -93,9 +93,15 @@ __device__ __forceinline__ float2 powers(float2 d, float2 k, float2 k_low) {
     const float2 t = __ffma2_rn(d, k_low, __fmul2_rn(d, k));
     return make_float2(exp2_fast(t.x), exp2_fast(t.y));
 }
-// The cluster's barrier without an order of memory: whoever has written for others fences first.
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+// The cluster's barrier without an order of memory: whoever has written for others fences first.  Both halves take converged warps.
+__device__ __forceinline__ void cluster_arrive() {
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait() {
+    __syncwarp();
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
 
 // A thread's vectors first, first + NT, ... of a row (NT: threads of the CTA), by way of shared memory: the thread's i-th in its slot i % ROW_SLOTS.
 // ROW_GROUP vectors are copied and waited for together, ROW_AHEAD groups ahead.

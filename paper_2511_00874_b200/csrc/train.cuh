@@ -1,5 +1,5 @@
-// Shared by the operators at the ends of a training step (embedding.cu, losses.cu, adamw.cu): whole-number operands, 16- and
-// 32-byte accesses, the device's size.
+// Shared by the operators at the ends of a training step (embedding.cu, losses.cu, adamw.cu): whole-number operands, 32-byte
+// stores, the device's size.
 #pragma once
 
 #include <atomic>
@@ -24,14 +24,8 @@ __device__ __forceinline__ int64_t whole_at(const void* p, int wide, int64_t i) 
     return wide ? reinterpret_cast<const int64_t*>(p)[i] : (int64_t)reinterpret_cast<const int32_t*>(p)[i];
 }
 
-// Ordinary 32-byte accesses (one instruction on this architecture).  Volatile, so that none moves ahead of the wait a kernel starts with.
+// Ordinary 32-byte stores (one instruction on this architecture).  Volatile, so that none moves ahead of the wait a kernel starts with.
 struct alignas(32) Word8 { uint32_t w[8]; };
-__device__ __forceinline__ Word8 load32(const void* p) {
-    Word8 r;
-    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                 : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]), "=r"(r.w[4]), "=r"(r.w[5]), "=r"(r.w[6]), "=r"(r.w[7]) : "l"(p) : "memory");
-    return r;
-}
 __device__ __forceinline__ void store32(void* p, const Word8& r) {
     asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
                  ::"l"(p), "r"(r.w[0]), "r"(r.w[1]), "r"(r.w[2]), "r"(r.w[3]), "r"(r.w[4]), "r"(r.w[5]), "r"(r.w[6]), "r"(r.w[7]) : "memory");
