@@ -473,8 +473,8 @@ srq_status_t srq_glu_bwd(const void *dh, srq_dtype_t dt, int64_t ld_dh, const sr
  *   - Token ids, targets and offsets are whole numbers of type srq_index_t on the device.  The host does not see them: one that
  *     is out of range is reported as SRQ_ERR_INVALID_ARG in device_status, nothing is read or written through it, and
  *     the call goes on as is said at each operator.
- *   - Sums over tokens, rows and classes are in binary32 or more and have an order that depends on sizes, ids and the device
- *     alone: the same call repeats bit for bit.
+ *   - Sums over tokens, rows and classes are in binary32 or more and have an order that depends on sizes, ids, alignment and the
+ *     device alone: the same call repeats bit for bit.
  *   - Base pointers of matrices and of AdamW's tensors are 16-byte aligned; pitches are in elements and may be odd.
  */
 typedef enum { SRQ_I32 = 0, SRQ_I64 = 1 } srq_index_t;
