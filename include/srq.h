@@ -501,14 +501,17 @@ srq_status_t srq_embedding_bwd(const void *dout, srq_dtype_t dt, int64_t tokens,
  *   lse = log(sum over j of e^(z_j)),  logp = z_target - lse.
  * logits[rows, classes] has type dt and pitch ld; logits of minus infinity (masked classes) have probability 0.  A target
  * below zero marks a row that does not count (padding, a prompt): its logits are not read, its logp and lse are 0.  A target
- * that is not below `classes` is treated the same and reported.  A logp that is not finite is reported (SRQ_ERR_NONFINITE).
+ * that is not below `classes` is treated the same and reported.  A logp that is not finite is reported (SRQ_ERR_NONFINITE), and so
+ * is an lse where it is asked for (large logits over a small temperature can leave binary32 while logp does not).
  * lse may be NULL.  temperature lies between 2^-100 and 2^100. */
 srq_status_t srq_logprob_fwd(const void *logits, srq_dtype_t dt, int64_t rows, int64_t classes, int64_t ld,
                              const void *targets, srq_index_t target_t, float temperature,
                              float *logp, float *lse, uint32_t *device_status, void *cuda_stream);
 
 /* Their gradient at the logits: dlogits_j = dlogp / temperature * ([j = target] - e^(z_j - lse)), type dt, from lse as
- * srq_logprob_fwd gave it and the gradient dlogp[rows] at logp (supervised training: minus each token's weight).  Rows that do
+ * srq_logprob_fwd gave it and the gradient dlogp[rows] at logp (supervised training: minus each token's weight).  One binary32 number
+ * holds lse to 2^-24 |lse|, which is an error of every z_j - lse: rows with |lse| above 32, or not finite, have their maximum and
+ * their sum formed anew from the logits, so that the error of a probability does not grow with the logits.  Rows that do
  * not count (target below zero or out of range, dlogp zero) become zero and their logits are not read.  dlogits may be
  * the logits themselves (same pointer and pitch). */
 srq_status_t srq_logprob_bwd(const void *logits, srq_dtype_t dt, int64_t rows, int64_t classes, int64_t ld,

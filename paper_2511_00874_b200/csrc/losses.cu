@@ -17,7 +17,7 @@
 // cover the barriers, and clusters of eight that do not fill the device).
 //
 // Exponentials: e^((x - m) / T) = 2^((x - m) k) with k = log2(e) / T, the difference first, so that large logits cost no precision
-// and the range is binary32's.  k is a sum of two numbers where probabilities are added up (one alone would shift every log-probability
+// and the range is binary32's (a gradient that is given lse alone: LSE_EXACT below).  k is a sum of two numbers where probabilities are added up (one alone would shift every log-probability
 // of a row the same way, which shows in sums over rows).  2^y is the hardware's approximation (2 units); sums are binary32, of at
 // most 16384 terms in 64 partial sums per warp.
 #include <math.h>
@@ -26,7 +26,14 @@
 
 namespace srq {
 
-enum RowMode { ROW_LOGP = 0, ROW_GRAD = 1, ROW_POLICY = 2 };
+// ROW_GRAD: the gradient from (max, 1 / sum) of every row; ROW_LSE: from lse, where that is exact enough, else the row is walked twice as for
+// ROW_POLICY.
+enum RowMode { ROW_LOGP = 0, ROW_GRAD = 1, ROW_POLICY = 2, ROW_LSE = 3 };
+// A gradient from one binary32 number for maximum and sum takes lse's rounding as an error of every exponent, 2^-24 |lse|: up to this |lse| it
+// is what a difference x - max of that size costs anyway (relative error of a probability: a few 1e-6).  Beyond, at 1e4 it would be 6e-4, at 1e8
+// probabilities of a row no longer add up to anything near 1.  The logits of a model at temperature 1 have an lse of 5 to 30.
+// (8044 x 50257 bfloat16: 258 us from lse, 334 walked twice; 1021 x 50257 binary32: 71 and 86.)
+constexpr float LSE_EXACT = 32.0f;
 #define SRQ_INF __int_as_float(0x7F800000)
 
 struct RowParams {
@@ -36,8 +43,8 @@ struct RowParams {
     int32_t parts;                              // CTAs per row
     uint32_t* status;
     float* logp; float* lse;
-    float2* stat;                               // (max, 1 / sum) of each row, instead of lse (ROW_LOGP writes, ROW_GRAD reads)
-    const float* dlogp;                         // ROW_GRAD
+    float2* stat;                               // (max, 1 / sum) of each row (ROW_LOGP writes, ROW_GRAD reads)
+    const float* dlogp;                         // ROW_GRAD, ROW_LSE
     void* dx; int64_t ldx;                      // gradient at the logits
     const float* old; const float* advantage; const float* weight; const float* ref;
     float clip_lo, clip_hi, kl;                 // bounds of the ratio
@@ -228,7 +235,7 @@ __global__ void __launch_bounds__(NT, ROW_CTAS<NT>) row_kernel(const RowParams P
     int64_t row = blockIdx.x / P.parts;
     const int rank = (int)(blockIdx.x - row * P.parts), tid = threadIdx.x;
     // the second walk over the same logits begins with the rows that the first one read last: some are still in L2
-    if (MODE == ROW_GRAD && P.stat) row = P.rows - 1 - row;
+    if (MODE == ROW_GRAD) row = P.rows - 1 - row;
     if (P.offsets) {
         if (row < whole_at(P.offsets, P.off_wide, 0) || row >= whole_at(P.offsets, P.off_wide, P.last)) return;     // the whole cluster
     }
@@ -246,16 +253,24 @@ __global__ void __launch_bounds__(NT, ROW_CTAS<NT>) row_kernel(const RowParams P
     const RowStream<T, NT> stream(span, j0, j1, staged);
     const float2 k2 = make_float2(P.k, P.k), low2 = make_float2(P.k_low, P.k_low);
     RowResult r = {0.0f, 0.0f, 0.0f};
-    if constexpr (MODE == ROW_GRAD) {
+    bool sums = MODE == ROW_LOGP || MODE == ROW_POLICY;        // the first walk takes place (the same for the whole cluster)
+    if constexpr (MODE == ROW_GRAD || MODE == ROW_LSE) {
         r.c = counts ? P.dlogp[row] : 0.0f;
         if (r.c != 0.0f) {
-            if (P.stat) { const float2 q = P.stat[row]; r.m = q.x; r.inv = q.y; }
-            else { r.m = P.lse[row] * P.t; r.inv = 1.0f; }
+            if constexpr (MODE == ROW_GRAD) {
+                const float2 q = P.stat[row];
+                r.m = q.x; r.inv = q.y;
+            } else {
+                const float lse = P.lse[row];
+                r.m = lse * P.t; r.inv = 1.0f;
+                sums = !(fabsf(lse) <= LSE_EXACT);             // (or lse is not finite, though the row's probabilities may be)
+            }
         }
-    } else {
+    }
+    if (MODE != ROW_GRAD && sums) {
         // what the row's first warp will need, requested before the walk
         float xt = 0.0f, old = 0.0f, adv = 0.0f, ref = 0.0f;
-        if (counts && tid < 32) {
+        if (MODE != ROW_LSE && counts && tid < 32) {
             xt = (float)x[target];
             if constexpr (MODE == ROW_POLICY) { old = P.old[row]; adv = P.advantage[row]; if (P.ref) ref = P.ref[row]; }
         }
@@ -329,7 +344,7 @@ __global__ void __launch_bounds__(NT, ROW_CTAS<NT>) row_kernel(const RowParams P
         }
         if (tid < 32) {                                        // (lane 0 holds the sums)
             r.m = m; r.inv = 1.0f / s;
-            const float log_s = logf(s), logp = counts ? (xt - m) * P.inv_t - log_s : 0.0f;
+            const float log_s = logf(s), logp = counts ? (xt - m) * P.inv_t - log_s : 0.0f, lse = counts ? m * P.inv_t + log_s : 0.0f;
             float loss = 0.0f;
             if constexpr (MODE == ROW_POLICY) {
                 if (counts) {
@@ -347,9 +362,12 @@ __global__ void __launch_bounds__(NT, ROW_CTAS<NT>) row_kernel(const RowParams P
             }
             if (tid == 0) {
                 shared_result = r;
-                if (rank == 0) {
+                if (MODE != ROW_LSE && rank == 0) {
                     if (P.logp) P.logp[row] = logp;
-                    if (P.lse) P.lse[row] = counts ? m * P.inv_t + log_s : 0.0f;
+                    if (MODE == ROW_LOGP && P.lse) {
+                        P.lse[row] = lse;
+                        if (abs_word(lse) >= 0x7F800000u) note(P.status, SRQ_ERR_NONFINITE);
+                    }
                     if (P.stat) P.stat[row] = make_float2(m, r.inv);
                     if constexpr (MODE == ROW_POLICY) if (P.row_loss) P.row_loss[row] = loss;
                     if (abs_word(logp) >= 0x7F800000u || abs_word(r.c) >= 0x7F800000u) note(P.status, SRQ_ERR_NONFINITE);
@@ -390,7 +408,7 @@ __global__ void __launch_bounds__(NT, ROW_CTAS<NT>) row_kernel(const RowParams P
                     }
                 }
             };
-            const bool copy = !zero && !(MODE == ROW_POLICY && stream.resident());
+            const bool copy = !zero && !(MODE != ROW_GRAD && sums && stream.resident());
             if (!same) {                                       // nothing of the gradient's row is aligned as the logits' is
                 stream.walk(copy, some, some);
             } else if (zero) {
@@ -416,7 +434,7 @@ __global__ void __launch_bounds__(NT, ROW_CTAS<NT>) row_kernel(const RowParams P
             if (has_target && !zero) y[target] = (T)at_target;
         }
     }
-    if (MODE != ROW_GRAD && P.parts > 1) cluster_wait();
+    if (MODE != ROW_GRAD && sums && P.parts > 1) cluster_wait();
 }
 
 // out[0] = scale * sum of x[0 .. n): one CTA, binary64, a fixed order.
@@ -574,7 +592,7 @@ cudaError_t launch_logprob_fwd(const LogitsArgs& a, float* logp, float* lse, cud
 cudaError_t launch_logprob_bwd(const LogitsArgs& a, const float* lse, const float* dlogp, void* dx, int64_t ldx, cudaStream_t st) {
     RowParams P = row_params(a);
     P.lse = const_cast<float*>(lse); P.dlogp = dlogp; P.dx = dx; P.ldx = ldx;
-    return launch_rows<ROW_GRAD>(P, a.dt, st);
+    return launch_rows<ROW_LSE>(P, a.dt, st);
 }
 static cudaError_t launch_loss_sum(const float* x, int64_t n, double scale, float* out, cudaStream_t st) {
     count_launch();
