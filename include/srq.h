@@ -116,6 +116,9 @@ typedef struct {
                             * i.e. over tokens other shards may hold; the row-major layout's row
                             * maxima are always computed here.  Values must not be smaller than the
                             * true maxima (codes are unspecified otherwise).  NULL: compute them. */
+    const int64_t *step_device; /* optional, DEVICE pointer, 8-byte aligned; the entry points that take SRQ_PER_BLOCK only.
+                            * The thresholds are those of tensor_id + *step_device * 2^32, read when the call runs: a step
+                            * that is recorded in a CUDA graph draws new ones at every replay.  NULL: those of tensor_id. */
 } srq_qspec_t;
 
 /* Optional copies of what a layer pass fed to its product: dense code matrices in the layout

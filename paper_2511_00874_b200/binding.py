@@ -46,7 +46,7 @@ class _QSpec(ctypes.Structure):
     _fields_ = [("bits", ctypes.c_int32), ("scale", ctypes.c_int32), ("round", ctypes.c_int32),
                 ("format", ctypes.c_int32), ("seed", ctypes.c_uint64),
                 ("tensor_id", ctypes.c_uint64), ("index_offset", ctypes.c_uint64),
-                ("absmax", ctypes.c_void_p)]
+                ("absmax", ctypes.c_void_p), ("step_device", ctypes.c_void_p)]
 
 
 class _DebugOut(ctypes.Structure):
@@ -72,10 +72,14 @@ class QSpec:
     index_offset: int = 0
     format: int = GRID_INT
     absmax: Optional[torch.Tensor] = None      # device float tensor of one element: known max |x| (per tensor)
+    step: Optional[torch.Tensor] = None        # device int64 tensor of one element: block codes draw the thresholds of tensor_id + step * 2^32
 
     def c(self) -> _QSpec:
+        step = self.step
+        if step is not None and (step.dtype is not torch.int64 or step.numel() != 1 or not step.is_cuda):
+            raise ValueError("step must be an int64 CUDA tensor of one element")
         return _QSpec(self.bits, self.scale, self.round, self.format, self.seed, self.tensor_id,
-                      self.index_offset, None if self.absmax is None else self.absmax.data_ptr())
+                      self.index_offset, None if self.absmax is None else self.absmax.data_ptr(), None if step is None else step.data_ptr())
 
 
 class _Blocks(ctypes.Structure):
@@ -582,9 +586,10 @@ BLOCK = 128
 BLOCK_RNE = QSpec(8, PER_BLOCK, RNE, format=GRID_E4M3)     # round to nearest even; SR: block_sr(seed, tensor_id)
 
 
-def block_sr(seed: int, tensor_id: int, index_offset: int = 0) -> QSpec:
-    """Stochastic rounding to block codes with the thresholds of (seed, tensor_id, index_offset)."""
-    return QSpec(8, PER_BLOCK, SR, seed, tensor_id, index_offset, GRID_E4M3)
+def block_sr(seed: int, tensor_id: int, index_offset: int = 0, step: Optional[torch.Tensor] = None) -> QSpec:
+    """Stochastic rounding to block codes with the thresholds of (seed, tensor_id, index_offset).  ``step``: a step's number on the
+    device, which is read when the call runs; without it a recorded call draws the same thresholds at every replay."""
+    return QSpec(8, PER_BLOCK, SR, seed, tensor_id, index_offset, GRID_E4M3, step=step)
 
 
 @dataclass

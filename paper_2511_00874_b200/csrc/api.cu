@@ -14,6 +14,7 @@ srq_status_t srq::check_qspec(const srq_qspec_t* q) {
     if (q->round != SRQ_SR && q->round != SRQ_RTN && q->round != SRQ_SR8) return SRQ_ERR_INVALID_ARG;
     if (q->round == SRQ_SR8 && q->format != SRQ_GRID_INT) return SRQ_ERR_UNSUPPORTED;
     if (q->absmax && ((uintptr_t)q->absmax % 4) != 0) return SRQ_ERR_INVALID_ARG;
+    if (q->step_device) return SRQ_ERR_UNSUPPORTED;            // block entry points only
     return SRQ_OK;
 }
 

@@ -35,7 +35,9 @@ srq_status_t check_rounding(const srq_qspec_t* q, BlockRounding* r) {
     if (q->format != SRQ_GRID_INT && q->format != SRQ_GRID_E4M3) return SRQ_ERR_INVALID_ARG;
     if (q->format != SRQ_GRID_E4M3 || q->bits != 8 || q->scale != SRQ_PER_BLOCK || (q->round != SRQ_SR && q->round != SRQ_RNE))
         return SRQ_ERR_UNSUPPORTED;
+    if (!aligned_to(q->step_device, 8)) return SRQ_ERR_INVALID_ARG;
     r->sr = q->round == SRQ_SR;
+    r->step = q->step_device;
     r->index_offset = q->index_offset; r->seed = q->seed; r->tensor_id = q->tensor_id;
     return SRQ_OK;
 }

@@ -172,18 +172,20 @@ __device__ __forceinline__ void store_codes8(uint8_t* row, int64_t c, int64_t co
     }
 }
 
+// What a step's number on the device adds to the thresholds' uppermost counter word; null: nothing.
+__device__ __forceinline__ uint32_t step_word(const int64_t* step) { return step ? (uint32_t)*step : 0u; }
 // Thresholds (Philox words) of eight consecutive elements whose flat indices start at i0.
-__device__ __forceinline__ void thresholds8(uint64_t i0, const PhiloxKeys& K, uint32_t rnd[8]) {
+__device__ __forceinline__ void thresholds8(uint64_t i0, const PhiloxKeys& K, uint32_t later, uint32_t rnd[8]) {
     if ((i0 & 3u) == 0) {
         const uint64_t j = i0 >> 2;
-        philox_rounds((uint32_t)j, (uint32_t)(j >> 32), K, rnd);
-        philox_rounds((uint32_t)(j + 1), (uint32_t)((j + 1) >> 32), K, rnd + 4);
+        philox_rounds((uint32_t)j, (uint32_t)(j >> 32), K, rnd, later);
+        philox_rounds((uint32_t)(j + 1), (uint32_t)((j + 1) >> 32), K, rnd + 4, later);
     } else {
 #pragma unroll 1
         for (int e = 0; e < 8; ++e) {
             uint32_t w[4];
             const uint64_t i = i0 + e, j = i >> 2;
-            philox_rounds((uint32_t)j, (uint32_t)(j >> 32), K, w);
+            philox_rounds((uint32_t)j, (uint32_t)(j >> 32), K, w, later);
             const uint32_t sel = (uint32_t)i & 3u;
             const uint32_t word = sel == 0 ? w[0] : sel == 1 ? w[1] : sel == 2 ? w[2] : w[3];
 #pragma unroll

@@ -76,8 +76,9 @@ struct PhiloxKeys {
     uint32_t tid0, tid1;     // counter words 2 and 3 (tensor_id)
 };
 
-__device__ __forceinline__ void philox_rounds(uint32_t c0, uint32_t c1, const PhiloxKeys& K, uint32_t out[4]) {
-    uint32_t c2 = K.tid0, c3 = K.tid1;
+// later: added to the uppermost counter word.
+__device__ __forceinline__ void philox_rounds(uint32_t c0, uint32_t c1, const PhiloxKeys& K, uint32_t out[4], uint32_t later = 0) {
+    uint32_t c2 = K.tid0, c3 = K.tid1 + later;
 #pragma unroll
     for (int r = 0; r < 10; ++r) {
         const uint64_t p0 = (uint64_t)0xD2511F53u * (uint64_t)c0;    // one wide multiply: hi and lo
@@ -233,7 +234,10 @@ struct BlockSource {
     Blocks coded;                                              // or a block-coded one
     int64_t rows = 0, cols = 0;
 };
-struct BlockRounding { int32_t sr = 0; uint64_t index_offset = 0; uint64_t seed = 0, tensor_id = 0; };
+struct BlockRounding {
+    int32_t sr = 0; uint64_t index_offset = 0; uint64_t seed = 0, tensor_id = 0;
+    const int64_t* step = nullptr;             // device: its value * 2^32 is added to tensor_id
+};
 
 cudaError_t launch_quantize_blocks(const BlockSource& src, const BlockRounding& rnd, const Blocks& rm, const Blocks& tr,
                                    uint32_t* status, cudaStream_t stream);

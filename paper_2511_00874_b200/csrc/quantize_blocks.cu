@@ -157,14 +157,15 @@ struct TileOut {
     int64_t rows, cols;
     uint64_t index_offset;
     PhiloxKeys keys[NOUT];
+    const int64_t* step;                 // of BlockRounding
     uint32_t* status;
 };
 
 // Quantizes the NOUT matrices whose tile is held as v (zeros outside the matrix).  All threads of the CTA call it
-// together, after a barrier that follows the previous call; `next` asks for the next tile.
+// together, after a barrier that follows the previous call; `next` asks for the next tile; later: step_word().
 template <int NOUT, bool SR, bool FULL, typename Next>
 __device__ __forceinline__ void emit_tile(const float (&v)[NOUT][R][8], const TileOut<NOUT>& O, const TilePos& p, int par,
-                                          TileShared<NOUT>* S, Next&& next) {
+                                          TileShared<NOUT>* S, uint32_t later, Next&& next) {
     const int tid = threadIdx.x, lane = tid & 31, l = tid & 15, g = tid >> 4;
     const int64_t r_first = p.r0 + R * g, c_first = p.c0 + 8 * l;
     bool any_tr = false, tiles = false;
@@ -256,7 +257,7 @@ __device__ __forceinline__ void emit_tile(const float (&v)[NOUT][R][8], const Ti
             const float f = __shfl_sync(0xFFFFFFFFu, inv, (lane & 16) + i);
             const float (&x)[8] = v[n][i];
             uint32_t rnd[8] = {};
-            if constexpr (SR) thresholds8(O.index_offset + (uint64_t)(r_first + i) * (uint64_t)O.cols + (uint64_t)c_first, O.keys[n], rnd);
+            if constexpr (SR) thresholds8(O.index_offset + (uint64_t)(r_first + i) * (uint64_t)O.cols + (uint64_t)c_first, O.keys[n], later, rnd);
             const uint32_t w0 = encode4<SR>(x[0], x[1], x[2], x[3], f, f, f, f, rnd[0], rnd[1], rnd[2], rnd[3]);
             const uint32_t w1 = encode4<SR>(x[4], x[5], x[6], x[7], f, f, f, f, rnd[4], rnd[5], rnd[6], rnd[7]);
             if (FULL) *reinterpret_cast<uint2*>(dst) = make_uint2(w0, w1);
@@ -275,7 +276,7 @@ __device__ __forceinline__ void emit_tile(const float (&v)[NOUT][R][8], const Ti
 #pragma unroll
             for (int i = 0; i < R; ++i) {                  // a row's thresholds at a time
                 uint32_t rnd[8];
-                thresholds8(O.index_offset + (uint64_t)(r_first + i) * (uint64_t)O.cols + (uint64_t)c_first, O.keys[n], rnd);
+                thresholds8(O.index_offset + (uint64_t)(r_first + i) * (uint64_t)O.cols + (uint64_t)c_first, O.keys[n], later, rnd);
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
                     w[j] |= (quantize_e4m3<MODE_SR | MODE_E4M3>(v[n][i][j], S->col_inv[n][(j >> 1) * 32 + 2 * l + (j & 1)], rnd[j], 0) & 0xFFu) << (8 * i);
@@ -347,6 +348,7 @@ __global__ void __launch_bounds__(TQ_THREADS, 2 - SR) quantize_blocks_kernel(con
     __shared__ TileShared<1> S;
     using T = std::conditional_t<SRC == 0, float, __nv_bfloat16>;
     const int64_t rows = P.out.rows, cols = P.out.cols;
+    const uint32_t later = SR ? step_word(P.out.step) : 0u;
     int par = 0;
     auto fetch = [&](const TilePos& p, int to) {
         if (p.full) {
@@ -375,8 +377,8 @@ __global__ void __launch_bounds__(TQ_THREADS, 2 - SR) quantize_blocks_kernel(con
             fetch(np, par ^ 1);
             if (SRC == 2 && threadIdx.x < QBLK && np.full) next_scale = fetch_scale(P.src.coded, np, threadIdx.x);
         };
-        if (p.full) emit_tile<1, SR, true>(v, P.out, p, par, &S, next);
-        else emit_tile<1, SR, false>(v, P.out, p, par, &S, next);
+        if (p.full) emit_tile<1, SR, true>(v, P.out, p, par, &S, later, next);
+        else emit_tile<1, SR, false>(v, P.out, p, par, &S, later, next);
         if (SRC == 2 && threadIdx.x < QBLK) coded_scales(ahead, par ^ 1)[threadIdx.x] = next_scale;
         tile = next_tile;
         p = np;
@@ -401,6 +403,7 @@ __global__ void __launch_bounds__(TQ_THREADS, 1) glu_bwd_kernel(const __grid_con
     uint8_t* ahead_g = ahead_dh + matrix_slot<T>();
     uint8_t* ahead_u = ahead_g + coded_slot();
     const int64_t rows = P.out.rows, cols = P.out.cols;
+    const uint32_t later = SR ? step_word(P.out.step) : 0u;
     int par = 0;
     auto fetch = [&](const TilePos& p, int to) {
         if (p.full) {
@@ -452,8 +455,8 @@ __global__ void __launch_bounds__(TQ_THREADS, 1) glu_bwd_kernel(const __grid_con
             fetch(np, par ^ 1);
             if (brings && np.full) next_scale = fetch_scale(scale_of, np, scale_row);
         };
-        if (p.full) emit_tile<3, SR, true>(v, P.out, p, par, S, next);
-        else emit_tile<3, SR, false>(v, P.out, p, par, S, next);
+        if (p.full) emit_tile<3, SR, true>(v, P.out, p, par, S, later, next);
+        else emit_tile<3, SR, false>(v, P.out, p, par, S, later, next);
         if (brings) coded_scales(scale_slot, par ^ 1)[scale_row] = next_scale;
         tile = next_tile;
         p = np;
@@ -506,7 +509,8 @@ cudaError_t launch_quantize_blocks(const BlockSource& src, const BlockRounding& 
     QuantBlocksParams P;
     P.src = src;
     P.out.rm[0] = rm; P.out.tr[0] = tr; P.out.rows = src.rows; P.out.cols = src.cols;
-    P.out.index_offset = rnd.index_offset; P.out.keys[0] = make_philox_keys(rnd.seed, rnd.tensor_id); P.out.status = status;
+    P.out.index_offset = rnd.index_offset; P.out.keys[0] = make_philox_keys(rnd.seed, rnd.tensor_id); P.out.step = rnd.step;
+    P.out.status = status;
     P.tiles = tiles_of(src.rows, src.cols); P.tiles_c = (uint32_t)((src.cols + QBLK - 1) / QBLK);
     P.vec = src.coded.codes ? 1 : (uintptr_t)src.x % 16 == 0 && src.ld % (src.dt == SRQ_F32 ? 4 : 8) == 0;
     const dim3 grid(persistent_grid(P.tiles, (uint32_t)sms * (rnd.sr ? 1 : 2))), block(TQ_THREADS);
@@ -539,7 +543,7 @@ cudaError_t launch_glu_bwd(const void* dh, int32_t dt, int64_t ld_dh, const Bloc
     GluBwdParams P;
     P.dh = dh; P.ld_dh = ld_dh; P.gate = gate; P.up = up;
     P.out.rm[0] = dg; P.out.rm[1] = du; P.out.tr[0] = dg_t; P.out.tr[1] = du_t; P.out.tr[2] = h_t;
-    P.out.rows = T; P.out.cols = F; P.out.index_offset = rnd.index_offset; P.out.status = status;
+    P.out.rows = T; P.out.cols = F; P.out.index_offset = rnd.index_offset; P.out.step = rnd.step; P.out.status = status;
     for (int i = 0; i < 3; ++i) P.out.keys[i] = make_philox_keys(rnd.seed, rnd.tensor_id + (uint64_t)i);
     P.tiles = tiles_of(T, F); P.tiles_c = (uint32_t)((F + QBLK - 1) / QBLK);
     P.vec = (uintptr_t)dh % 16 == 0 && ld_dh % (dt == SRQ_F32 ? 4 : 8) == 0;

@@ -285,7 +285,7 @@ __device__ __forceinline__ void norm_emit(const NormFwdParams& P, int64_t row, i
             if (block_nonfinite(m)) note(a.status, SRQ_ERR_NONFINITE);
             if ((c & (QBLK - 1)) == 0) a.y.scale[row * a.y.ld_scale + c / QBLK] = step;
             uint32_t rnd[8] = {};
-            if constexpr (SR) thresholds8(a.rnd.index_offset + (uint64_t)row * (uint64_t)a.cols + (uint64_t)c, P.keys, rnd);
+            if constexpr (SR) thresholds8(a.rnd.index_offset + (uint64_t)row * (uint64_t)a.cols + (uint64_t)c, P.keys, step_word(a.rnd.step), rnd);
             const uint32_t lo = encode4<SR>(y[0], y[1], y[2], y[3], inv, inv, inv, inv, rnd[0], rnd[1], rnd[2], rnd[3]);
             const uint32_t hi = encode4<SR>(y[4], y[5], y[6], y[7], inv, inv, inv, inv, rnd[4], rnd[5], rnd[6], rnd[7]);
             store_codes8(a.y.codes + row * a.y.ld, c, a.cols, lo, hi);

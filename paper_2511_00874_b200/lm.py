@@ -14,6 +14,7 @@ learning rate live on the device).
 """
 from __future__ import annotations
 
+import dataclasses
 from typing import Optional
 
 import torch
@@ -104,8 +105,11 @@ class TokenModel:
 
     def backward(self, ids: torch.Tensor, q: B.QSpec = B.BLOCK_RNE) -> None:
         """Gradients of every weight from the gradient at the logits; ``q``: how gradients are rounded, with tensor_id ..
-        tensor_id + 4 * (layers + 1) under stochastic rounding."""
+        tensor_id + 4 * (layers + 1) under stochastic rounding, and thresholds of their own for every step (``self.step``, read on
+        the device, so that replays of a recorded step draw new ones too)."""
         s = self.status
+        if q.round == B.SR and q.step is None:
+            q = dataclasses.replace(q, step=self.step)
         at = lambda i: GatedMLP._stream(q, 4 * i)  # noqa: E731
         B.srq_quantize_blocks(self.logits, q, self.dl, self.dl_t, s)
         B.srq_quantize_blocks(self.y, B.BLOCK_RNE, None, self.y_t, s)

@@ -16,6 +16,7 @@ writes the checkpoints; a program that only generates calls the operators itself
 """
 from __future__ import annotations
 
+import dataclasses
 from typing import Optional
 
 import torch
@@ -55,7 +56,7 @@ class GatedMLP:
     @staticmethod
     def _stream(q: B.QSpec, i: int) -> B.QSpec:
         """q with the thresholds of the i-th stream after its own."""
-        return B.QSpec(q.bits, q.scale, q.round, q.seed, q.tensor_id + i, q.index_offset, q.format)
+        return dataclasses.replace(q, tensor_id=q.tensor_id + i)
 
     def load(self, w: torch.Tensor, wg: torch.Tensor, wu: torch.Tensor, wd: torch.Tensor, q: B.QSpec = B.BLOCK_RNE) -> None:
         """Codes the weights once per step: wg, wu [hidden, features], wd [features, hidden]; w is the norm's.  Under
@@ -76,7 +77,8 @@ class GatedMLP:
     def backward(self, dout: torch.Tensor, dr: Optional[torch.Tensor] = None, q: B.QSpec = B.BLOCK_RNE) -> torch.Tensor:
         """Gradient at x (and residual) from the gradients at out and r; the weights' gradients land in ``dwg``,
         ``dwu``, ``dwd`` and ``dw``.  ``q``: how gradients are rounded (block_sr(seed, tensor_id) for stochastic
-        rounding; tensor_id .. tensor_id + 3 are used)."""
+        rounding; tensor_id .. tensor_id + 3 are used; with a step on the device where the pass is recorded, or every
+        replay rounds an element with the same threshold)."""
         F = self.shape[2]
         s = self.status
         B.srq_quantize_blocks(dout, q, self.dout, self.dout_t, s)
