@@ -54,6 +54,7 @@ class TokenModel:
         tensors = lambda ws, gs: B.AdamTensors([B.AdamTensor(w, g, *B.new_adam_state(w, state_bits)) for w, g in zip(ws, gs)])  # noqa: E731
         self.decaying, self.plain = tensors(weights, grads), tensors(self.norms, norm_grads)
         self.step, self.lr = torch.zeros(1, dtype=torch.int64, device=device), torch.zeros(1, device=device)
+        self.next_step = torch.zeros_like(self.step)
 
     def initialise(self, std: float = 0.02) -> None:
         """Weights from N(0, std^2), norms one."""
@@ -123,10 +124,15 @@ class TokenModel:
 
     def update(self, beta1: float = 0.9, beta2: float = 0.95, eps: float = 1e-8, weight_decay: float = 0.1,
                grad_scale: Optional[torch.Tensor] = None) -> None:
-        """AdamW step number ``self.step`` + 1 with the learning rate in ``self.lr``, and the new weights' codes."""
-        self.step.add_(1)
-        kw = dict(lr=0.0, beta1=beta1, beta2=beta2, eps=eps, seed=self.seed, lr_device=self.lr, step_device=self.step, grad_scale=grad_scale,
+        """AdamW step number ``self.step`` + 1 with the learning rate in ``self.lr``, and the new weights' codes.  A step that is refused
+        because the learning rate or ``grad_scale`` is not finite changes nothing and is not counted: ``self.step`` stays."""
+        torch.add(self.step, 1, out=self.next_step)
+        kw = dict(lr=0.0, beta1=beta1, beta2=beta2, eps=eps, seed=self.seed, lr_device=self.lr, step_device=self.next_step, grad_scale=grad_scale,
                   device_status=self.status)
         B.srq_adamw_step(self.decaying, weight_decay=weight_decay, tensor_id=1 << 16, **kw)
         B.srq_adamw_step(self.plain, weight_decay=0.0, tensor_id=(1 << 16) + len(self.decaying), **kw)
+        done = self.lr.isfinite()
+        if grad_scale is not None:
+            done &= grad_scale.view(-1)[:1].isfinite()
+        self.step.add_(done)
         self.load()

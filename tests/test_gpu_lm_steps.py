@@ -1,0 +1,83 @@
+"""GPU: what lm.TokenModel does with steps that are refused, with rows that belong to no answer and with what its parts report, and its
+gradients under the policy loss."""
+import math
+
+import pytest
+import torch
+
+import paper_2511_00874_b200 as srq
+from paper_2511_00874_b200 import binding, lm
+
+pytestmark = pytest.mark.gpu
+T, V, K, F = 130, 300, 256, 384
+
+
+def model(layers=1, **kw):
+    m = lm.TokenModel(T, V, K, F, layers, embedding_scale=50.0, seed=3, **kw)
+    m.initialise(0.03)
+    m.lr.fill_(1e-3)
+    return m
+
+
+def batch(seed=0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    pick = lambda: torch.randint(0, V, (T,), generator=g, device="cuda")  # noqa: E731
+    return pick(), pick(), torch.full((T,), 1.0 / T, device="cuda")
+
+
+def state(m):
+    out = [m.table, m.head, *m.norms] + [w for layer in m.layers for w in layer] + [m.step]
+    for group in (m.decaying, m.plain):
+        out += [x for t in group.tensors for x in (t.m, t.v, t.m_step, t.v_step) if x is not None]
+    return out
+
+
+def step(m, args, grad_scale=None):
+    ids, targets, weight = args
+    m.forward(ids)
+    m.supervised(targets, weight)
+    m.backward(ids, srq.block_sr(5, 10))
+    m.update(grad_scale=grad_scale)
+
+
+@pytest.mark.parametrize("state_bits", [8, 32])
+@pytest.mark.parametrize("what", ["grad_scale", "lr"])
+def test_a_refused_update_is_not_counted(what, state_bits):
+    args, one = batch(), torch.ones(1, device="cuda")
+    plain, other = model(state_bits=state_bits), model(state_bits=state_bits)
+    for bad in (math.nan, math.inf, -math.inf):
+        before = [x.clone() for x in state(other)]
+        if what == "lr":
+            other.lr.fill_(bad)
+            step(other, args)
+            other.lr.fill_(1e-3)
+        else:
+            step(other, args, torch.tensor([bad], device="cuda"))
+        assert other.status.item() == binding.ERR_NONFINITE
+        for a, b in zip(state(other), before):
+            assert torch.equal(a, b)
+        other.status.zero_()
+        step(plain, args, one)
+        step(other, args, one)
+        assert other.status.item() == 0
+        for a, b in zip(state(plain), state(other)):
+            assert torch.equal(a, b)
+    assert plain.step.item() == 3
+
+
+def test_recorded_updates_count_themselves():
+    args, scale = batch(1), torch.ones(1, device="cuda")
+    eager, recorded = model(), model()
+    g = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g):
+        step(recorded, args, scale)
+    for value in (math.nan, 0.5, math.inf, math.nan, 2.0, 1.0):
+        scale.fill_(value)
+        g.replay()
+        if math.isfinite(value):
+            step(eager, args, scale)
+    torch.cuda.synchronize()
+    assert recorded.step.item() == 3 and recorded.status.item() == binding.ERR_NONFINITE
+    for a, b in zip(state(eager), state(recorded)):
+        assert torch.equal(a, b)
