@@ -76,8 +76,10 @@ class QSpec:
 
     def c(self) -> _QSpec:
         step = self.step
-        if step is not None and (step.dtype is not torch.int64 or step.numel() != 1 or not step.is_cuda):
-            raise ValueError("step must be an int64 CUDA tensor of one element")
+        if step is not None:
+            if step.dtype is not torch.int64 or step.numel() != 1 or not step.is_cuda:
+                raise ValueError("step must be an int64 CUDA tensor of one element")
+            _here(step)
         return _QSpec(self.bits, self.scale, self.round, self.format, self.seed, self.tensor_id,
                       self.index_offset, None if self.absmax is None else self.absmax.data_ptr(), None if step is None else step.data_ptr())
 
@@ -792,10 +794,12 @@ def _whole(t: torch.Tensor, name: str, n: Optional[int] = None):
     return t.data_ptr(), wide
 
 
-def _here(t: torch.Tensor, name: str) -> None:
-    """The calls go to the current device's current stream: their tensors have to live on that device."""
-    if t.get_device() != torch._C._cuda_getDevice():
-        raise ValueError(f"{name} is on another device than the current one")
+def _here(*tensors: Optional[torch.Tensor]) -> None:
+    """The calls go to the current device's current stream: all their operands have to live on that device."""
+    here = torch._C._cuda_getDevice()
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            raise ValueError(f"an operand of shape {tuple(t.shape)} and {t.dtype} is on device {t.get_device()}, the current device is {here}")
 
 
 def _workspace(ws: Optional[torch.Tensor], need: int, device):
@@ -811,10 +815,10 @@ def srq_embedding_fwd(table: torch.Tensor, ids: torch.Tensor, out: torch.Tensor,
                       device_status: Optional[torch.Tensor] = None) -> None:
     """out[t] = scale * table[ids[t]]; an id below zero is padding and gives a row of zeros."""
     pi, wide = _whole(ids, "ids")
-    _here(ids, "ids")
     T, (rows, cols) = ids.numel(), table.shape
     pt, ldt = _mat(table, "table")
     po, ldo = _mat(out, "out", (T, cols))
+    _here(table, ids, out, device_status)
     st = lib().srq_embedding_fwd(pt, _dtype_of(table), rows, cols, ldt, pi, wide, T, scale, po, _dtype_of(out), ldo, _status_word(device_status), _stream())
     _check(st, "srq_embedding_fwd")
 
@@ -830,10 +834,10 @@ def srq_embedding_bwd(dout: torch.Tensor, ids: torch.Tensor, dtable: torch.Tenso
     T, cols = dout.shape
     rows = dtable.shape[0]
     pi, wide = _whole(ids, "ids", T)
-    _here(ids, "ids")
     pd, ldd = _mat(dout, "dout")
     pt, ldt = _mat(dtable, "dtable", (rows, cols))
     pw, nb, ws = _workspace(ws, srq_embedding_workspace_bytes(T, rows, cols) if ws is None else 0, dout.device)
+    _here(dout, ids, dtable, ws, device_status)
     st = lib().srq_embedding_bwd(pd, _dtype_of(dout), T, cols, ldd, pi, wide, rows, scale, pt, _dtype_of(dtable), ldt, int(accumulate), pw, nb,
                                  _status_word(device_status), _stream())
     _check(st, "srq_embedding_bwd")
@@ -844,7 +848,6 @@ def _logits(logits: torch.Tensor, targets: torch.Tensor):
     rows, classes = logits.shape
     px, ld = _mat(logits, "logits")
     pt, wide = _whole(targets, "targets", rows)
-    _here(targets, "targets")
     return px, _dtype_of(logits), rows, classes, ld, pt, wide
 
 
@@ -866,6 +869,7 @@ def srq_logprob_fwd(logits: torch.Tensor, targets: torch.Tensor, logp: torch.Ten
                     device_status: Optional[torch.Tensor] = None) -> None:
     """logp[r] = log softmax(logits[r] / temperature)[targets[r]] and lse[r]; 0 for rows whose target is below zero."""
     x = _logits(logits, targets)
+    _here(logits, targets, logp, lse, device_status)
     st = lib().srq_logprob_fwd(*x, temperature, _vec(logp, "logp", x[2]), _vec(lse, "lse", x[2]), _status_word(device_status), _stream())
     _check(st, "srq_logprob_fwd")
 
@@ -875,6 +879,7 @@ def srq_logprob_bwd(logits: torch.Tensor, targets: torch.Tensor, lse: torch.Tens
     """Gradient at the logits from the gradient at logp; ``dlogits`` may be ``logits``."""
     x = _logits(logits, targets)
     pd, ldd = _mat(dlogits, "dlogits", logits.shape, logits.dtype)
+    _here(logits, targets, lse, dlogp, dlogits, device_status)
     st = lib().srq_logprob_bwd(*x, temperature, _vec(lse, "lse", x[2]), _vec(dlogp, "dlogp", x[2]), pd, ldd, _status_word(device_status), _stream())
     _check(st, "srq_logprob_bwd")
 
@@ -889,6 +894,7 @@ def srq_policy_loss(logits: torch.Tensor, targets: torch.Tensor, logp_old: torch
     n = x[2]
     pd, ldd = _mat(dlogits, "dlogits", logits.shape, logits.dtype)
     po, pa, pw, pr, prow, plogp = _vecs(n, logp_old=logp_old, advantage=advantage, weight=weight, logp_ref=logp_ref, row_loss=row_loss, logp=logp)
+    _here(logits, targets, logp_old, advantage, weight, logp_ref, row_loss, loss, logp, dlogits, device_status)
     st = lib().srq_policy_loss(*x, po, pa, pw, pr, _Policy(temperature, clip_low, clip_high, kl_coef), prow, _vec(loss, "loss", 1), plogp, pd, ldd,
                                _status_word(device_status), _stream())
     _check(st, "srq_policy_loss")
@@ -912,6 +918,7 @@ def srq_preference_loss(logits: torch.Tensor, targets: torch.Tensor, logp_ref: t
     pairs = offsets.numel() // 2
     pd, ldd = _mat(dlogits, "dlogits", logits.shape, logits.dtype)
     pw, nb, ws = _workspace(ws, srq_preference_workspace_bytes(n) if ws is None else 0, logits.device)
+    _here(logits, targets, logp_ref, offsets, pair_loss, loss, logp, dlogits, ws, device_status)
     st = lib().srq_preference_loss(*x, _vec(logp_ref, "logp_ref", n), po, wide, pairs, _Preference(temperature, beta, label_smoothing),
                                    _vec(pair_loss, "pair_loss", pairs), _vec(loss, "loss", 1), _vec(logp, "logp", n), pd, ldd, pw, nb,
                                    _status_word(device_status), _stream())
@@ -951,6 +958,7 @@ class AdamTensors:
         t0 = self.tensors[0] if self.tensors else None
         self.param_dtype, self.grad_dtype = (F32, F32) if t0 is None else (_dtype_of(t0.param), _dtype_of(t0.grad))
         self.bits = 32 if t0 is None or t0.m.dtype is torch.float32 else 8
+        self.device = None if t0 is None else t0.param.get_device()
         self.c = (_AdamTensor * max(1, len(self.tensors)))()
         state, coded, check = torch.float32 if self.bits == 32 else torch.uint8, self.bits == 8, self._check
         for i, t in enumerate(self.tensors):
@@ -960,10 +968,11 @@ class AdamTensors:
             self.c[i] = _AdamTensor(param, None, m, v, *steps, n)
             self.set_grad(i, t.grad)
 
-    @staticmethod
-    def _check(i, name, x, dtype, size):
+    def _check(self, i, name, x, dtype, size):
         if x is None or x.dtype is not dtype or x.numel() != size or not x.is_cuda or not x.is_contiguous():
             raise ValueError(f"tensor {i}: {name} must hold {size} contiguous values of {dtype} on the device")
+        if x.get_device() != self.device:
+            raise ValueError(f"tensor {i}: {name} is on device {x.get_device()}, the list's first weight on device {self.device}")
         return x.data_ptr()
 
     def set_grad(self, i: int, grad: torch.Tensor) -> None:
@@ -984,7 +993,7 @@ def srq_adamw_step(tensors: AdamTensors, lr: float, beta1: float = 0.9, beta2: f
     if step_device is not None and (step_device.dtype is not torch.int64 or not step_device.is_cuda):
         raise ValueError("step_device must be an int64 CUDA tensor of one element")
     if tensors.tensors:
-        _here(tensors.tensors[0].param, "param")
+        _here(tensors.tensors[0].param, lr_device, step_device, grad_scale, device_status)
     h = _AdamW(lr, beta1, beta2, eps, weight_decay, step, round, seed, tensor_id, _vec(lr_device, "lr_device", 1), _ptr(step_device),
                _vec(grad_scale, "grad_scale", 1))
     st = lib().srq_adamw_step(tensors.c, len(tensors.tensors), tensors.param_dtype, tensors.grad_dtype, tensors.bits, h, _status_word(device_status), _stream())
