@@ -650,7 +650,7 @@ def _bref(b: Optional[Blocks], shape, name):
 def _status_word(device_status: Optional[torch.Tensor]):
     if device_status is None:
         return None
-    if device_status.dtype != torch.int32 or not device_status.is_cuda:
+    if device_status.dtype != torch.int32 or device_status.numel() < 1 or not device_status.is_cuda:
         raise TypeError("device_status must be an int32 CUDA tensor of one element")
     return device_status.data_ptr()
 
@@ -990,7 +990,7 @@ def srq_adamw_step(tensors: AdamTensors, lr: float, beta1: float = 0.9, beta2: f
                    device_status: Optional[torch.Tensor] = None) -> None:
     """One AdamW step in place over all tensors; ``round``: SR or RNE, of bfloat16 weights.  ``lr_device`` (float32),
     ``step_device`` (int64) and ``grad_scale`` (float32) are device scalars that are read when the step runs."""
-    if step_device is not None and (step_device.dtype is not torch.int64 or not step_device.is_cuda):
+    if step_device is not None and (step_device.dtype is not torch.int64 or step_device.numel() < 1 or not step_device.is_cuda):
         raise ValueError("step_device must be an int64 CUDA tensor of one element")
     if tensors.tensors:
         _here(tensors.tensors[0].param, lr_device, step_device, grad_scale, device_status)

@@ -97,3 +97,12 @@ def test_the_step_of_a_quantization_point_is_on_the_current_device(stub):
     B.block_sr(1, 2, step=on(0, 1, dtype=I)).c()
     with pytest.raises(ValueError, match="device"):
         B.block_sr(1, 2, step=on(1, 1, dtype=I)).c()
+
+
+def test_scalars_without_an_element_are_refused(stub):
+    # (their pointer is null, which would mean that the argument was not given)
+    tensors = B.AdamTensors([entry(200)])
+    for name, dtype, error in (("lr_device", torch.float32, ValueError), ("step_device", I, ValueError), ("grad_scale", torch.float32, ValueError), ("device_status", S, TypeError)):
+        with pytest.raises(error):
+            B.srq_adamw_step(tensors, 1e-3, **{name: on(0, 0, dtype=dtype)})
+    assert stub.calls == 0
