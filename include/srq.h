@@ -553,13 +553,14 @@ size_t srq_preference_workspace_bytes(int64_t rows);
  * and dlogits is the gradient of loss.  logp_ref[rows] comes from srq_logprob_fwd on the reference model's logits.  Rows whose
  * target is below zero or out of range (reported) do not count: logp and dlogits are 0, logp_ref is not read.  Rows before
  * offsets[0] and from offsets[2 * pairs] on belong to no answer: their logits are not read, and logp and dlogits are left as
- * they were.  Offsets that fall, or lie outside, are reported, and what the call then writes within its arrays is unspecified.
+ * they were, or become 0 (clear_rest: what a backward pass over all rows needs).  Offsets that fall, or lie outside, are reported, and what the call then writes within its arrays is unspecified.
  * pair_loss [pairs] and logp [rows] are required; loss [1] and dlogits may be NULL.  dlogits may be
  * the logits themselves. */
 typedef struct {
     float temperature;       /* 2^-100 .. 2^100 */
     float beta;              /* finite */
     float label_smoothing;   /* 0 .. 1 */
+    int32_t clear_rest;      /* 1: logp and dlogits of rows that belong to no answer become 0; 0: they are left as they were */
 } srq_preference_t;
 srq_status_t srq_preference_loss(const void *logits, srq_dtype_t dt, int64_t rows, int64_t classes, int64_t ld,
                                  const void *targets, srq_index_t target_t, const float *logp_ref,

@@ -94,7 +94,7 @@ class _Policy(ctypes.Structure):
 
 
 class _Preference(ctypes.Structure):
-    _fields_ = [(n, ctypes.c_float) for n in ("temperature", "beta", "label_smoothing")]
+    _fields_ = [(n, ctypes.c_float) for n in ("temperature", "beta", "label_smoothing")] + [("clear_rest", ctypes.c_int32)]
 
 
 class _AdamTensor(ctypes.Structure):
@@ -907,9 +907,10 @@ def srq_preference_workspace_bytes(rows: int) -> int:
 def srq_preference_loss(logits: torch.Tensor, targets: torch.Tensor, logp_ref: torch.Tensor, offsets: torch.Tensor, pair_loss: torch.Tensor,
                         loss: Optional[torch.Tensor], logp: torch.Tensor, dlogits: Optional[torch.Tensor] = None, beta: float = 0.1,
                         label_smoothing: float = 0.0, temperature: float = 1.0, ws: Optional[torch.Tensor] = None,
-                        device_status: Optional[torch.Tensor] = None) -> None:
+                        device_status: Optional[torch.Tensor] = None, clear_rest: bool = False) -> None:
     """Preference loss over pairs of answers (rows offsets[2 i] .. of the chosen, offsets[2 i + 1] .. of the rejected one) and its
-    gradient at the logits; ``dlogits`` may be ``logits``."""
+    gradient at the logits; ``dlogits`` may be ``logits``.  ``logp`` and ``dlogits`` of rows that belong to no answer are left as they
+    are, or become zero (``clear_rest``)."""
     x = _logits(logits, targets)
     n = x[2]
     po, wide = _whole(offsets, "offsets")
@@ -919,7 +920,7 @@ def srq_preference_loss(logits: torch.Tensor, targets: torch.Tensor, logp_ref: t
     pd, ldd = _mat(dlogits, "dlogits", logits.shape, logits.dtype)
     pw, nb, ws = _workspace(ws, srq_preference_workspace_bytes(n) if ws is None else 0, logits.device)
     _here(logits, targets, logp_ref, offsets, pair_loss, loss, logp, dlogits, ws, device_status)
-    st = lib().srq_preference_loss(*x, _vec(logp_ref, "logp_ref", n), po, wide, pairs, _Preference(temperature, beta, label_smoothing),
+    st = lib().srq_preference_loss(*x, _vec(logp_ref, "logp_ref", n), po, wide, pairs, _Preference(temperature, beta, label_smoothing, int(clear_rest)),
                                    _vec(pair_loss, "pair_loss", pairs), _vec(loss, "loss", 1), _vec(logp, "logp", n), pd, ldd, pw, nb,
                                    _status_word(device_status), _stream())
     _check(st, "srq_preference_loss")

@@ -126,6 +126,7 @@ srq_status_t srq_preference_loss(const void* logits, srq_dtype_t dt, int64_t row
     const srq_preference_t& h = *preference;
     SRQ_TRY(check_logits(logits, dt, rows, classes, ld, targets, target_t, h.temperature, device_status));
     if (!isfinite(h.beta) || !(h.label_smoothing >= 0.0f && h.label_smoothing <= 1.0f) || pairs < 0 || !known_index(offset_t)) return SRQ_ERR_INVALID_ARG;
+    if (h.clear_rest != 0 && h.clear_rest != 1) return SRQ_ERR_INVALID_ARG;
     if (pairs > kMaxExtent / 2) return SRQ_ERR_UNSUPPORTED;
     if ((rows && (!logp_ref || !logp)) || (pairs && (!pair_loss || !offsets))) return SRQ_ERR_INVALID_ARG;
     if (!aligned_to(logp_ref, 4) || !aligned_to(offsets, index_bytes(offset_t)) || !aligned_to(pair_loss, 4) || !aligned_to(loss, 4) || !aligned_to(logp, 4))
@@ -134,7 +135,13 @@ srq_status_t srq_preference_loss(const void* logits, srq_dtype_t dt, int64_t row
     if (!ws || !aligned_to(ws, 256)) return SRQ_ERR_INVALID_ARG;
     if (ws_bytes < srq_preference_workspace_bytes(rows)) return SRQ_ERR_WORKSPACE;
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    if (pairs == 0) return loss ? status_of(cudaMemsetAsync(loss, 0, 4, st)) : SRQ_OK;
+    if (pairs == 0) {                                          // no row belongs to an answer
+        const size_t esize = dt == SRQ_F32 ? 4 : 2;
+        if (h.clear_rest && rows) SRQ_TRY(status_of(cudaMemsetAsync(logp, 0, (size_t)rows * 4, st)));
+        if (h.clear_rest && dlogits && !empty(rows, classes))
+            SRQ_TRY(status_of(cudaMemset2DAsync(dlogits, (size_t)ld_dlogits * esize, 0, (size_t)classes * esize, (size_t)rows, st)));
+        return loss ? status_of(cudaMemsetAsync(loss, 0, 4, st)) : SRQ_OK;
+    }
     const LogitsArgs a = {logits, dt, rows, classes, ld, targets, target_t, h.temperature, device_status};
     const PreferenceArgs p = {logp_ref, offsets, offset_t, pairs, h, pair_loss, loss, logp, dlogits, ld_dlogits};
     return status_of(launch_preference(a, p, ws, st));

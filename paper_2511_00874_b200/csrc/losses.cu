@@ -50,6 +50,7 @@ struct RowParams {
     float clip_lo, clip_hi, kl;                 // bounds of the ratio
     float* row_loss;
     const void* offsets; int32_t off_wide; int64_t last;      // rows outside offsets[0] .. offsets[last] are left alone; may be null
+    int32_t clear_rest;                         // or do not count
 };
 
 // A row's elements as vectors of 16 bytes at 16-byte boundaries; the first and the last vector may lie partly outside.
@@ -236,10 +237,12 @@ __global__ void __launch_bounds__(NT, ROW_CTAS<NT>) row_kernel(const RowParams P
     const int rank = (int)(blockIdx.x - row * P.parts), tid = threadIdx.x;
     // the second walk over the same logits begins with the rows that the first one read last: some are still in L2
     if (MODE == ROW_GRAD) row = P.rows - 1 - row;
+    bool rest = false;
     if (P.offsets) {
-        if (row < whole_at(P.offsets, P.off_wide, 0) || row >= whole_at(P.offsets, P.off_wide, P.last)) return;     // the whole cluster
+        rest = row < whole_at(P.offsets, P.off_wide, 0) || row >= whole_at(P.offsets, P.off_wide, P.last);
+        if (rest && !P.clear_rest) return;                     // the whole cluster
     }
-    const int64_t target = whole_at(P.targets, P.wide, row);
+    const int64_t target = rest ? -1 : whole_at(P.targets, P.wide, row);
     bool counts = target >= 0 && target < P.classes;
     if (target >= P.classes && tid == 0 && rank == 0) note(P.status, SRQ_ERR_INVALID_ARG);
     float weight = 1.0f;
@@ -614,7 +617,7 @@ cudaError_t launch_preference(const LogitsArgs& a, const PreferenceArgs& p, void
     RowParams P = row_params(a);
     P.stat = reinterpret_cast<float2*>(ws);
     float* dlogp = reinterpret_cast<float*>((char*)ws + align_up((size_t)a.rows * 8));
-    P.logp = p.logp; P.offsets = p.offsets; P.off_wide = p.offset_t == SRQ_I64; P.last = 2 * p.pairs;
+    P.logp = p.logp; P.offsets = p.offsets; P.off_wide = p.offset_t == SRQ_I64; P.last = 2 * p.pairs; P.clear_rest = p.h.clear_rest;
     cudaError_t e = a.rows ? launch_rows<ROW_LOGP>(P, a.dt, st) : cudaSuccess;
     if (e != cudaSuccess) return e;
     PairParams Q = {};

@@ -99,9 +99,9 @@ class TokenModel:
         return self.loss
 
     def preference(self, targets: torch.Tensor, logp_ref: torch.Tensor, offsets: torch.Tensor, pair_loss: torch.Tensor, **kw) -> torch.Tensor:
-        """Preference loss over pairs of answers (srq_preference_loss); logits become gradients.  The answers fill all rows."""
+        """Preference loss over pairs of answers (srq_preference_loss); logits become gradients, zero for tokens that belong to no answer."""
         B.srq_preference_loss(self.logits, targets, logp_ref, offsets, pair_loss, self.loss, self.logp, self.logits, ws=self.ws,
-                              device_status=self.status, **kw)
+                              device_status=self.status, clear_rest=True, **kw)
         return self.loss
 
     def backward(self, ids: torch.Tensor, q: B.QSpec = B.BLOCK_RNE) -> None:
