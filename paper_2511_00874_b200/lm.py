@@ -46,7 +46,9 @@ class TokenModel:
         self.dtable, self.dhead, self.dnorm = e(V, K, d=f), e(V, K, d=f), e(K, d=f)
         self.logp, self.lse, self.row_loss, self.loss = e(T, d=f), e(T, d=f), e(T, d=f), e(1, d=f)
         self.ws = B.new_workspace(max(B.srq_embedding_workspace_bytes(T, V, K), B.srq_rmsnorm_workspace_bytes(T, K), B.srq_preference_workspace_bytes(T)), device)
-        self.status = torch.zeros(1, dtype=torch.int32, device=device)
+        self.status = torch.zeros(1, dtype=torch.int32, device=device)      # what any part of a step reports, the layers included
+        for b in self.blocks:
+            b.status = self.status
         # update
         weights = [self.table, self.head] + [w for layer in self.layers for w in layer]
         grads = [self.dtable, self.dhead] + [g for b in self.blocks for g in (b.dwg, b.dwu, b.dwd)]

@@ -81,3 +81,21 @@ def test_recorded_updates_count_themselves():
     assert recorded.step.item() == 3 and recorded.status.item() == binding.ERR_NONFINITE
     for a, b in zip(state(eager), state(recorded)):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("where", ["gate", "up", "down", "gradient"])
+def test_what_the_layers_report_reaches_the_model(where):
+    # the last layer's codes hold a NaN: found while they are coded, before any product
+    m = model(2)
+    args = batch(2)
+    step(m, args)
+    assert m.status.item() == 0
+    if where == "gradient":
+        m.forward(args[0])
+        m.supervised(*args[1:])
+        m.dy.zero_()
+        m.blocks[1].backward(torch.full((T, K), math.nan, dtype=torch.bfloat16, device="cuda"))
+    else:
+        m.layers[1][("gate", "up", "down").index(where)][5, 7] = math.nan
+        m.load()
+    assert m.status.item() == binding.ERR_NONFINITE
