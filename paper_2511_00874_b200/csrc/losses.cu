@@ -20,6 +20,7 @@
 // and the range is binary32's (a gradient that is given lse alone: LSE_EXACT below).  k is a sum of two numbers where probabilities are added up (one alone would shift every log-probability
 // of a row the same way, which shows in sums over rows).  2^y is the hardware's approximation (2 units); sums are binary32, of at
 // most 16384 terms in 64 partial sums per warp.
+#include <float.h>
 #include <math.h>
 
 #include "train.cuh"
@@ -351,7 +352,9 @@ __global__ void __launch_bounds__(NT, ROW_CTAS<NT>) row_kernel(const RowParams P
             float loss = 0.0f;
             if constexpr (MODE == ROW_POLICY) {
                 if (counts) {
-                    const float rho = expf(logp - old), a = rho * adv, b = fminf(fmaxf(rho, P.clip_lo), P.clip_hi) * adv;
+                    float rho = expf(logp - old);
+                    if (adv == 0.0f && rho == SRQ_INF) rho = FLT_MAX;          // the ratio is finite, and so its product with 0 is 0
+                    const float a = rho * adv, b = fminf(fmaxf(rho, P.clip_lo), P.clip_hi) * adv;
                     loss = a <= b ? -a : -b;
                     r.c = a <= b ? -a : 0.0f;
                     if (a != a) loss = r.c = a;                // NaN stays NaN
@@ -603,7 +606,8 @@ static cudaError_t launch_loss_sum(const float* x, int64_t n, double scale, floa
 }
 cudaError_t launch_policy(const LogitsArgs& a, const PolicyArgs& p, cudaStream_t st) {
     RowParams P = row_params(a);
-    P.logp = p.logp; P.dx = p.dx; P.ldx = p.ldx; P.old = p.old; P.advantage = p.advantage; P.weight = p.weight; P.ref = p.ref;
+    P.logp = p.logp; P.dx = p.dx; P.ldx = p.ldx; P.old = p.old; P.advantage = p.advantage; P.weight = p.weight;
+    P.ref = p.h.kl_coef != 0.0f ? p.ref : nullptr;             // (0 times an exponential that left binary32 would be NaN)
     P.clip_lo = 1.0f - p.h.clip_low; P.clip_hi = 1.0f + p.h.clip_high; P.kl = p.h.kl_coef; P.row_loss = p.row_loss;
     const cudaError_t e = launch_rows<ROW_POLICY>(P, a.dt, st);
     if (e != cudaSuccess || !p.loss) return e;
