@@ -529,7 +529,7 @@ srq_status_t srq_logprob_bwd(const void *logits, srq_dtype_t dt, int64_t rows, i
  * from which dlogits follows as in srq_logprob_bwd.  weight[rows] holds what the caller's mean asks for (1 / number of tokens,
  * or per sequence).  A row with weight zero, or with a target as above, does not count: its logits and its other inputs are
  * not read, its logp, row_loss and dlogits are 0.  logp_ref may be NULL: no KL term (kl_coef is then ignored); with a
- * kl_coef of 0 it is not read.
+ * kl_coef of 0 it is not read.  A logp, a gradient at it or a row's loss (where row_loss is asked for) that is not finite is reported.
  * row_loss [rows], loss [1] (the sum of row_loss; needs row_loss), logp [rows] and dlogits may each be NULL, but not all of them.
  * dlogits may be the logits themselves. */
 typedef struct {

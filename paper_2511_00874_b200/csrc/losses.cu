@@ -376,7 +376,7 @@ __global__ void __launch_bounds__(NT, ROW_CTAS<NT>) row_kernel(const RowParams P
                     }
                     if (P.stat) P.stat[row] = make_float2(m, r.inv);
                     if constexpr (MODE == ROW_POLICY) if (P.row_loss) P.row_loss[row] = loss;
-                    if (abs_word(logp) >= 0x7F800000u || abs_word(r.c) >= 0x7F800000u) note(P.status, SRQ_ERR_NONFINITE);
+                    if (abs_word(logp) >= 0x7F800000u || abs_word(r.c) >= 0x7F800000u || (P.row_loss && abs_word(loss) >= 0x7F800000u)) note(P.status, SRQ_ERR_NONFINITE);
                 }
             }
         }

@@ -50,3 +50,16 @@ def test_ratios_beyond_binary32():
     for adv, kw in ((-1.0, {}), (1.0, dict(clip_high=math.inf))):
         status, row, loss, _ = call([-500.0, LOGP], [adv, 0.5], **kw)
         assert status == binding.ERR_NONFINITE and row[0].isinf() and loss.isinf() and row[1].isfinite()
+
+
+def test_a_row_loss_that_is_not_finite_is_reported():
+    # the reference gives the class no probability: d = -inf, the loss is infinite, its slope kl is not
+    status, row, loss, dx = call([LOGP], [1.0], [-math.inf], kl_coef=0.25)
+    assert status == binding.ERR_NONFINITE and row.isposinf().all() and loss.isposinf().all()
+    assert abs(slope(dx).item() - (0.25 - 1.0)) < 1e-5
+    status, _, _, dx = call([LOGP], [1.0], [-math.inf], rows=False, kl_coef=0.25)        # nobody asks for the loss
+    assert status == 0 and abs(slope(dx).item() - (0.25 - 1.0)) < 1e-5
+    x = torch.zeros((1, C), device="cuda")
+    x[0, 9] = math.nan                                                      # no zero factor hides it
+    status, row, _, dx = call([LOGP], [0.0], x=x)
+    assert status == binding.ERR_NONFINITE and row.isnan().all()
