@@ -952,7 +952,9 @@ def new_adam_state(param: torch.Tensor, bits: int = 32):
 
 class AdamTensors:
     """The tensors of a group of an AdamW step, listed once: all weights have one type, all gradients one, all moments 8 or 32
-    bits.  Holds the tensors, whose memory must stay where it is; a gradient that moves is given anew with ``set_grad``."""
+    bits.  Holds the tensors and the memory they have when they are listed, which is where the steps go: a gradient that moves is
+    given anew with ``set_grad``; a weight or a moment whose storage is replaced (``.data``) has to be listed anew, and its old memory is
+    kept and updated until then."""
 
     def __init__(self, tensors):
         self.tensors = list(tensors)
@@ -961,25 +963,26 @@ class AdamTensors:
         self.bits = 32 if t0 is None or t0.m.dtype is torch.float32 else 8
         self.device = None if t0 is None else t0.param.get_device()
         self.c = (_AdamTensor * max(1, len(self.tensors)))()
+        self._memory = [[] for _ in self.tensors]
         state, coded, check = torch.float32 if self.bits == 32 else torch.uint8, self.bits == 8, self._check
         for i, t in enumerate(self.tensors):
             n = t.param.numel()
             param, m, v = check(i, "param", t.param, t0.param.dtype, n), check(i, "m", t.m, state, n), check(i, "v", t.v, state, n)
             steps = [check(i, name, x, torch.float32, -(-n // BLOCK)) for name, x in (("m_step", t.m_step), ("v_step", t.v_step))] if coded else (None, None)
             self.c[i] = _AdamTensor(param, None, m, v, *steps, n)
+            self._memory[i] = [x.untyped_storage() for x in (t.grad, t.param, t.m, t.v, t.m_step, t.v_step)[:6 if coded else 4]]
             self.set_grad(i, t.grad)
 
     def _check(self, i, name, x, dtype, size):
-        if x is None or x.dtype is not dtype or x.numel() != size or not x.is_cuda or not x.is_contiguous():
-            raise ValueError(f"tensor {i}: {name} must hold {size} contiguous values of {dtype} on the device")
-        if x.get_device() != self.device:
-            raise ValueError(f"tensor {i}: {name} is on device {x.get_device()}, the list's first weight on device {self.device}")
+        if x is None or x.dtype is not dtype or x.numel() != size or not x.is_contiguous() or x.get_device() != self.device or self.device < 0:
+            raise ValueError(f"tensor {i}: {name} must hold {size} contiguous values of {dtype} on the device of the first weight")
         return x.data_ptr()
 
     def set_grad(self, i: int, grad: torch.Tensor) -> None:
         """The gradient of tensor i from now on."""
         self.c[i].grad = self._check(i, "grad", grad, torch.float32 if self.grad_dtype == F32 else torch.bfloat16, self.c[i].n)
         self.tensors[i].grad = grad
+        self._memory[i][0] = grad.untyped_storage()
 
     def __len__(self):
         return len(self.tensors)
