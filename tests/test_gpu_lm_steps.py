@@ -99,3 +99,41 @@ def test_what_the_layers_report_reaches_the_model(where):
         m.layers[1][("gate", "up", "down").index(where)][5, 7] = math.nan
         m.load()
     assert m.status.item() == binding.ERR_NONFINITE
+
+
+def test_policy_gradients_of_the_model_against_autograd():
+    # ratios far from the clip's bounds (log 0.7 = -0.36, log 1.3 = 0.26), half of them inside: log ratios of +-0.02 and +-1.2.  The coded
+    # logits have a deviation of 12 % of 0.5, so that none of the rows crosses over.
+    import test_gpu_lm as path
+    m = path.model()
+    ids, targets, weight, _, _, adv = path.inputs(3)
+    counts = (targets >= 0).double()
+    gap = torch.tensor([0.02, 1.2, -0.02, -1.2], device="cuda").repeat(path.T // 4).double()
+    logits, _, _ = path.reference(m, ids, lambda z: z.sum())
+    assert logits.abs().max() < 4 and logits.std() < 0.6
+    base = path.token_logp(logits, targets)
+    old, ref = (base - gap).float(), (base + 0.1).float()
+
+    def plain(logits):
+        logp = path.token_logp(logits, targets)
+        rho, d = torch.exp(logp - old.double()), ref.double() - logp
+        row = -torch.minimum(rho * adv, rho.clamp(0.7, 1.3) * adv) + 0.2 * (torch.expm1(d) - d)
+        return (row * weight.double() * counts).sum()
+    _, value, want = path.reference(m, ids, plain)
+    m.forward(ids)
+    got = m.policy(targets, old, adv, weight, ref, clip_low=0.3, clip_high=0.3, kl_coef=0.2)
+    assert abs(got.item() - value) < path.LIMIT * max(1.0, abs(value))
+    m.backward(ids)
+    assert m.status.item() == 0
+    for name, g in path.gradients(m).items():
+        assert path.rel(g, want[name]) < path.LIMIT, name
+
+
+def test_a_step_moves_the_rows_of_all_its_tokens():
+    m = model(2)
+    ids, targets, weight = batch(3)
+    ids[:9], targets[-7:] = -1, -100
+    start = m.table.clone()
+    step(m, (ids, targets, weight))
+    moved = (m.table != start).any(1)
+    assert moved[ids[(ids >= 0) & (targets >= 0)]].all() and m.status.item() == 0
