@@ -85,7 +85,9 @@ class TokenModel:
         return self.logits
 
     def supervised(self, targets: torch.Tensor, weight: torch.Tensor) -> torch.Tensor:
-        """Minus the weighted sum of the targets' log-probabilities; targets below zero do not count.  Logits become gradients."""
+        """Minus the weighted sum of the targets' log-probabilities; targets below zero and weights of zero do not count.  Logits become
+        gradients."""
+        targets = torch.where(weight != 0, targets, -1)
         B.srq_logprob_fwd(self.logits, targets, self.logp, self.lse, device_status=self.status)
         torch.mul(weight, -1.0, out=self.row_loss)
         B.srq_logprob_bwd(self.logits, targets, self.lse, self.row_loss, self.logits, device_status=self.status)

@@ -137,3 +137,16 @@ def test_a_step_moves_the_rows_of_all_its_tokens():
     step(m, (ids, targets, weight))
     moved = (m.table != start).any(1)
     assert moved[ids[(ids >= 0) & (targets >= 0)]].all() and m.status.item() == 0
+
+
+def test_supervised_rows_of_weight_zero_do_not_count():
+    m, other = model(), model()
+    ids, targets, weight = batch(4)
+    weight[[5, 60, 129]] = 0.0
+    m.forward(ids)
+    m.logits[5], m.logits[60, targets[60]] = math.nan, -math.inf             # not read; minus infinity times zero would be NaN
+    loss = m.supervised(targets, weight)
+    other.forward(ids)
+    want = other.supervised(torch.where(weight != 0, targets, -1), weight)
+    assert m.status.item() == 0 and loss.isfinite().all() and torch.equal(loss, want)
+    assert torch.equal(m.logits, other.logits) and not m.logits[[5, 60, 129]].any()
