@@ -87,6 +87,8 @@ class TokenModel:
     def supervised(self, targets: torch.Tensor, weight: torch.Tensor) -> torch.Tensor:
         """Minus the weighted sum of the targets' log-probabilities; targets below zero and weights of zero do not count.  Logits become
         gradients."""
+        if weight.shape != self.row_loss.shape:
+            raise ValueError(f"weight must hold {len(self.row_loss)} values, got {tuple(weight.shape)}")
         targets = torch.where(weight != 0, targets, -1)
         B.srq_logprob_fwd(self.logits, targets, self.logp, self.lse, device_status=self.status)
         torch.mul(weight, -1.0, out=self.row_loss)

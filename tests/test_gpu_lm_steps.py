@@ -150,3 +150,12 @@ def test_supervised_rows_of_weight_zero_do_not_count():
     want = other.supervised(torch.where(weight != 0, targets, -1), weight)
     assert m.status.item() == 0 and loss.isfinite().all() and torch.equal(loss, want)
     assert torch.equal(m.logits, other.logits) and not m.logits[[5, 60, 129]].any()
+
+
+def test_supervised_weights_of_another_size_are_refused():
+    m, args = model(), batch(5)
+    m.forward(args[0])
+    for bad in (args[2][:1], args[2][:-1], args[2][:, None]):
+        with pytest.raises(ValueError, match="weight"):
+            m.supervised(args[1], bad)
+    assert m.supervised(args[1], args[2]).isfinite().all()                   # and leave the model as it was
