@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from array import array
 from dataclasses import dataclass
 from typing import Optional
 
@@ -962,16 +963,19 @@ class AdamTensors:
         self.param_dtype, self.grad_dtype = (F32, F32) if t0 is None else (_dtype_of(t0.param), _dtype_of(t0.grad))
         self.bits = 32 if t0 is None or t0.m.dtype is torch.float32 else 8
         self.device = None if t0 is None else t0.param.get_device()
-        self.c = (_AdamTensor * max(1, len(self.tensors)))()
-        self._memory = [[] for _ in self.tensors]
-        state, coded, check = torch.float32 if self.bits == 32 else torch.uint8, self.bits == 8, self._check
+        self._grad = torch.float32 if self.grad_dtype == F32 else torch.bfloat16
+        self._memory = []
+        f32, coded, entries = torch.float32, self.bits == 8, []
+        state = torch.uint8 if coded else f32
         for i, t in enumerate(self.tensors):
             n = t.param.numel()
-            param, m, v = check(i, "param", t.param, t0.param.dtype, n), check(i, "m", t.m, state, n), check(i, "v", t.v, state, n)
-            steps = [check(i, name, x, torch.float32, -(-n // BLOCK)) for name, x in (("m_step", t.m_step), ("v_step", t.v_step))] if coded else (None, None)
-            self.c[i] = _AdamTensor(param, None, m, v, *steps, n)
-            self._memory[i] = [x.untyped_storage() for x in (t.grad, t.param, t.m, t.v, t.m_step, t.v_step)[:6 if coded else 4]]
-            self.set_grad(i, t.grad)
+            fields = [("param", t.param, t0.param.dtype, n), ("grad", t.grad, self._grad, n), ("m", t.m, state, n), ("v", t.v, state, n)]
+            if coded:
+                fields += [("m_step", t.m_step, f32, -(-n // BLOCK)), ("v_step", t.v_step, f32, -(-n // BLOCK))]
+            entries += [self._check(i, *x) for x in fields] + [0] * (6 - len(fields)) + [n]
+            self._memory.append([x.untyped_storage() for _, x, _, _ in fields])
+        # an array of _AdamTensor, whose members are all of 8 bytes
+        self.c = (_AdamTensor * max(1, len(self.tensors))).from_buffer(array("q", entries or [0] * 7))
 
     def _check(self, i, name, x, dtype, size):
         if x is None or x.dtype is not dtype or x.numel() != size or not x.is_contiguous() or x.get_device() != self.device or self.device < 0:
@@ -980,9 +984,9 @@ class AdamTensors:
 
     def set_grad(self, i: int, grad: torch.Tensor) -> None:
         """The gradient of tensor i from now on."""
-        self.c[i].grad = self._check(i, "grad", grad, torch.float32 if self.grad_dtype == F32 else torch.bfloat16, self.c[i].n)
+        self.c[i].grad = self._check(i, "grad", grad, self._grad, self.c[i].n)
         self.tensors[i].grad = grad
-        self._memory[i][0] = grad.untyped_storage()
+        self._memory[i][1] = grad.untyped_storage()
 
     def __len__(self):
         return len(self.tensors)

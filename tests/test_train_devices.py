@@ -106,3 +106,12 @@ def test_scalars_without_an_element_are_refused(stub):
         with pytest.raises(error):
             B.srq_adamw_step(tensors, 1e-3, **{name: on(0, 0, dtype=dtype)})
     assert stub.calls == 0
+
+
+def test_a_missing_operand_of_a_list_is_named(stub):
+    for name in ("grad", "m", "v", "m_step", "v_step"):
+        bad = entry(40)
+        setattr(bad, name, None)
+        with pytest.raises(ValueError, match=f"tensor 1: {name}"):
+            B.AdamTensors([entry(200), bad])
+    assert len(B.AdamTensors([])) == 0 and stub.calls == 0
