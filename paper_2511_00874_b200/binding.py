@@ -974,6 +974,10 @@ class AdamTensors:
                 fields += [("m_step", t.m_step, f32, -(-n // BLOCK)), ("v_step", t.v_step, f32, -(-n // BLOCK))]
             entries += [self._check(i, *x) for x in fields] + [0] * (6 - len(fields)) + [n]
             self._memory.append([x.untyped_storage() for _, x, _, _ in fields])
+        for first in ([0, 2, 3, 4, 5] if coded else [0, 2, 3]):            # what is written, of tensors that have elements
+            written = [q for q, n in zip(entries[first::7], entries[6::7]) if n]
+            if len(set(written)) != len(written):
+                raise ValueError("a weight, a moment or its step sizes are listed twice")
         # an array of _AdamTensor, whose members are all of 8 bytes
         self.c = (_AdamTensor * max(1, len(self.tensors))).from_buffer(array("q", entries or [0] * 7))
 

@@ -115,3 +115,16 @@ def test_a_missing_operand_of_a_list_is_named(stub):
         with pytest.raises(ValueError, match=f"tensor 1: {name}"):
             B.AdamTensors([entry(200), bad])
     assert len(B.AdamTensors([])) == 0 and stub.calls == 0
+
+
+def test_a_weight_that_is_listed_twice_is_refused(stub):
+    # two entries would update the same memory at the same time (tied weights are listed once, with the sum of their gradients)
+    a, b = entry(200), entry(200)
+    for name in ("param", "m", "v", "m_step", "v_step"):
+        c = entry(200)
+        setattr(c, name, getattr(a, name))
+        with pytest.raises(ValueError, match="twice"):
+            B.AdamTensors([a, b, c])
+    c = entry(200)
+    c.grad = a.grad                                                         # read only
+    assert len(B.AdamTensors([a, b, c, entry(0), entry(0)])) == 5
