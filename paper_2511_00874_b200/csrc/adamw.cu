@@ -6,9 +6,10 @@
 //   each), 186 us = 6.6 TB/s, the rate of a copy.
 //   8-bit states: a warp takes groups of 512, a lane sixteen neighbouring ones, so that a block of 128 (the unit of a step size) is eight
 //   lanes, whose new moments stay in registers between their absmax and their codes.  With bfloat16 weights and gradients 10 bytes
-//   move per element, but 54 instructions are issued per 32 elements (10 of them Philox), so that issue is the bound: the arithmetic is on
+//   move per element, but 54 instructions are issued per 32 elements (10 of them Philox), and neither side is saturated: the arithmetic is on
 //   pairs, thresholds and codes are put together byte-wise, and the next group's bytes arrive in shared memory while one is worked on
-//   (without that 813 us).  352 M elements: 733 - 840 us on different machines, 4.3 - 4.9 TB/s, 0.69 of the issue slots.
+//   (without that 813 us).  352 M elements: 733 - 840 us on different machines, 4.3 - 4.9 TB/s (0.65 - 0.74 of a copy's rate)
+//   and 0.69 of the issue slots.
 #include "train.cuh"
 
 namespace srq {
@@ -127,8 +128,8 @@ __device__ __forceinline__ float2 adam_weight(const AdamScalars& s, const AdamNo
     return __ffma2_rn(u, make_float2(-n.rate, -n.rate), __fmul2_rn(p, make_float2(n.decay, n.decay)));
 }
 // Two bfloat16 numbers by cutting off 16 bits after a threshold was added to them: the low halves of w0 (for x.x) and w1.  The
-// conversion instruction does just that with the halves of its random operand (checked against the bits of a million numbers of every
-// kind; infinities stay, a NaN becomes 0x7FFF).
+// conversion instruction does just that with the halves of its random operand (tests/test_gpu_bf16_cut.py holds it to the bits, over
+// every finite pattern).
 __device__ __forceinline__ uint32_t bf16_pair_sr(float2 x, uint32_t w0, uint32_t w1) {
     uint32_t r;
     asm("cvt.rs.bf16x2.f32 %0, %1, %2, %3;" : "=r"(r) : "f"(x.y), "f"(x.x), "r"(__byte_perm(w0, w1, 0x5410)));
