@@ -554,7 +554,8 @@ size_t srq_preference_workspace_bytes(int64_t rows);
  * and dlogits is the gradient of loss.  logp_ref[rows] comes from srq_logprob_fwd on the reference model's logits.  Rows whose
  * target is below zero or out of range (reported) do not count: logp and dlogits are 0, logp_ref is not read.  Rows before
  * offsets[0] and from offsets[2 * pairs] on belong to no answer: their logits are not read, and logp and dlogits are left as
- * they were, or become 0 (clear_rest: what a backward pass over all rows needs).  Offsets that fall, or lie outside, are reported, and what the call then writes within its arrays is unspecified.
+ * they were, or become 0 (clear_rest: what a backward pass over all rows needs).  Offsets that fall, or lie outside, are
+ * reported, and what the call then writes within its arrays is unspecified.
  * pair_loss [pairs] and logp [rows] are required; loss [1] and dlogits may be NULL.  dlogits may be
  * the logits themselves. */
 typedef struct {

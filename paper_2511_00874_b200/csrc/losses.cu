@@ -12,14 +12,15 @@
 // Bound: HBM at best (2 bytes in, 2 bytes out per bfloat16 logit); what keeps the policy loss from it is that a row's phases follow one another
 // (flags, copies, sums, the cluster's barrier, gradient) and six CTAs per SM do not cover all of them, with two exponentials per logit taking
 // 0.6 of their pipe's cycles.  Policy loss, 4096 x 131072 bfloat16, an eighth of the rows masked: 381 - 423 us = 4.8 - 5.3 TB/s; 1021 x 50257
-// binary32: 78 - 81 us = 4.9 - 5.0 TB/s.  Preference loss, 8044 rows x 50257 bfloat16: 388 - 430 us on different machines, of the 388 140 for the
-// sums (5.8 TB/s) and 242 for the gradient (6.7 TB/s, some of it out of L2).  A persistent form that copied the next row meanwhile was slower (608 us: two large CTAs fewer per SM to
-// cover the barriers, and clusters of eight that do not fill the device).
+// binary32: 78 - 81 us = 4.9 - 5.0 TB/s.  Preference loss, 8044 rows x 50257 bfloat16: 388 - 430 us on different machines; where it took 388,
+// 140 were for the sums (5.8 TB/s) and 242 for the gradient (6.7 TB/s, some of it out of L2).  A persistent form that copied the next row
+// meanwhile was slower (608 us: two large CTAs fewer per SM to cover the barriers, and clusters of eight that do not fill the device).
 //
 // Exponentials: e^((x - m) / T) = 2^((x - m) k) with k = log2(e) / T, the difference first, so that large logits cost no precision
-// and the range is binary32's (a gradient that is given lse alone: LSE_EXACT below).  k is a sum of two numbers where probabilities are added up (one alone would shift every log-probability
-// of a row the same way, which shows in sums over rows).  2^y is the hardware's approximation (2 units).  Sums are binary32: a thread has two, of
-// at most classes / 256 terms each where a row is one CTA's (512 at 131072 classes), and their joins follow.
+// and the range is binary32's (a gradient that is given lse alone: LSE_EXACT below).  k is a sum of two numbers where probabilities
+// are added up (one alone would shift every log-probability of a row the same way, which shows in sums over rows).  2^y is the
+// hardware's approximation (2 units).  Sums are binary32: a thread has two, of at most classes / 256 terms each where a row is one
+// CTA's (512 at 131072 classes), and their joins follow.
 #include <float.h>
 #include <math.h>
 
